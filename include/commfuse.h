@@ -46,7 +46,11 @@ typedef enum {
     CF_ERR_HIP = -5           /* a HIP runtime call failed (see last_error)     */
 } cf_status;
 
-typedef enum { CF_BF16 = 0, CF_F32 = 1 } cf_dtype;
+typedef enum {
+    CF_BF16 = 0,
+    CF_F32 = 1,
+    CF_E4M3 = 2               /* 8 bits, cache pages only (commfuse_cache_write) */
+} cf_dtype;
 typedef enum {
     CF_KIND_RS = 0,       /* FuseReduceScatter on the ring (Alg. 2 / Alg. 3)                      */
     CF_KIND_AG = 1,       /* FuseAllGather on the ring (Alg. 1)                                   */
@@ -457,6 +461,104 @@ typedef struct {
  * key split), then the projections with their B_in adds as one persistent launch over attn_out. */
 cf_status commfuse_run_attn_schedule(const cf_attn_desc *desc, const cf_attn_buffers *bufs, void *compute_stream,
                                      void *copy_stream, uint32_t flags);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Between a decoder layer's two projections: what a rank does with the bf16 output [tokens x (heads + 2 kv_heads) *
+ * head_dim] of its column-parallel QKV projection (commfuse_ag_step) before its row-parallel output projection
+ * (commfuse_rs_step).  Rows of tokens are [tokens][heads][head_dim] with a token and a head stride in elements (0 =
+ * packed; multiples of 8 for bf16, of 4 for fp32; a head's features are contiguous), so that Q, K and V may lie side
+ * by side in the projection's output.  Tables of positions, slots, lengths and pages are DEVICE memory, aligned to
+ * their type, read by the kernels only: the calls can be captured into a HIP graph and replayed with other contents.
+ * Whatever those tables hold, no access leaves the tensors that the descriptors describe.  Calls and streams belong
+ * to the current device.  A call without tokens (sequences, rows) enqueues nothing.
+ * ------------------------------------------------------------------------------------------------------------- */
+
+/* Rotary positions.  Pair j of a head (j < rot_dim / 2) turns by position * f_j:
+ *     y_a = magnitude * (x_a cos - x_b sin),   y_b = magnitude * (x_b cos + x_a sin)
+ * with (a, b) = (j, j + rot_dim / 2) or (2 j, 2 j + 1); features from rot_dim on are copied.  Unscaled, f_j =
+ * base^(-2 j / rot_dim).  For contexts longer than `trained_len` the frequencies become f_j * (r_j + (1 - r_j) / factor):
+ *     CF_ROPE_LINEAR      r_j = 0 (factor 1: as trained)
+ *     CF_ROPE_WAVELENGTH  r_j = clamp((n_j - low) / (high - low), 0, 1), n_j = trained_len * f_j / (2 pi) the turns
+ *                         that pair j makes over the trained length
+ *     CF_ROPE_INDEX       r_j = 1 - clamp((j - j_high) / (j_low - j_high), 0, 1), a ramp over the pair's index between
+ *                         the pairs that make `high` and `low` turns: j_high = max(0, floor(d(high))), j_low =
+ *                         min(rot_dim / 2 - 1, ceil(d(low))), d(t) = rot_dim * ln(trained_len / (2 pi t)) / (2 ln base),
+ *                         a ramp of no width taken as one of 0.001
+ * Positions are int32 of either sign; the angle is exact modulo one turn at any of them: a frequency is kept in turns
+ * as a 64-bit binary fraction, whose product with the position wraps at whole turns. */
+typedef enum { CF_ROPE_HALF = 0, CF_ROPE_INTERLEAVED = 1 } cf_rope_layout;
+typedef enum { CF_ROPE_LINEAR = 0, CF_ROPE_WAVELENGTH = 1, CF_ROPE_INDEX = 2 } cf_rope_scaling;
+typedef struct {
+    int32_t head_dim;       /* multiple of 8, at most 256                                     */
+    int32_t rot_dim;        /* even, 2 .. head_dim                                            */
+    int32_t layout;         /* cf_rope_layout                                                 */
+    int32_t scaling;        /* cf_rope_scaling                                                */
+    int64_t trained_len;    /* CF_ROPE_WAVELENGTH, CF_ROPE_INDEX                              */
+    double base;            /* > 1                                                            */
+    double factor;          /* >= 1                                                           */
+    double low, high;       /* 0 < low < high (CF_ROPE_WAVELENGTH, CF_ROPE_INDEX)             */
+    double magnitude;       /* > 0                                                            */
+} cf_rope_desc;
+typedef struct {            /* HOST struct that commfuse_rope_make fills in; the caller keeps it */
+    int32_t head_dim, rot_dim, layout;
+    float magnitude;
+    uint64_t turn[128];     /* turns per position of pair j, in units of 2^-64                */
+} cf_rope;
+/* Host-only arithmetic. */
+cf_status commfuse_rope_make(const cf_rope_desc *desc, cf_rope *rope);
+
+/* Rotates `heads` heads of every token: out = rotation of x, or with `gradient` != 0 the gradient with respect to x given
+ * the one with respect to y (the transposed matrix: the other way round, the same magnitude).  out may be x itself with the
+ * same strides (in place); they may not overlap otherwise. */
+typedef struct {
+    int64_t tokens;
+    int32_t heads;
+    int32_t dtype;                       /* CF_BF16 or CF_F32, of x and out                   */
+    int64_t x_token, x_head, o_token, o_head;
+} cf_rope_rows;
+cf_status commfuse_rope(const cf_rope *rope, const cf_rope_rows *rows, const void *x, const int32_t *positions, void *out,
+                        int gradient, void *hip_stream);
+
+/* A paged cache: K and V in pages of `page_size` tokens, [n_pages][kv_heads][page_size][head_dim] with the strides below
+ * (of pages, heads and tokens, in elements; 0, 0, 0 = packed in that order).  Slot s stands for token s % page_size of page
+ * s / page_size.
+ *   CF_BF16: the values, rounded to nearest even.
+ *   CF_E4M3: one exponent per token and head, and one byte per value (four significant bits): with e the smallest integer
+ *     for which the largest finite magnitude of the row is at most 448 * 2^e (e in [-126, 120]; 0 for a row of zeros), a value
+ *     is stored as x * 2^-e rounded to nearest even (to 240 at the most where e = 120: no finite value becomes infinite), and
+ *     stands for that times 2^e -- which bf16 holds exactly.  Powers of two: scaling itself rounds nothing.  NaN and infinities
+ *     become NaN.  k_exp / v_exp hold e + 127. */
+typedef struct {
+    int32_t dtype;                       /* CF_BF16 or CF_E4M3                                */
+    int32_t page_size;                   /* power of two, 16 .. 1024                          */
+    int32_t kv_heads;
+    int32_t head_dim;                    /* multiple of 16, at most 256; commfuse_attn_paged: 128 */
+    int64_t n_pages;
+    int64_t page_stride, head_stride, token_stride;   /* multiples of 8 (CF_BF16) or 16 (CF_E4M3) */
+} cf_cache_desc;
+typedef struct {                         /* HOST struct of DEVICE pointers                    */
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;              /* CF_E4M3: [n_pages][kv_heads][page_size], packed; CF_BF16: unused */
+} cf_cache;
+typedef struct {                         /* rows of new tokens                                */
+    int64_t tokens;
+    int32_t heads;                       /* query heads to rotate (0: none)                   */
+    int32_t reserved;                    /* 0                                                 */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   /* o: of q_out */
+} cf_cache_rows;
+
+/* Writes K and V (bf16) of new tokens into the cache, in one launch.  With `rope` (head_dim as the cache's, rot_dim a multiple
+ * of 16; NULL: none, `positions` unused) K is rotated on the way, rounded once, to the cache's type; and with Q (NULL: none;
+ * it needs `rope`) q_out = rotated Q in bf16 (may be Q itself, in place).
+ *   slots  int64 [tokens]: where each token goes, no slot twice in a call.  A token whose slot is out of range (below 0, or
+ *          n_pages * page_size and above: padding) is not stored; its row of q_out is. */
+cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const cf_rope *rope,
+                               const void *Q, const void *K, const void *V, const int32_t *positions, const int64_t *slots,
+                               void *q_out, void *hip_stream);
+/* Reads tokens back as bf16 rows (k_token .. v_head of `rows`; exact): K and V of slot slots[i] into row i.  Rows whose slot is
+ * out of range are left as they were.  A slot may be read into several rows. */
+cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const int64_t *slots,
+                              void *K, void *V, void *hip_stream);
 
 /* Synchronises `hip_stream` and reports whether any step kernel since the last call gave up a
  * bounded device-side wait (CF_DEVICE_WAIT; CF_ERR_HIP, the status word in the workspace is cleared).  CF_OK if none did

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libcommfuse.so")
 
 CF_OK = 0
 CF_ERR_INVALID_ARG, CF_ERR_NULL_PTR, CF_ERR_UNSUPPORTED, CF_ERR_MISALIGNED, CF_ERR_HIP = -1, -2, -3, -4, -5
-CF_BF16, CF_F32 = 0, 1
+CF_BF16, CF_F32, CF_E4M3 = 0, 1, 2
 CF_KIND_RS, CF_KIND_AG, CF_KIND_DP, CF_KIND_RS_PAIR, CF_KIND_DP_PAIR, CF_KIND_WGRAD_X, CF_KIND_WGRAD_G = 0, 1, 2, 3, 4, 5, 6
 CF_W_KN, CF_W_NK = 0, 1
 CF_NO_COPY, CF_NO_COMPUTE, CF_SERIAL, CF_POISON, CF_GRAPH, CF_FUSED_COPY, CF_DEVICE_WAIT = 1, 2, 4, 8, 16, 32, 64
@@ -24,13 +24,17 @@ CF_PERSISTENT = 128
 
 KINDS = {"rs": CF_KIND_RS, "ag": CF_KIND_AG, "dp": CF_KIND_DP, "rs_pair": CF_KIND_RS_PAIR, "dp_pair": CF_KIND_DP_PAIR,
          "wgrad_x": CF_KIND_WGRAD_X, "wgrad_g": CF_KIND_WGRAD_G}
-DTYPES = {"bf16": CF_BF16, "f32": CF_F32}
+DTYPES = {"bf16": CF_BF16, "f32": CF_F32, "e4m3": CF_E4M3}
+CF_ROPE_HALF, CF_ROPE_INTERLEAVED = 0, 1
+CF_ROPE_LINEAR, CF_ROPE_WAVELENGTH, CF_ROPE_INDEX = 0, 1, 2
+ROPE_LAYOUTS = {"half": CF_ROPE_HALF, "interleaved": CF_ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"linear": CF_ROPE_LINEAR, "wavelength": CF_ROPE_WAVELENGTH, "index": CF_ROPE_INDEX}
 
 EXPORTS = [
     "commfuse_chunk_index", "commfuse_subslice_index", "commfuse_pair_partner", "commfuse_rs_pair_step", "commfuse_rs_pair_last_step", "commfuse_dp_pair_step", "commfuse_wgrad_step", "commfuse_attn_slice", "commfuse_attn_rs_step",
     "commfuse_run_attn_schedule", "commfuse_rs_step", "commfuse_rs_step_noalloc", "commfuse_ag_step", "commfuse_dp_reduce_step",
     "commfuse_run_schedule", "commfuse_last_error", "commfuse_workspace_bytes", "commfuse_set_workspace",
-    "commfuse_device_status",
+    "commfuse_device_status", "commfuse_rope_make", "commfuse_rope", "commfuse_cache_write", "commfuse_cache_read",
     "commfuse_destroy_cache", "commfuse_version",
 ]
 
@@ -75,6 +79,38 @@ class AttnBuffers(ctypes.Structure):
         ("recv_each", ctypes.POINTER(ctypes.c_void_p)),
         ("send_each", ctypes.POINTER(ctypes.c_void_p)),
     ]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("trained_len", ctypes.c_int64), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+        ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double),
+    ]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("turn", ctypes.c_uint64 * 128)]
+
+
+class RopeRows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("heads", ctypes.c_int32), ("dtype", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("x_token", "x_head", "o_token", "o_head")]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "page_size", "kv_heads", "head_dim")] + \
+               [(n, ctypes.c_int64) for n in ("n_pages", "page_stride", "head_stride", "token_stride")]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")]
+
+
+class CacheRows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "o_token", "o_head")]
 
 
 class CommFuseError(RuntimeError):
@@ -135,6 +171,15 @@ def load():
     lib.commfuse_set_workspace.restype = i32
     lib.commfuse_device_status.argtypes = [vp]
     lib.commfuse_device_status.restype = i32
+    ref = ctypes.POINTER
+    lib.commfuse_rope_make.argtypes = [ref(RopeDesc), ref(Rope)]
+    lib.commfuse_rope_make.restype = i32
+    lib.commfuse_rope.argtypes = [ref(Rope), ref(RopeRows), vp, vp, vp, i32, vp]
+    lib.commfuse_rope.restype = i32
+    lib.commfuse_cache_write.argtypes = [ref(CacheDesc), ref(Cache), ref(CacheRows), ref(Rope)] + [vp] * 7
+    lib.commfuse_cache_write.restype = i32
+    lib.commfuse_cache_read.argtypes = [ref(CacheDesc), ref(Cache), ref(CacheRows)] + [vp] * 4
+    lib.commfuse_cache_read.restype = i32
     lib.commfuse_destroy_cache.argtypes = []
     lib.commfuse_destroy_cache.restype = None
     lib.commfuse_version.argtypes = []
@@ -370,3 +415,45 @@ def device_status(stream=None) -> None:
 
 def destroy_cache() -> None:
     load().commfuse_destroy_cache()
+
+
+# Between a decoder layer's projections.  Rows of tokens are [tokens, heads, head_dim]; a pair of strides is (token, head) in
+# elements, (0, 0) = packed: of a tensor t (t.stride(0), t.stride(1)).
+def rope_make(head_dim: int, rot_dim: int = 0, layout="half", base: float = 10000.0, scaling="linear", factor: float = 1.0,
+              trained_len: int = 0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0) -> Rope:
+    d = RopeDesc(head_dim, rot_dim or head_dim, ROPE_LAYOUTS[layout] if isinstance(layout, str) else layout,
+                 ROPE_SCALINGS[scaling] if isinstance(scaling, str) else scaling, trained_len, base, factor, low, high, magnitude)
+    r = Rope()
+    _check(load().commfuse_rope_make(ctypes.byref(d), ctypes.byref(r)))
+    return r
+
+
+def rope_rows(tokens: int, heads: int, dtype="bf16", x=(0, 0), o=(0, 0)) -> RopeRows:
+    return RopeRows(tokens, heads, DTYPES[dtype] if isinstance(dtype, str) else dtype, *x, *o)
+
+
+def rope(rope_: Rope, rows: RopeRows, x, positions, out, gradient=False, stream=None) -> None:
+    _check((_lib or load()).commfuse_rope(rope_, rows, _ptr(x), _ptr(positions), _ptr(out), int(gradient), _stream(stream)))
+
+
+def cache_desc(dtype, n_pages: int, page_size: int, kv_heads: int, head_dim: int = 128, strides=(0, 0, 0)) -> CacheDesc:
+    """``strides``: of pages, heads and tokens; (0, 0, 0) = packed [n_pages, kv_heads, page_size, head_dim]."""
+    return CacheDesc(DTYPES[dtype] if isinstance(dtype, str) else dtype, page_size, kv_heads, head_dim, n_pages, *strides)
+
+
+def make_cache(k, v, k_exp=None, v_exp=None) -> Cache:
+    """The caller keeps the tensors alive."""
+    return Cache(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp))
+
+
+def cache_rows(tokens: int, heads: int = 0, q=(0, 0), k=(0, 0), v=(0, 0), o=(0, 0)) -> CacheRows:
+    return CacheRows(tokens, heads, 0, *q, *k, *v, *o)
+
+
+def cache_write(desc: CacheDesc, cache: Cache, rows: CacheRows, rope_: Optional[Rope], Q, K, V, positions, slots, q_out, stream=None) -> None:
+    _check((_lib or load()).commfuse_cache_write(desc, cache, rows, rope_, _ptr(Q), _ptr(K), _ptr(V), _ptr(positions), _ptr(slots),
+                                                 _ptr(q_out), _stream(stream)))
+
+
+def cache_read(desc: CacheDesc, cache: Cache, rows: CacheRows, slots, K, V, stream=None) -> None:
+    _check((_lib or load()).commfuse_cache_read(desc, cache, rows, _ptr(slots), _ptr(K), _ptr(V), _stream(stream)))

@@ -2,7 +2,7 @@
 // of Alg. 1 and Alg. 2), kernel dispatch, and the two-stream emulated rank step.
 // The contract of every entry point is stated in include/commfuse.h.
 #include "../../include/commfuse.h"
-#include "cf_internal.h"
+#include "decoder_internal.h"
 
 #include <climits>
 #include <cstdarg>
@@ -1480,6 +1480,31 @@ cf_status check_attn_ptrs(const void *Q, const void *K, const void *V, const voi
 }  // namespace
 
 namespace cf {
+
+int fail(int status, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return status;
+}
+
+int num_cu() { return num_cu_of_current_device(); }
+
+WorkspaceView workspace_view(hipStream_t s)
+{
+    static_assert(WORKSPACE_HEAD_BYTES == WS_COUNTER_BYTES, "the workspace's head");
+    WorkspaceView v;
+    const Workspace ws = workspace_for(s);
+    if (ws.ptr == nullptr || ws.bytes <= WS_COUNTER_BYTES)
+        return v;
+    v.counters = static_cast<unsigned *>(ws.ptr);
+    v.parts = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + WS_COUNTER_BYTES);
+    v.bytes = ws.bytes - WS_COUNTER_BYTES;
+    v.max_counters = (int)(WS_TILE_COUNTER_BYTES / sizeof(unsigned));
+    return v;
+}
 
 static Tuning read_tuning_from_environment()
 {
