@@ -538,7 +538,7 @@ typedef struct {
 } cf_cache_desc;
 typedef struct {                         /* HOST struct of DEVICE pointers                    */
     void *k, *v;
-    uint8_t *k_exp, *v_exp;              /* CF_E4M3: [n_pages][kv_heads][page_size], packed; CF_BF16: unused */
+    uint8_t *k_exp, *v_exp;              /* CF_E4M3: [n_pages][kv_heads][page_size], packed, 8-byte aligned; CF_BF16: unused */
 } cf_cache;
 typedef struct {                         /* rows of new tokens                                */
     int64_t tokens;
@@ -559,6 +559,56 @@ cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache,
  * out of range are left as they were.  A slot may be read into several rows. */
 cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const int64_t *slots,
                               void *K, void *V, void *hip_stream);
+
+/* Causal attention over packed prompts, query heads sharing key heads: with g = heads / kv_heads, query head h reads key head
+ * h / g, and token t of a sequence sees the tokens of its sequence up to itself:
+ *     out = softmax(scale * q K^T) V,    lse = ln sum exp(scale * q k)
+ *   Q [tokens][heads][128], K, V [tokens][kv_heads][128] bf16;  out [tokens][heads][128] bf16
+ *   lse  fp32 [heads][tokens]; may be NULL.  The gradient needs it.
+ *   seq_start  int32 [n_seqs + 1], ascending, within [0, tokens]: sequence s is rows [seq_start[s], seq_start[s+1]) (it may be
+ *        empty).  Rows of no sequence (in front of seq_start[0], behind seq_start[n_seqs]) are left as they were.
+ * Scores, softmax and sums in fp32; probabilities are rounded to bf16 for the product with V.  What a token does not see has no
+ * influence on its result, infinities and NaN included.  With a registered workspace (commfuse_set_workspace; size that lets
+ * every choice be used: commfuse_attn_prompt_workspace_bytes) long rows of keys are split over several workgroups.
+ * head_dim must be 128 (CF_ERR_UNSUPPORTED otherwise). */
+typedef struct {
+    int64_t tokens;
+    int32_t n_seqs;
+    int32_t heads, kv_heads;             /* kv_heads divides heads                            */
+    int32_t head_dim;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   /* o: of out and its gradient */
+    float scale;                         /* > 0                                               */
+    int32_t reserved;                    /* 0                                                 */
+} cf_prompt_desc;
+cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *seq_start,
+                               void *out, float *lse, void *hip_stream);
+size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc);
+
+/* Attention of new tokens over the paged cache (their own keys and values among it, written before): sequence s brings the rows
+ * [q_start[s], q_start[s+1]) of Q -- one for a decoded token, many for a chunk of a prompt -- and has kv_len[s] tokens in the cache;
+ * its row i of m sees the first kv_len[s] - m + i + 1 of them.  A row that sees none (an idle place of the batch: kv_len 0) gets
+ * out = 0 and lse = -inf.  Rows of no sequence are left as they were.
+ *   Q, out [total_q][heads][128] bf16, lse fp32 [heads][total_q] (may be NULL), heads a multiple of the cache's kv_heads
+ *   q_start int32 [n_seqs + 1], ascending within [0, total_q]; kv_len int32 [n_seqs];
+ *   page_table int32 [n_seqs][max_pages]: the pages of each sequence, in order.  An entry outside [0, n_pages) is a page without
+ *        tokens: its keys are not seen.  Sequences may share pages.
+ *   max_q, max_kv  upper bounds of the rows and cached tokens of a sequence, which choose the kernel and its grid (for a captured
+ *        graph: over all replays).  Rows of a sequence beyond max_q are left as they were; cached tokens beyond max_kv, or beyond the table's
+ *        row, are not there.
+ * Workspace as above: keys are split over workgroups where rows are few (commfuse_attn_paged_workspace_bytes).  Calls that overlap
+ * in time must not share one; without one keys are not split. */
+typedef struct {
+    int32_t n_seqs, heads;
+    int32_t max_q, max_kv;
+    int32_t max_pages;
+    float scale;                         /* > 0                                               */
+    int64_t total_q;
+    int64_t q_token, q_head, o_token, o_head;
+} cf_paged_desc;
+cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const void *Q,
+                              const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out, float *lse,
+                              void *hip_stream);
+size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc);
 
 /* Synchronises `hip_stream` and reports whether any step kernel since the last call gave up a
  * bounded device-side wait (CF_DEVICE_WAIT; CF_ERR_HIP, the status word in the workspace is cleared).  CF_OK if none did

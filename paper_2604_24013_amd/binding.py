@@ -35,6 +35,7 @@ EXPORTS = [
     "commfuse_run_attn_schedule", "commfuse_rs_step", "commfuse_rs_step_noalloc", "commfuse_ag_step", "commfuse_dp_reduce_step",
     "commfuse_run_schedule", "commfuse_last_error", "commfuse_workspace_bytes", "commfuse_set_workspace",
     "commfuse_device_status", "commfuse_rope_make", "commfuse_rope", "commfuse_cache_write", "commfuse_cache_read",
+    "commfuse_attn_prompt", "commfuse_attn_prompt_workspace_bytes", "commfuse_attn_paged", "commfuse_attn_paged_workspace_bytes",
     "commfuse_destroy_cache", "commfuse_version",
 ]
 
@@ -113,6 +114,18 @@ class CacheRows(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "o_token", "o_head")]
 
 
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "o_token", "o_head")] + \
+               [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "heads", "max_q", "max_kv", "max_pages")] + [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("total_q", "q_token", "q_head", "o_token", "o_head")]
+
+
 class CommFuseError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"commfuse status {status}: {text}")
@@ -180,6 +193,14 @@ def load():
     lib.commfuse_cache_write.restype = i32
     lib.commfuse_cache_read.argtypes = [ref(CacheDesc), ref(Cache), ref(CacheRows)] + [vp] * 4
     lib.commfuse_cache_read.restype = i32
+    lib.commfuse_attn_prompt.argtypes = [ref(PromptDesc)] + [vp] * 7
+    lib.commfuse_attn_prompt.restype = i32
+    lib.commfuse_attn_prompt_workspace_bytes.argtypes = [ref(PromptDesc)]
+    lib.commfuse_attn_prompt_workspace_bytes.restype = ctypes.c_size_t
+    lib.commfuse_attn_paged.argtypes = [ref(CacheDesc), ref(Cache), ref(PagedDesc)] + [vp] * 7
+    lib.commfuse_attn_paged.restype = i32
+    lib.commfuse_attn_paged_workspace_bytes.argtypes = [ref(CacheDesc), ref(PagedDesc)]
+    lib.commfuse_attn_paged_workspace_bytes.restype = ctypes.c_size_t
     lib.commfuse_destroy_cache.argtypes = []
     lib.commfuse_destroy_cache.restype = None
     lib.commfuse_version.argtypes = []
@@ -457,3 +478,30 @@ def cache_write(desc: CacheDesc, cache: Cache, rows: CacheRows, rope_: Optional[
 
 def cache_read(desc: CacheDesc, cache: Cache, rows: CacheRows, slots, K, V, stream=None) -> None:
     _check((_lib or load()).commfuse_cache_read(desc, cache, rows, _ptr(slots), _ptr(K), _ptr(V), _stream(stream)))
+
+
+def prompt_desc(tokens: int, n_seqs: int, heads: int, kv_heads: int, scale: float, head_dim: int = 128, q=(0, 0), k=(0, 0), v=(0, 0),
+                o=(0, 0)) -> PromptDesc:
+    return PromptDesc(tokens, n_seqs, heads, kv_heads, head_dim, *q, *k, *v, *o, scale, 0)
+
+
+def attn_prompt(desc: PromptDesc, Q, K, V, seq_start, out, lse=None, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_prompt(desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(seq_start), _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def attn_prompt_workspace_bytes(desc: PromptDesc) -> int:
+    return int(load().commfuse_attn_prompt_workspace_bytes(desc))
+
+
+def paged_desc(n_seqs: int, heads: int, total_q: int, max_q: int, max_kv: int, max_pages: int, scale: float, q=(0, 0), o=(0, 0)) -> PagedDesc:
+    """``max_pages``: entries of a row of the page table."""
+    return PagedDesc(n_seqs, heads, max_q, max_kv, max_pages, scale, total_q, *q, *o)
+
+
+def attn_paged(cache_desc_: CacheDesc, cache: Cache, desc: PagedDesc, Q, q_start, kv_len, page_table, out, lse=None, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_paged(cache_desc_, cache, desc, _ptr(Q), _ptr(q_start), _ptr(kv_len), _ptr(page_table), _ptr(out),
+                                                _ptr(lse), _stream(stream)))
+
+
+def attn_paged_workspace_bytes(cache_desc_: CacheDesc, desc: PagedDesc) -> int:
+    return int(load().commfuse_attn_paged_workspace_bytes(cache_desc_, desc))

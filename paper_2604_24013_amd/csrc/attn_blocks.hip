@@ -1,0 +1,744 @@
+// Causal attention of many rows for gfx950: packed prompts over their own keys, chunks of new tokens over a paged cache.
+// bf16 MFMAs, fp32 online softmax.
+//
+// Rows.  A row is one token of one query head; the query heads that share a key head are neighbours (row = token * group +
+// head in group), so that a workgroup's rows read the same key tiles and span few tokens -- under the causal mask few keys that
+// only some of them see.  One workgroup = NW waves of 32 rows each; it walks over the keys in tiles of 64.
+// Per tile and wave (as in the kernels of one query slice):
+//   S^T = K Q^T      the key tile as the MFMA "A" operand, the wave's rows (in registers) as "B": a lane owns ONE row (lane & 31)
+//                    and 16 of every 32 keys, so a row's statistics and its mask (keys first .. last) live in two lanes;
+//   online softmax   P = exp2(S - m), m kept until a probability would exceed 2^8;
+//   O^T += V^T P^T   P, rounded to bf16, is in the layout of an MFMA "B" operand when the 16 contraction slots are taken to mean
+//                    the keys that the lane holds; V^T comes from the [key x feature] tile by the transposing LDS read.
+// Mask.  A wave multiplies only the tiles from its rows' first key to their last; for the others of the workgroup's walk it moves its
+// share of the loads.  Tiles on the border are masked by a select on the scores, so that what a row does not see has no weight --
+// but zero times an infinite or NaN V is NaN: a row whose result is not finite is computed once more, key by key
+// (`careful_row`), which reads visible keys only.
+// Packed prompts: a workgroup takes consecutive rows whatever sequences they belong to; keys of the walk that belong to another
+// sequence are masked like any others.  Bound: the matrix pipe; see choose_prompt for the split of the keys.
+#include "attn_tiles.h"
+
+namespace cf {
+namespace {
+
+template <int NW, int SRC, bool LSE>
+__global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
+{
+    constexpr int NT = 64 * NW;          // threads per workgroup
+    constexpr int BQ = NW * 32;          // rows per workgroup
+    constexpr int KT = BKV / 32;         // 32-key MFMA tiles per key tile
+    constexpr int DS = DH / 16;          // 16-wide feature slices (contraction of S^T)
+    constexpr int DT = DH / 32;          // 32-wide feature tiles (rows of O^T)
+    constexpr int LOADS = TILE_BYTES / 1024 / NW;   // wave-loads per wave of a bf16 K or V tile: four rows each
+    constexpr int LOADS8 = LOADS / 2;               // of an e4m3 tile: eight rows each
+    constexpr int V_BASE = 2 * TILE_BYTES;          // LDS: two K tiles, two V tiles
+
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * 2 * TILE_BYTES];
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 31, lh = lane >> 5;
+    const int G = P.group;
+
+    // neighbouring workgroups (one per XCD in turn) take different key heads; long blocks first; splits, of which short blocks have fewer,
+    // outermost: dealt out innermost, the missing ones would always be the same XCDs'
+    const int kvh = blockIdx.x % P.kv_heads;
+    int rest = blockIdx.x / P.kv_heads;
+    const int groups = gridDim.x / (unsigned)(P.kv_heads * P.max_splits);
+    const int split = rest / groups;
+    rest -= split * groups;
+
+    // The block's rows: tokens [t0, ..) of `count`, and the walk over keys [lo, hi).
+    int t_base, count, lo, hi, shown = 0;            // shown: keys that token t_base sees, less one (paged)
+    int seq_a = 0, seq_b = 0;
+    const int32_t *table = nullptr;
+    int row0;                                        // the block's first row, counted from token t_base
+    if constexpr (SRC == PACKED) {
+        const int blocks = (int)(((int64_t)P.tokens * G + BQ - 1) / BQ);
+        const int64_t r0 = (int64_t)(blocks - 1 - rest) * BQ;
+        const int64_t r1 = r0 + BQ < (int64_t)P.tokens * G ? r0 + BQ : (int64_t)P.tokens * G;
+        t_base = (int)(r0 / G);
+        row0 = (int)(r0 - (int64_t)t_base * G);
+        const int t_last = (int)((r1 - 1) / G);
+        count = t_last - t_base + 1;
+        seq_a = sequence_of(P.starts, P.n_seqs, t_base);
+        if (seq_a == P.n_seqs)
+            return;                                  // behind the last sequence
+        seq_b = sequence_of(P.starts, P.n_seqs, t_last);
+        const int first = P.starts[seq_a], end = P.starts[P.n_seqs];
+        lo = first < 0 ? 0 : first;
+        hi = t_last + 1 < end ? t_last + 1 : end;
+        if (lo >= hi)
+            return;
+    } else {
+        const int blocks = (int)(((int64_t)P.max_q * G + BQ - 1) / BQ);
+        const int seq = rest % P.n_seqs, block = blocks - 1 - rest / P.n_seqs;
+        const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
+        const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens;
+        int m = to - from;
+        int n = P.kv_len[seq];
+        n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
+        const int64_t room = (int64_t)P.max_pages << P.pool.page_shift;
+        n = n < room ? n : (int)room;
+        const int rows = m < P.max_q ? m : P.max_q;  // rows behind max_q are left as they were
+        const int64_t r0 = (int64_t)block * BQ;
+        if (r0 >= (int64_t)rows * G)
+            return;
+        const int b0 = (int)(r0 / G);
+        row0 = (int)(r0 - (int64_t)b0 * G);
+        const int64_t r1 = r0 + BQ < (int64_t)rows * G ? r0 + BQ : (int64_t)rows * G;
+        const int last = (int)((r1 - 1) / G);
+        t_base = from + b0;
+        count = last - b0 + 1;
+        shown = n - m + b0;
+        lo = 0;
+        hi = n - m + last + 1;
+        hi = hi < 0 ? 0 : hi;
+        table = P.table + (int64_t)seq * P.max_pages;
+    }
+
+    // This workgroup's key tiles: [kt0, nkt) of the block's
+    const int tiles = (hi - lo + BKV - 1) / BKV;
+    const int splits = P.chunk > 0 && tiles > P.chunk ? (tiles + P.chunk - 1) / P.chunk : 1;
+    if (split >= splits)
+        return;
+    const int kt0 = (int)(((int64_t)tiles * split) / splits);
+    const int nkt = (int)(((int64_t)tiles * (split + 1)) / splits);
+
+    // The lane's row
+    const int r = row0 + wave * 32 + lq;
+    const int token = r / G, g = r - token * G;      // token: from t_base on
+    const int head = kvh * G + g;
+    bool there = token < count;
+    int first = 0, last;
+    if constexpr (SRC == PACKED) {
+        const int t = t_base + (there ? token : 0);
+        int a = seq_a, b = seq_b;                    // how many of starts[1 ..] are <= t
+        while (a < b) {
+            const int mid = (a + b) >> 1;
+            if (P.starts[mid + 1] <= t)
+                a = mid + 1;
+            else
+                b = mid;
+        }
+        first = a < P.n_seqs ? P.starts[a] : t + 1;
+        there = there && first <= t;
+        first = there ? (first < 0 ? 0 : first) : t; // (a row of no sequence: any visible key will do, it is not stored)
+        last = t;
+    } else {
+        last = shown + (there ? token : 0);
+    }
+    // ... and its wave's: tiles [wt0, wt1) have keys that a row of it sees; all see tiles that start at `all_from` or later and end at
+    // `all_to` or earlier
+    int wt0 = kt0, wt1 = kt0, all_from = 0, all_to = 0;
+    {
+        int f_min = there ? first : 0x7FFFFFFF, f_max = there ? first : 0, l_min = there ? last : 0x7FFFFFFF, l_max = there ? last : -1;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            f_min = min(f_min, __shfl_xor(f_min, d));
+            f_max = max(f_max, __shfl_xor(f_max, d));
+            l_min = min(l_min, __shfl_xor(l_min, d));
+            l_max = max(l_max, __shfl_xor(l_max, d));
+        }
+        f_min = uniform(f_min);
+        l_max = uniform(l_max);
+        all_from = uniform(f_max) - lo;
+        all_to = uniform(l_min) - lo;
+        if (l_max >= f_min) {
+            wt0 = max(kt0, (f_min - lo) / BKV);
+            wt0 -= (wt0 - kt0) & 1;                  // (buffers and registers alternate together)
+            wt1 = min(nkt, (l_max - lo) / BKV + 1);
+        }
+    }
+    const bool busy = wt0 < wt1;
+
+    const __bf16 *qrow = static_cast<const __bf16 *>(P.Q) + (int64_t)(t_base + (there ? token : 0)) * P.q_token + head * P.q_head;
+    bf16x8_t qf[DS];
+#pragma unroll
+    for (int ks = 0; ks < DS; ++ks)
+        qf[ks] = *reinterpret_cast<const bf16x8_t *>(qrow + ks * 16 + lh * 8);
+
+    Keys<SRC> Kk, Kv;
+    if constexpr (SRC == PACKED) {
+        Kk.base = static_cast<const unsigned char *>(P.K) + kvh * P.k_head * 2;
+        Kv.base = static_cast<const unsigned char *>(P.V) + kvh * P.v_head * 2;
+        Kk.row_bytes = P.k_token * 2;
+        Kv.row_bytes = P.v_token * 2;
+    } else {
+        constexpr int E = SRC == PAGED_E4M3 ? 1 : 2;
+        Kk.base = static_cast<const unsigned char *>(P.pool.k) + kvh * P.pool.head_stride * E;
+        Kk.row_bytes = P.pool.token_stride * E;
+        Kk.table = table;
+        Kk.exps = SRC == PAGED_E4M3 ? P.pool.k_exp + ((int64_t)kvh << P.pool.page_shift) : nullptr;
+        Kk.page_bytes = P.pool.page_stride * E;
+        Kk.n_pages = P.pool.n_pages;
+        Kk.exp_page = (int64_t)P.pool.kv_heads << P.pool.page_shift;
+        Kk.shift = P.pool.page_shift;
+        Kv = Kk;
+        Kv.base = static_cast<const unsigned char *>(P.pool.v) + kvh * P.pool.head_stride * E;
+        Kv.exps = SRC == PAGED_E4M3 ? P.pool.v_exp + ((int64_t)kvh << P.pool.page_shift) : nullptr;
+    }
+    const unsigned lds_base = lds_address(smem);
+
+    // Paged: the page table by windows of 64 entries, one a lane; `bad`: which of a window's pages do not exist.  The walk asks for V of
+    // tile kt + 1, then for K of tile kt + 2, so that windows change upwards only, and a tile that is masked lies in the present
+    // window or in the one before.
+    int window = -1, entry = 0;
+    unsigned long long bad = 0, bad_before = 0;
+    auto window_of = [&](int kt) __attribute__((always_inline)) { return ((kt * BKV) >> Kk.shift) >> 6; };
+    auto page_of = [&](int key) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(entry, (key >> Kk.shift) & 63); };
+    auto turn_to = [&](int kt) __attribute__((always_inline)) {
+        const int w = window_of(kt);
+        if (w != window) {
+            const int i = w * 64 + lane;
+            entry = i < P.max_pages ? table[i] : -1;
+            bad_before = w == window + 1 ? bad : 0;
+            bad = __builtin_amdgcn_ballot_w64((unsigned)entry >= (unsigned)Kk.n_pages);
+            window = w;
+        }
+    };
+
+    // Loads of key tile `kt` into a K or V buffer.  bf16: wave-load j covers 4 rows of 256 bytes, straight into LDS.
+    // K: the lane at LDS chunk position cp of row r fetches global chunk cp ^ (r & 15); V: the 64-byte groups of a row are XOR-ed
+    // with (row & 3).  (The rows of a wave-load lie a multiple of sixteen from those of the wave's first.)  Rows behind the walk,
+    // and those of pages that do not exist, read as zero and move no data.
+    static_assert(NW * 4 % 16 == 0, "key rows of a wave-load");
+    const int ld_row = wave * 4 + (lane >> 4), ld_cp = lane & 15;
+    const unsigned k_off = (unsigned)((lane >> 4) * (int)Kk.row_bytes + ((ld_cp ^ (ld_row & 15)) << 4));
+    const unsigned v_off = (unsigned)((lane >> 4) * (int)Kv.row_bytes + (((ld_cp >> 2) ^ (ld_row & 3)) << 6) + ((ld_cp & 3) << 4));
+    auto issue = [&](int kt, const Keys<SRC> &from, unsigned off, unsigned lds) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int row = wave * 4 + j * NW * 4, key = lo + kt * BKV + row;
+            const int left = hi - key < 4 ? hi - key : 4;
+            unsigned bytes = left > 0 ? (unsigned)(left * (int)from.row_bytes) : 0u;
+            const unsigned char *at;
+            if constexpr (SRC == PACKED) {
+                at = from.base + (int64_t)key * from.row_bytes;
+            } else {
+                const int page = page_of(key);
+                bytes = (unsigned)page < (unsigned)from.n_pages ? bytes : 0u;
+                at = from.base + (int64_t)page * from.page_bytes + (int64_t)(key & ((1 << from.shift) - 1)) * from.row_bytes;
+            }
+            direct_load_16(make_rsrc(at, bytes), off, lds + wave * 1024 + j * NW * 1024);
+        }
+    };
+    // e4m3: a lane fetches 16 codes of a row (eight lanes a row, eight rows a wave-load) and the row's exponent into registers, and
+    // writes the bf16 values that they stand for where the direct loads would have put them.
+    const int ld_row8 = wave * 8 + (lane >> 3), ld_c8 = lane & 7;
+    u32x4_t code_k[LOADS8], code_v[LOADS8];
+    int exp_k[LOADS8], exp_v[LOADS8];
+    auto issue8 = [&](int kt, const Keys<SRC> &from, u32x4_t (&code)[LOADS8], int (&ex)[LOADS8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < LOADS8; ++j) {
+            const int key = kt * BKV + wave * 8 + j * NW * 8;
+            const int left = hi - key < 8 ? hi - key : 8, page = page_of(key), in_page = key & ((1 << from.shift) - 1);
+            const bool some = left > 0 && (unsigned)page < (unsigned)from.n_pages;
+            const auto rows = plain_rsrc(from.base + (int64_t)page * from.page_bytes + (int64_t)in_page * from.row_bytes, some ? left * (int)from.row_bytes : 0);
+            const auto exps = plain_rsrc(from.exps + page * from.exp_page + in_page, some ? left : 0);
+            code[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, (lane >> 3) * (int)from.row_bytes + ld_c8 * 16, 0, 0);
+            ex[j] = __builtin_amdgcn_raw_buffer_load_b8(exps, lane >> 3, 0, 0);
+        }
+    };
+    auto put8 = [&](const u32x4_t (&code)[LOADS8], const int (&ex)[LOADS8], int base, bool is_v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < LOADS8; ++j) {
+            const float scale = __builtin_bit_cast(float, (unsigned)ex[j] << 23);
+            u32x4_t out[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                out[i >> 1][2 * (i & 1)] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[j][i], scale, false));
+                out[i >> 1][2 * (i & 1) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[j][i], scale, true));
+            }
+            const int row = ld_row8 + j * NW * 8;
+            unsigned char *to = smem + base + row * ROWB;
+            const int at = is_v ? (((ld_c8 >> 1) ^ (row & 3)) << 6) + ((ld_c8 & 1) << 5) : ((2 * ld_c8) ^ (row & 15)) << 4;
+            *reinterpret_cast<u32x4_t *>(to + at) = out[0];
+            *reinterpret_cast<u32x4_t *>(to + (at ^ 16)) = out[1];
+        }
+    };
+
+    // Fragment addresses inside a buffer.
+    // K as "A" operand: lane (key = lq, lh) reads chunk (2 ks + lh) of its key row, swizzled.
+    // V^T as "A" operand: transposing reads; the two reads of a slice start at key rows 4 lh + (i16 >> 2) and 8 more.
+    int k_addr[DS];
+#pragma unroll
+    for (int ks = 0; ks < DS; ++ks)
+        k_addr[ks] = lq * ROWB + (((2 * ks + lh) ^ (lq & 15)) << 4);
+    const int blk = lane >> 4, i16 = lane & 15;
+    const int v_kl = 4 * (blk >> 1) + (i16 >> 2);
+    const int v_nl = (blk & 1) * 16 + (i16 & 3) * 4;
+    int v_addr[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+        v_addr[t] = V_BASE + v_kl * ROWB + (((t) ^ (v_kl & 3)) << 6) + v_nl * 2;
+
+    f32x16_t oacc[DT];
+    float m_run = -3.402823466e38f;      // (finite: against -inf a tile whose scores are all -inf would give NaN)
+    float l_run = 0.0f, l_pair = 0.0f;   // of the rounded probabilities of this lane's keys; of a pair of tiles
+    float e_run = 0.0f, e_pair = 0.0f;   // LSE: of the probabilities before rounding
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            oacc[d][e] = 0.0f;
+    const float sl2 = P.scale * LOG2E;   // scores are kept in units of log2(e)
+
+    auto scores = [&](int buf, f32x16_t (&sn)[KT]) __attribute__((always_inline)) {
+        const unsigned char *st = smem + buf * TILE_BYTES;
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                sn[j][e] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks)
+#pragma unroll
+            for (int j = 0; j < KT; ++j) {
+                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t *>(st + k_addr[ks] + j * 32 * ROWB);
+                sn[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sn[j], 0, 0, 0);
+            }
+    };
+    auto maximum = [&](const f32x16_t (&sn)[KT]) __attribute__((always_inline)) {
+        float mx = sn[0][0];
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                mx = fmaxf(mx, sn[j][e]);
+        return mx;
+    };
+    // Before a tile's scores are exponentiated: keys that a row does not see are masked (border tiles only), and the running reference
+    // m is raised where the tile's maximum exceeds it by more than 2^RAISE (probabilities stay below 2^RAISE), so that the rescaling
+    // of the accumulators is rare and sits in a wave-uniform branch.
+    constexpr float RAISE = 8.0f;
+    auto settle = [&](int kt, f32x16_t (&sn)[KT], float mx) __attribute__((always_inline)) {
+        if (kt * BKV < all_from || (kt + 1) * BKV - 1 > all_to) {    // uniform
+            float ninf = -INFINITY;
+            asm volatile("" : "+v"(ninf));                           // (keeps this a branch: not 32 selects in every tile)
+            const int key0 = lo + kt * BKV + 4 * lh;
+            if constexpr (SRC == PACKED) {
+                const unsigned at = (unsigned)(key0 - first), span = (unsigned)(last - first);
+#pragma unroll
+                for (int j = 0; j < KT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (at + (unsigned)(j * 32 + 8 * (e >> 2) + (e & 3)) > span)
+                            sn[j][e] = ninf;
+            } else {
+#pragma unroll
+                for (int j = 0; j < KT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (key0 + j * 32 + 8 * (e >> 2) + (e & 3) > last)
+                            sn[j][e] = ninf;
+            }
+            mx = maximum(sn);
+        }
+        if constexpr (SRC != PACKED) {
+            const unsigned long long none = window_of(kt) == window ? bad : bad_before;
+            if (none != 0) {                                         // uniform
+                const int key0 = kt * BKV + 4 * lh;
+#pragma unroll
+                for (int j = 0; j < KT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (none >> (((key0 + j * 32 + 8 * (e >> 2) + (e & 3)) >> Kk.shift) & 63) & 1)
+                            sn[j][e] = -INFINITY;
+                mx = maximum(sn);
+            }
+        }
+        const float mxs = max_of_halves(mx) * sl2;                   // scale > 0: the maximum of the scaled scores
+        if (__builtin_amdgcn_ballot_w64(mxs > m_run + RAISE) != 0) { // (not where all scores so far are -inf)
+            const float m_new = fmaxf(m_run, mxs);
+            float alpha = exp2f(m_run - m_new);                      // 0 on the first tile with a finite score
+            asm volatile("" : "+v"(alpha));                          // (keeps this a branch, as above)
+            m_run = m_new;
+            l_run *= alpha;
+            l_pair *= alpha;
+            if constexpr (LSE) {
+                e_run *= alpha;
+                e_pair *= alpha;
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    oacc[d][e] *= alpha;
+        }
+    };
+    auto load_next = [&](int kt, int b) __attribute__((always_inline)) {   // into what the last barrier released
+        if constexpr (SRC != PACKED)
+            turn_to(kt + 1);
+        if constexpr (SRC == PAGED_E4M3)
+            issue8(kt + 1, Kv, code_v, exp_v);
+        else
+            issue(kt + 1, Kv, v_off, lds_base + V_BASE + (1 - b) * TILE_BYTES);
+        if constexpr (SRC != PACKED)
+            turn_to(kt + 2);
+        if constexpr (SRC == PAGED_E4M3)
+            issue8(kt + 2, Kk, code_k, exp_k);
+        else
+            issue(kt + 2, Kk, k_off, lds_base + b * TILE_BYTES);
+    };
+    auto finish = [&](int b) __attribute__((always_inline)) {        // V of tile kt+1 and K of tile kt+2 have landed
+        if constexpr (SRC == PAGED_E4M3) {
+            put8(code_v, exp_v, V_BASE + (1 - b) * TILE_BYTES, true);
+            put8(code_k, exp_k, b * TILE_BYTES, false);
+        } else {
+            wait_vmcnt<0>();
+        }
+        __syncthreads();                                             // ... for every wave, and V of kt, K of kt+1 are read by all
+    };
+    // One tile: probabilities P = exp2(S - m) rounded to bf16, their row sums (of the rounded values that multiply V, two to a dot
+    // product with ones), O^T += V^T P^T; and under it, with `next`, the scores of tile kt+1 and their maximum.  Thirty-two segments
+    // of one MFMA each -- sixteen of the scores, sixteen of V's product --, the fragment of the third segment ahead requested in each,
+    // the 32 exponentials spread over segments 0 .. 22 and the maximum over the last eight.
+    bf16x2_t ones;
+    ones[0] = ones[1] = (__bf16)1.0f;
+    auto tile = [&](int kt, f32x16_t (&sc)[KT], f32x16_t (&sn)[KT], auto b_tag, auto next_tag) __attribute__((always_inline)) {
+        constexpr int B = decltype(b_tag)::value;
+        constexpr bool NEXT = decltype(next_tag)::value;
+        constexpr int FIRST = NEXT ? 0 : 16;                         // first segment
+        constexpr int AHEAD = 3;
+        bf16x8_t frag[AHEAD + 1], pf[KT * 2];                        // pf: "B" fragments of the 16-key slices
+        auto fetch = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int s = decltype(s_tag)::value;
+            if constexpr (s < 16) {
+                frag[s % (AHEAD + 1)] = *reinterpret_cast<const bf16x8_t *>(smem + k_addr[s >> 1] + (1 - B) * TILE_BYTES + (s & 1) * 32 * ROWB);
+            } else if constexpr (s < 32) {
+                const unsigned char *pv = smem + v_addr[s & 3] + B * TILE_BYTES + ((s - 16) >> 2) * 16 * ROWB;
+                const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(pv));
+                const s16x4_t c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(pv + 8 * ROWB));
+                frag[s % (AHEAD + 1)] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        const float nm = -m_run;
+        auto exponentials = [&](auto e_tag) __attribute__((always_inline)) {   // of elements e and e+1
+            constexpr int e = decltype(e_tag)::value;
+            bf16x2_t two;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {                            // bare v_exp_f32: arguments below -126 give 0
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 4][(e & 15) + i], sl2, nm));
+                if constexpr (LSE)
+                    e_pair = (e == 0 && i == 0 && B == 0 ? 0.0f : e_pair) + p;
+                two[i] = (__bf16)p;
+            }
+            pf[e >> 3][(e & 7)] = two[0];
+            pf[e >> 3][(e & 7) + 1] = two[1];
+            l_pair = __builtin_amdgcn_fdot2_f32_bf16(two, ones, e == 0 && B == 0 ? 0.0f : l_pair, false);
+            if constexpr (e == 30 && (B == 1 || !NEXT)) {
+                l_run += l_pair;
+                if constexpr (LSE)
+                    e_run += e_pair;
+            }
+        };
+        float mx = -INFINITY;
+        auto segment = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int s = decltype(s_tag)::value;
+            fetch(std::integral_constant<int, s + AHEAD>{});
+            if constexpr (s < 16) {
+                if constexpr (s < 2)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        sn[s & 1][e] = 0.0f;
+                sn[s & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s % (AHEAD + 1)], qf[s >> 1], sn[s & 1], 0, 0, 0);
+                if constexpr (s % 4 != 3)
+                    exponentials(std::integral_constant<int, 2 * (s - s / 4)>{});
+            } else {
+                oacc[s & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[s % (AHEAD + 1)], pf[(s - 16) >> 2], oacc[s & 3], 0, 0, 0);
+                if constexpr (NEXT && s < 24 && s % 2 == 0)
+                    exponentials(std::integral_constant<int, 24 + (s - 16)>{});
+                if constexpr (NEXT && s >= 24) {
+                    constexpr int e0 = 4 * ((s - 24) & 3);
+#pragma unroll
+                    for (int e = e0; e < e0 + 4; ++e)
+                        mx = fmaxf(mx, sn[(s - 24) >> 2][e]);
+                    asm volatile("" : "+v"(mx));                     // (here, not where it is used)
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const bool more = NEXT || kt + 1 < nkt;
+        if (more)
+            load_next(kt, B);
+        fetch(std::integral_constant<int, FIRST>{});
+        fetch(std::integral_constant<int, FIRST + 1>{});
+        fetch(std::integral_constant<int, FIRST + 2>{});
+        if constexpr (!NEXT)
+            each<0, 2>(exponentials, std::make_integer_sequence<int, 16>{});
+        __builtin_amdgcn_sched_barrier(0);
+        each<FIRST, 1>(segment, std::make_integer_sequence<int, 32 - FIRST>{});
+        if constexpr (NEXT)
+            settle(kt + 1, sn, mx);
+        if (more)
+            finish(B);
+    };
+
+    if (nkt > kt0) {
+        if constexpr (SRC != PACKED)
+            turn_to(kt0);
+        if constexpr (SRC == PAGED_E4M3) {
+            issue8(kt0, Kk, code_k, exp_k);
+            issue8(kt0, Kv, code_v, exp_v);
+            put8(code_k, exp_k, 0, false);
+        } else {
+            issue(kt0, Kk, k_off, lds_base);
+            issue(kt0, Kv, v_off, lds_base + V_BASE);
+        }
+        if constexpr (SRC != PACKED)
+            turn_to(kt0 + 1);
+        if constexpr (SRC == PAGED_E4M3) {
+            issue8(kt0 + 1, Kk, code_k, exp_k);
+            put8(code_v, exp_v, V_BASE, true);
+            put8(code_k, exp_k, TILE_BYTES, false);
+        } else {
+            issue(kt0 + 1, Kk, k_off, lds_base + TILE_BYTES);
+            wait_vmcnt<0>();
+        }
+        __syncthreads();
+        f32x16_t sa[KT], sb[KT];
+        int kt = kt0;
+        if (busy && wt0 == kt0) {
+            scores(0, sa);
+            settle(kt0, sa, maximum(sa));
+        }
+        __syncthreads();                                             // K of tile kt0 is read by all
+        if (busy) {
+            for (; kt < wt0; ++kt) {                                 // tiles of other waves only
+                load_next(kt, (kt - kt0) & 1);
+                if (kt + 1 == wt0) {
+                    scores(0, sa);
+                    settle(wt0, sa, maximum(sa));
+                }
+                finish((kt - kt0) & 1);
+            }
+            using buf0 = std::integral_constant<int, 0>;
+            using buf1 = std::integral_constant<int, 1>;
+            for (; kt + 2 < wt1; kt += 2) {
+                tile(kt, sa, sb, buf0{}, std::true_type{});
+                tile(kt + 1, sb, sa, buf1{}, std::true_type{});
+            }
+            if (kt + 2 == wt1) {
+                tile(kt, sa, sb, buf0{}, std::true_type{});
+                tile(kt + 1, sb, sa, buf1{}, std::false_type{});
+                kt += 2;
+            } else {
+                tile(kt, sa, sb, buf0{}, std::false_type{});
+                ++kt;
+            }
+        }
+        for (; kt + 1 < nkt; ++kt) {
+            load_next(kt, (kt - kt0) & 1);
+            finish((kt - kt0) & 1);
+        }
+    }
+    l_run = sum_of_halves(l_run);                                    // the whole row sums, in both lanes of the row
+    if constexpr (LSE)
+        e_run = sum_of_halves(e_run);
+
+    // Key split: park (m, l, O) in the workspace, thread-major so that every access is a coalesced 4 bytes per lane; the
+    // workgroup that arrives last merges all splits in split order.  Device-coherent cache policy on exactly these accesses, relaxed
+    // agent-scope atomics on the counter.
+    if (splits > 1) {
+        constexpr int COHERENT = 1 | 16;
+        constexpr int NV = DT * 16 + (LSE ? 3 : 2);                  // floats per thread
+        const size_t part = (size_t)NV * NT;
+        const int group = rest * P.kv_heads + kvh;
+        auto part_rsrc = [&](int sp) {
+            return __builtin_amdgcn_make_buffer_rsrc(P.parts + ((size_t)group * P.max_splits + sp) * part, 0, (int)(part * 4), 0x00020000);
+        };
+        {
+            __amdgpu_buffer_rsrc_t rs = part_rsrc(split);
+            auto park = [&](float x, int i) __attribute__((always_inline)) {
+                // (through a plain VGPR: storing the accumulator elements straight from their AGPRs
+                // came out of this compiler as sixteen stores of element 0)
+                asm volatile("" : "+v"(x));
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), rs, (i * NT + tid) * 4, 0, COHERENT);
+            };
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    park(oacc[d][e], d * 16 + e);
+            park(m_run, DT * 16);
+            park(l_run, DT * 16 + 1);
+            if constexpr (LSE)
+                park(e_run, DT * 16 + 2);
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        unsigned *arrived = reinterpret_cast<unsigned *>(smem);       // the key tiles are no longer read
+        if (tid == 0)
+            *arrived = __hip_atomic_fetch_add(&P.counters[group], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (*arrived != (unsigned)(splits - 1))
+            return;
+        if (tid == 0)
+            __hip_atomic_store(&P.counters[group], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        auto ld = [&](__amdgpu_buffer_rsrc_t rs, int i) {
+            return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (i * NT + tid) * 4, 0, COHERENT));
+        };
+        float m_all = -INFINITY;
+        for (int sp0 = 0; sp0 < splits; sp0 += 8) {                  // eight maxima in flight (beyond the last: the last once more)
+            float m[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                m[i] = ld(part_rsrc(sp0 + i < splits ? sp0 + i : splits - 1), DT * 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                m_all = fmaxf(m_all, m[i]);
+        }
+        l_run = e_run = 0.0f;
+        m_run = m_all;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                oacc[d][e] = 0.0f;
+        for (int sp = 0; sp < splits; ++sp) {
+            __amdgpu_buffer_rsrc_t rs = part_rsrc(sp);
+            const float m = ld(rs, DT * 16), l = ld(rs, DT * 16 + 1), x = LSE ? ld(rs, DT * 16 + 2) : 0.0f;
+            float v[DT][16];
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    v[d][e] = ld(rs, d * 16 + e);
+            const float f = exp2f(m - m_all);                        // (a row that sees no key of a split: nothing times a factor)
+            l_run += l * f;
+            e_run += x * f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    oacc[d][e] += f * v[d][e];
+        }
+    }
+
+    // O = O^T / l, rounded to bf16; a row without a visible key is 0 and its log-sum-exp -inf.
+    const int64_t t = t_base + token;
+    __bf16 *orow = static_cast<__bf16 *>(P.out) + t * P.o_token + head * P.o_head;
+    const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+    float odd = 0.0f;                                                // NaN if a value is not finite
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            oacc[d][e] *= inv;
+            odd = __builtin_fmaf(oacc[d][e], 0.0f, odd);
+        }
+    if (there) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                bf16x4_t h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    h[e] = (__bf16)oacc[d][4 * gq + e];
+                *reinterpret_cast<u32x2_t *>(orow + d * 32 + 8 * gq + 4 * lh) = __builtin_bit_cast(u32x2_t, h);
+            }
+        if (LSE && lh == 0)
+            P.lse[(int64_t)head * P.lse_stride + t] = e_run == 0.0f ? -INFINITY : (m_run + __log2f(e_run)) * LN2;
+    }
+    unsigned long long again = __builtin_amdgcn_ballot_w64(there && odd != 0.0f);
+    again = (again | again >> 32) & 0xFFFFFFFFull;
+    if (again != 0) {
+        __builtin_amdgcn_s_waitcnt(0);                               // the row's first result is written before its second
+        for (; again != 0; again &= again - 1) {
+            const int at = __builtin_ctzll(again);
+            const int64_t tr = __shfl(t, at);
+            const int hr = __shfl(head, at);
+            careful_row<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
+                             static_cast<__bf16 *>(P.out) + tr * P.o_token + hr * P.o_head, __shfl(first, at), __shfl(last, at), sl2);
+        }
+    }
+}
+
+template <int NW, int SRC>
+hipError_t launch(const CausalParams &p, int64_t groups, hipStream_t s)
+{
+    const int64_t wgs = groups * p.max_splits;
+    if (wgs * 64 * NW >= ((int64_t)1 << 32))
+        return hipErrorInvalidValue;
+    if (p.lse != nullptr)
+        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, true>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+    else
+        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, false>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+    return hipGetLastError();
+}
+
+struct BlockChoice {
+    int waves = 8, chunk = 0, max_splits = 1;
+};
+
+size_t part_bytes(int waves) { return (size_t)(64 + 3) * (64 * waves) * sizeof(float); }
+
+BlockChoice choose_prompt(const CausalParams &p, int num_cu)
+{
+    BlockChoice c;
+    const Tuning tn = tuning();
+    const int64_t rows = (int64_t)p.tokens * p.group;
+    const int tiles = (p.tokens + BKV - 1) / BKV;
+    if ((rows + 255) / 256 * p.kv_heads < 2 * num_cu)
+        c.waves = 4;
+    if (tn.causal_waves)
+        c.waves = tn.causal_waves;
+    const int64_t groups = (rows + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads;
+    c.chunk = tn.causal_chunk;
+    if (c.chunk > 0) {
+        c.max_splits = (tiles + c.chunk - 1) / c.chunk;
+        if (c.max_splits < 2 || p.parts == nullptr || groups > p.max_counters || (size_t)groups * c.max_splits * part_bytes(c.waves) > p.part_bytes) {
+            c.chunk = 0;
+            c.max_splits = 1;
+        }
+    }
+    return c;
+}
+
+}  // namespace
+
+hipError_t launch_attn_prompt(const CausalParams &p_in, hipStream_t s, int num_cu)
+{
+    CausalParams p = p_in;
+    const BlockChoice c = choose_prompt(p, num_cu);
+    p.chunk = c.chunk;
+    p.max_splits = c.max_splits;
+    const int64_t groups = ((int64_t)p.tokens * p.group + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads;
+    return c.waves == 8 ? launch<8, PACKED>(p, groups, s) : launch<4, PACKED>(p, groups, s);
+}
+
+hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int num_cu)
+{
+    CausalParams p = p_in;
+    BlockChoice c;
+    const Tuning tn = tuning();
+    const int64_t rows = (int64_t)p.max_q * p.group;
+    c.waves = tn.causal_waves ? tn.causal_waves : 4;
+    const int64_t groups = (rows + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads * p.n_seqs;
+    const int tiles = (p.max_kv + BKV - 1) / BKV;
+    c.chunk = tn.causal_chunk;
+    if (c.chunk > 0) {
+        c.max_splits = (tiles + c.chunk - 1) / c.chunk;
+        if (c.max_splits < 2 || p.parts == nullptr || groups > p.max_counters || (size_t)groups * c.max_splits * part_bytes(c.waves) > p.part_bytes) {
+            c.chunk = 0;
+            c.max_splits = 1;
+        }
+    }
+    p.chunk = c.chunk;
+    p.max_splits = c.max_splits;
+    if (p.pool.e4m3)
+        return c.waves == 8 ? launch<8, PAGED_E4M3>(p, groups, s) : launch<4, PAGED_E4M3>(p, groups, s);
+    return c.waves == 8 ? launch<8, PAGED_BF16>(p, groups, s) : launch<4, PAGED_BF16>(p, groups, s);
+}
+
+size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu) { return 0; }
+
+size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu)
+{
+    return 0;
+}
+
+}  // namespace cf

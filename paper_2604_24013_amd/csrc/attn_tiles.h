@@ -1,0 +1,192 @@
+// Device helpers of the causal attention kernels: direct loads to LDS, fragment types, the search of a packed sequence.
+#pragma once
+#include "decoder_internal.h"
+
+#include <cmath>
+#include <type_traits>
+#include <utility>
+
+namespace cf {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int DH = 128;                  // head dimension these kernels are written for
+constexpr int BKV = 64;                  // keys per tile
+constexpr int ROWB = DH * 2;             // bytes of one key / value row in LDS (bf16)
+constexpr int TILE_BYTES = BKV * ROWB;   // 16 KiB
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+template <typename T>
+__device__ __forceinline__ T uniform(T v)
+{
+    if constexpr (sizeof(T) == 8) {
+        const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+        const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)u), hi = __builtin_amdgcn_readfirstlane((int)(unsigned)(u >> 32));
+        return __builtin_bit_cast(T, ((unsigned long long)hi << 32) | lo);
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+    }
+}
+
+// A buffer of `bytes` bytes from a wave-uniform address: what lies behind it reads as zero.
+__device__ __forceinline__ i32x4_t make_rsrc(const void *base, unsigned bytes)
+{
+    const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+    i32x4_t r;
+    r[0] = __builtin_amdgcn_readfirstlane((int)(a & 0xFFFFFFFFull));
+    r[1] = __builtin_amdgcn_readfirstlane((int)((a >> 32) & 0xFFFFull));
+    r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+// The same for the compiler's own buffer accesses.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t plain_rsrc(const void *base, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(uniform(base)), 0, uniform(bytes), 0x00020000);
+}
+
+// Wave-wide 16-byte-per-lane load from global memory straight into LDS (lane L lands at lds_addr + 16 L).
+__device__ __forceinline__ void direct_load_16(i32x4_t rsrc, unsigned voffset, unsigned lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\t"
+                 "buffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(lds_addr), "v"(voffset), "s"(rsrc)
+                 : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt()
+{
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | (0x7 << 4) | (0xF << 8) | ((N >> 4) << 14));
+}
+
+// f(FIRST), f(FIRST + STEP), ... as compile-time constants
+template <int FIRST, int STEP, int... I, typename F>
+__device__ __forceinline__ void each(F &f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, FIRST + STEP * I>{}), ...);
+}
+
+__device__ __forceinline__ unsigned lds_address(const void *p)
+{
+    return __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const unsigned char *)p);
+}
+
+// Maximum / sum over the two lanes (lane, lane ^ 32) that share a query.
+__device__ __forceinline__ float max_of_halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = both[0], b = both[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float sum_of_halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = both[0], b = both[1];
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+
+// How many of starts[1 .. n] are <= t, for a wave-uniform t: sixty-four probes at a time.
+__device__ __forceinline__ int sequence_of(const int32_t *starts, int n, int t)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && starts[1 + (i < hi ? i : lo)] <= t));
+        const int end = lo + c * step;
+        hi = c == 0 ? lo : hi < end ? hi : end;
+        lo = c == 0 ? lo : end - step + 1;
+    }
+    return uniform(lo);
+}
+
+enum { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
+
+// Where a sequence's (or the pack's) keys lie, for single rows: the pointer of key `key` (nullptr: its page does not exist), and its
+// scale.
+template <int SRC>
+struct Keys {
+    const unsigned char *base;       // packed: key 0 of this head
+    int64_t row_bytes;
+    const int32_t *table;            // paged: this sequence's row
+    const uint8_t *exps;
+    int64_t page_bytes, n_pages, exp_page;
+    int shift;
+
+    __device__ __forceinline__ const unsigned char *row(int key, int *e) const
+    {
+        if constexpr (SRC == PACKED) {
+            return base + (int64_t)key * row_bytes;
+        } else {
+            const int64_t page = table[key >> shift];
+            if ((uint64_t)page >= (uint64_t)n_pages)
+                return nullptr;
+            const int in_page = key & ((1 << shift) - 1);
+            if constexpr (SRC == PAGED_E4M3)
+                *e = (int)exps[page * exp_page + in_page] - 127;
+            return base + page * page_bytes + in_page * row_bytes;
+        }
+    }
+    __device__ __forceinline__ f32x2_t pair(const unsigned char *row, int i, int e) const    // features 2 i and 2 i + 1
+    {
+        if constexpr (SRC == PAGED_E4M3) {
+            const f32x2_t v = __builtin_amdgcn_cvt_pk_f32_fp8((int)reinterpret_cast<const unsigned short *>(row)[i], false);
+            return f32x2_t{ldexpf(v[0], e), ldexpf(v[1], e)};
+        } else {
+            const bf16x2_t v = reinterpret_cast<const bf16x2_t *>(row)[i];
+            return f32x2_t{(float)v[0], (float)v[1]};
+        }
+    }
+};
+
+// One row's attention by one wave, key by key, in two passes; lane i holds features 2 i and 2 i + 1.
+template <int SRC>
+__device__ __noinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
+{
+    const int lane = threadIdx.x & 63;
+    const float q0 = (float)q[2 * lane], q1 = (float)q[2 * lane + 1];
+    float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int pass = 0; pass < 2; ++pass)
+        for (int key = first; key <= last; ++key) {
+            int e = 0;
+            const unsigned char *k = K.row(key, &e);
+            if (k == nullptr)
+                continue;
+            const f32x2_t kv = K.pair(k, lane, e);
+            float s = q0 * kv[0] + q1 * kv[1];
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2)
+                s += __shfl_xor(s, d);
+            s *= sl2;
+            if (pass == 0) {
+                m = fmaxf(m, s);
+            } else {
+                const float p = exp2f(s - (m == -INFINITY ? 0.0f : m));
+                const f32x2_t v = V.pair(V.row(key, &e), lane, e);
+                l += p;
+                o0 += p * v[0];
+                o1 += p * v[1];
+            }
+        }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bf16x2_t r;
+    r[0] = (__bf16)(o0 * inv);
+    r[1] = (__bf16)(o1 * inv);
+    reinterpret_cast<bf16x2_t *>(out)[lane] = r;
+}
+
+}  // namespace
+}  // namespace cf

@@ -128,6 +128,8 @@ struct Tuning {
     int attn_qt = -1;               // COMMFUSE_ATTN_QT = 0 | 1 | 2                        (-1 = unset)
     int attn_waves = 0;             // COMMFUSE_ATTN_WAVES = 4 | 8                         (0 = unset)
     int attn_ksplit = 0;            // COMMFUSE_ATTN_KSPLIT                                (0 = unset)
+    int causal_waves = 0, causal_chunk = 0;   // COMMFUSE_CAUSAL = "WAVESxTILES": 4 or 8 waves, key tiles of a split at the most
+                                    // (a large number: no split) of the causal attention of many rows (0 = unset)
 };
 Tuning tuning();
 

@@ -1567,6 +1567,9 @@ static Tuning read_tuning_from_environment()
         t.attn_waves = atoi(e) == 8 ? 8 : 4;
     if (const char *e = getenv("COMMFUSE_ATTN_KSPLIT"))
         t.attn_ksplit = atoi(e);
+    if (const char *e = getenv("COMMFUSE_CAUSAL"))
+        if (sscanf(e, "%dx%d", &t.causal_waves, &t.causal_chunk) != 2 || (t.causal_waves != 4 && t.causal_waves != 8) || t.causal_chunk < 1)
+            t.causal_waves = t.causal_chunk = 0;
     return t;
 }
 

@@ -107,8 +107,8 @@ cf_status resolve_cache(const cf_cache_desc *d, const cf_cache *c, cf::CachePool
     p.v_exp = c->v_exp;
     if (p.k == nullptr || p.v == nullptr || (p.e4m3 && (p.k_exp == nullptr || p.v_exp == nullptr)))
         return CF_FAIL(CF_ERR_NULL_PTR, "cache tensors must not be NULL");
-    if (!aligned(p.k, 16) || !aligned(p.v, 16))
-        return CF_FAIL(CF_ERR_MISALIGNED, "cache tensors must be 16-byte aligned");
+    if (!aligned(p.k, 16) || !aligned(p.v, 16) || (p.e4m3 && (!aligned(p.k_exp, 8) || !aligned(p.v_exp, 8))))
+        return CF_FAIL(CF_ERR_MISALIGNED, "cache tensors must be 16-byte aligned, their exponents 8-byte");
     *out = p;
     return CF_OK;
 }
@@ -120,6 +120,107 @@ cf_status check_tokens(int64_t tokens, int64_t rows_of_a_token)
         return CF_FAIL(CF_ERR_INVALID_ARG, "tokens = %lld", (long long)tokens);
     if (tokens > INT32_MAX / (rows_of_a_token > 0 ? rows_of_a_token : 1))
         return CF_FAIL(CF_ERR_INVALID_ARG, "%lld tokens of %lld rows exceed the 32-bit index range of the kernels", (long long)tokens, (long long)rows_of_a_token);
+    return CF_OK;
+}
+
+// Rows of K or V in a direct load's 32-bit offsets.
+constexpr int64_t MAX_TOKEN_STRIDE = (int64_t)1 << 27;
+
+cf_status check_scale(float scale)
+{
+    if (!(scale > 0.0f) || !(scale < 1e30f))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "scale must be a positive finite number");
+    return CF_OK;
+}
+
+void use_workspace(cf::CausalParams &p, hipStream_t s)
+{
+    const cf::WorkspaceView v = cf::workspace_view(s);
+    p.parts = v.parts;
+    p.counters = v.counters;
+    p.part_bytes = v.bytes;
+    p.max_counters = v.max_counters;
+}
+
+// The packed prompts' geometry.  `nothing`: no row to compute.
+cf_status resolve_prompt(const cf_prompt_desc *d, cf::CausalParams *out, bool *nothing)
+{
+    if (d == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "descriptor is NULL");
+    if (d->n_seqs < 0 || d->heads < 1 || d->kv_heads < 1 || d->reserved != 0)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "n_seqs = %d, heads = %d, kv_heads = %d, reserved = %d", d->n_seqs, d->heads, d->kv_heads, d->reserved);
+    if (d->heads % d->kv_heads)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "kv_heads = %d must divide heads = %d", d->kv_heads, d->heads);
+    if (d->head_dim != 128)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "head_dim %d: the attention kernel is written for 128", d->head_dim);
+    if (cf_status st = check_tokens(d->tokens, d->heads))
+        return st;
+    if (cf_status st = check_scale(d->scale))
+        return st;
+    cf::CausalParams p = {};
+    p.q_token = d->q_token, p.q_head = d->q_head, p.k_token = d->k_token, p.k_head = d->k_head;
+    p.v_token = d->v_token, p.v_head = d->v_head, p.o_token = d->o_token, p.o_head = d->o_head;
+    if (cf_status st = resolve_rows("Q", &p.q_token, &p.q_head, d->tokens, d->heads, 128, 8))
+        return st;
+    if (cf_status st = resolve_rows("K", &p.k_token, &p.k_head, d->tokens, d->kv_heads, 128, 8))
+        return st;
+    if (cf_status st = resolve_rows("V", &p.v_token, &p.v_head, d->tokens, d->kv_heads, 128, 8))
+        return st;
+    if (cf_status st = resolve_rows("out", &p.o_token, &p.o_head, d->tokens, d->heads, 128, 8))
+        return st;
+    if (p.q_token > MAX_TOKEN_STRIDE || p.k_token > MAX_TOKEN_STRIDE || p.v_token > MAX_TOKEN_STRIDE || p.o_token > MAX_TOKEN_STRIDE)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "token strides of more than %lld elements", (long long)MAX_TOKEN_STRIDE);
+    p.heads = d->heads;
+    p.kv_heads = d->kv_heads;
+    p.group = d->heads / d->kv_heads;
+    p.scale = d->scale;
+    p.tokens = (int)d->tokens;
+    p.n_seqs = d->n_seqs;
+    p.lse_stride = d->tokens;
+    p.max_splits = 1;
+    *nothing = d->tokens == 0 || d->n_seqs == 0;
+    *out = p;
+    return CF_OK;
+}
+
+cf_status resolve_paged(const cf_cache_desc *cd, const cf_cache *c, const cf_paged_desc *d, cf::CausalParams *out, bool *nothing)
+{
+    cf::CausalParams p = {};
+    if (cf_status st = resolve_cache(cd, c, &p.pool))
+        return st;
+    if (d == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "descriptor is NULL");
+    if (p.pool.head_dim != 128)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "head_dim %d: the attention kernel is written for 128", p.pool.head_dim);
+    if (d->n_seqs < 0 || d->heads < 1 || d->max_q < 0 || d->max_kv < 0 || d->max_pages < 0)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "n_seqs = %d, heads = %d, max_q = %d, max_kv = %d, max_pages = %d", d->n_seqs, d->heads, d->max_q, d->max_kv, d->max_pages);
+    if (d->heads % p.pool.kv_heads)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "the cache's %d key heads must divide heads = %d", p.pool.kv_heads, d->heads);
+    if (cf_status st = check_tokens(d->total_q, d->heads))
+        return st;
+    if (cf_status st = check_scale(d->scale))
+        return st;
+    if ((int64_t)d->max_q * d->heads > INT32_MAX || d->max_kv > INT32_MAX - 4096)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "max_q = %d, max_kv = %d exceed the 32-bit index range of the kernels", d->max_q, d->max_kv);
+    p.q_token = d->q_token, p.q_head = d->q_head, p.o_token = d->o_token, p.o_head = d->o_head;
+    if (cf_status st = resolve_rows("Q", &p.q_token, &p.q_head, d->total_q, d->heads, 128, 8))
+        return st;
+    if (cf_status st = resolve_rows("out", &p.o_token, &p.o_head, d->total_q, d->heads, 128, 8))
+        return st;
+    p.heads = d->heads;
+    p.kv_heads = p.pool.kv_heads;
+    p.group = d->heads / p.kv_heads;
+    p.scale = d->scale;
+    p.tokens = (int)d->total_q;
+    p.n_seqs = d->n_seqs;
+    p.lse_stride = d->total_q;
+    p.max_q = d->max_q;
+    p.max_pages = d->max_pages;
+    const int64_t room = (int64_t)d->max_pages * cd->page_size;
+    p.max_kv = p.pool.n_pages == 0 ? 0 : room < d->max_kv ? (int)room : d->max_kv;
+    p.max_splits = 1;
+    *nothing = d->total_q == 0 || d->n_seqs == 0 || d->max_q == 0;
+    *out = p;
     return CF_OK;
 }
 
@@ -312,6 +413,81 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
     r.tokens = (unsigned)rows->tokens;
     r.slots = slots;
     return launched(cf::launch_cache_read(c, r, K, V, static_cast<hipStream_t>(hip_stream)), "cache read launch");
+}
+
+cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *seq_start,
+                               void *out, float *lse, void *hip_stream)
+{
+    cf::CausalParams p;
+    bool nothing;
+    if (cf_status st = resolve_prompt(desc, &p, &nothing))
+        return st;
+    if (nothing)
+        return CF_OK;
+    if (Q == nullptr || K == nullptr || V == nullptr || seq_start == nullptr || out == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "Q, K, V, seq_start and out must not be NULL");
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(seq_start, 4))
+        return CF_FAIL(CF_ERR_MISALIGNED, "tensor pointers must be 16-byte aligned, lse and seq_start 4-byte");
+    if (out == Q || out == K || out == V)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "out may not alias an operand");
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    p.Q = Q;
+    p.K = K;
+    p.V = V;
+    p.starts = seq_start;
+    p.out = out;
+    p.lse = lse;
+    use_workspace(p, s);
+    return launched(cf::launch_attn_prompt(p, s, cf::num_cu()), "attention launch");
+}
+
+size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc)
+{
+    cf::CausalParams p;
+    bool nothing;
+    if (resolve_prompt(desc, &p, &nothing) != CF_OK || nothing)
+        return 0;
+    const size_t parts = cf::attn_prompt_part_bytes(p, cf::num_cu());
+    return parts > 0 ? cf::WORKSPACE_HEAD_BYTES + parts : 0;
+}
+
+cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const void *Q,
+                              const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out, float *lse,
+                              void *hip_stream)
+{
+    cf::CausalParams p;
+    bool nothing;
+    if (cf_status st = resolve_paged(cache_desc, cache, desc, &p, &nothing))
+        return st;
+    if (nothing)
+        return CF_OK;
+    if (Q == nullptr || q_start == nullptr || kv_len == nullptr || (page_table == nullptr && desc->max_pages > 0) || out == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "Q, q_start, kv_len, page_table and out must not be NULL");
+    if (!aligned(Q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(q_start, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4))
+        return CF_FAIL(CF_ERR_MISALIGNED, "tensor pointers must be 16-byte aligned, lse and the tables 4-byte");
+    if (out == Q || out == p.pool.k || out == p.pool.v)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "out may not alias an operand");
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    p.Q = Q;
+    p.starts = q_start;
+    p.kv_len = kv_len;
+    p.table = page_table;
+    p.out = out;
+    p.lse = lse;
+    use_workspace(p, s);
+    return launched(cf::attn_few_takes(p) ? cf::launch_attn_few(p, s, cf::num_cu()) : cf::launch_attn_paged_blocks(p, s, cf::num_cu()), "attention launch");
+}
+
+size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc)
+{
+    cf_cache any = {};
+    any.k = any.v = any.k_exp = any.v_exp = reinterpret_cast<uint8_t *>(256);      // (of the pool's geometry, addresses are not looked at)
+    cf::CausalParams p;
+    bool nothing;
+    if (resolve_paged(cache_desc, &any, desc, &p, &nothing) != CF_OK || nothing)
+        return 0;
+    const size_t parts = cf::attn_few_takes(p) ? cf::attn_few_part_bytes(p, cf::num_cu()) : cf::attn_paged_blocks_part_bytes(p, cf::num_cu());
+    return parts > 0 ? cf::WORKSPACE_HEAD_BYTES + parts : 0;
 }
 
 }  // extern "C"

@@ -56,4 +56,40 @@ struct CacheRows {
 hipError_t launch_cache_write(const CachePool &c, const CacheRows &r, hipStream_t s, int num_cu);
 hipError_t launch_cache_read(const CachePool &c, const CacheRows &r, void *K, void *V, hipStream_t s);
 
+// Causal attention of rows (token, query head of one key head's group) over keys that lie packed (a prompt's own) or in a
+// paged cache.  Strides in elements.
+struct CausalParams {
+    const void *Q;
+    void *out;
+    float *lse;                                     // [heads][lse_stride], nullable
+    int64_t lse_stride;
+    int64_t q_token, q_head, o_token, o_head;
+    int heads, kv_heads, group;                     // group = heads / kv_heads
+    float scale;
+    // packed: K, V [tokens], sequences at starts[0 .. n_seqs]
+    const void *K, *V;
+    int64_t k_token, k_head, v_token, v_head;
+    int tokens, n_seqs;
+    const int32_t *starts;                          // (paged: of the query rows)
+    // paged
+    CachePool pool;
+    const int32_t *kv_len, *table;
+    int max_q, max_kv, max_pages;
+    // key tiles split over workgroups
+    int chunk = 0;                                  // tiles of a split at the most (0: all)
+    int max_splits = 1;
+    float *parts = nullptr;
+    unsigned *counters = nullptr;
+    size_t part_bytes = 0;
+    int max_counters = 0;
+};
+hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
+hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);
+bool attn_few_takes(const CausalParams &p);         // few rows of a sequence and key head: the kernel that splits keys over waves
+hipError_t launch_attn_few(const CausalParams &p, hipStream_t s, int num_cu);
+// Bytes of the partial results that the kernels park for their choice of splits.
+size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu);
+size_t attn_few_part_bytes(const CausalParams &p, int num_cu);
+size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu);
+
 }  // namespace cf

@@ -128,3 +128,46 @@ def test_cache_refusals():
     assert write(w=cf.cache_rows(5, 4, q=(256, 128))) == write(w=cf.cache_rows(5, 4, o=(256, 128))) == cf.CF_ERR_INVALID_ARG
     assert write(w=cf.cache_rows(5, -1)) == cf.CF_ERR_INVALID_ARG
     assert write(w=cf.cache_rows(5, 4, q=(640, 128)), out=A) == cf.CF_ERR_INVALID_ARG           # in place with other strides
+
+
+def test_prompt_refusals():
+    assert ctypes.sizeof(cf.PromptDesc) == 96 and cf.PromptDesc.q_token.offset == 24 and cf.PromptDesc.scale.offset == 88
+    desc = lambda tokens=9, n=2, h=4, kv=2, scale=0.1, **kw: cf.prompt_desc(tokens, n, h, kv, scale, **kw)
+    call = lambda d=desc(), q=A, k=B, v=C, at=D, out=E, lse=F: status(cf.attn_prompt, d, q, k, v, at, out, lse)
+    assert call(desc(tokens=0)) == call(desc(n=0)) == cf.CF_OK
+    assert call(desc(head_dim=64)) == cf.CF_ERR_UNSUPPORTED
+    assert call(desc(q=(2 ** 28, 128))) == cf.CF_ERR_UNSUPPORTED
+    nan = float("nan")
+    for d in (desc(tokens=-1), desc(tokens=2 ** 30), desc(n=-1), desc(h=0), desc(kv=0), desc(kv=3), desc(scale=0.0), desc(scale=nan), desc(scale=-1.0),
+              desc(q=(256, 128)), desc(k=(128, 128)), desc(v=(-512, 128)), desc(o=(512, 64))):
+        assert call(d) == cf.CF_ERR_INVALID_ARG
+    assert call(desc(q=(516, 128))) == call(desc(o=(528, 132))) == cf.CF_ERR_MISALIGNED
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(at=None), dict(out=None)):
+        assert call(**kw) == cf.CF_ERR_NULL_PTR
+    for kw in (dict(q=A + 8), dict(k=B + 2), dict(v=C + 4), dict(at=D + 2), dict(out=E + 8), dict(lse=F + 2)):
+        assert call(**kw) == cf.CF_ERR_MISALIGNED
+    assert call(out=A) == call(out=B) == call(out=C) == cf.CF_ERR_INVALID_ARG
+    assert cf.load().commfuse_attn_prompt(None, A, B, C, D, E, F, None) == cf.CF_ERR_NULL_PTR
+    assert cf.attn_prompt_workspace_bytes(desc(kv=3)) == cf.attn_prompt_workspace_bytes(desc(tokens=0)) == 0
+
+
+def test_paged_refusals():
+    assert ctypes.sizeof(cf.PagedDesc) == 64 and cf.PagedDesc.scale.offset == 20 and cf.PagedDesc.total_q.offset == 24
+    pool = lambda dtype="e4m3", dim=128, kv=2: cf.cache_desc(dtype, 9, 16, kv, dim)
+    cache = cf.make_cache(A, B, C, D)
+    desc = lambda n=2, h=4, total=9, max_q=5, max_kv=100, pages=7, scale=0.1, **kw: cf.paged_desc(n, h, total, max_q, max_kv, pages, scale, **kw)
+    call = lambda d=desc(), p=pool(), c=cache, q=A + 256, at=B, n=C, table=D, out=E, lse=F: status(cf.attn_paged, p, c, d, q, at, n, table, out, lse)
+    assert call(desc(n=0)) == call(desc(total=0)) == call(desc(max_q=0)) == cf.CF_OK
+    assert call(p=pool(dim=64)) == call(p=pool("f32")) == cf.CF_ERR_UNSUPPORTED
+    nan = float("nan")
+    for d in (desc(n=-1), desc(h=0), desc(h=3), desc(total=-1), desc(total=2 ** 30), desc(max_q=-1), desc(max_q=2 ** 30), desc(max_kv=-1), desc(max_kv=2 ** 31 - 1),
+              desc(pages=-1), desc(scale=0.0), desc(scale=nan), desc(q=(256, 128)), desc(o=(-512, 128))):
+        assert call(d) == cf.CF_ERR_INVALID_ARG
+    assert call(desc(q=(516, 128))) == cf.CF_ERR_MISALIGNED
+    for kw in (dict(q=None), dict(at=None), dict(n=None), dict(table=None), dict(out=None), dict(c=cf.make_cache(A, B))):
+        assert call(**kw) == cf.CF_ERR_NULL_PTR
+    for kw in (dict(q=A + 8), dict(at=B + 2), dict(n=C + 1), dict(table=D + 2), dict(out=E + 8), dict(lse=F + 2), dict(c=cf.make_cache(A, B, C + 4, D))):
+        assert call(**kw) == cf.CF_ERR_MISALIGNED
+    assert call(out=A) == call(out=B) == call(out=A + 256) == cf.CF_ERR_INVALID_ARG
+    assert cf.load().commfuse_attn_paged(pool(), cache, None, A, B, C, D, E, F, None) == cf.CF_ERR_NULL_PTR
+    assert cf.attn_paged_workspace_bytes(pool(), desc(h=3)) == cf.attn_paged_workspace_bytes(pool(), desc(n=0)) == 0
