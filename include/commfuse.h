@@ -584,6 +584,16 @@ cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const 
                                void *out, float *lse, void *hip_stream);
 size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc);
 
+/* Its gradient: with P = exp(scale q k - lse), dP = dout V^T and delta = sum over features of dout * out,
+ *     dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dout
+ * (dK, dV summed over the query heads of a key head).  out and lse as the forward call left them; dout bf16 with the strides of
+ * out; dQ, dK, dV bf16 with the strides of Q, K, V; delta fp32 [heads][tokens], scratch of the caller's.  P and dS are rounded to
+ * bf16 for their products, sums are fp32, no atomics: the same call gives the same bits.  Rows of no sequence are left as they
+ * were.  None of dQ, dK, dV may overlap an operand. */
+cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const void *out,
+                                    const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK,
+                                    void *dV, void *hip_stream);
+
 /* Attention of new tokens over the paged cache (their own keys and values among it, written before): sequence s brings the rows
  * [q_start[s], q_start[s+1]) of Q -- one for a decoded token, many for a chunk of a prompt -- and has kv_len[s] tokens in the cache;
  * its row i of m sees the first kv_len[s] - m + i + 1 of them.  A row that sees none (an idle place of the batch: kv_len 0) gets

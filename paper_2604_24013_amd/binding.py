@@ -35,7 +35,7 @@ EXPORTS = [
     "commfuse_run_attn_schedule", "commfuse_rs_step", "commfuse_rs_step_noalloc", "commfuse_ag_step", "commfuse_dp_reduce_step",
     "commfuse_run_schedule", "commfuse_last_error", "commfuse_workspace_bytes", "commfuse_set_workspace",
     "commfuse_device_status", "commfuse_rope_make", "commfuse_rope", "commfuse_cache_write", "commfuse_cache_read",
-    "commfuse_attn_prompt", "commfuse_attn_prompt_workspace_bytes", "commfuse_attn_paged", "commfuse_attn_paged_workspace_bytes",
+    "commfuse_attn_prompt", "commfuse_attn_prompt_workspace_bytes", "commfuse_attn_prompt_grad", "commfuse_attn_paged", "commfuse_attn_paged_workspace_bytes",
     "commfuse_destroy_cache", "commfuse_version",
 ]
 
@@ -195,6 +195,8 @@ def load():
     lib.commfuse_cache_read.restype = i32
     lib.commfuse_attn_prompt.argtypes = [ref(PromptDesc)] + [vp] * 7
     lib.commfuse_attn_prompt.restype = i32
+    lib.commfuse_attn_prompt_grad.argtypes = [ref(PromptDesc)] + [vp] * 12
+    lib.commfuse_attn_prompt_grad.restype = i32
     lib.commfuse_attn_prompt_workspace_bytes.argtypes = [ref(PromptDesc)]
     lib.commfuse_attn_prompt_workspace_bytes.restype = ctypes.c_size_t
     lib.commfuse_attn_paged.argtypes = [ref(CacheDesc), ref(Cache), ref(PagedDesc)] + [vp] * 7
@@ -487,6 +489,11 @@ def prompt_desc(tokens: int, n_seqs: int, heads: int, kv_heads: int, scale: floa
 
 def attn_prompt(desc: PromptDesc, Q, K, V, seq_start, out, lse=None, stream=None) -> None:
     _check((_lib or load()).commfuse_attn_prompt(desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(seq_start), _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def attn_prompt_grad(desc: PromptDesc, Q, K, V, out, lse, dout, seq_start, delta, dQ, dK, dV, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_prompt_grad(desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(lse), _ptr(dout), _ptr(seq_start),
+                                                      _ptr(delta), _ptr(dQ), _ptr(dK), _ptr(dV), _stream(stream)))
 
 
 def attn_prompt_workspace_bytes(desc: PromptDesc) -> int:

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcommfuse.so")
 SOURCES = ["commfuse_api.hip", "gemm_bf16.hip", "gemm_bf16_dl.hip", "gemm_rows.hip", "gemm_f32.hip", "dp_reduce.hip", "attn_slice.hip",
-           "decoder_api.hip", "rope_cache.hip", "attn_blocks.hip", "attn_few.hip"]
+           "decoder_api.hip", "rope_cache.hip", "attn_blocks.hip", "attn_few.hip", "attn_grad.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # keep the compiler from forming packed-fp32 VALU instructions

@@ -21,6 +21,13 @@
 namespace cf {
 namespace {
 
+// (a call: inlined, its loops would have the walk's registers spilled)
+template <int SRC>
+__device__ __noinline__ void careful_row_called(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
+{
+    careful_row<SRC>(K, V, q, out, first, last, sl2);
+}
+
 template <int NW, int SRC, bool LSE>
 __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 {
@@ -651,7 +658,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             const int at = __builtin_ctzll(again);
             const int64_t tr = __shfl(t, at);
             const int hr = __shfl(head, at);
-            careful_row<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
+            careful_row_called<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
                              static_cast<__bf16 *>(P.out) + tr * P.o_token + hr * P.o_head, __shfl(first, at), __shfl(last, at), sl2);
         }
     }

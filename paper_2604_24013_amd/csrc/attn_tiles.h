@@ -154,7 +154,7 @@ struct Keys {
 
 // One row's attention by one wave, key by key, in two passes; lane i holds features 2 i and 2 i + 1.
 template <int SRC>
-__device__ __noinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
+__device__ __forceinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
 {
     const int lane = threadIdx.x & 63;
     const float q0 = (float)q[2 * lane], q1 = (float)q[2 * lane + 1];

@@ -155,6 +155,8 @@ cf_status resolve_prompt(const cf_prompt_desc *d, cf::CausalParams *out, bool *n
         return CF_FAIL(CF_ERR_UNSUPPORTED, "head_dim %d: the attention kernel is written for 128", d->head_dim);
     if (cf_status st = check_tokens(d->tokens, d->heads))
         return st;
+    if (d->tokens * d->heads > INT32_MAX - 65536)                // (rows are counted beyond the last by less than this)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "%lld tokens of %d heads exceed the 32-bit index range of the kernels", (long long)d->tokens, d->heads);
     if (cf_status st = check_scale(d->scale))
         return st;
     cf::CausalParams p = {};
@@ -439,6 +441,53 @@ cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const 
     p.lse = lse;
     use_workspace(p, s);
     return launched(cf::launch_attn_prompt(p, s, cf::num_cu()), "attention launch");
+}
+
+cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const void *out,
+                                    const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK,
+                                    void *dV, void *hip_stream)
+{
+    cf::GradParams p = {};
+    bool nothing;
+    if (cf_status st = resolve_prompt(desc, &p.c, &nothing))
+        return st;
+    if (nothing)
+        return CF_OK;
+    const void *const in[] = {Q, K, V, out, lse, dout, seq_start};
+    const void *const result[] = {dQ, dK, dV, delta};
+    for (const void *x : in)
+        if (x == nullptr)
+            return CF_FAIL(CF_ERR_NULL_PTR, "Q, K, V, out, lse, dout and seq_start must not be NULL");
+    for (const void *x : result)
+        if (x == nullptr)
+            return CF_FAIL(CF_ERR_NULL_PTR, "delta, dQ, dK and dV must not be NULL");
+    for (const void *x : {Q, K, V, out, dout, static_cast<const void *>(dQ), static_cast<const void *>(dK), static_cast<const void *>(dV)})
+        if (!aligned(x, 16))
+            return CF_FAIL(CF_ERR_MISALIGNED, "tensor pointers must be 16-byte aligned");
+    if (!aligned(lse, 4) || !aligned(delta, 4) || !aligned(seq_start, 4))
+        return CF_FAIL(CF_ERR_MISALIGNED, "lse, delta and seq_start must be 4-byte aligned");
+    for (int i = 0; i < 4; ++i) {
+        for (const void *x : in)
+            if (result[i] == x)
+                return CF_FAIL(CF_ERR_INVALID_ARG, "delta, dQ, dK and dV may not alias an operand");
+        for (int j = 0; j < i; ++j)
+            if (result[i] == result[j])
+                return CF_FAIL(CF_ERR_INVALID_ARG, "delta, dQ, dK and dV may not alias each other");
+    }
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    p.c.Q = Q;
+    p.c.K = K;
+    p.c.V = V;
+    p.c.out = const_cast<void *>(out);                           // (read only, as lse)
+    p.c.lse = const_cast<float *>(lse);
+    p.c.starts = seq_start;
+    p.dout = dout;
+    p.delta = delta;
+    p.dq = dQ;
+    p.dk = dK;
+    p.dv = dV;
+    use_workspace(p.c, s);
+    return launched(cf::launch_attn_prompt_grad(p, s, cf::num_cu()), "attention gradient launch");
 }
 
 size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc)

@@ -87,6 +87,14 @@ hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
 hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);
 bool attn_few_takes(const CausalParams &p);         // few rows of a sequence and key head: the kernel that splits keys over waves
 hipError_t launch_attn_few(const CausalParams &p, hipStream_t s, int num_cu);
+// The gradient of packed prompts; c.out and c.lse as the forward call left them, dq, dk, dv with the strides of Q, K, V.
+struct GradParams {
+    CausalParams c;
+    const void *dout;
+    float *delta;                                   // [heads][lse_stride]
+    void *dq, *dk, *dv;
+};
+hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_cu);
 // Bytes of the partial results that the kernels park for their choice of splits.
 size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu);
 size_t attn_few_part_bytes(const CausalParams &p, int num_cu);

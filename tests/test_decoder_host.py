@@ -171,3 +171,21 @@ def test_paged_refusals():
     assert call(out=A) == call(out=B) == call(out=A + 256) == cf.CF_ERR_INVALID_ARG
     assert cf.load().commfuse_attn_paged(pool(), cache, None, A, B, C, D, E, F, None) == cf.CF_ERR_NULL_PTR
     assert cf.attn_paged_workspace_bytes(pool(), desc(h=3)) == cf.attn_paged_workspace_bytes(pool(), desc(n=0)) == 0
+
+
+def test_prompt_gradient_refusals():
+    desc = lambda tokens=9, n=2, h=4, kv=2, **kw: cf.prompt_desc(tokens, n, h, kv, 0.1, **kw)
+    names = ["q", "k", "v", "out", "lse", "dout", "at", "delta", "dq", "dk", "dv"]
+    good = {n: 0x10000 * (i + 1) for i, n in enumerate(names)}
+    call = lambda d=desc(), **kw: status(cf.attn_prompt_grad, d, *({**good, **kw}[n] for n in names))
+    assert call(desc(tokens=0)) == call(desc(n=0)) == cf.CF_OK
+    assert call(desc(head_dim=64)) == cf.CF_ERR_UNSUPPORTED
+    for d in (desc(tokens=-1), desc(tokens=2 ** 29), desc(kv=3), desc(q=(256, 128)), desc(o=(512, 64))):
+        assert call(d) == cf.CF_ERR_INVALID_ARG
+    for n in names:
+        assert call(**{n: None}) == cf.CF_ERR_NULL_PTR
+        assert call(**{n: good[n] + 2}) == cf.CF_ERR_MISALIGNED
+    for n in ("dq", "dk", "dv"):
+        for m in names:
+            if m != n:
+                assert call(**{n: good[m]}) == cf.CF_ERR_INVALID_ARG
