@@ -21,6 +21,8 @@
 namespace cf {
 namespace {
 
+constexpr int LEAST_TILES = 4;           // of a split: less than that its hand-over takes
+
 // (a call: inlined, its loops would have the walk's registers spilled)
 template <int SRC>
 __device__ __noinline__ void careful_row_called(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
@@ -107,7 +109,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 
     // This workgroup's key tiles: [kt0, nkt) of the block's
     const int tiles = (hi - lo + BKV - 1) / BKV;
-    const int splits = P.chunk > 0 && tiles > P.chunk ? (tiles + P.chunk - 1) / P.chunk : 1;
+    int chunk = P.chunk;
+    if (chunk < 0)
+        chunk = chunk_by_work(P.n_seqs, P.num_cu, LEAST_TILES, [&](int i, float &all, float &blocks) {
+            const int q0 = P.starts[i], q1 = P.starts[i + 1];
+            const float m = (float)max(0, q1 - q0), here = SRC == PACKED ? m * G / BQ : ceilf(fminf(m, (float)P.max_q) * G / BQ);
+            const float seen = SRC == PACKED ? 0.5f * m : fmaxf(0.0f, (float)min(P.kv_len[i], P.max_kv) - 0.5f * m);
+            blocks += here * P.kv_heads;
+            all += here * P.kv_heads * (seen / BKV + 0.5f);
+        });
+    const int splits = splits_of(tiles, chunk, P.max_splits);
     if (split >= splits)
         return;
     const int kt0 = (int)(((int64_t)tiles * split) / splits);
@@ -677,32 +688,42 @@ hipError_t launch(const CausalParams &p, int64_t groups, hipStream_t s)
     return hipGetLastError();
 }
 
-struct BlockChoice {
-    int waves = 8, chunk = 0, max_splits = 1;
-};
-
 size_t part_bytes(int waves) { return (size_t)(64 + 3) * (64 * waves) * sizeof(float); }
 
-BlockChoice choose_prompt(const CausalParams &p, int num_cu)
+// Splits that the grid has room for: what one sequence as long as all tokens needs, twice over for several shorter ones.  `tiles`: of the
+// longest walk, `blocks`: of rows, over all key heads.
+int room_for_splits(const CausalParams &p, int64_t blocks, int64_t tiles, size_t part)
 {
-    BlockChoice c;
+    if (p.parts == nullptr || blocks > p.max_counters || p.n_seqs > 1024 || blocks < 1)
+        return 1;
+    const double rounds = ceil(1.25 * (double)blocks / p.num_cu), items = (rounds < 1 ? 1 : rounds) * p.num_cu - 0.5 * blocks;
+    double chunk = 0.5 * (double)tiles * blocks / items;
+    chunk = chunk < 4 ? 4 : chunk;
+    int64_t n = (int64_t)(2.0 * tiles / chunk + 1.0);
+    n = n > 16 ? 16 : n;
+    n = n > tiles ? tiles : n;
+    const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
+    n = n > fit ? fit : n;
+    return n < 2 ? 1 : (int)n;
+}
+
+// Four waves (128 rows) or eight, and the room for splits.
+int choose_blocks(CausalParams &p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
+{
     const Tuning tn = tuning();
-    const int64_t rows = (int64_t)p.tokens * p.group;
-    const int tiles = (p.tokens + BKV - 1) / BKV;
-    if ((rows + 255) / 256 * p.kv_heads < 2 * num_cu)
-        c.waves = 4;
-    if (tn.causal_waves)
-        c.waves = tn.causal_waves;
-    const int64_t groups = (rows + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads;
-    c.chunk = tn.causal_chunk;
-    if (c.chunk > 0) {
-        c.max_splits = (tiles + c.chunk - 1) / c.chunk;
-        if (c.max_splits < 2 || p.parts == nullptr || groups > p.max_counters || (size_t)groups * c.max_splits * part_bytes(c.waves) > p.part_bytes) {
-            c.chunk = 0;
-            c.max_splits = 1;
-        }
+    p.num_cu = num_cu;
+    const int waves = tn.causal_waves ? tn.causal_waves : 4;
+    const int64_t blocks = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads * sequences;
+    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
+    if (p.chunk > 0) {
+        const int64_t n = (tiles + p.chunk - 1) / p.chunk;
+        p.max_splits = n < 2 || p.parts == nullptr || blocks > p.max_counters || (size_t)blocks * n * part_bytes(waves) > p.part_bytes ? 1 : (int)n;
+    } else {
+        p.max_splits = room_for_splits(p, blocks, tiles, part_bytes(waves));
     }
-    return c;
+    if (p.max_splits == 1)
+        p.chunk = 0;
+    return waves;
 }
 
 }  // namespace
@@ -710,42 +731,45 @@ BlockChoice choose_prompt(const CausalParams &p, int num_cu)
 hipError_t launch_attn_prompt(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    const BlockChoice c = choose_prompt(p, num_cu);
-    p.chunk = c.chunk;
-    p.max_splits = c.max_splits;
-    const int64_t groups = ((int64_t)p.tokens * p.group + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads;
-    return c.waves == 8 ? launch<8, PACKED>(p, groups, s) : launch<4, PACKED>(p, groups, s);
+    const int64_t rows = (int64_t)p.tokens * p.group;
+    const int waves = choose_blocks(p, rows, 1, (p.tokens + BKV - 1) / BKV, num_cu);
+    const int64_t groups = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads;
+    return waves == 8 ? launch<8, PACKED>(p, groups, s) : launch<4, PACKED>(p, groups, s);
 }
 
 hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    BlockChoice c;
-    const Tuning tn = tuning();
     const int64_t rows = (int64_t)p.max_q * p.group;
-    c.waves = tn.causal_waves ? tn.causal_waves : 4;
-    const int64_t groups = (rows + c.waves * 32 - 1) / (c.waves * 32) * p.kv_heads * p.n_seqs;
-    const int tiles = (p.max_kv + BKV - 1) / BKV;
-    c.chunk = tn.causal_chunk;
-    if (c.chunk > 0) {
-        c.max_splits = (tiles + c.chunk - 1) / c.chunk;
-        if (c.max_splits < 2 || p.parts == nullptr || groups > p.max_counters || (size_t)groups * c.max_splits * part_bytes(c.waves) > p.part_bytes) {
-            c.chunk = 0;
-            c.max_splits = 1;
-        }
-    }
-    p.chunk = c.chunk;
-    p.max_splits = c.max_splits;
+    const int waves = choose_blocks(p, rows, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
+    const int64_t groups = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads * p.n_seqs;
     if (p.pool.e4m3)
-        return c.waves == 8 ? launch<8, PAGED_E4M3>(p, groups, s) : launch<4, PAGED_E4M3>(p, groups, s);
-    return c.waves == 8 ? launch<8, PAGED_BF16>(p, groups, s) : launch<4, PAGED_BF16>(p, groups, s);
+        return waves == 8 ? launch<8, PAGED_E4M3>(p, groups, s) : launch<4, PAGED_E4M3>(p, groups, s);
+    return waves == 8 ? launch<8, PAGED_BF16>(p, groups, s) : launch<4, PAGED_BF16>(p, groups, s);
 }
 
-size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu) { return 0; }
+namespace {
+// (as if any workspace were there)
+size_t part_bytes_of(CausalParams p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
+{
+    p.parts = reinterpret_cast<float *>(256);
+    p.part_bytes = ~(size_t)0 >> 1;
+    p.max_counters = 1 << 30;
+    const int waves = choose_blocks(p, rows, sequences, tiles, num_cu);
+    const size_t blocks = (size_t)((rows + waves * 32 - 1) / (waves * 32)) * p.kv_heads * sequences;
+    return p.max_splits > 1 ? blocks * p.max_splits * part_bytes(waves) : 0;
+}
+}  // namespace
+
+size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu)
+{
+    return part_bytes_of(p, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
+}
 
 size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu)
 {
-    return 0;
+    const size_t f = part_bytes_of(p, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu), g = attn_grad_part_bytes(p, num_cu);
+    return f > g ? f : g;
 }
 
 }  // namespace cf

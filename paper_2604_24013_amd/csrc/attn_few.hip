@@ -57,7 +57,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         return;
     const int hi = n - m + (rows - 1) / G + 1 > 0 ? n - m + (rows - 1) / G + 1 : 0;   // keys that the last row sees
     const int tiles = (hi + FEW_KEYS - 1) / FEW_KEYS;
-    const int splits = tiles > P.chunk ? (tiles + P.chunk - 1) / P.chunk : 1;
+    int chunk = P.chunk;
+    if (chunk < 0)
+        chunk = chunk_by_work(P.n_seqs, P.num_cu, NW, [&](int x, float &all, float &blocks) {
+            const int len = min(P.kv_len[x], P.max_kv);
+            blocks += len > 0 ? P.kv_heads : 0;
+            all += (float)max(0, (len + FEW_KEYS - 1) / FEW_KEYS) * P.kv_heads;
+        });
+    const int splits = splits_of(tiles, chunk, P.max_splits);
     if (split >= splits)
         return;
     const int t0 = (int)(((int64_t)tiles * split) / splits), t1 = (int)(((int64_t)tiles * (split + 1)) / splits);
@@ -453,25 +460,47 @@ hipError_t launch(const CausalParams &p, hipStream_t s)
 
 bool attn_few_takes(const CausalParams &p) { return (int64_t)p.max_q * p.group <= 32; }
 
+namespace {
+int choose_few(CausalParams &p, int num_cu)          // 16-row tiles; the room for splits
+{
+    const int rows = p.max_q * p.group, qt = rows <= 16 ? 1 : 2;
+    const int64_t tiles = (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, blocks = (int64_t)p.n_seqs * p.kv_heads;
+    const size_t part = (size_t)(qt * 16) * (DH + 4) * sizeof(float);
+    const Tuning tn = tuning();
+    p.num_cu = num_cu;
+    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
+    int64_t n = 1;
+    if (p.parts != nullptr && blocks <= p.max_counters && p.n_seqs <= 1024) {
+        const double rounds = ceil(1.25 * (double)blocks / num_cu), items = (rounds < 1 ? 1 : rounds) * num_cu - 0.5 * blocks;
+        double chunk = (double)tiles * blocks / items;       // all contexts as long as the longest ...
+        chunk = chunk < 8 ? 8 : chunk;
+        n = p.chunk > 0 ? (tiles + p.chunk - 1) / p.chunk : (int64_t)(3.0 * tiles / chunk + 1.0);    // ... or one of them, by far
+        if (p.chunk < 0 && n > 64)
+            n = 64;
+        const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
+        n = n <= fit ? n : p.chunk > 0 ? 1 : fit;
+    }
+    p.max_splits = n < 2 ? 1 : (int)n;
+    if (p.max_splits == 1)
+        p.chunk = 0;
+    return qt;
+}
+}  // namespace
+
 hipError_t launch_attn_few(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    const int rows = p.max_q * p.group, qt = rows <= 16 ? 1 : 2;
-    const int tiles = (p.max_kv + FEW_KEYS - 1) / FEW_KEYS;
-    const int64_t groups = (int64_t)p.n_seqs * p.kv_heads;
-    const Tuning tn = tuning();
-    p.chunk = tn.causal_chunk ? tn.causal_chunk : 64;
-    p.max_splits = tiles > p.chunk ? (tiles + p.chunk - 1) / p.chunk : 1;
-    if (p.max_splits > 1 && (p.parts == nullptr || groups > p.max_counters ||
-                             (size_t)groups * p.max_splits * (qt * 16) * (DH + 4) * sizeof(float) > p.part_bytes)) {
-        p.max_splits = 1;
-        p.chunk = tiles;
-    }
-    if (p.chunk < 1)
-        p.chunk = 1;
-    return qt == 1 ? launch<8, 1>(p, s) : launch<8, 2>(p, s);
+    return choose_few(p, num_cu) == 1 ? launch<8, 1>(p, s) : launch<8, 2>(p, s);
 }
 
-size_t attn_few_part_bytes(const CausalParams &p, int num_cu) { return 0; }
+size_t attn_few_part_bytes(const CausalParams &p_in, int num_cu)
+{
+    CausalParams p = p_in;                                           // as if any workspace were there
+    p.parts = reinterpret_cast<float *>(256);
+    p.part_bytes = ~(size_t)0 >> 1;
+    p.max_counters = 1 << 30;
+    const int qt = choose_few(p, num_cu);
+    return p.max_splits > 1 ? (size_t)p.n_seqs * p.kv_heads * p.max_splits * (qt * 16) * (DH + 4) * sizeof(float) : 0;
+}
 
 }  // namespace cf

@@ -14,10 +14,11 @@
 namespace cf {
 namespace {
 
+constexpr int LEAST_TILES = 4;           // of a split: less than that its hand-over takes
 constexpr int DS = DH / 16;              // 16-wide feature slices
 constexpr int DT = DH / 32;              // 32-wide feature tiles
 
-// Wave-wide 16-byte-per-lane (or 4-byte) load from per-lane addresses straight into LDS (lane L lands at lds_addr + 16 L or 4 L).
+// Wave-wide 16-byte-per-lane load from per-lane addresses straight into LDS (lane L lands at lds_addr + 16 L).
 __device__ __forceinline__ void gather_load_16(const void *at, unsigned lds_addr)
 {
     asm volatile("s_mov_b32 m0, %0\n\t"
@@ -26,7 +27,7 @@ __device__ __forceinline__ void gather_load_16(const void *at, unsigned lds_addr
                  : "s"(lds_addr), "v"(at)
                  : "memory");
 }
-__device__ __forceinline__ void gather_load_4(const void *at, unsigned lds_addr)
+__device__ __forceinline__ void gather_load_4(const void *at, unsigned lds_addr)      // (... at lds_addr + 4 L)
 {
     asm volatile("s_mov_b32 m0, %0\n\t"
                  "global_load_lds_dword %1, off"
@@ -35,76 +36,112 @@ __device__ __forceinline__ void gather_load_4(const void *at, unsigned lds_addr)
                  : "memory");
 }
 
-// Addresses inside a tile of rows of 256 bytes whose 16-byte chunks are XOR-ed with (row & 15).
-struct TileRead {
-    int row[DS];                         // "A" operand: lane (row = lane & 31, half = lane >> 5), chunk 2 ks + half
-    int lo, hi;                          // its transposed: rows 4 half + .. and 8 more of a slice of 16; feature tile t at (lo ^ t << 6)
-    __device__ __forceinline__ TileRead()
+// Tiles of rows of 256 bytes: chunk c of 16 bytes of a row lies at position c ^ spread(row & 15).  Sixteen rows' chunk c (a read by
+// rows) lie on sixteen positions, and so do chunks 4 t .. 4 t + 3 of four rows (a transposing read): all 64 banks either way.  (With
+// row & 15 itself the four rows of a transposing read share four positions.)
+__device__ __forceinline__ int spread(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
+
+// Addresses in such a tile, in registers, so that a read costs no arithmetic: what is added to them is a constant.  `move` takes them to another tile (16 additions instead of one a read).
+struct RowRead {                         // "A" operand: lane (row = lane & 31, half = lane >> 5), chunk 2 ks + half
+    int at[DS];
+    __device__ __forceinline__ RowRead()
     {
-        const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5, blk = lane >> 4, i16 = lane & 15;
+        const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5;
 #pragma unroll
         for (int ks = 0; ks < DS; ++ks)
-            row[ks] = lq * ROWB + (((2 * ks + lh) ^ (lq & 15)) << 4);
-        const int r = 4 * (blk >> 1) + (i16 >> 2), c = 2 * (blk & 1) + ((i16 & 3) >> 1);
-        lo = r * ROWB + ((c ^ r) << 4) + (i16 & 1) * 8;
-        hi = (r + 8) * ROWB + ((c ^ (r + 8)) << 4) + (i16 & 1) * 8;
+            at[ks] = lq * ROWB + (((2 * ks + lh) ^ spread(lq)) << 4);
     }
-    __device__ __forceinline__ bf16x8_t rows(const unsigned char *tile, int ks) const { return *reinterpret_cast<const bf16x8_t *>(tile + row[ks]); }
-    __device__ __forceinline__ bf16x8_t transposed(const unsigned char *slice, int t) const
+    __device__ __forceinline__ void move(int bytes)
     {
-        const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(slice + (lo ^ (t << 6))));
-        const s16x4_t c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(slice + (hi ^ (t << 6))));
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+            at[ks] += bytes;
+            asm volatile("" : "+v"(at[ks]));
+        }
+    }
+    __device__ __forceinline__ bf16x8_t read(const unsigned char *lds, int off, int ks) const { return *reinterpret_cast<const bf16x8_t *>(lds + at[ks] + off); }
+};
+struct TransposedRead {                  // its transposed: rows 4 half + .. and 8 more of a slice of 16, feature tile t
+    int lo[DT], hi[DT];
+    __device__ __forceinline__ TransposedRead()
+    {
+        const int lane = threadIdx.x & 63, blk = lane >> 4, i16 = lane & 15;
+        const int r = 4 * (blk >> 1) + (i16 >> 2), c = 2 * (blk & 1) + ((i16 & 3) >> 1);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            lo[t] = r * ROWB + (((4 * t + c) ^ spread(r)) << 4) + (i16 & 1) * 8;
+            hi[t] = (r + 8) * ROWB + (((4 * t + c) ^ spread(r + 8)) << 4) + (i16 & 1) * 8;
+        }
+    }
+    __device__ __forceinline__ void move(int bytes)
+    {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            lo[t] += bytes;
+            hi[t] += bytes;
+            asm volatile("" : "+v"(lo[t]), "+v"(hi[t]));
+        }
+    }
+    __device__ __forceinline__ bf16x8_t read(const unsigned char *lds, int off, int t) const
+    {
+        const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(lds + lo[t] + off));
+        const s16x4_t c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(lds + hi[t] + off));
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
-// Split sums: N registers of every thread parked in the workspace, added up in split order by the workgroup that arrives last; false:
-// not this one.
-template <int N, int NT>
-__device__ __forceinline__ bool join_splits(float (&x)[N], const CausalParams &P, int group, int split, int splits, unsigned *arrived)
+// The exponentials of a unit, spread over the MFMAs that run meanwhile.  A wave issues in order and has the SIMD for itself, so that between
+// two MFMAs (32 cycles each) there is room for a handful of vector instructions, none of which should wait for the one before: element
+// e begins in segment 4 e / 3, and its three steps -- argument, exponential, products -- lie in three segments.
+template <int SEGMENT, typename F1, typename F2, typename F3>
+__device__ __forceinline__ void stages(F1 &&argument, F2 &&exponential, F3 &&product)
 {
-    constexpr int COHERENT = 1 | 16;
-    const int tid = threadIdx.x;
-    const size_t part = (size_t)N * NT;
-    auto rsrc = [&](int sp) {
-        return __builtin_amdgcn_make_buffer_rsrc(P.parts + ((size_t)group * P.max_splits + sp) * part, 0, (int)(part * 4), 0x00020000);
-    };
-    {
-        __amdgpu_buffer_rsrc_t rs = rsrc(split);
+    constexpr auto begins = [](int segment) { return segment >= 0 && segment <= 20 && segment % 4 != 3 ? segment - segment / 4 : -1; };
+    constexpr int e3 = begins(SEGMENT - 2), e2 = begins(SEGMENT - 1), e1 = begins(SEGMENT);
+    if constexpr (e3 >= 0)
+        product(std::integral_constant<int, e3>{});
+    if constexpr (e2 >= 0)
+        exponential(std::integral_constant<int, e2>{});
+    if constexpr (e1 >= 0)
+        argument(std::integral_constant<int, e1>{});
+}
+
+// A split's sums, N registers of every thread of the workgroup, sixteen (a feature tile) after sixteen; a launch of their own adds them up in
+// split order, eight or four workgroups a block, one a feature tile.  (The last workgroup to arrive adding up all by itself: 4096 tokens, 8
+// heads of one key head, 16 splits of 128 KiB: 575 us instead of TODO for dK and dV.)
+template <int NT>
+__device__ __forceinline__ float *part_of(const CausalParams &P, int regs, int group, int split, int tile)
+{
+    return P.parts + ((size_t)group * P.max_splits + split) * ((size_t)regs * NT) + ((size_t)tile * 16 * NT + threadIdx.x * 4);
+}
+template <int NT>
+__device__ __forceinline__ void park(const f32x16_t &x, float *at)
+{
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float v = x[i];
-            asm volatile("" : "+v"(v));      // (through a plain VGPR, as in the forward kernel)
-            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rs, (i * NT + tid) * 4, 0, COHERENT);
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4_t *>(at + q * 4 * NT) = f32x4_t{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+}
+template <int NT>
+__device__ __forceinline__ f32x16_t sum_of_parts(const CausalParams &P, int regs, int group, int splits, int tile)
+{
+    f32x16_t x = {};
+    constexpr int AT = 4;                // splits in flight (beyond the last: the last once more, unused)
+    for (int sp0 = 0; sp0 < splits; sp0 += AT) {
+        f32x4_t v[AT][4];
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            const float *at = part_of<NT>(P, regs, group, sp0 + k < splits ? sp0 + k : splits - 1, tile);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[k][q] = *reinterpret_cast<const f32x4_t *>(at + q * 4 * NT);
         }
+#pragma unroll
+        for (int k = 0; k < AT; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] += sp0 + k < splits ? v[k][e >> 2][e & 3] : 0.0f;
     }
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (tid == 0)
-        *arrived = __hip_atomic_fetch_add(&P.counters[group], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (*arrived != (unsigned)(splits - 1))
-        return false;
-    if (tid == 0)
-        __hip_atomic_store(&P.counters[group], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        x[i] = 0.0f;
-    for (int sp = 0; sp < splits; ++sp) {
-        __amdgpu_buffer_rsrc_t rs = rsrc(sp);
-        constexpr int AT = 64;
-#pragma unroll
-        for (int i0 = 0; i0 < N; i0 += AT) {
-            float v[AT];
-#pragma unroll
-            for (int i = 0; i < AT; ++i)
-                v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, ((i0 + i) * NT + tid) * 4, 0, COHERENT));
-#pragma unroll
-            for (int i = 0; i < AT; ++i)
-                x[i0 + i] += v[i];
-        }
-    }
-    return true;
+    return x;
 }
 
 __device__ __forceinline__ float wave_sum(float x)
@@ -119,23 +156,25 @@ __device__ __forceinline__ f32x2_t pair_at(const void *row)          // features
     const bf16x2_t v = static_cast<const bf16x2_t *>(row)[threadIdx.x & 63];
     return f32x2_t{(float)v[0], (float)v[1]};
 }
-__device__ __forceinline__ void put_pair(void *row, float a, float b)
+__device__ __forceinline__ void put_pair(void *row, float a, float b, int tile)     // (of a feature tile, or -1: of all)
 {
+    const int lane = threadIdx.x & 63;
     bf16x2_t v;
     v[0] = (__bf16)a;
     v[1] = (__bf16)b;
-    static_cast<bf16x2_t *>(row)[threadIdx.x & 63] = v;
+    if (tile < 0 || lane >> 4 == tile)
+        static_cast<bf16x2_t *>(row)[lane] = v;
 }
 
-// dQ of one row, key by key.
-__device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head, int first, float delta)
+// dQ of one row, key by key (all of it, or one feature tile).
+__device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head, int first, int tile)
 {
     const CausalParams &C = P.c;
     const int kvh = head / C.group;
     const __bf16 *K = static_cast<const __bf16 *>(C.K) + kvh * C.k_head, *V = static_cast<const __bf16 *>(C.V) + kvh * C.v_head;
     const f32x2_t q = pair_at(static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head);
     const f32x2_t g = pair_at(static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head);
-    const float lse = C.lse[(int64_t)head * C.lse_stride + t];
+    const float lse = C.lse[(int64_t)head * C.lse_stride + t], delta = P.delta[(int64_t)head * C.lse_stride + t];
     float a = 0.0f, b = 0.0f;
     for (int key = first; key <= t; ++key) {
         const f32x2_t k = pair_at(K + (int64_t)key * C.k_token), v = pair_at(V + (int64_t)key * C.v_token);
@@ -144,11 +183,11 @@ __device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head,
         a += ds * k[0];
         b += ds * k[1];
     }
-    put_pair(static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, a * C.scale, b * C.scale);
+    put_pair(static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, a * C.scale, b * C.scale, tile);
 }
 
-// dK and dV of one key, row by row.
-__device__ __forceinline__ void careful_key(const GradParams &P, int key, int kvh, int end)
+// dK and dV of one key, row by row (all of both, or a feature tile: 0 .. 3 of dK, 4 .. 7 of dV).
+__device__ __forceinline__ void careful_key(const GradParams &P, int key, int kvh, int end, int tile)
 {
     const CausalParams &C = P.c;
     const f32x2_t k = pair_at(static_cast<const __bf16 *>(C.K) + (int64_t)key * C.k_token + kvh * C.k_head);
@@ -166,30 +205,43 @@ __device__ __forceinline__ void careful_key(const GradParams &P, int key, int kv
             va += p * g[0];
             vb += p * g[1];
         }
-    put_pair(static_cast<__bf16 *>(P.dk) + (int64_t)key * C.k_token + kvh * C.k_head, ka * C.scale, kb * C.scale);
-    put_pair(static_cast<__bf16 *>(P.dv) + (int64_t)key * C.v_token + kvh * C.v_head, va, vb);
+    if (tile < 4)
+        put_pair(static_cast<__bf16 *>(P.dk) + (int64_t)key * C.k_token + kvh * C.k_head, ka * C.scale, kb * C.scale, tile);
+    if (tile < 0 || tile >= 4)
+        put_pair(static_cast<__bf16 *>(P.dv) + (int64_t)key * C.v_token + kvh * C.v_head, va, vb, tile < 0 ? -1 : tile - 4);
 }
 
-// A lane's row of a result X^T (feature tiles by registers), times `factor`, as bf16.  True if a value is not finite.
-__device__ __forceinline__ bool store_row(const float *x, float factor, __bf16 *row, bool there)
+// A lane's row of a feature tile of a result X^T, times `factor`, as bf16.  True if a value is not finite.
+__device__ __forceinline__ bool store_tile(const f32x16_t &x, float factor, __bf16 *row, int tile, bool there)
 {
     const int lh = (threadIdx.x & 63) >> 5;
     float odd = 0.0f;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int g = 0; g < 4; ++g) {
+        bf16x4_t h;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            bf16x4_t h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y = x[d * 16 + 4 * g + e] * factor;
-                odd = __builtin_fmaf(y, 0.0f, odd);
-                h[e] = (__bf16)y;
-            }
-            if (there)
-                *reinterpret_cast<u32x2_t *>(row + d * 32 + 8 * g + 4 * lh) = __builtin_bit_cast(u32x2_t, h);
+        for (int e = 0; e < 4; ++e) {
+            const float y = x[4 * g + e] * factor;
+            odd = __builtin_fmaf(y, 0.0f, odd);
+            h[e] = (__bf16)y;
         }
+        if (there)
+            *reinterpret_cast<u32x2_t *>(row + tile * 32 + 8 * g + 4 * lh) = __builtin_bit_cast(u32x2_t, h);
+    }
     return there && odd != 0.0f;
+}
+
+// f(lane) for every row (or key) of the wave that has a value that is not finite, once its first result is written.
+template <typename F>
+__device__ __forceinline__ void once_more(bool odd, F &&f)
+{
+    unsigned long long again = __builtin_amdgcn_ballot_w64(odd);
+    again = (again | again >> 32) & 0xFFFFFFFFull;
+    if (again != 0) {
+        __builtin_amdgcn_s_waitcnt(0);
+        for (; again != 0; again &= again - 1)
+            f(__builtin_ctzll(again));
+    }
 }
 
 // The sequence of token t, between two that enclose it: how many of starts[1 ..] are <= t.
@@ -205,51 +257,79 @@ __device__ __forceinline__ int sequence_between(const int32_t *starts, int a, in
     return a;
 }
 
-template <int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(GradParams P)
+// A workgroup's rows and walk, as in the forward kernel.
+constexpr int DQ_WAVES = 4, DQ_ROWS = DQ_WAVES * 32;
+struct RowBlock {
+    int t_base, t_last, row0, seq_a, seq_b, lo, hi, tiles, splits;   // splits 0: nothing to do
+    __device__ __forceinline__ RowBlock(const CausalParams &C, int block)
+    {
+        const int G = C.group;
+        splits = 0;
+        const int64_t r0 = (int64_t)block * DQ_ROWS, all = (int64_t)C.tokens * G, r1 = r0 + DQ_ROWS < all ? r0 + DQ_ROWS : all;
+        t_base = (int)(r0 / G);
+        t_last = (int)((r1 - 1) / G);
+        row0 = (int)(r0 - (int64_t)t_base * G);
+        seq_a = sequence_of(C.starts, C.n_seqs, t_base);
+        if (seq_a == C.n_seqs)
+            return;
+        seq_b = sequence_of(C.starts, C.n_seqs, t_last);
+        const int begin = C.starts[seq_a], stop = C.starts[C.n_seqs];
+        lo = begin < 0 ? 0 : begin;
+        hi = t_last + 1 < stop ? t_last + 1 : stop;
+        if (lo >= hi)
+            return;
+        tiles = (hi - lo + BKV - 1) / BKV;
+        int chunk = C.chunk;
+        if (chunk < 0)
+            chunk = chunk_by_work(C.n_seqs, C.num_cu, LEAST_TILES, [&](int i, float &work, float &blocks) {
+                const float m = (float)max(0, C.starts[i + 1] - C.starts[i]), here = m * G / DQ_ROWS * C.kv_heads;
+                blocks += here;
+                work += here * (0.5f * m / BKV + 0.5f);
+            });
+        splits = splits_of(tiles, chunk, C.max_splits);
+    }
+};
+struct DqRow {                           // a lane's row: token t sees keys first .. t
+    int t, head, first;
+    bool there;
+    __device__ __forceinline__ DqRow(const CausalParams &C, const RowBlock &B, int kvh)
+    {
+        const int r = B.row0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31), rt = r / C.group;
+        head = kvh * C.group + r - rt * C.group;
+        there = B.t_base + rt <= B.t_last;
+        t = B.t_base + (there ? rt : 0);
+        const int a = sequence_between(C.starts, B.seq_a, B.seq_b, t);
+        first = a < C.n_seqs ? C.starts[a] : t + 1;
+        there = there && first <= t;
+        first = there ? (first < 0 ? 0 : first) : t;                 // (a row of no sequence: any visible key will do, it is not stored)
+    }
+};
+
+__global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
-    constexpr int NT = 64 * NW, BQ = NW * 32;
+    constexpr int NW = DQ_WAVES, NT = 64 * NW;
     constexpr int LOADS = TILE_BYTES / 1024 / NW;                    // wave-loads per wave of a K or V tile: four rows each
     __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_BYTES];    // K, K, V, V
 
-    const int tid = threadIdx.x;
-    const int lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lq = lane & 31, lh = lane >> 5;
-    const int G = C.group;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lh = lane >> 5;
 
-    // Rows and walk as in the forward kernel
+    // (long blocks first, splits outermost: see the forward kernel)
     const int kvh = blockIdx.x % C.kv_heads;
     int rest = blockIdx.x / C.kv_heads;
     const int groups = gridDim.x / (unsigned)(C.kv_heads * C.max_splits);
     const int split = rest / groups;
-    rest -= split * groups;
-    const int64_t r0 = (int64_t)(groups - 1 - rest) * BQ;
-    const int64_t r1 = r0 + BQ < (int64_t)C.tokens * G ? r0 + BQ : (int64_t)C.tokens * G;
-    const int t_base = (int)(r0 / G), t_last = (int)((r1 - 1) / G), row0 = (int)(r0 - (int64_t)t_base * G);
-    const int seq_a = sequence_of(C.starts, C.n_seqs, t_base);
-    if (seq_a == C.n_seqs)
+    rest = groups - 1 - (rest - split * groups);
+    const RowBlock block(C, rest);
+    if (split >= block.splits)
         return;
-    const int seq_b = sequence_of(C.starts, C.n_seqs, t_last);
-    const int begin = C.starts[seq_a], stop = C.starts[C.n_seqs];
-    const int lo = begin < 0 ? 0 : begin, hi = t_last + 1 < stop ? t_last + 1 : stop;
-    if (lo >= hi)
-        return;
-    const int tiles = (hi - lo + BKV - 1) / BKV;
-    const int splits = C.chunk > 0 && tiles > C.chunk ? (tiles + C.chunk - 1) / C.chunk : 1;
-    if (split >= splits)
-        return;
-    const int kt0 = (int)(((int64_t)tiles * split) / splits), nkt = (int)(((int64_t)tiles * (split + 1)) / splits);
-
-    const int r = row0 + wave * 32 + lq;
-    const int rt = r / G, head = kvh * G + r - rt * G;
-    bool there = t_base + rt <= t_last;
-    const int t = t_base + (there ? rt : 0);
-    const int a = sequence_between(C.starts, seq_a, seq_b, t);
-    int first = a < C.n_seqs ? C.starts[a] : t + 1;
-    there = there && first <= t;
-    first = there ? (first < 0 ? 0 : first) : t;
+    const int lo = block.lo, hi = block.hi;
+    const int kt0 = (int)(((int64_t)block.tiles * split) / block.splits), nkt = (int)(((int64_t)block.tiles * (split + 1)) / block.splits);
+    const DqRow row(C, block, kvh);
+    const int t = row.t, head = row.head, first = row.first;
+    const bool there = row.there;
     int wt0 = kt0, wt1 = kt0, all_from, all_to;
     {
         int f_min = there ? first : 0x7FFFFFFF, f_max = there ? first : 0, l_min = there ? t : 0x7FFFFFFF, l_max = there ? t : -1;
@@ -273,7 +353,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(GradParams P)
     // Tile loads, straight into LDS
     const unsigned lds_base = lds_address(smem);
     const int ld_row = wave * 4 + (lane >> 4);
-    const unsigned swizzled = ((lane & 15) ^ (ld_row & 15)) << 4;
+    const unsigned swizzled = ((lane & 15) ^ spread(ld_row)) << 4;
     const unsigned k_off = (unsigned)((lane >> 4) * (int)(C.k_token * 2)) + swizzled, v_off = (unsigned)((lane >> 4) * (int)(C.v_token * 2)) + swizzled;
     const unsigned char *kb = static_cast<const unsigned char *>(C.K) + kvh * C.k_head * 2, *vb = static_cast<const unsigned char *>(C.V) + kvh * C.v_head * 2;
     auto issue = [&](int kt, const unsigned char *base, int64_t row_bytes, unsigned off, unsigned lds) __attribute__((always_inline)) {
@@ -308,7 +388,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(GradParams P)
         P.delta[(int64_t)head * C.lse_stride + t] = delta;
     const float sl2 = C.scale * LOG2E, lse2 = C.lse[(int64_t)head * C.lse_stride + t] * LOG2E;
 
-    const TileRead at;
+    RowRead row_read;
+    TransposedRead col_read;
     f32x16_t acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -328,15 +409,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(GradParams P)
             const bool border = kt * BKV < all_from || (kt + 1) * BKV - 1 > all_to;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {                            // 32 keys at a time
-                const unsigned char *kt_at = smem + b * TILE_BYTES + j * 32 * ROWB, *vt_at = smem + (2 + b) * TILE_BYTES + j * 32 * ROWB;
+                constexpr int V_AT = 2 * TILE_BYTES;
+                const int half = j * 32 * ROWB;
                 f32x16_t s, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     s[e] = dp[e] = 0.0f;
 #pragma unroll
                 for (int ks = 0; ks < DS; ++ks) {
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(kt_at, ks), qf[ks], s, 0, 0, 0);
-                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(vt_at, ks), gf[ks], dp, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, half, ks), qf[ks], s, 0, 0, 0);
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, V_AT + half, ks), gf[ks], dp, 0, 0, 0);
                 }
                 if (border) {
                     const unsigned key0 = (unsigned)(lo + kt * BKV + j * 32 + 4 * lh - first), span = (unsigned)(t - first);
@@ -355,88 +437,120 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_kernel(GradParams P)
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.transposed(kt_at + c * 16 * ROWB, d), df[c], acc[d], 0, 0, 0);
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_read.read(smem, half + c * 16 * ROWB, d), df[c], acc[d], 0, 0, 0);
             }
         }
         if (kt + 1 < nkt) {
+            row_read.move(b ? -TILE_BYTES : TILE_BYTES);
+            col_read.move(b ? -TILE_BYTES : TILE_BYTES);
             wait_vmcnt<0>();
             __syncthreads();
         }
     }
 
-    float x[DT * 16];
+    if (block.splits > 1) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            park<NT>(acc[d], part_of<NT>(C, DT * 16, rest * C.kv_heads + kvh, split, d));
+        return;
+    }
+    __bf16 *out = static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head;
+    bool odd = false;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            x[d * 16 + e] = acc[d][e];
-    if (splits > 1) {
-        __syncthreads();
-        if (!join_splits<DT * 16, NT>(x, C, rest * C.kv_heads + kvh, split, splits, reinterpret_cast<unsigned *>(smem)))
-            return;
-    }
-    const bool odd = store_row(x, C.scale, static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, there);
-    unsigned long long again = __builtin_amdgcn_ballot_w64(odd);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
-    if (again != 0) {
-        __builtin_amdgcn_s_waitcnt(0);                               // the row's first result is written before its second
-        for (; again != 0; again &= again - 1) {
-            const int l = __builtin_ctzll(again);
-            careful_dq(P, __shfl(t, l), __shfl(head, l), __shfl(first, l), __shfl(delta, l));
-        }
-    }
+        odd = store_tile(acc[d], C.scale, out, d, there) || odd;
+    once_more(odd, [&](int l) { careful_dq(P, __shfl(t, l), __shfl(head, l), __shfl(first, l), -1); });
+}
+
+__global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams P)
+{
+    const CausalParams &C = P.c;
+    const int tile = blockIdx.x % DT, group = blockIdx.x / DT, kvh = group % C.kv_heads;
+    const RowBlock block(C, group / C.kv_heads);
+    if (block.splits < 2)
+        return;
+    const DqRow row(C, block, kvh);
+    const f32x16_t x = sum_of_parts<64 * DQ_WAVES>(C, DT * 16, group, block.splits, tile);
+    const bool odd = store_tile(x, C.scale, static_cast<__bf16 *>(P.dq) + (int64_t)row.t * C.q_token + row.head * C.q_head, tile, row.there);
+    once_more(odd, [&](int l) { careful_dq(P, __shfl(row.t, l), __shfl(row.head, l), __shfl(row.first, l), tile); });
 }
 
 constexpr int GRAD_KEYS = 128;           // keys of a workgroup of the second launch: four waves of 32
+constexpr int GRAD_ROWS = 64;            // rows per tile
+// Its keys [begin, k1), and the walk over rows [lo, hi) = (token, head of the group), tokens [begin, end_b)
+struct KeyBlock {
+    int k0, k1, begin, seq_a, seq_b, end_b, lo, hi, tiles, splits;   // splits 0: nothing to do
+    __device__ __forceinline__ KeyBlock(const CausalParams &C, int block)
+    {
+        const int G = C.group, stop = C.starts[C.n_seqs] < C.tokens ? C.starts[C.n_seqs] : C.tokens;
+        splits = 0;
+        k0 = block * GRAD_KEYS;
+        k1 = k0 + GRAD_KEYS < stop ? k0 + GRAD_KEYS : stop;
+        begin = C.starts[0] > k0 ? C.starts[0] : k0;
+        if (begin >= k1)
+            return;
+        seq_a = sequence_of(C.starts, C.n_seqs, begin);
+        seq_b = sequence_of(C.starts, C.n_seqs, k1 - 1);
+        if (seq_b >= C.n_seqs)
+            return;
+        end_b = C.starts[seq_b + 1] < C.tokens ? C.starts[seq_b + 1] : C.tokens;
+        if (end_b <= begin)
+            return;
+        lo = begin * G;
+        hi = end_b * G;
+        tiles = (int)(((int64_t)hi - lo + GRAD_ROWS - 1) / GRAD_ROWS);
+        int chunk = C.chunk;
+        if (chunk < 0)
+            chunk = chunk_by_work(C.n_seqs, C.num_cu, LEAST_TILES, [&](int i, float &work, float &blocks) {
+                const float m = (float)max(0, C.starts[i + 1] - C.starts[i]), here = m / GRAD_KEYS * C.kv_heads;
+                blocks += here;
+                work += here * (0.5f * m * G / GRAD_ROWS + 0.5f);
+            });
+        splits = splits_of(tiles, chunk, C.max_splits);
+    }
+};
+struct GradKey {                         // a lane's key, seen by tokens key .. end - 1 of its sequence
+    int key, end;
+    bool there;
+    __device__ __forceinline__ GradKey(const CausalParams &C, const KeyBlock &B)
+    {
+        const int k = B.k0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
+        there = k >= B.begin && k < B.k1;
+        key = there ? k : B.begin;
+        const int a = sequence_between(C.starts, B.seq_a, B.seq_b, key);
+        end = a < C.n_seqs ? C.starts[a + 1] : 0;
+        end = end < B.end_b ? end : B.end_b;
+        there = there && end > key;
+    }
+};
 
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
-    constexpr int NT = 256, ROWS = 64;                               // rows per tile
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_BYTES];    // Q, Q, dout, dout
-    __shared__ __attribute__((aligned(16))) float stat[2][2][ROWS];  // buffer; lse, delta
-    __shared__ unsigned arrived;
+    constexpr int NT = 256, ROWS = GRAD_ROWS;
+    constexpr int NB = 4;                                            // tiles in LDS: two that are multiplied, two that land
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[NB * 2 * TILE_BYTES];   // Q, dout
+    __shared__ __attribute__((aligned(16))) float stat[NB][2][ROWS]; // lse, delta
 
-    const int tid = threadIdx.x;
-    const int lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lq = lane & 31, lh = lane >> 5;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lh = lane >> 5;
     const int G = C.group;
 
     const int kvh = blockIdx.x % C.kv_heads;
     int rest = blockIdx.x / C.kv_heads;
     const int groups = gridDim.x / (unsigned)(C.kv_heads * C.max_splits);
     const int split = rest / groups;
-    rest -= split * groups;
-    const int k0 = rest * GRAD_KEYS;                                 // (the first keys are seen by most rows)
-    const int stop = C.starts[C.n_seqs] < C.tokens ? C.starts[C.n_seqs] : C.tokens;
-    const int k1 = k0 + GRAD_KEYS < stop ? k0 + GRAD_KEYS : stop;
-    const int begin = C.starts[0] > k0 ? C.starts[0] : k0;
-    if (begin >= k1)
+    rest -= split * groups;                                          // (the first keys are seen by most rows)
+    const KeyBlock block(C, rest);
+    if (split >= block.splits)
         return;
-    const int seq_a = sequence_of(C.starts, C.n_seqs, begin), seq_b = sequence_of(C.starts, C.n_seqs, k1 - 1);
-    if (seq_b >= C.n_seqs)
-        return;
-    const int end_b = C.starts[seq_b + 1] < C.tokens ? C.starts[seq_b + 1] : C.tokens;
-    if (end_b <= begin)
-        return;
-    // The walk over rows [lo, hi) = (token, head of the group), tokens [begin, end_b)
-    const int lo = begin * G, hi = end_b * G;
-    const int tiles = (int)(((int64_t)hi - lo + ROWS - 1) / ROWS);
-    const int splits = C.chunk > 0 && tiles > C.chunk ? (tiles + C.chunk - 1) / C.chunk : 1;
-    if (split >= splits)
-        return;
-    const int rt0 = (int)(((int64_t)tiles * split) / splits), nrt = (int)(((int64_t)tiles * (split + 1)) / splits);
-
-    // The lane's key, seen by rows [from, to)
-    const int key = k0 + wave * 32 + lq;
-    bool there = key >= begin && key < k1;
-    const int kk = there ? key : begin;
-    const int a = sequence_between(C.starts, seq_a, seq_b, kk);
-    int end = a < C.n_seqs ? C.starts[a + 1] : 0;
-    end = end < end_b ? end : end_b;
-    there = there && end > kk;
-    const int from = kk * G, to = there ? end * G : from;
+    const int lo = block.lo, hi = block.hi, end_b = block.end_b;
+    const int rt0 = (int)(((int64_t)block.tiles * split) / block.splits), nrt = (int)(((int64_t)block.tiles * (split + 1)) / block.splits);
+    const GradKey mine(C, block);
+    const int kk = mine.key, end = mine.end;
+    const bool there = mine.there;
+    const int from = kk * G, to = there ? end * G : from;            // the rows that see it
     int wr0 = rt0, wr1 = rt0, all_from, all_to;
     {
         int f_min = there ? from : 0x7FFFFFFF, f_max = there ? from : 0, l_min = there ? to : 0x7FFFFFFF, l_max = there ? to : 0;
@@ -469,52 +583,81 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     }
 
     // Row loads: wave w takes rows 16 w + 4 j + (lane >> 4) of a tile, j = 0 .. 3, by four wave-loads of Q and of dout; wave 0 the 64
-    // lse, wave 1 the deltas.  Rows are (token, head) pairs that advance by 64 a tile.
-    const unsigned lds_base = lds_address(smem), stat_base = lds_address(stat);
+    // lse, wave 1 the deltas (and waves 2 and 3 the same once more, so that every wave has nine loads in flight).  Rows are (token, head) pairs that advance by 64 a tile: by step_t tokens and step_g
+    // heads, and where those run over by a token more and a group of heads less.
+    const unsigned lds_base = lds_address(smem), stat_base = lds_address(stat) + (wave & 1) * ROWS * 4;
     const int step_t = ROWS / G, step_g = ROWS - step_t * G;
-    struct Row {
-        int t, g;
-    };
-    auto row_at = [&](int row) __attribute__((always_inline)) {      // row of the walk, from lo on
-        Row x;
-        const int64_t at = (int64_t)lo + row;
-        x.t = (int)(at / G);
-        x.g = (int)(at - (int64_t)x.t * G);
-        return x;
-    };
-    auto advance = [&](Row &x) __attribute__((always_inline)) {
-        x.g += step_g;
-        x.t += step_t;
-        if (x.g >= G) {
-            x.g -= G;
-            x.t += 1;
-        }
-    };
-    Row rows[4], srow = row_at(rt0 * ROWS + lane);
+    const int64_t q_step = 2 * (step_t * C.q_token + step_g * C.q_head), q_wrap = q_step + 2 * (C.q_token - G * C.q_head);
+    const int64_t o_step = 2 * (step_t * C.o_token + step_g * C.o_head), o_wrap = o_step + 2 * (C.o_token - G * C.o_head);
+    const int64_t l_step = 4 * (step_t + step_g * C.lse_stride), l_wrap = l_step + 4 * (1 - G * C.lse_stride);
+    const char *qb = static_cast<const char *>(C.Q) + 2 * (int64_t)kvh * G * C.q_head, *gb = static_cast<const char *>(P.dout) + 2 * (int64_t)kvh * G * C.o_head;
+    const char *lb = reinterpret_cast<const char *>(((wave & 1) == 0 ? C.lse : P.delta) + (int64_t)kvh * G * C.lse_stride);
+    const int row_in = wave * 16 + (lane >> 4);                      // row inside a tile: row_in + 4 j; of the statistics: lane
+    const char *q_at[4], *g_at[4], *l_at;
+    int g_of[4], g_of_l;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        rows[j] = row_at(rt0 * ROWS + wave * 16 + j * 4 + (lane >> 4));
-    const __bf16 *qb = static_cast<const __bf16 *>(C.Q) + (int64_t)kvh * G * C.q_head, *gb = static_cast<const __bf16 *>(P.dout) + (int64_t)kvh * G * C.o_head;
-    const float *lb = C.lse + (int64_t)kvh * G * C.lse_stride, *db = P.delta + (int64_t)kvh * G * C.lse_stride;
-    auto issue = [&](int b) __attribute__((always_inline)) {         // the next tile: rows behind the walk are its last row
+    for (int j = 0; j < 5; ++j) {
+        const int64_t row = (int64_t)lo + (int64_t)rt0 * ROWS + (j < 4 ? row_in + 4 * j : lane), t = row / G;
+        const int g = (int)(row - t * G);
+        if (j < 4) {
+            const int chunk = ((lane & 15) ^ spread(j * 4 + (lane >> 4))) * 16;
+            q_at[j] = qb + 2 * (t * C.q_token + g * C.q_head) + chunk;
+            g_at[j] = gb + 2 * (t * C.o_token + g * C.o_head) + chunk;
+            g_of[j] = g;
+        } else {
+            l_at = lb + 4 * (t + g * C.lse_stride);
+            g_of_l = g;
+        }
+    }
+    int rows_left = hi - lo - rt0 * ROWS;                            // of the walk, from the next tile to load on
+    constexpr int LOADS = 9;                                         // of a wave and tile
+    auto issue = [&](int b) __attribute__((always_inline)) {         // the next tile
+        const char *q[4], *g[4], *l = l_at;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool in = rows[j].t < end_b;
-            const int64_t tt = in ? rows[j].t : end_b - 1, g = in ? rows[j].g : G - 1;
-            const int chunk = ((lane & 15) ^ ((j * 4 + (lane >> 4)) & 15)) * 8;
-            gather_load_16(qb + tt * C.q_token + g * C.q_head + chunk, lds_base + b * TILE_BYTES + wave * 4096 + j * 1024);
-            gather_load_16(gb + tt * C.o_token + g * C.o_head + chunk, lds_base + (2 + b) * TILE_BYTES + wave * 4096 + j * 1024);
-            advance(rows[j]);
+            q[j] = q_at[j];
+            g[j] = g_at[j];
         }
-        if (wave < 2) {
-            const bool in = srow.t < end_b;
-            const int64_t i = (in ? srow.g : G - 1) * C.lse_stride + (in ? srow.t : end_b - 1);
-            gather_load_4((wave == 0 ? lb : db) + i, stat_base + (b * 2 + wave) * ROWS * 4);
-            advance(srow);
+        if (rows_left < ROWS) {                                      // uniform: rows behind the walk are its last row
+            const int64_t q_last = 2 * ((end_b - 1) * C.q_token + (G - 1) * C.q_head), o_last = 2 * ((end_b - 1) * C.o_token + (G - 1) * C.o_head);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (row_in + 4 * j >= rows_left) {
+                    const int chunk = ((lane & 15) ^ spread(j * 4 + (lane >> 4))) * 16;
+                    q[j] = qb + q_last + chunk;
+                    g[j] = gb + o_last + chunk;
+                }
+            if (lane >= rows_left)
+                l = lb + 4 * ((int64_t)(end_b - 1) + (G - 1) * C.lse_stride);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            gather_load_16(q[j], lds_base + 2 * b * TILE_BYTES + wave * 4096 + j * 1024);
+            gather_load_16(g[j], lds_base + (2 * b + 1) * TILE_BYTES + wave * 4096 + j * 1024);
+        }
+        gather_load_4(l, stat_base + b * 2 * ROWS * 4);
+    };
+    // ... and to the one after it, in five pieces (four rows, the statistics) that find their place among the MFMAs
+    auto advance = [&](auto j_tag) __attribute__((always_inline)) {
+        constexpr int j = decltype(j_tag)::value;
+        int &g = j < 4 ? g_of[j & 3] : g_of_l;
+        g += step_g;
+        const bool over = g >= G;
+        g -= over ? G : 0;
+        if constexpr (j < 4) {
+            q_at[j] += over ? q_wrap : q_step;
+            g_at[j] += over ? o_wrap : o_step;
+            asm volatile("" : "+v"(q_at[j]), "+v"(g_at[j]), "+v"(g));
+        } else {
+            l_at += over ? l_wrap : l_step;
+            asm volatile("" : "+v"(l_at), "+v"(g));
+            rows_left -= ROWS;
         }
     };
+    auto advance_all = [&]() __attribute__((always_inline)) { each<0, 1>(advance, std::make_integer_sequence<int, 5>{}); };
 
-    const TileRead at;
+    RowRead row_read;
+    TransposedRead col_read;
     const float sl2 = C.scale * LOG2E;
     f32x16_t dk[DT], dv[DT];
 #pragma unroll
@@ -523,115 +666,279 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
         for (int e = 0; e < 16; ++e)
             dk[d][e] = dv[d][e] = 0.0f;
 
-    issue(0);
-    wait_vmcnt<0>();
-    __syncthreads();
-    for (int rt = rt0; rt < nrt; ++rt) {
-        const int b = (rt - rt0) & 1;
-        if (rt + 1 < nrt)
-            issue(1 - b);
-        if (rt >= wr0 && rt < wr1) {
-            const bool border = rt * ROWS < all_from || (rt + 1) * ROWS > all_to;
+    // A pipeline of one unit's depth, a unit being 32 rows: under the exponentials of unit u the products of unit u + 1 with K and V
+    // (segments 0 .. 15), and under the rest of them those of unit u with dout and Q (16 .. 31), one MFMA a segment, its fragment
+    // requested three segments ahead.
+    f32x4_t lse[4], del[4];                                          // of the unit's rows; -lse in units of log2(e)
+    auto stats = [&](int b, int j) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {                            // 32 rows at a time
-                const unsigned char *q_at = smem + b * TILE_BYTES + j * 32 * ROWB, *g_at = smem + (2 + b) * TILE_BYTES + j * 32 * ROWB;
-                f32x16_t s, dp;
+        for (int q = 0; q < 4; ++q) {
+            lse[q] = *reinterpret_cast<const f32x4_t *>(&stat[b][0][j * 32 + 8 * q + 4 * lh]);
+            del[q] = *reinterpret_cast<const f32x4_t *>(&stat[b][1][j * 32 + 8 * q + 4 * lh]);
+        }
+    };
+    auto products = [&](f32x16_t &s, f32x16_t &dp) __attribute__((always_inline)) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    s[e] = dp[e] = 0.0f;
+        for (int e = 0; e < 16; ++e)
+            s[e] = dp[e] = 0.0f;
 #pragma unroll
-                for (int ks = 0; ks < DS; ++ks) {
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(q_at, ks), kf[ks], s, 0, 0, 0);
-                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(g_at, ks), vf[ks], dp, 0, 0, 0);
-                }
-                if (border) {
-                    const unsigned row0 = (unsigned)(lo + rt * ROWS + j * 32 + 4 * lh - from), span = (unsigned)(to - from);
+        for (int ks = 0; ks < DS; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, 0, ks), kf[ks], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, TILE_BYTES, ks), vf[ks], dp, 0, 0, 0);
+        }
+    };
+    // unit (rt, J) from s, dp; the next, (bn, 1 - J), into sn, dpn.  row_read is at the next unit's tile, col_read at this one's.
+    auto unit = [&](int rt, int bn, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn, auto j_tag, auto next_tag) __attribute__((always_inline)) {
+        constexpr int J = decltype(j_tag)::value;
+        constexpr bool NEXT = decltype(next_tag)::value;
+        constexpr int FIRST = NEXT ? 0 : 16, AHEAD = 6, RING = 8;
+        constexpr int NOW = J * 32 * ROWB, THEN = (1 - J) * 32 * ROWB;
+        if (rt * ROWS < all_from || (rt + 1) * ROWS > all_to) {      // border tiles, uniform
+            float ninf = -INFINITY;
+            asm volatile("" : "+v"(ninf));
+            const unsigned row0 = (unsigned)(lo + rt * ROWS + J * 32 + 4 * lh - from), span = (unsigned)(to - from);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (row0 + (unsigned)(8 * (e >> 2) + (e & 3)) >= span)
-                            s[e] = -INFINITY;
-                }
-                bf16x8_t pf[2], df[2];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x4_t lse = *reinterpret_cast<const f32x4_t *>(&stat[b][0][j * 32 + 8 * q + 4 * lh]);
-                    const f32x4_t del = *reinterpret_cast<const f32x4_t *>(&stat[b][1][j * 32 + 8 * q + 4 * lh]);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int e = 4 * q + c;
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse[c] * LOG2E));
-                        pf[e >> 3][e & 7] = (__bf16)p;
-                        df[e >> 3][e & 7] = (__bf16)(p * (dp[e] - del[c]));
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.transposed(g_at + c * 16 * ROWB, d), pf[c], dv[d], 0, 0, 0);
-                        dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.transposed(q_at + c * 16 * ROWB, d), df[c], dk[d], 0, 0, 0);
-                    }
+            for (int e = 0; e < 16; ++e)
+                if (row0 + (unsigned)(8 * (e >> 2) + (e & 3)) >= span)
+                    s[e] = ninf;
+        }
+        bf16x8_t frag[RING], pf[2], df[2];
+        auto fetch = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(s_tag)::value;
+            if constexpr (i < 16)
+                frag[i % RING] = row_read.read(smem, THEN + (i & 1) * TILE_BYTES, i >> 1);
+            else if constexpr (i < 32)
+                frag[i % RING] = col_read.read(smem, NOW + (1 - (i & 1)) * TILE_BYTES + ((i - 16) >> 3) * 16 * ROWB, ((i - 16) >> 1) & 3);
+        };
+        float x[16];                                                 // arguments, then probabilities
+        auto argument = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            x[e] = __builtin_fmaf(s[e], sl2, lse[e >> 2][e & 3]);
+        };
+        auto exponential = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            x[e] = __builtin_amdgcn_exp2f(x[e]);
+            dp[e] -= del[e >> 2][e & 3];
+        };
+        auto product = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            dp[e] *= x[e];
+            if constexpr (e & 1) {                                   // rounded in pairs
+                pf[e >> 3][(e & 7) - 1] = (__bf16)x[e - 1];
+                pf[e >> 3][e & 7] = (__bf16)x[e];
+                df[e >> 3][(e & 7) - 1] = (__bf16)dp[e - 1];
+                df[e >> 3][e & 7] = (__bf16)dp[e];
             }
+        };
+        constexpr f32x16_t zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        auto segment = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(s_tag)::value;
+            fetch(std::integral_constant<int, i + AHEAD>{});
+            if constexpr (i < 16) {
+                if constexpr (i & 1)
+                    dpn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], vf[i >> 1], i < 2 ? zero : dpn, 0, 0, 0);
+                else
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], kf[i >> 1], i < 2 ? zero : sn, 0, 0, 0);
+            } else {
+                constexpr int c = (i - 16) >> 3, d = ((i - 16) >> 1) & 3;
+                if constexpr (i & 1)
+                    dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], df[c], dk[d], 0, 0, 0);
+                else
+                    dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], pf[c], dv[d], 0, 0, 0);
+            }
+            if constexpr (NEXT)
+                stages<i>(argument, exponential, product);
+            if constexpr (NEXT && i == 24)
+                stats(bn, 1 - J);
+            if constexpr (NEXT && i >= 28) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    lse[i - 28][c] *= -LOG2E;
+                asm volatile("" : "+v"(lse[i - 28]));                // (here, not where it is used)
+            }
+            if constexpr (J == 0 && i >= 23 && i < 28)
+                advance(std::integral_constant<int, i - 23>{});
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each<FIRST, 1>(fetch, std::make_integer_sequence<int, AHEAD>{});
+        if constexpr (!NEXT) {
+            each<0, 1>(argument, std::make_integer_sequence<int, 16>{});
+            each<0, 1>(exponential, std::make_integer_sequence<int, 16>{});
+            each<0, 1>(product, std::make_integer_sequence<int, 16>{});
         }
-        if (rt + 1 < nrt) {
-            wait_vmcnt<0>();
-            __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        each<FIRST, 1>(segment, std::make_integer_sequence<int, 32 - FIRST>{});
+    };
+
+    // (behind the walk's last tile rows are asked for once more, which nothing reads: the number of loads in flight stays the same)
+    issue(0);
+    advance_all();
+    issue(1);
+    advance_all();
+    issue(2);
+    advance_all();
+    wait_vmcnt<LOADS>();
+    __syncthreads();
+    f32x16_t sa, da, sb, db2;
+    int b = 0, rt = rt0;
+    auto next_of = [](int i) { return (i + 1) & (NB - 1); };
+    auto to_next = [&]() { return b == NB - 1 ? -2 * (NB - 1) * TILE_BYTES : 2 * TILE_BYTES; };
+    // Tiles rt and rt + 1 have landed, rt + 2 is on its way, rt + 3 goes over tile rt - 1, which every wave is done with.
+    auto load_ahead = [&]() __attribute__((always_inline)) { issue((b + 3) & (NB - 1)); };
+    auto turn = [&]() __attribute__((always_inline)) {
+        wait_vmcnt<LOADS>();
+        __syncthreads();
+        b = next_of(b);
+        ++rt;
+    };
+    using first = std::integral_constant<int, 0>;
+    using second = std::integral_constant<int, 1>;
+    if (wr0 < wr1) {
+        while (rt < wr0) {                                           // tiles of other waves only
+            load_ahead();
+            advance_all();
+            turn();
         }
+        row_read.move(2 * b * TILE_BYTES);
+        col_read.move(2 * b * TILE_BYTES);
+        products(sa, da);
+        stats(b, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                lse[q][c] *= -LOG2E;
+        while (rt + 1 < wr1) {
+            load_ahead();
+            unit(rt, b, sa, da, sb, db2, first{}, std::true_type{});
+            row_read.move(to_next());
+            unit(rt, next_of(b), sb, db2, sa, da, second{}, std::true_type{});
+            col_read.move(to_next());
+            turn();
+        }
+        load_ahead();
+        unit(rt, b, sa, da, sb, db2, first{}, std::true_type{});
+        unit(rt, b, sb, db2, sa, da, second{}, std::false_type{});
+        turn();
+    }
+    while (rt < nrt) {
+        load_ahead();
+        advance_all();
+        turn();
     }
 
-    float x[2 * DT * 16];
+    wait_vmcnt<0>();                                                 // (nothing lands behind the kernel's end)
+    if (block.splits > 1) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[d * 16 + e] = dk[d][e];
-            x[DT * 16 + d * 16 + e] = dv[d][e];
+        for (int d = 0; d < DT; ++d) {
+            park<NT>(dk[d], part_of<NT>(C, 2 * DT * 16, rest * C.kv_heads + kvh, split, d));
+            park<NT>(dv[d], part_of<NT>(C, 2 * DT * 16, rest * C.kv_heads + kvh, split, DT + d));
         }
-    if (splits > 1 && !join_splits<2 * DT * 16, NT>(x, C, rest * C.kv_heads + kvh, split, splits, &arrived))
         return;
-    const bool odd_k = store_row(x, C.scale, static_cast<__bf16 *>(P.dk) + (int64_t)kk * C.k_token + kvh * C.k_head, there);
-    const bool odd_v = store_row(x + DT * 16, 1.0f, static_cast<__bf16 *>(P.dv) + (int64_t)kk * C.v_token + kvh * C.v_head, there);
-    unsigned long long again = __builtin_amdgcn_ballot_w64(odd_k || odd_v);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
-    if (again != 0) {
-        __builtin_amdgcn_s_waitcnt(0);                               // the key's first result is written before its second
-        for (; again != 0; again &= again - 1) {
-            const int l = __builtin_ctzll(again);
-            careful_key(P, __shfl(kk, l), kvh, __shfl(end, l));
-        }
     }
+    __bf16 *out_k = static_cast<__bf16 *>(P.dk) + (int64_t)kk * C.k_token + kvh * C.k_head;
+    __bf16 *out_v = static_cast<__bf16 *>(P.dv) + (int64_t)kk * C.v_token + kvh * C.v_head;
+    bool odd = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        odd = store_tile(dk[d], C.scale, out_k, d, there) || odd;
+        odd = store_tile(dv[d], 1.0f, out_v, d, there) || odd;
+    }
+    once_more(odd, [&](int l) { careful_key(P, __shfl(kk, l), kvh, __shfl(end, l), -1); });
+}
+
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
+{
+    const CausalParams &C = P.c;
+    const int tile = blockIdx.x % (2 * DT), group = blockIdx.x / (2 * DT), kvh = group % C.kv_heads;
+    const KeyBlock block(C, group / C.kv_heads);
+    if (block.splits < 2)
+        return;
+    const GradKey mine(C, block);
+    const f32x16_t x = sum_of_parts<256>(C, 2 * DT * 16, group, block.splits, tile);
+    __bf16 *out = tile < DT ? static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head
+                            : static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head;
+    const bool odd = store_tile(x, tile < DT ? C.scale : 1.0f, out, tile & (DT - 1), mine.there);
+    once_more(odd, [&](int l) { careful_key(P, __shfl(mine.key, l), kvh, __shfl(mine.end, l), tile); });
+}
+
+}  // namespace
+
+namespace {
+
+// Splits of one of the two launches: `blocks` over all key heads, `tiles` of the longest walk, `part` bytes parked by a workgroup.
+void room_for_splits(CausalParams &p, int64_t blocks, int64_t tiles, size_t part, int most)
+{
+    const Tuning tn = tuning();
+    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
+    int64_t n = 1;
+    if (p.parts != nullptr && p.n_seqs <= 1024) {
+        const double rounds = ceil(1.25 * (double)blocks / p.num_cu), items = (rounds < 1 ? 1 : rounds) * p.num_cu - 0.5 * blocks;
+        double chunk = 0.5 * (double)tiles * blocks / items;
+        chunk = chunk < LEAST_TILES ? LEAST_TILES : chunk;
+        n = p.chunk > 0 ? (tiles + p.chunk - 1) / p.chunk : (int64_t)(1.25 * tiles / chunk + 1.0);
+        if (p.chunk < 0 && n > most)
+            n = most;
+        n = n > tiles ? tiles : n;
+        const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
+        n = n <= fit ? n : p.chunk > 0 ? 1 : fit;
+    }
+    p.max_splits = n < 2 ? 1 : (int)n;
+    if (p.max_splits == 1)
+        p.chunk = 0;
+}
+
+struct GradLaunches {
+    CausalParams dq, dkv;
+    int64_t row_blocks, key_blocks;      // of one key head
+    size_t dq_bytes, dkv_bytes;          // parked
+};
+GradLaunches plan_grad(const CausalParams &c, int num_cu)
+{
+    GradLaunches g;
+    g.dq = g.dkv = c;
+    g.dq.num_cu = g.dkv.num_cu = num_cu;
+    const int64_t rows = (int64_t)c.tokens * c.group;
+    g.row_blocks = (rows + DQ_WAVES * 32 - 1) / (DQ_WAVES * 32);
+    g.key_blocks = (c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
+    const size_t dq_part = (size_t)64 * 64 * DQ_WAVES * 4, dkv_part = (size_t)128 * 256 * 4;
+    room_for_splits(g.dq, g.row_blocks * c.kv_heads, (c.tokens + BKV - 1) / BKV, dq_part, 16);
+    room_for_splits(g.dkv, g.key_blocks * c.kv_heads, (rows + 63) / 64, dkv_part, 32);
+    g.dq_bytes = g.dq.max_splits > 1 ? (size_t)g.row_blocks * c.kv_heads * g.dq.max_splits * dq_part : 0;
+    g.dkv_bytes = g.dkv.max_splits > 1 ? (size_t)g.key_blocks * c.kv_heads * g.dkv.max_splits * dkv_part : 0;
+    return g;
 }
 
 }  // namespace
 
 hipError_t launch_attn_prompt_grad(const GradParams &p_in, hipStream_t s, int num_cu)
 {
-    const Tuning tn = tuning();
-    auto split = [&](CausalParams &c, int64_t groups, int tiles, size_t part) {
-        c.chunk = tn.causal_chunk;
-        c.max_splits = c.chunk > 0 ? (tiles + c.chunk - 1) / c.chunk : 1;
-        if (c.max_splits < 2 || c.parts == nullptr || groups > c.max_counters || (size_t)groups * c.max_splits * part > c.part_bytes) {
-            c.chunk = 0;
-            c.max_splits = 1;
-        }
-    };
+    const GradLaunches g = plan_grad(p_in.c, num_cu);
+    if ((g.row_blocks * (g.dq.max_splits + DT) + g.key_blocks * (g.dkv.max_splits + 2 * DT)) * p_in.c.kv_heads * 256 >= (int64_t)1 << 32)
+        return hipErrorInvalidValue;
     GradParams p = p_in;
-    const int64_t rows = (int64_t)p.c.tokens * p.c.group;
-    const int waves = tn.causal_waves == 8 ? 8 : 4;
-    const int64_t blocks = (rows + waves * 32 - 1) / (waves * 32);
-    split(p.c, blocks * p.c.kv_heads, (p.c.tokens + BKV - 1) / BKV, (size_t)64 * 64 * waves * 4);
-    const dim3 grid((unsigned)(blocks * p.c.kv_heads * p.c.max_splits));
-    if (waves == 8)
-        hipLaunchKernelGGL((attn_dq_kernel<8>), grid, dim3(512), 0, s, p);
-    else
-        hipLaunchKernelGGL((attn_dq_kernel<4>), grid, dim3(256), 0, s, p);
-    hipError_t e = hipGetLastError();
+    p.c = g.dq;
+    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)(g.row_blocks * p.c.kv_heads * p.c.max_splits)), dim3(64 * DQ_WAVES), 0, s, p);
+    if (p.c.max_splits > 1)
+        hipLaunchKernelGGL(attn_dq_join_kernel, dim3((unsigned)(g.row_blocks * p.c.kv_heads * DT)), dim3(64 * DQ_WAVES), 0, s, p);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    const int64_t key_blocks = (p.c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
-    split(p.c, key_blocks * p.c.kv_heads, (int)((rows + 63) / 64), (size_t)128 * 256 * 4);
-    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)(key_blocks * p.c.kv_heads * p.c.max_splits)), dim3(256), 0, s, p);
+    p.c = g.dkv;
+    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)(g.key_blocks * p.c.kv_heads * p.c.max_splits)), dim3(256), 0, s, p);
+    if (p.c.max_splits > 1)
+        hipLaunchKernelGGL(attn_dkv_join_kernel, dim3((unsigned)(g.key_blocks * p.c.kv_heads * 2 * DT)), dim3(256), 0, s, p);
     return hipGetLastError();
+}
+
+size_t attn_grad_part_bytes(const CausalParams &p_in, int num_cu)
+{
+    CausalParams p = p_in;                                           // as if any workspace were there
+    p.parts = reinterpret_cast<float *>(256);
+    p.part_bytes = ~(size_t)0 >> 1;
+    p.max_counters = 1 << 30;
+    const GradLaunches g = plan_grad(p, num_cu);
+    return g.dq_bytes > g.dkv_bytes ? g.dq_bytes : g.dkv_bytes;
 }
 
 }  // namespace cf

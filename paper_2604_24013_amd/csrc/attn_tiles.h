@@ -113,6 +113,35 @@ __device__ __forceinline__ int sequence_of(const int32_t *starts, int n, int t)
     return uniform(lo);
 }
 
+// Tiles that a split has at the most, for launches whose lengths only the tables on the device know: every workgroup adds up the work
+// of all sequences (`count` of them, tiles and blocks of sequence i by `of`) and comes to the same number.
+// Walks under a causal mask are of all lengths, and a launch takes as long as its longest compute unit; with ceil(tiles / chunk) splits of a
+// block a launch has about tiles / chunk + blocks / 2 workgroups.  So chunk is such that these are as many as fit the chip k times, k the
+// least that leaves three quarters of a workgroup per block over for whole chunks.  (Computed for one and eight heads, one sequence and
+// several, workgroups one by one on the compute units: within 10 % of the best chunk; 20 % more workgroups than fit cost up to 50 %.)
+template <typename F>
+__device__ __forceinline__ int chunk_by_work(int count, int num_cu, int least, F &&of)
+{
+    float tiles = 0.0f, blocks = 0.0f;
+    for (int i = threadIdx.x & 63; i < count; i += 64)
+        of(i, tiles, blocks);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        tiles += __shfl_xor(tiles, d);
+        blocks += __shfl_xor(blocks, d);
+    }
+    const float rounds = ceilf(1.25f * blocks / num_cu);
+    const float items = fmaxf(rounds, 1.0f) * num_cu - 0.5f * blocks;
+    return uniform(max(least, (int)ceilf(tiles / items)));
+}
+
+// Splits of a walk of `tiles` tiles.
+__device__ __forceinline__ int splits_of(int tiles, int chunk, int most)
+{
+    const int n = chunk > 0 && tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
+    return n < most ? n : most;
+}
+
 enum { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
 
 // Where a sequence's (or the pack's) keys lie, for single rows: the pointer of key `key` (nullptr: its page does not exist), and its

@@ -75,9 +75,10 @@ struct CausalParams {
     CachePool pool;
     const int32_t *kv_len, *table;
     int max_q, max_kv, max_pages;
-    // key tiles split over workgroups
-    int chunk = 0;                                  // tiles of a split at the most (0: all)
+    // a walk's tiles split over workgroups
+    int chunk = 0;                                  // tiles of a split at the most (0: all, -1: by the work that the tables hold)
     int max_splits = 1;
+    int num_cu = 0;
     float *parts = nullptr;
     unsigned *counters = nullptr;
     size_t part_bytes = 0;
@@ -97,6 +98,7 @@ struct GradParams {
 hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_cu);
 // Bytes of the partial results that the kernels park for their choice of splits.
 size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu);
+size_t attn_grad_part_bytes(const CausalParams &p, int num_cu);
 size_t attn_few_part_bytes(const CausalParams &p, int num_cu);
 size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu);
 
