@@ -63,6 +63,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     int seq_a = 0, seq_b = 0;
     const int32_t *table = nullptr;
     int row0;                                        // the block's first row, counted from token t_base
+    const Sequences seqs(P.starts, P.n_seqs);
     if constexpr (SRC == PACKED) {
         const int blocks = (int)(((int64_t)P.tokens * G + BQ - 1) / BQ);
         const int64_t r0 = (int64_t)(blocks - 1 - rest) * BQ;
@@ -71,11 +72,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         row0 = (int)(r0 - (int64_t)t_base * G);
         const int t_last = (int)((r1 - 1) / G);
         count = t_last - t_base + 1;
-        seq_a = sequence_of(P.starts, P.n_seqs, t_base);
+        seq_a = seqs.at(t_base);
         if (seq_a == P.n_seqs)
             return;                                  // behind the last sequence
-        seq_b = sequence_of(P.starts, P.n_seqs, t_last);
-        const int first = P.starts[seq_a], end = P.starts[P.n_seqs];
+        seq_b = seqs.at(t_last);
+        const int first = seqs.start_of(seq_a), end = seqs.end_of(P.n_seqs - 1);
         lo = first < 0 ? 0 : first;
         hi = t_last + 1 < end ? t_last + 1 : end;
         if (lo >= hi)
@@ -110,14 +111,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // This workgroup's key tiles: [kt0, nkt) of the block's
     const int tiles = (hi - lo + BKV - 1) / BKV;
     int chunk = P.chunk;
-    if (chunk < 0)
-        chunk = chunk_by_work(P.n_seqs, P.num_cu, LEAST_TILES, [&](int i, float &all, float &blocks) {
-            const int q0 = P.starts[i], q1 = P.starts[i + 1];
-            const float m = (float)max(0, q1 - q0), here = SRC == PACKED ? m * G / BQ : ceilf(fminf(m, (float)P.max_q) * G / BQ);
-            const float seen = SRC == PACKED ? 0.5f * m : fmaxf(0.0f, (float)min(P.kv_len[i], P.max_kv) - 0.5f * m);
-            blocks += here * P.kv_heads;
-            all += here * P.kv_heads * (seen / BKV + 0.5f);
-        });
+    if (chunk < 0) {
+        float all = 0.0f, blocks = 0.0f;
+        if constexpr (SRC == PACKED) {
+            seqs.lengths([&](float m) {
+                const float here = m * G / BQ * P.kv_heads;
+                blocks += here;
+                all += here * (0.5f * m / BKV + 0.5f);
+            });
+        } else {
+            for (int i = lane; i < P.n_seqs; i += 64) {
+                const float m = (float)max(0, P.starts[i + 1] - P.starts[i]), here = ceilf(fminf(m, (float)P.max_q) * G / BQ) * P.kv_heads;
+                blocks += here;
+                all += here * (fmaxf(0.0f, (float)min(P.kv_len[i], P.max_kv) - 0.5f * m) / BKV + 0.5f);
+            }
+        }
+        chunk = chunk_by_work(all, blocks, P.num_cu, LEAST_TILES);
+    }
     const int splits = splits_of(tiles, chunk, P.max_splits);
     if (split >= splits)
         return;
@@ -132,15 +142,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     int first = 0, last;
     if constexpr (SRC == PACKED) {
         const int t = t_base + (there ? token : 0);
-        int a = seq_a, b = seq_b;                    // how many of starts[1 ..] are <= t
-        while (a < b) {
-            const int mid = (a + b) >> 1;
-            if (P.starts[mid + 1] <= t)
-                a = mid + 1;
-            else
-                b = mid;
-        }
-        first = a < P.n_seqs ? P.starts[a] : t + 1;
+        int end;
+        const int a = seqs.between(seq_a, seq_b, t, &first, &end);
+        first = a < P.n_seqs ? first : t + 1;
         there = there && first <= t;
         first = there ? (first < 0 ? 0 : first) : t; // (a row of no sequence: any visible key will do, it is not stored)
         last = t;

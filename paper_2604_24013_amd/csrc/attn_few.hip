@@ -58,12 +58,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     const int hi = n - m + (rows - 1) / G + 1 > 0 ? n - m + (rows - 1) / G + 1 : 0;   // keys that the last row sees
     const int tiles = (hi + FEW_KEYS - 1) / FEW_KEYS;
     int chunk = P.chunk;
-    if (chunk < 0)
-        chunk = chunk_by_work(P.n_seqs, P.num_cu, NW, [&](int x, float &all, float &blocks) {
+    if (chunk < 0) {
+        float all = 0.0f, blocks = 0.0f;
+        for (int x = lane; x < P.n_seqs; x += 64) {
             const int len = min(P.kv_len[x], P.max_kv);
             blocks += len > 0 ? P.kv_heads : 0;
             all += (float)max(0, (len + FEW_KEYS - 1) / FEW_KEYS) * P.kv_heads;
-        });
+        }
+        chunk = chunk_by_work(all, blocks, P.num_cu, NW);
+    }
     const int splits = splits_of(tiles, chunk, P.max_splits);
     if (split >= splits)
         return;

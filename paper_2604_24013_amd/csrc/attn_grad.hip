@@ -244,24 +244,12 @@ __device__ __forceinline__ void once_more(bool odd, F &&f)
     }
 }
 
-// The sequence of token t, between two that enclose it: how many of starts[1 ..] are <= t.
-__device__ __forceinline__ int sequence_between(const int32_t *starts, int a, int b, int t)
-{
-    while (a < b) {
-        const int mid = (a + b) >> 1;
-        if (starts[mid + 1] <= t)
-            a = mid + 1;
-        else
-            b = mid;
-    }
-    return a;
-}
-
 // A workgroup's rows and walk, as in the forward kernel.
 constexpr int DQ_WAVES = 4, DQ_ROWS = DQ_WAVES * 32;
 struct RowBlock {
+    Sequences seqs;
     int t_base, t_last, row0, seq_a, seq_b, lo, hi, tiles, splits;   // splits 0: nothing to do
-    __device__ __forceinline__ RowBlock(const CausalParams &C, int block)
+    __device__ __forceinline__ RowBlock(const CausalParams &C, int block) : seqs(C.starts, C.n_seqs)
     {
         const int G = C.group;
         splits = 0;
@@ -269,23 +257,26 @@ struct RowBlock {
         t_base = (int)(r0 / G);
         t_last = (int)((r1 - 1) / G);
         row0 = (int)(r0 - (int64_t)t_base * G);
-        seq_a = sequence_of(C.starts, C.n_seqs, t_base);
+        seq_a = seqs.at(t_base);
         if (seq_a == C.n_seqs)
             return;
-        seq_b = sequence_of(C.starts, C.n_seqs, t_last);
-        const int begin = C.starts[seq_a], stop = C.starts[C.n_seqs];
+        seq_b = seqs.at(t_last);
+        const int begin = seqs.start_of(seq_a), stop = seqs.end_of(C.n_seqs - 1);
         lo = begin < 0 ? 0 : begin;
         hi = t_last + 1 < stop ? t_last + 1 : stop;
         if (lo >= hi)
             return;
         tiles = (hi - lo + BKV - 1) / BKV;
         int chunk = C.chunk;
-        if (chunk < 0)
-            chunk = chunk_by_work(C.n_seqs, C.num_cu, LEAST_TILES, [&](int i, float &work, float &blocks) {
-                const float m = (float)max(0, C.starts[i + 1] - C.starts[i]), here = m * G / DQ_ROWS * C.kv_heads;
+        if (chunk < 0) {
+            float work = 0.0f, blocks = 0.0f;
+            seqs.lengths([&](float m) {
+                const float here = m * G / DQ_ROWS * C.kv_heads;
                 blocks += here;
                 work += here * (0.5f * m / BKV + 0.5f);
             });
+            chunk = chunk_by_work(work, blocks, C.num_cu, LEAST_TILES);
+        }
         splits = splits_of(tiles, chunk, C.max_splits);
     }
 };
@@ -298,8 +289,9 @@ struct DqRow {                           // a lane's row: token t sees keys firs
         head = kvh * C.group + r - rt * C.group;
         there = B.t_base + rt <= B.t_last;
         t = B.t_base + (there ? rt : 0);
-        const int a = sequence_between(C.starts, B.seq_a, B.seq_b, t);
-        first = a < C.n_seqs ? C.starts[a] : t + 1;
+        int end;
+        const int a = B.seqs.between(B.seq_a, B.seq_b, t, &first, &end);
+        first = a < C.n_seqs ? first : t + 1;
         there = there && first <= t;
         first = there ? (first < 0 ? 0 : first) : t;                 // (a row of no sequence: any visible key will do, it is not stored)
     }
@@ -479,33 +471,37 @@ constexpr int GRAD_KEYS = 128;           // keys of a workgroup of the second la
 constexpr int GRAD_ROWS = 64;            // rows per tile
 // Its keys [begin, k1), and the walk over rows [lo, hi) = (token, head of the group), tokens [begin, end_b)
 struct KeyBlock {
+    Sequences seqs;
     int k0, k1, begin, seq_a, seq_b, end_b, lo, hi, tiles, splits;   // splits 0: nothing to do
-    __device__ __forceinline__ KeyBlock(const CausalParams &C, int block)
+    __device__ __forceinline__ KeyBlock(const CausalParams &C, int block) : seqs(C.starts, C.n_seqs)
     {
-        const int G = C.group, stop = C.starts[C.n_seqs] < C.tokens ? C.starts[C.n_seqs] : C.tokens;
+        const int G = C.group, last = seqs.end_of(C.n_seqs - 1), stop = last < C.tokens ? last : C.tokens;
         splits = 0;
         k0 = block * GRAD_KEYS;
         k1 = k0 + GRAD_KEYS < stop ? k0 + GRAD_KEYS : stop;
-        begin = C.starts[0] > k0 ? C.starts[0] : k0;
+        begin = seqs.start_of(0) > k0 ? seqs.start_of(0) : k0;
         if (begin >= k1)
             return;
-        seq_a = sequence_of(C.starts, C.n_seqs, begin);
-        seq_b = sequence_of(C.starts, C.n_seqs, k1 - 1);
+        seq_a = seqs.at(begin);
+        seq_b = seqs.at(k1 - 1);
         if (seq_b >= C.n_seqs)
             return;
-        end_b = C.starts[seq_b + 1] < C.tokens ? C.starts[seq_b + 1] : C.tokens;
+        end_b = seqs.end_of(seq_b) < C.tokens ? seqs.end_of(seq_b) : C.tokens;
         if (end_b <= begin)
             return;
         lo = begin * G;
         hi = end_b * G;
         tiles = (int)(((int64_t)hi - lo + GRAD_ROWS - 1) / GRAD_ROWS);
         int chunk = C.chunk;
-        if (chunk < 0)
-            chunk = chunk_by_work(C.n_seqs, C.num_cu, LEAST_TILES, [&](int i, float &work, float &blocks) {
-                const float m = (float)max(0, C.starts[i + 1] - C.starts[i]), here = m / GRAD_KEYS * C.kv_heads;
+        if (chunk < 0) {
+            float work = 0.0f, blocks = 0.0f;
+            seqs.lengths([&](float m) {
+                const float here = m / GRAD_KEYS * C.kv_heads;
                 blocks += here;
                 work += here * (0.5f * m * G / GRAD_ROWS + 0.5f);
             });
+            chunk = chunk_by_work(work, blocks, C.num_cu, LEAST_TILES);
+        }
         splits = splits_of(tiles, chunk, C.max_splits);
     }
 };
@@ -517,8 +513,9 @@ struct GradKey {                         // a lane's key, seen by tokens key .. 
         const int k = B.k0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
         there = k >= B.begin && k < B.k1;
         key = there ? k : B.begin;
-        const int a = sequence_between(C.starts, B.seq_a, B.seq_b, key);
-        end = a < C.n_seqs ? C.starts[a + 1] : 0;
+        int start;
+        const int a = B.seqs.between(B.seq_a, B.seq_b, key, &start, &end);
+        end = a < C.n_seqs ? end : 0;
         end = end < B.end_b ? end : B.end_b;
         there = there && end > key;
     }
@@ -597,8 +594,9 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     int g_of[4], g_of_l;
 #pragma unroll
     for (int j = 0; j < 5; ++j) {
-        const int64_t row = (int64_t)lo + (int64_t)rt0 * ROWS + (j < 4 ? row_in + 4 * j : lane), t = row / G;
-        const int g = (int)(row - t * G);
+        const unsigned row = (unsigned)(lo + rt0 * ROWS + (j < 4 ? row_in + 4 * j : lane));
+        const int64_t t = row / (unsigned)G;
+        const int g = (int)(row - (unsigned)t * G);
         if (j < 4) {
             const int chunk = ((lane & 15) ^ spread(j * 4 + (lane >> 4))) * 16;
             q_at[j] = qb + 2 * (t * C.q_token + g * C.q_head) + chunk;

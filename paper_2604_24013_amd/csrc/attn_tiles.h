@@ -98,33 +98,73 @@ __device__ __forceinline__ float sum_of_halves(float x)
     return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
-// How many of starts[1 .. n] are <= t, for a wave-uniform t: sixty-four probes at a time.
-__device__ __forceinline__ int sequence_of(const int32_t *starts, int n, int t)
-{
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-        const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && starts[1 + (i < hi ? i : lo)] <= t));
-        const int end = lo + c * step;
-        hi = c == 0 ? lo : hi < end ? hi : end;
-        lo = c == 0 ? lo : end - step + 1;
+// The packed sequences' starts, as every wave needs them: up to 64 sequences from one load, a start a lane; more from memory.
+struct Sequences {
+    const int32_t *starts;
+    int n, first, mine;                  // starts[0]; starts[1 + lane] (behind the last: 2^31 - 1)
+    __device__ __forceinline__ Sequences(const int32_t *s, int count) : starts(s), n(count)
+    {
+        const int lane = threadIdx.x & 63;
+        first = s[0];
+        mine = lane < n ? s[1 + lane] : 0x7FFFFFFF;
     }
-    return uniform(lo);
-}
+    // starts[1 + i], i wave-uniform, in [0, n)
+    __device__ __forceinline__ int end_of(int i) const { return n <= 64 ? __builtin_amdgcn_readlane(mine, i) : uniform(starts[1 + i]); }
+    __device__ __forceinline__ int start_of(int i) const { return i == 0 ? uniform(first) : end_of(i - 1); }
+    // how many of starts[1 ..] are <= t, for a wave-uniform t: sixty-four probes at a time
+    __device__ __forceinline__ int at(int t) const
+    {
+        if (n <= 64)
+            return __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine <= t));
+        const int lane = threadIdx.x & 63;
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+            const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && starts[1 + (i < hi ? i : lo)] <= t));
+            const int end = lo + c * step;
+            hi = c == 0 ? lo : hi < end ? hi : end;
+            lo = c == 0 ? lo : end - step + 1;
+        }
+        return uniform(lo);
+    }
+    // ... for a t of the lane's own, between two answers that enclose it (every lane takes part), and that sequence's two ends
+    __device__ __forceinline__ int between(int a, int b, int t, int *start, int *end) const
+    {
+        while (__builtin_amdgcn_ballot_w64(a < b) != 0) {
+            const int mid = (a + b) >> 1, s = n <= 64 ? __shfl(mine, mid & 63) : starts[1 + (mid < n ? mid : n - 1)];
+            if (a < b) {
+                if (s <= t)
+                    a = mid + 1;
+                else
+                    b = mid;
+            }
+        }
+        const int i = a < n ? a : n - 1;
+        const int before = n <= 64 ? __shfl(mine, i > 0 ? i - 1 : 0) : starts[i];
+        *end = n <= 64 ? __shfl(mine, i) : starts[1 + i];
+        *start = i > 0 ? before : first;
+        return a;
+    }
+    // f(length, tiles, blocks) over all sequences, a lane's share
+    template <typename F>
+    __device__ __forceinline__ void lengths(F &&f) const
+    {
+        const int lane = threadIdx.x & 63, before = __shfl_up(mine, 1);
+        if (lane < n)
+            f((float)max(0, mine - (lane > 0 ? before : first)));
+        for (int i = lane + 64; i < n; i += 64)
+            f((float)max(0, starts[i + 1] - starts[i]));
+    }
+};
 
 // Tiles that a split has at the most, for launches whose lengths only the tables on the device know: every workgroup adds up the work
-// of all sequences (`count` of them, tiles and blocks of sequence i by `of`) and comes to the same number.
+// of all sequences (a lane's share of it: `tiles` in `blocks`) and comes to the same number.
 // Walks under a causal mask are of all lengths, and a launch takes as long as its longest compute unit; with ceil(tiles / chunk) splits of a
 // block a launch has about tiles / chunk + blocks / 2 workgroups.  So chunk is such that these are as many as fit the chip k times, k the
 // least that leaves three quarters of a workgroup per block over for whole chunks.  (Computed for one and eight heads, one sequence and
 // several, workgroups one by one on the compute units: within 10 % of the best chunk; 20 % more workgroups than fit cost up to 50 %.)
-template <typename F>
-__device__ __forceinline__ int chunk_by_work(int count, int num_cu, int least, F &&of)
+__device__ __forceinline__ int chunk_by_work(float tiles, float blocks, int num_cu, int least)
 {
-    float tiles = 0.0f, blocks = 0.0f;
-    for (int i = threadIdx.x & 63; i < count; i += 64)
-        of(i, tiles, blocks);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         tiles += __shfl_xor(tiles, d);
