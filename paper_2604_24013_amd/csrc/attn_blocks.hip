@@ -50,13 +50,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     const int lq = lane & 31, lh = lane >> 5;
     const int G = P.group;
 
-    // neighbouring workgroups (one per XCD in turn) take different key heads; long blocks first; splits, of which short blocks have fewer,
-    // outermost: dealt out innermost, the missing ones would always be the same XCDs'
-    const int kvh = blockIdx.x % P.kv_heads;
-    int rest = blockIdx.x / P.kv_heads;
-    const int groups = gridDim.x / (unsigned)(P.kv_heads * P.max_splits);
-    const int split = rest / groups;
-    rest -= split * groups;
+    int kvh, rest, split;
+    my_block(P, &kvh, &rest, &split);                // (long blocks first)
 
     // The block's rows: tokens [t0, ..) of `count`, and the walk over keys [lo, hi).
     int t_base, count, lo, hi, shown = 0;            // shown: keys that token t_base sees, less one (paged)

@@ -308,12 +308,9 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lh = lane >> 5;
 
-    // (long blocks first, splits outermost: see the forward kernel)
-    const int kvh = blockIdx.x % C.kv_heads;
-    int rest = blockIdx.x / C.kv_heads;
-    const int groups = gridDim.x / (unsigned)(C.kv_heads * C.max_splits);
-    const int split = rest / groups;
-    rest = groups - 1 - (rest - split * groups);
+    int kvh, rest, split;
+    my_block(C, &kvh, &rest, &split);
+    rest = (int)(gridDim.x / (unsigned)(C.kv_heads * C.max_splits)) - 1 - rest;          // long blocks first
     const RowBlock block(C, rest);
     if (split >= block.splits)
         return;
@@ -534,11 +531,8 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int lh = lane >> 5;
     const int G = C.group;
 
-    const int kvh = blockIdx.x % C.kv_heads;
-    int rest = blockIdx.x / C.kv_heads;
-    const int groups = gridDim.x / (unsigned)(C.kv_heads * C.max_splits);
-    const int split = rest / groups;
-    rest -= split * groups;                                          // (the first keys are seen by most rows)
+    int kvh, rest, split;
+    my_block(C, &kvh, &rest, &split);                                // (the first keys are seen by most rows)
     const KeyBlock block(C, rest);
     if (split >= block.splits)
         return;
@@ -686,10 +680,9 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
         }
     };
     // unit (rt, J) from s, dp; the next, (bn, 1 - J), into sn, dpn.  row_read is at the next unit's tile, col_read at this one's.
-    auto unit = [&](int rt, int bn, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn, auto j_tag, auto next_tag) __attribute__((always_inline)) {
+    auto unit = [&](int rt, int bn, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn, auto j_tag) __attribute__((always_inline)) {
         constexpr int J = decltype(j_tag)::value;
-        constexpr bool NEXT = decltype(next_tag)::value;
-        constexpr int FIRST = NEXT ? 0 : 16, AHEAD = 6, RING = 8;
+        constexpr int AHEAD = 6, RING = 8;
         constexpr int NOW = J * 32 * ROWB, THEN = (1 - J) * 32 * ROWB;
         if (rt * ROWS < all_from || (rt + 1) * ROWS > all_to) {      // border tiles, uniform
             float ninf = -INFINITY;
@@ -744,11 +737,10 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
                 else
                     dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], pf[c], dv[d], 0, 0, 0);
             }
-            if constexpr (NEXT)
-                stages<i>(argument, exponential, product);
-            if constexpr (NEXT && i == 24)
+            stages<i>(argument, exponential, product);
+            if constexpr (i == 24)
                 stats(bn, 1 - J);
-            if constexpr (NEXT && i >= 28) {
+            if constexpr (i >= 28) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     lse[i - 28][c] *= -LOG2E;
@@ -758,14 +750,9 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
                 advance(std::integral_constant<int, i - 23>{});
             __builtin_amdgcn_sched_barrier(0);
         };
-        each<FIRST, 1>(fetch, std::make_integer_sequence<int, AHEAD>{});
-        if constexpr (!NEXT) {
-            each<0, 1>(argument, std::make_integer_sequence<int, 16>{});
-            each<0, 1>(exponential, std::make_integer_sequence<int, 16>{});
-            each<0, 1>(product, std::make_integer_sequence<int, 16>{});
-        }
+        each<0, 1>(fetch, std::make_integer_sequence<int, AHEAD>{});
         __builtin_amdgcn_sched_barrier(0);
-        each<FIRST, 1>(segment, std::make_integer_sequence<int, 32 - FIRST>{});
+        each<0, 1>(segment, std::make_integer_sequence<int, 32>{});
     };
 
     // (behind the walk's last tile rows are asked for once more, which nothing reads: the number of loads in flight stays the same)
@@ -806,18 +793,14 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 lse[q][c] *= -LOG2E;
-        while (rt + 1 < wr1) {
+        while (rt < wr1) {                                           // (behind the last tile the products of one more, unused: half the code)
             load_ahead();
-            unit(rt, b, sa, da, sb, db2, first{}, std::true_type{});
+            unit(rt, b, sa, da, sb, db2, first{});
             row_read.move(to_next());
-            unit(rt, next_of(b), sb, db2, sa, da, second{}, std::true_type{});
+            unit(rt, next_of(b), sb, db2, sa, da, second{});
             col_read.move(to_next());
             turn();
         }
-        load_ahead();
-        unit(rt, b, sa, da, sb, db2, first{}, std::true_type{});
-        unit(rt, b, sb, db2, sa, da, second{}, std::false_type{});
-        turn();
     }
     while (rt < nrt) {
         load_ahead();

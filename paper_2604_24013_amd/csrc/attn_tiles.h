@@ -170,8 +170,8 @@ __device__ __forceinline__ int chunk_by_work(float tiles, float blocks, int num_
         tiles += __shfl_xor(tiles, d);
         blocks += __shfl_xor(blocks, d);
     }
-    const float rounds = ceilf(1.25f * blocks / num_cu);
-    const float items = fmaxf(rounds, 1.0f) * num_cu - 0.5f * blocks;
+    const float rounds = ceilf(1.36f * blocks / num_cu);
+    const float items = 0.92f * fmaxf(rounds, 1.0f) * num_cu - 0.5f * blocks;    // (not one too many)
     return uniform(max(least, (int)ceilf(tiles / items)));
 }
 
@@ -180,6 +180,17 @@ __device__ __forceinline__ int splits_of(int tiles, int chunk, int most)
 {
     const int n = chunk > 0 && tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
     return n < most ? n : most;
+}
+
+// Which block and split a workgroup takes: key heads innermost (neighbouring workgroups go to one XCD in turn, whose L2 then holds few
+// heads' keys), splits outermost, so that those that short blocks do not have come last, and turned by five blocks from split to
+// split, so that they are not always the same XCDs' (32 blocks of 1 to 14 splits: 36 of 238 workgroups on one XCD's 32 compute units, now 30).
+__device__ __forceinline__ void my_block(const CausalParams &P, int *kvh, int *block, int *split)
+{
+    const int blocks = gridDim.x / (unsigned)(P.kv_heads * P.max_splits), rest = blockIdx.x / P.kv_heads;
+    *kvh = blockIdx.x - rest * P.kv_heads;
+    *split = rest / blocks;
+    *block = (int)((unsigned)(rest - *split * blocks + 5 * *split) % (unsigned)blocks);
 }
 
 enum { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
