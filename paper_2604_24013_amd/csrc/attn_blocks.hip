@@ -50,82 +50,82 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     const int lq = lane & 31, lh = lane >> 5;
     const int G = P.group;
 
-    int kvh, rest, split;
-    my_block(P, &kvh, &rest, &split);                // (long blocks first)
-
-    // The block's rows: tokens [t0, ..) of `count`, and the walk over keys [lo, hi).
-    int t_base, count, lo, hi, shown = 0;            // shown: keys that token t_base sees, less one (paged)
-    int seq_a = 0, seq_b = 0;
-    const int32_t *table = nullptr;
-    int row0;                                        // the block's first row, counted from token t_base
+    const int blocks = (int)(((SRC == PACKED ? (int64_t)P.tokens : (int64_t)P.max_q) * G + BQ - 1) / BQ);    // (paged: of one sequence)
     const Sequences seqs(P.starts, P.n_seqs);
+    // A block's rows (tokens t_base .. t_last from row row0 of the first on) and walk over keys [lo, hi)
+    struct Walk {
+        int t_base, t_last, row0, lo, hi, shown;     // shown: keys that token t_base sees, less one (paged)
+        const int32_t *table;
+        bool any;
+    };
+    auto walk_of = [&](int block) {                  // of the lane's block; packed: but for lo
+        Walk w;
+        w.any = false;
+        w.lo = w.shown = 0;
+        w.table = nullptr;
+        if constexpr (SRC == PACKED) {
+            const int64_t r0 = (int64_t)(blocks - 1 - block) * BQ, all = (int64_t)P.tokens * G, r1 = r0 + BQ < all ? r0 + BQ : all;   // long blocks first
+            w.t_base = (int)((unsigned)r0 / (unsigned)G);
+            w.row0 = (int)(r0 - (int64_t)w.t_base * G);
+            w.t_last = (int)((unsigned)(r1 - 1) / (unsigned)G);
+            const int stop = seqs.end_of(P.n_seqs - 1);
+            w.hi = w.t_last + 1 < stop ? w.t_last + 1 : stop;
+            w.any = true;
+        } else {
+            const int seq = block % P.n_seqs, nth = blocks - 1 - block / P.n_seqs;
+            const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
+            const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens, m = to - from;
+            int n = P.kv_len[seq];
+            n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
+            const int rows = m < P.max_q ? m : P.max_q;              // rows behind max_q are left as they were
+            const int64_t r0 = (int64_t)nth * BQ, all = (int64_t)rows * G, r1 = r0 + BQ < all ? r0 + BQ : all;
+            w.any = r0 < all;
+            const int b0 = (int)((unsigned)r0 / (unsigned)G);
+            w.row0 = (int)(r0 - (int64_t)b0 * G);
+            const int last = w.any ? (int)((unsigned)(r1 - 1) / (unsigned)G) : 0;
+            w.t_base = from + b0;
+            w.t_last = from + last;
+            w.shown = n - m + b0;
+            w.hi = n - m + last + 1 > 0 ? n - m + last + 1 : 0;
+            w.table = P.table + (int64_t)seq * P.max_pages;
+        }
+        return w;
+    };
+    Item it;
+    const int all_blocks = SRC == PACKED ? blocks : blocks * P.n_seqs;
+    if (!my_item(P, all_blocks, LEAST_TILES, [&](int block) {
+            Walk w = walk_of(block);
+            if constexpr (SRC == PACKED) {
+                int end;
+                seqs.around(w.t_base, &w.lo, &end);
+                w.lo = w.lo < 0 ? 0 : w.lo;
+                return w.lo < w.hi ? (w.hi - w.lo + BKV - 1) / BKV : 0;
+            } else {
+                return w.any ? max(1, (w.hi + BKV - 1) / BKV) : 0;
+            }
+        }, &it))
+        return;
+    const int kvh = it.kvh, split = it.split, splits = it.splits;
+    const Walk walk = walk_of(it.block);
+    const int t_base = uniform(walk.t_base), t_last = uniform(walk.t_last), row0 = uniform(walk.row0), hi = uniform(walk.hi), shown = uniform(walk.shown);
+    const int count = t_last - t_base + 1;
+    const int32_t *table = uniform(walk.table);
+    int lo = 0, seq_a = 0, seq_b = 0;
     if constexpr (SRC == PACKED) {
-        const int blocks = (int)(((int64_t)P.tokens * G + BQ - 1) / BQ);
-        const int64_t r0 = (int64_t)(blocks - 1 - rest) * BQ;
-        const int64_t r1 = r0 + BQ < (int64_t)P.tokens * G ? r0 + BQ : (int64_t)P.tokens * G;
-        t_base = (int)(r0 / G);
-        row0 = (int)(r0 - (int64_t)t_base * G);
-        const int t_last = (int)((r1 - 1) / G);
-        count = t_last - t_base + 1;
         seq_a = seqs.at(t_base);
         if (seq_a == P.n_seqs)
             return;                                  // behind the last sequence
         seq_b = seqs.at(t_last);
-        const int first = seqs.start_of(seq_a), end = seqs.end_of(P.n_seqs - 1);
-        lo = first < 0 ? 0 : first;
-        hi = t_last + 1 < end ? t_last + 1 : end;
+        lo = seqs.start_of(seq_a);
+        lo = lo < 0 ? 0 : lo;
         if (lo >= hi)
             return;
-    } else {
-        const int blocks = (int)(((int64_t)P.max_q * G + BQ - 1) / BQ);
-        const int seq = rest % P.n_seqs, block = blocks - 1 - rest / P.n_seqs;
-        const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
-        const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens;
-        int m = to - from;
-        int n = P.kv_len[seq];
-        n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
-        const int64_t room = (int64_t)P.max_pages << P.pool.page_shift;
-        n = n < room ? n : (int)room;
-        const int rows = m < P.max_q ? m : P.max_q;  // rows behind max_q are left as they were
-        const int64_t r0 = (int64_t)block * BQ;
-        if (r0 >= (int64_t)rows * G)
-            return;
-        const int b0 = (int)(r0 / G);
-        row0 = (int)(r0 - (int64_t)b0 * G);
-        const int64_t r1 = r0 + BQ < (int64_t)rows * G ? r0 + BQ : (int64_t)rows * G;
-        const int last = (int)((r1 - 1) / G);
-        t_base = from + b0;
-        count = last - b0 + 1;
-        shown = n - m + b0;
-        lo = 0;
-        hi = n - m + last + 1;
-        hi = hi < 0 ? 0 : hi;
-        table = P.table + (int64_t)seq * P.max_pages;
+    } else if (__builtin_amdgcn_readfirstlane(walk.any) == 0) {
+        return;
     }
 
     // This workgroup's key tiles: [kt0, nkt) of the block's
     const int tiles = (hi - lo + BKV - 1) / BKV;
-    int chunk = P.chunk;
-    if (chunk < 0) {
-        float all = 0.0f, blocks = 0.0f;
-        if constexpr (SRC == PACKED) {
-            seqs.lengths([&](float m) {
-                const float here = m * G / BQ * P.kv_heads;
-                blocks += here;
-                all += here * (0.5f * m / BKV + 0.5f);
-            });
-        } else {
-            for (int i = lane; i < P.n_seqs; i += 64) {
-                const float m = (float)max(0, P.starts[i + 1] - P.starts[i]), here = ceilf(fminf(m, (float)P.max_q) * G / BQ) * P.kv_heads;
-                blocks += here;
-                all += here * (fmaxf(0.0f, (float)min(P.kv_len[i], P.max_kv) - 0.5f * m) / BKV + 0.5f);
-            }
-        }
-        chunk = chunk_by_work(all, blocks, P.num_cu, LEAST_TILES);
-    }
-    const int splits = splits_of(tiles, chunk, P.max_splits);
-    if (split >= splits)
-        return;
     const int kt0 = (int)(((int64_t)tiles * split) / splits);
     const int nkt = (int)(((int64_t)tiles * (split + 1)) / splits);
 
@@ -562,9 +562,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         constexpr int COHERENT = 1 | 16;
         constexpr int NV = DT * 16 + (LSE ? 3 : 2);                  // floats per thread
         const size_t part = (size_t)NV * NT;
-        const int group = rest * P.kv_heads + kvh;
+        const int group = it.block * P.kv_heads + kvh;
         auto part_rsrc = [&](int sp) {
-            return __builtin_amdgcn_make_buffer_rsrc(P.parts + ((size_t)group * P.max_splits + sp) * part, 0, (int)(part * 4), 0x00020000);
+            return __builtin_amdgcn_make_buffer_rsrc(parked_at(P, it, sp, part), 0, (int)(part * 4), 0x00020000);
         };
         {
             __amdgpu_buffer_rsrc_t rs = part_rsrc(split);
@@ -675,9 +675,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 }
 
 template <int NW, int SRC>
-hipError_t launch(const CausalParams &p, int64_t groups, hipStream_t s)
+hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
 {
-    const int64_t wgs = groups * p.max_splits;
     if (wgs * 64 * NW >= ((int64_t)1 << 32))
         return hipErrorInvalidValue;
     if (p.lse != nullptr)
@@ -689,62 +688,54 @@ hipError_t launch(const CausalParams &p, int64_t groups, hipStream_t s)
 
 size_t part_bytes(int waves) { return (size_t)(64 + 3) * (64 * waves) * sizeof(float); }
 
-// Splits that the grid has room for: what one sequence as long as all tokens needs, twice over for several shorter ones.  `tiles`: of the
-// longest walk, `blocks`: of rows, over all key heads.
-int room_for_splits(const CausalParams &p, int64_t blocks, int64_t tiles, size_t part)
-{
-    if (p.parts == nullptr || blocks > p.max_counters || p.n_seqs > 1024 || blocks < 1)
-        return 1;
-    const double rounds = ceil(1.25 * (double)blocks / p.num_cu), items = (rounds < 1 ? 1 : rounds) * p.num_cu - 0.5 * blocks;
-    double chunk = 0.5 * (double)tiles * blocks / items;
-    chunk = chunk < 4 ? 4 : chunk;
-    int64_t n = (int64_t)(2.0 * tiles / chunk + 1.0);
-    n = n > 16 ? 16 : n;
-    n = n > tiles ? tiles : n;
-    const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
-    n = n > fit ? fit : n;
-    return n < 2 ? 1 : (int)n;
-}
-
-// Four waves (128 rows) or eight, and the room for splits.
-int choose_blocks(CausalParams &p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
+// Four waves (128 rows) or eight; the launch's workgroups.
+int choose_blocks(CausalParams &p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu, int64_t *wgs)
 {
     const Tuning tn = tuning();
-    p.num_cu = num_cu;
     const int waves = tn.causal_waves ? tn.causal_waves : 4;
-    const int64_t blocks = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads * sequences;
-    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
-    if (p.chunk > 0) {
-        const int64_t n = (tiles + p.chunk - 1) / p.chunk;
-        p.max_splits = n < 2 || p.parts == nullptr || blocks > p.max_counters || (size_t)blocks * n * part_bytes(waves) > p.part_bytes ? 1 : (int)n;
-    } else {
-        p.max_splits = room_for_splits(p, blocks, tiles, part_bytes(waves));
-    }
-    if (p.max_splits == 1)
-        p.chunk = 0;
+    *wgs = plan_items(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, part_bytes(waves), true, num_cu);
     return waves;
 }
 
 }  // namespace
 
+int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part, bool counted, int num_cu)
+{
+    const Tuning tn = tuning();
+    const int64_t all = blocks * p.kv_heads;
+    p.items = p.chunk = 0;
+    if (p.parts == nullptr || blocks > 512 || p.n_seqs > 64 || (counted && all > p.max_counters) || longest < 2)
+        return all;
+    const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);
+    int64_t items = tn.causal_chunk ? all * ((longest + tn.causal_chunk - 1) / tn.causal_chunk) : (rounds > 1 ? rounds : 1) * num_cu / p.kv_heads * p.kv_heads;
+    if (items > fit) {
+        if (tn.causal_chunk)
+            return all;
+        items = fit / p.kv_heads * p.kv_heads;
+    }
+    if (items <= all)
+        return all;
+    p.items = (int)items;
+    p.chunk = tn.causal_chunk;
+    return items;
+}
+
 hipError_t launch_attn_prompt(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    const int64_t rows = (int64_t)p.tokens * p.group;
-    const int waves = choose_blocks(p, rows, 1, (p.tokens + BKV - 1) / BKV, num_cu);
-    const int64_t groups = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads;
-    return waves == 8 ? launch<8, PACKED>(p, groups, s) : launch<4, PACKED>(p, groups, s);
+    int64_t wgs;
+    const int waves = choose_blocks(p, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu, &wgs);
+    return waves == 8 ? launch<8, PACKED>(p, wgs, s) : launch<4, PACKED>(p, wgs, s);
 }
 
 hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    const int64_t rows = (int64_t)p.max_q * p.group;
-    const int waves = choose_blocks(p, rows, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
-    const int64_t groups = (rows + waves * 32 - 1) / (waves * 32) * p.kv_heads * p.n_seqs;
+    int64_t wgs;
+    const int waves = choose_blocks(p, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu, &wgs);
     if (p.pool.e4m3)
-        return waves == 8 ? launch<8, PAGED_E4M3>(p, groups, s) : launch<4, PAGED_E4M3>(p, groups, s);
-    return waves == 8 ? launch<8, PAGED_BF16>(p, groups, s) : launch<4, PAGED_BF16>(p, groups, s);
+        return waves == 8 ? launch<8, PAGED_E4M3>(p, wgs, s) : launch<4, PAGED_E4M3>(p, wgs, s);
+    return waves == 8 ? launch<8, PAGED_BF16>(p, wgs, s) : launch<4, PAGED_BF16>(p, wgs, s);
 }
 
 namespace {
@@ -752,11 +743,11 @@ namespace {
 size_t part_bytes_of(CausalParams p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
 {
     p.parts = reinterpret_cast<float *>(256);
-    p.part_bytes = ~(size_t)0 >> 1;
+    p.part_bytes = (size_t)1 << 48;
     p.max_counters = 1 << 30;
-    const int waves = choose_blocks(p, rows, sequences, tiles, num_cu);
-    const size_t blocks = (size_t)((rows + waves * 32 - 1) / (waves * 32)) * p.kv_heads * sequences;
-    return p.max_splits > 1 ? blocks * p.max_splits * part_bytes(waves) : 0;
+    int64_t wgs;
+    const int waves = choose_blocks(p, rows, sequences, tiles, num_cu, &wgs);
+    return p.items > 0 ? (size_t)p.items * part_bytes(waves) : 0;
 }
 }  // namespace
 

@@ -40,9 +40,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     const int i = lane & 15, gq = lane >> 4;
     const int G = P.group;
 
-    const int kvh = blockIdx.x % P.kv_heads;
-    int rest = blockIdx.x / P.kv_heads;
-    const int seq = rest % P.n_seqs, split = rest / P.n_seqs;
+    // Keys that a sequence's last row sees, over all of which its waves walk
+    auto keys_of = [&](int seq) {
+        const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
+        const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens, m = to - from, some = m < P.max_q ? m : P.max_q;
+        int n = P.kv_len[seq];
+        n = (n < 0 ? 0 : n < P.max_kv ? n : P.max_kv) - m + some;
+        return some <= 0 ? -1 : n > 0 ? n : 0;
+    };
+    Item it;
+    if (!my_item(P, P.n_seqs, NW, [&](int seq) {
+            const int keys = keys_of(seq);
+            return keys < 0 ? 0 : max(1, (keys + FEW_KEYS - 1) / FEW_KEYS);
+        }, &it))
+        return;
+    const int kvh = it.kvh, seq = it.block, split = it.split, splits = it.splits;
     const int group = seq * P.kv_heads + kvh;
 
     const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
@@ -50,26 +62,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     const int m = to - from;                                         // rows of the sequence
     int n = P.kv_len[seq];
     n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
-    const int64_t room = (int64_t)P.max_pages << P.pool.page_shift;
-    n = n < room ? n : (int)room;
     const int rows = (m < P.max_q ? m : P.max_q) * G;                // at most 16 QT
     if (rows <= 0)
         return;
     const int hi = n - m + (rows - 1) / G + 1 > 0 ? n - m + (rows - 1) / G + 1 : 0;   // keys that the last row sees
     const int tiles = (hi + FEW_KEYS - 1) / FEW_KEYS;
-    int chunk = P.chunk;
-    if (chunk < 0) {
-        float all = 0.0f, blocks = 0.0f;
-        for (int x = lane; x < P.n_seqs; x += 64) {
-            const int len = min(P.kv_len[x], P.max_kv);
-            blocks += len > 0 ? P.kv_heads : 0;
-            all += (float)max(0, (len + FEW_KEYS - 1) / FEW_KEYS) * P.kv_heads;
-        }
-        chunk = chunk_by_work(all, blocks, P.num_cu, NW);
-    }
-    const int splits = splits_of(tiles, chunk, P.max_splits);
-    if (split >= splits)
-        return;
     const int t0 = (int)(((int64_t)tiles * split) / splits), t1 = (int)(((int64_t)tiles * (split + 1)) / splits);
 
     const int32_t *table = P.table + (int64_t)seq * P.max_pages;
@@ -298,7 +295,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
 
     // Merge the waves, one row tile at a time; a thread takes four features of a row.
     const int64_t row_floats = DH + 4;                               // a parked row: O, m, l, e
-    float *mine = P.parts == nullptr ? nullptr : P.parts + ((size_t)group * P.max_splits + split) * (QT * ROWS) * row_floats;
+    float *mine = P.parts == nullptr ? nullptr : parked_at(P, it, split, (size_t)QT * ROWS * row_floats);
     constexpr int COHERENT = 1 | 16;
     auto finish_row = [&](int r, int c, const f32x4_t &o, float mm, float l, float e) __attribute__((always_inline)) {
         const int token = r / G, head = kvh * G + r - token * G;
@@ -381,7 +378,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
             return;
         if (tid == 0)
             __hip_atomic_store(&P.counters[group], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const float *base = P.parts + (size_t)group * P.max_splits * (QT * ROWS) * row_floats;
         const int bytes = (int)(QT * ROWS * row_floats * 4);
         for (int u = tid; u < rows * 32; u += NT) {
             const int row = u >> 5, c = u & 31;
@@ -393,7 +389,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
 #pragma unroll
                 for (int k = 0; k < AT; ++k) {
                     const int sp = sp0 + k < splits ? sp0 + k : splits - 1;
-                    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(base + (size_t)sp * (QT * ROWS) * row_floats), 0, bytes, 0x00020000);
+                    const auto rs = __builtin_amdgcn_make_buffer_rsrc(parked_at(P, it, sp, (size_t)QT * ROWS * row_floats), 0, bytes, 0x00020000);
                     st[k] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((row * row_floats + DH) * 4), 0, COHERENT));
                     x[k] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((row * row_floats + c * 4) * 4), 0, COHERENT));
                 }
@@ -447,9 +443,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
 }
 
 template <int NW, int QT>
-hipError_t launch(const CausalParams &p, hipStream_t s)
+hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
 {
-    const int64_t wgs = (int64_t)p.n_seqs * p.kv_heads * p.max_splits;
     if (wgs * 64 * NW >= ((int64_t)1 << 32))
         return hipErrorInvalidValue;
     if (p.pool.e4m3)
@@ -459,51 +454,36 @@ hipError_t launch(const CausalParams &p, hipStream_t s)
     return hipGetLastError();
 }
 
+int choose_few(CausalParams &p, int num_cu, int64_t *wgs, size_t *part)          // 16-row tiles; the launch's workgroups
+{
+    const int qt = p.max_q * p.group <= 16 ? 1 : 2;
+    *part = (size_t)(qt * 16) * (DH + 4) * sizeof(float);
+    *wgs = plan_items(p, p.n_seqs, (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, *part, true, num_cu);
+    return qt;
+}
+
 }  // namespace
 
 bool attn_few_takes(const CausalParams &p) { return (int64_t)p.max_q * p.group <= 32; }
 
-namespace {
-int choose_few(CausalParams &p, int num_cu)          // 16-row tiles; the room for splits
-{
-    const int rows = p.max_q * p.group, qt = rows <= 16 ? 1 : 2;
-    const int64_t tiles = (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, blocks = (int64_t)p.n_seqs * p.kv_heads;
-    const size_t part = (size_t)(qt * 16) * (DH + 4) * sizeof(float);
-    const Tuning tn = tuning();
-    p.num_cu = num_cu;
-    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
-    int64_t n = 1;
-    if (p.parts != nullptr && blocks <= p.max_counters && p.n_seqs <= 1024) {
-        const double rounds = ceil(1.25 * (double)blocks / num_cu), items = (rounds < 1 ? 1 : rounds) * num_cu - 0.5 * blocks;
-        double chunk = (double)tiles * blocks / items;       // all contexts as long as the longest ...
-        chunk = chunk < 8 ? 8 : chunk;
-        n = p.chunk > 0 ? (tiles + p.chunk - 1) / p.chunk : (int64_t)(3.0 * tiles / chunk + 1.0);    // ... or one of them, by far
-        if (p.chunk < 0 && n > 64)
-            n = 64;
-        const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
-        n = n <= fit ? n : p.chunk > 0 ? 1 : fit;
-    }
-    p.max_splits = n < 2 ? 1 : (int)n;
-    if (p.max_splits == 1)
-        p.chunk = 0;
-    return qt;
-}
-}  // namespace
-
 hipError_t launch_attn_few(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
-    return choose_few(p, num_cu) == 1 ? launch<8, 1>(p, s) : launch<8, 2>(p, s);
+    int64_t wgs;
+    size_t part;
+    return choose_few(p, num_cu, &wgs, &part) == 1 ? launch<8, 1>(p, wgs, s) : launch<8, 2>(p, wgs, s);
 }
 
 size_t attn_few_part_bytes(const CausalParams &p_in, int num_cu)
 {
     CausalParams p = p_in;                                           // as if any workspace were there
     p.parts = reinterpret_cast<float *>(256);
-    p.part_bytes = ~(size_t)0 >> 1;
+    p.part_bytes = (size_t)1 << 48;
     p.max_counters = 1 << 30;
-    const int qt = choose_few(p, num_cu);
-    return p.max_splits > 1 ? (size_t)p.n_seqs * p.kv_heads * p.max_splits * (qt * 16) * (DH + 4) * sizeof(float) : 0;
+    int64_t wgs;
+    size_t part;
+    choose_few(p, num_cu, &wgs, &part);
+    return (size_t)p.items * part;
 }
 
 }  // namespace cf

@@ -110,9 +110,9 @@ __device__ __forceinline__ void stages(F1 &&argument, F2 &&exponential, F3 &&pro
 // split order, eight or four workgroups a block, one a feature tile.  (The last workgroup to arrive adding up all by itself: 4096 tokens, 8
 // heads of one key head, 16 splits of 128 KiB: 575 us instead of TODO for dK and dV.)
 template <int NT>
-__device__ __forceinline__ float *part_of(const CausalParams &P, int regs, int group, int split, int tile)
+__device__ __forceinline__ float *part_of(const CausalParams &P, int regs, const Item &it, int split, int tile)
 {
-    return P.parts + ((size_t)group * P.max_splits + split) * ((size_t)regs * NT) + ((size_t)tile * 16 * NT + threadIdx.x * 4);
+    return parked_at(P, it, split, (size_t)regs * NT) + ((size_t)tile * 16 * NT + threadIdx.x * 4);
 }
 template <int NT>
 __device__ __forceinline__ void park(const f32x16_t &x, float *at)
@@ -122,15 +122,16 @@ __device__ __forceinline__ void park(const f32x16_t &x, float *at)
         *reinterpret_cast<f32x4_t *>(at + q * 4 * NT) = f32x4_t{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
 }
 template <int NT>
-__device__ __forceinline__ f32x16_t sum_of_parts(const CausalParams &P, int regs, int group, int splits, int tile)
+__device__ __forceinline__ f32x16_t sum_of_parts(const CausalParams &P, int regs, const Item &it, int tile)
 {
+    const int splits = it.splits;
     f32x16_t x = {};
     constexpr int AT = 4;                // splits in flight (beyond the last: the last once more, unused)
     for (int sp0 = 0; sp0 < splits; sp0 += AT) {
         f32x4_t v[AT][4];
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            const float *at = part_of<NT>(P, regs, group, sp0 + k < splits ? sp0 + k : splits - 1, tile);
+            const float *at = part_of<NT>(P, regs, it, sp0 + k < splits ? sp0 + k : splits - 1, tile);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 v[k][q] = *reinterpret_cast<const f32x4_t *>(at + q * 4 * NT);
@@ -247,37 +248,39 @@ __device__ __forceinline__ void once_more(bool odd, F &&f)
 // A workgroup's rows and walk, as in the forward kernel.
 constexpr int DQ_WAVES = 4, DQ_ROWS = DQ_WAVES * 32;
 struct RowBlock {
-    Sequences seqs;
-    int t_base, t_last, row0, seq_a, seq_b, lo, hi, tiles, splits;   // splits 0: nothing to do
-    __device__ __forceinline__ RowBlock(const CausalParams &C, int block) : seqs(C.starts, C.n_seqs)
+    const Sequences seqs;
+    int blocks;                          // of one key head
+    Item it;
+    int t_base, t_last, row0, seq_a, seq_b, lo, hi, tiles;
+    __device__ __forceinline__ void rows_of(const CausalParams &C, int block, int *base, int *row, int *last) const
     {
-        const int G = C.group;
-        splits = 0;
-        const int64_t r0 = (int64_t)block * DQ_ROWS, all = (int64_t)C.tokens * G, r1 = r0 + DQ_ROWS < all ? r0 + DQ_ROWS : all;
-        t_base = (int)(r0 / G);
-        t_last = (int)((r1 - 1) / G);
-        row0 = (int)(r0 - (int64_t)t_base * G);
+        const int64_t r0 = (int64_t)(blocks - 1 - block) * DQ_ROWS, all = (int64_t)C.tokens * C.group, r1 = r0 + DQ_ROWS < all ? r0 + DQ_ROWS : all;   // long blocks first
+        *base = (int)((unsigned)r0 / (unsigned)C.group);
+        *row = (int)(r0 - (int64_t)*base * C.group);
+        *last = (int)((unsigned)(r1 - 1) / (unsigned)C.group);
+    }
+    __device__ __forceinline__ int tiles_of(const CausalParams &C, int block) const
+    {
+        int base, row, last, start, end;
+        rows_of(C, block, &base, &row, &last);
+        seqs.around(base, &start, &end);
+        const int stop = seqs.end_of(C.n_seqs - 1), from = start < 0 ? 0 : start, to = last + 1 < stop ? last + 1 : stop;
+        return from < to ? (to - from + BKV - 1) / BKV : 0;
+    }
+    __device__ __forceinline__ RowBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((int)(((int64_t)C.tokens * C.group + DQ_ROWS - 1) / DQ_ROWS)) {}
+    // the rows and the walk of it.block; false: nothing to do
+    __device__ __forceinline__ bool look(const CausalParams &C)
+    {
+        rows_of(C, it.block, &t_base, &row0, &t_last);
         seq_a = seqs.at(t_base);
         if (seq_a == C.n_seqs)
-            return;
+            return false;
         seq_b = seqs.at(t_last);
         const int begin = seqs.start_of(seq_a), stop = seqs.end_of(C.n_seqs - 1);
         lo = begin < 0 ? 0 : begin;
         hi = t_last + 1 < stop ? t_last + 1 : stop;
-        if (lo >= hi)
-            return;
         tiles = (hi - lo + BKV - 1) / BKV;
-        int chunk = C.chunk;
-        if (chunk < 0) {
-            float work = 0.0f, blocks = 0.0f;
-            seqs.lengths([&](float m) {
-                const float here = m * G / DQ_ROWS * C.kv_heads;
-                blocks += here;
-                work += here * (0.5f * m / BKV + 0.5f);
-            });
-            chunk = chunk_by_work(work, blocks, C.num_cu, LEAST_TILES);
-        }
-        splits = splits_of(tiles, chunk, C.max_splits);
+        return lo < hi;
     }
 };
 struct DqRow {                           // a lane's row: token t sees keys first .. t
@@ -308,14 +311,12 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lh = lane >> 5;
 
-    int kvh, rest, split;
-    my_block(C, &kvh, &rest, &split);
-    rest = (int)(gridDim.x / (unsigned)(C.kv_heads * C.max_splits)) - 1 - rest;          // long blocks first
-    const RowBlock block(C, rest);
-    if (split >= block.splits)
+    RowBlock block(C);
+    if (!my_item(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
+    const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
-    const int kt0 = (int)(((int64_t)block.tiles * split) / block.splits), nkt = (int)(((int64_t)block.tiles * (split + 1)) / block.splits);
+    const int kt0 = (int)(((int64_t)block.tiles * split) / splits), nkt = (int)(((int64_t)block.tiles * (split + 1)) / splits);
     const DqRow row(C, block, kvh);
     const int t = row.t, head = row.head, first = row.first;
     const bool there = row.there;
@@ -437,10 +438,10 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
         }
     }
 
-    if (block.splits > 1) {
+    if (splits > 1) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            park<NT>(acc[d], part_of<NT>(C, DT * 16, rest * C.kv_heads + kvh, split, d));
+            park<NT>(acc[d], part_of<NT>(C, DT * 16, block.it, split, d));
         return;
     }
     __bf16 *out = static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head;
@@ -455,11 +456,14 @@ __global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams 
 {
     const CausalParams &C = P.c;
     const int tile = blockIdx.x % DT, group = blockIdx.x / DT, kvh = group % C.kv_heads;
-    const RowBlock block(C, group / C.kv_heads);
-    if (block.splits < 2)
+    RowBlock block(C);
+    block.it.kvh = kvh;
+    block.it.block = group / C.kv_heads;
+    Splits(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
-    const f32x16_t x = sum_of_parts<64 * DQ_WAVES>(C, DT * 16, group, block.splits, tile);
+    const f32x16_t x = sum_of_parts<64 * DQ_WAVES>(C, DT * 16, block.it, tile);
     const bool odd = store_tile(x, C.scale, static_cast<__bf16 *>(P.dq) + (int64_t)row.t * C.q_token + row.head * C.q_head, tile, row.there);
     once_more(odd, [&](int l) { careful_dq(P, __shfl(row.t, l), __shfl(row.head, l), __shfl(row.first, l), tile); });
 }
@@ -468,38 +472,43 @@ constexpr int GRAD_KEYS = 128;           // keys of a workgroup of the second la
 constexpr int GRAD_ROWS = 64;            // rows per tile
 // Its keys [begin, k1), and the walk over rows [lo, hi) = (token, head of the group), tokens [begin, end_b)
 struct KeyBlock {
-    Sequences seqs;
-    int k0, k1, begin, seq_a, seq_b, end_b, lo, hi, tiles, splits;   // splits 0: nothing to do
-    __device__ __forceinline__ KeyBlock(const CausalParams &C, int block) : seqs(C.starts, C.n_seqs)
+    const Sequences seqs;
+    int blocks;                          // of one key head
+    Item it;
+    int k0, k1, begin, seq_a, seq_b, end_b, lo, hi, tiles;
+    __device__ __forceinline__ int stop(const CausalParams &C) const
     {
-        const int G = C.group, last = seqs.end_of(C.n_seqs - 1), stop = last < C.tokens ? last : C.tokens;
-        splits = 0;
-        k0 = block * GRAD_KEYS;
-        k1 = k0 + GRAD_KEYS < stop ? k0 + GRAD_KEYS : stop;
+        const int last = seqs.end_of(C.n_seqs - 1);
+        return last < C.tokens ? last : C.tokens;
+    }
+    __device__ __forceinline__ int tiles_of(const CausalParams &C, int block) const
+    {
+        const int a = block * GRAD_KEYS, s = seqs.start_of(0), b = a + GRAD_KEYS < stop(C) ? a + GRAD_KEYS : stop(C), from = s > a ? s : a;
+        int start, end;
+        seqs.around(b - 1, &start, &end);
+        end = end < C.tokens ? end : C.tokens;
+        return from < b && end > from ? (int)(((int64_t)(end - from) * C.group + GRAD_ROWS - 1) / GRAD_ROWS) : 0;
+    }
+    __device__ __forceinline__ KeyBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((C.tokens + GRAD_KEYS - 1) / GRAD_KEYS) {}
+    // the keys and the walk of it.block; false: nothing to do
+    __device__ __forceinline__ bool look(const CausalParams &C)
+    {
+        k0 = it.block * GRAD_KEYS;           // (the first keys are seen by most rows)
+        k1 = k0 + GRAD_KEYS < stop(C) ? k0 + GRAD_KEYS : stop(C);
         begin = seqs.start_of(0) > k0 ? seqs.start_of(0) : k0;
         if (begin >= k1)
-            return;
+            return false;
         seq_a = seqs.at(begin);
         seq_b = seqs.at(k1 - 1);
         if (seq_b >= C.n_seqs)
-            return;
+            return false;
         end_b = seqs.end_of(seq_b) < C.tokens ? seqs.end_of(seq_b) : C.tokens;
         if (end_b <= begin)
-            return;
-        lo = begin * G;
-        hi = end_b * G;
+            return false;
+        lo = begin * C.group;
+        hi = end_b * C.group;
         tiles = (int)(((int64_t)hi - lo + GRAD_ROWS - 1) / GRAD_ROWS);
-        int chunk = C.chunk;
-        if (chunk < 0) {
-            float work = 0.0f, blocks = 0.0f;
-            seqs.lengths([&](float m) {
-                const float here = m / GRAD_KEYS * C.kv_heads;
-                blocks += here;
-                work += here * (0.5f * m * G / GRAD_ROWS + 0.5f);
-            });
-            chunk = chunk_by_work(work, blocks, C.num_cu, LEAST_TILES);
-        }
-        splits = splits_of(tiles, chunk, C.max_splits);
+        return true;
     }
 };
 struct GradKey {                         // a lane's key, seen by tokens key .. end - 1 of its sequence
@@ -531,13 +540,12 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int lh = lane >> 5;
     const int G = C.group;
 
-    int kvh, rest, split;
-    my_block(C, &kvh, &rest, &split);                                // (the first keys are seen by most rows)
-    const KeyBlock block(C, rest);
-    if (split >= block.splits)
+    KeyBlock block(C);
+    if (!my_item(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
+    const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi, end_b = block.end_b;
-    const int rt0 = (int)(((int64_t)block.tiles * split) / block.splits), nrt = (int)(((int64_t)block.tiles * (split + 1)) / block.splits);
+    const int rt0 = (int)(((int64_t)block.tiles * split) / splits), nrt = (int)(((int64_t)block.tiles * (split + 1)) / splits);
     const GradKey mine(C, block);
     const int kk = mine.key, end = mine.end;
     const bool there = mine.there;
@@ -809,11 +817,11 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     }
 
     wait_vmcnt<0>();                                                 // (nothing lands behind the kernel's end)
-    if (block.splits > 1) {
+    if (splits > 1) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            park<NT>(dk[d], part_of<NT>(C, 2 * DT * 16, rest * C.kv_heads + kvh, split, d));
-            park<NT>(dv[d], part_of<NT>(C, 2 * DT * 16, rest * C.kv_heads + kvh, split, DT + d));
+            park<NT>(dk[d], part_of<NT>(C, 2 * DT * 16, block.it, split, d));
+            park<NT>(dv[d], part_of<NT>(C, 2 * DT * 16, block.it, split, DT + d));
         }
         return;
     }
@@ -832,61 +840,38 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
     const int tile = blockIdx.x % (2 * DT), group = blockIdx.x / (2 * DT), kvh = group % C.kv_heads;
-    const KeyBlock block(C, group / C.kv_heads);
-    if (block.splits < 2)
+    KeyBlock block(C);
+    block.it.kvh = kvh;
+    block.it.block = group / C.kv_heads;
+    Splits(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);
-    const f32x16_t x = sum_of_parts<256>(C, 2 * DT * 16, group, block.splits, tile);
+    const f32x16_t x = sum_of_parts<256>(C, 2 * DT * 16, block.it, tile);
     __bf16 *out = tile < DT ? static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head
                             : static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head;
     const bool odd = store_tile(x, tile < DT ? C.scale : 1.0f, out, tile & (DT - 1), mine.there);
     once_more(odd, [&](int l) { careful_key(P, __shfl(mine.key, l), kvh, __shfl(mine.end, l), tile); });
 }
 
-}  // namespace
-
-namespace {
-
-// Splits of one of the two launches: `blocks` over all key heads, `tiles` of the longest walk, `part` bytes parked by a workgroup.
-void room_for_splits(CausalParams &p, int64_t blocks, int64_t tiles, size_t part, int most)
-{
-    const Tuning tn = tuning();
-    p.chunk = tn.causal_chunk ? tn.causal_chunk : -1;
-    int64_t n = 1;
-    if (p.parts != nullptr && p.n_seqs <= 1024) {
-        const double rounds = ceil(1.25 * (double)blocks / p.num_cu), items = (rounds < 1 ? 1 : rounds) * p.num_cu - 0.5 * blocks;
-        double chunk = 0.5 * (double)tiles * blocks / items;
-        chunk = chunk < LEAST_TILES ? LEAST_TILES : chunk;
-        n = p.chunk > 0 ? (tiles + p.chunk - 1) / p.chunk : (int64_t)(1.25 * tiles / chunk + 1.0);
-        if (p.chunk < 0 && n > most)
-            n = most;
-        n = n > tiles ? tiles : n;
-        const int64_t fit = (int64_t)(p.part_bytes / part / (size_t)blocks);
-        n = n <= fit ? n : p.chunk > 0 ? 1 : fit;
-    }
-    p.max_splits = n < 2 ? 1 : (int)n;
-    if (p.max_splits == 1)
-        p.chunk = 0;
-}
-
 struct GradLaunches {
     CausalParams dq, dkv;
     int64_t row_blocks, key_blocks;      // of one key head
-    size_t dq_bytes, dkv_bytes;          // parked
+    int64_t dq_wgs, dkv_wgs;
+    size_t bytes;                        // parked, one launch after the other
 };
 GradLaunches plan_grad(const CausalParams &c, int num_cu)
 {
     GradLaunches g;
     g.dq = g.dkv = c;
-    g.dq.num_cu = g.dkv.num_cu = num_cu;
     const int64_t rows = (int64_t)c.tokens * c.group;
-    g.row_blocks = (rows + DQ_WAVES * 32 - 1) / (DQ_WAVES * 32);
+    g.row_blocks = (rows + DQ_ROWS - 1) / DQ_ROWS;
     g.key_blocks = (c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
     const size_t dq_part = (size_t)64 * 64 * DQ_WAVES * 4, dkv_part = (size_t)128 * 256 * 4;
-    room_for_splits(g.dq, g.row_blocks * c.kv_heads, (c.tokens + BKV - 1) / BKV, dq_part, 16);
-    room_for_splits(g.dkv, g.key_blocks * c.kv_heads, (rows + 63) / 64, dkv_part, 32);
-    g.dq_bytes = g.dq.max_splits > 1 ? (size_t)g.row_blocks * c.kv_heads * g.dq.max_splits * dq_part : 0;
-    g.dkv_bytes = g.dkv.max_splits > 1 ? (size_t)g.key_blocks * c.kv_heads * g.dkv.max_splits * dkv_part : 0;
+    g.dq_wgs = plan_items(g.dq, g.row_blocks, (c.tokens + BKV - 1) / BKV, dq_part, false, num_cu);
+    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, (rows + GRAD_ROWS - 1) / GRAD_ROWS, dkv_part, false, num_cu);
+    const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)g.dkv.items * dkv_part;
+    g.bytes = a > b ? a : b;
     return g;
 }
 
@@ -895,19 +880,20 @@ GradLaunches plan_grad(const CausalParams &c, int num_cu)
 hipError_t launch_attn_prompt_grad(const GradParams &p_in, hipStream_t s, int num_cu)
 {
     const GradLaunches g = plan_grad(p_in.c, num_cu);
-    if ((g.row_blocks * (g.dq.max_splits + DT) + g.key_blocks * (g.dkv.max_splits + 2 * DT)) * p_in.c.kv_heads * 256 >= (int64_t)1 << 32)
+    const int64_t most = (int64_t)1 << 24;                           // workgroups, of 256 threads
+    if (g.dq_wgs >= most || g.dkv_wgs >= most || g.row_blocks * p_in.c.kv_heads * DT >= most || g.key_blocks * p_in.c.kv_heads * 2 * DT >= most)
         return hipErrorInvalidValue;
     GradParams p = p_in;
     p.c = g.dq;
-    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)(g.row_blocks * p.c.kv_heads * p.c.max_splits)), dim3(64 * DQ_WAVES), 0, s, p);
-    if (p.c.max_splits > 1)
+    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)g.dq_wgs), dim3(64 * DQ_WAVES), 0, s, p);
+    if (p.c.items > 0)
         hipLaunchKernelGGL(attn_dq_join_kernel, dim3((unsigned)(g.row_blocks * p.c.kv_heads * DT)), dim3(64 * DQ_WAVES), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
     p.c = g.dkv;
-    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)(g.key_blocks * p.c.kv_heads * p.c.max_splits)), dim3(256), 0, s, p);
-    if (p.c.max_splits > 1)
+    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)g.dkv_wgs), dim3(256), 0, s, p);
+    if (p.c.items > 0)
         hipLaunchKernelGGL(attn_dkv_join_kernel, dim3((unsigned)(g.key_blocks * p.c.kv_heads * 2 * DT)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
@@ -916,10 +902,9 @@ size_t attn_grad_part_bytes(const CausalParams &p_in, int num_cu)
 {
     CausalParams p = p_in;                                           // as if any workspace were there
     p.parts = reinterpret_cast<float *>(256);
-    p.part_bytes = ~(size_t)0 >> 1;
+    p.part_bytes = (size_t)1 << 48;
     p.max_counters = 1 << 30;
-    const GradLaunches g = plan_grad(p, num_cu);
-    return g.dq_bytes > g.dkv_bytes ? g.dq_bytes : g.dkv_bytes;
+    return plan_grad(p, num_cu).bytes;
 }
 
 }  // namespace cf

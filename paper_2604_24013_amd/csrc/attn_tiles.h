@@ -145,52 +145,136 @@ struct Sequences {
         *start = i > 0 ? before : first;
         return a;
     }
-    // f(length, tiles, blocks) over all sequences, a lane's share
-    template <typename F>
-    __device__ __forceinline__ void lengths(F &&f) const
+    // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences
+    __device__ __forceinline__ void around(int t, int *start, int *end) const
     {
-        const int lane = threadIdx.x & 63, before = __shfl_up(mine, 1);
-        if (lane < n)
-            f((float)max(0, mine - (lane > 0 ? before : first)));
-        for (int i = lane + 64; i < n; i += 64)
-            f((float)max(0, starts[i + 1] - starts[i]));
+        *start = first;
+        *end = 0x7FFFFFFF;
+        for (int i = 0; i < n; ++i) {
+            const int e = __builtin_amdgcn_readlane(mine, i);
+            *start = e <= t ? e : *start;
+            *end = e > t && e < *end ? e : *end;
+        }
     }
 };
 
-// Tiles that a split has at the most, for launches whose lengths only the tables on the device know: every workgroup adds up the work
-// of all sequences (a lane's share of it: `tiles` in `blocks`) and comes to the same number.
-// Walks under a causal mask are of all lengths, and a launch takes as long as its longest compute unit; with ceil(tiles / chunk) splits of a
-// block a launch has about tiles / chunk + blocks / 2 workgroups.  So chunk is such that these are as many as fit the chip k times, k the
-// least that leaves three quarters of a workgroup per block over for whole chunks.  (Computed for one and eight heads, one sequence and
-// several, workgroups one by one on the compute units: within 10 % of the best chunk; 20 % more workgroups than fit cost up to 50 %.)
-__device__ __forceinline__ int chunk_by_work(float tiles, float blocks, int num_cu, int least)
+// Inclusive sums over the wave's lanes.
+__device__ __forceinline__ int scan(int x)
 {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below in a row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // rows 1 and 3: the last lane of the row below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // rows 2 and 3: lane 31
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan(x), 63); }
+
+// What a workgroup works on.  Walks under a causal mask are of all lengths, which only the tables on the device know, and a launch takes as
+// long as its fullest compute unit.  So every workgroup looks at the walks of all blocks, a lane a block, and cuts them into splits of at most
+// `chunk` tiles, the same for all, as few as make no more than P.items workgroups: as many as fit the chip a whole number of times.
+// (Computed for one and eight heads, one sequence and several, workgroups one by one on the compute units: with 256 of 128 to 252
+// workgroups each takes 33 us, with a quarter more than fit, 47.)  A grid of all blocks by the largest number of splits needs no
+// search, but three workgroups of four then have nothing to do and hold up the others: dK and dV of 4096 tokens, 8 heads on one key
+// head, took 148 us so.
+constexpr int MAX_BLOCKS = 512;          // of one key head, that are looked at: eight a lane
+struct Item {
+    int kvh, block, split, splits;       // key heads innermost: neighbouring workgroups go to one XCD in turn, whose L2 holds few heads' keys
+    int first;                           // the block's split 0 is this one of its key head's items
+};
+
+// The splits of all blocks.  tiles_of(block): tiles of a lane's block (0: nothing to do), in the order of dispatch.
+struct Splits {
+    static constexpr int R = MAX_BLOCKS / 64;
+    int tiles[R], chunk, blocks;
+    template <typename F>
+    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, F &&tiles_of) : chunk(P.chunk), blocks(count)
+    {
+        int all = 0, some = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        tiles += __shfl_xor(tiles, d);
-        blocks += __shfl_xor(blocks, d);
+        for (int r = 0; r < R; ++r) {
+            tiles[r] = 0;
+            if (r * 64 < count) {
+                const int b = r * 64 + (threadIdx.x & 63);
+                tiles[r] = b < count ? tiles_of(b) : 0;
+                all += tiles[r];
+                some += tiles[r] > 0;
+            }
+        }
+        if (chunk > 0)
+            return;
+        const int total = wave_total(all), active = wave_total(some), items = P.items / P.kv_heads;
+        const float wanted = fmaxf((float)items - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
+        chunk = max(least, (int)(total / wanted) + 1);
+        while (number() > items)
+            chunk += chunk / 16 + 1;
     }
-    const float rounds = ceilf(1.36f * blocks / num_cu);
-    const float items = 0.92f * fmaxf(rounds, 1.0f) * num_cu - 0.5f * blocks;    // (not one too many)
-    return uniform(max(least, (int)ceilf(tiles / items)));
-}
+    __device__ __forceinline__ int of(int t) const { return t <= 0 ? 0 : (int)((float)(t + chunk - 1) * __builtin_amdgcn_rcpf((float)chunk) * 1.0000002f); }
+    __device__ __forceinline__ int number() const
+    {
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r * 64 < blocks)
+                n += of(tiles[r]);
+        return wave_total(n);
+    }
+    // Item j of a key head: false: there are not so many.
+    __device__ __forceinline__ bool item(int j, Item *it) const
+    {
+        int base = 0;
+        bool found = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r * 64 < blocks && !found) {
+                const int n = of(tiles[r]), end = base + scan(n);
+                const unsigned long long behind = __builtin_amdgcn_ballot_w64(end > j);
+                base = __builtin_amdgcn_readlane(end, 63);
+                if (behind != 0) {
+                    const int lane = __builtin_ctzll(behind);
+                    it->splits = __builtin_amdgcn_readlane(n, lane);
+                    it->first = __builtin_amdgcn_readlane(end, lane) - it->splits;
+                    it->block = r * 64 + lane;
+                    it->split = j - it->first;
+                    found = true;
+                }
+            }
+        return found;
+    }
+    // The splits of a block, and the first of their items.
+    __device__ __forceinline__ void of_block(int block, Item *it) const
+    {
+        int base = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r * 64 <= block) {
+                const int n = of(tiles[r]), end = base + scan(n);
+                it->splits = __builtin_amdgcn_readlane(n, block & 63);
+                it->first = __builtin_amdgcn_readlane(end, block & 63) - it->splits;
+                base = __builtin_amdgcn_readlane(end, 63);
+            }
+    }
+};
 
-// Splits of a walk of `tiles` tiles.
-__device__ __forceinline__ int splits_of(int tiles, int chunk, int most)
+// This workgroup's item; `blocks`: of one key head.
+template <typename F>
+__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, F &&tiles_of, Item *it)
 {
-    const int n = chunk > 0 && tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
-    return n < most ? n : most;
+    const int j = blockIdx.x / P.kv_heads;
+    it->kvh = blockIdx.x - j * P.kv_heads;
+    if (P.items == 0) {
+        it->block = it->first = j;
+        it->split = 0;
+        it->splits = 1;
+        return true;
+    }
+    return Splits(P, blocks, least, tiles_of).item(j, it);
 }
-
-// Which block and split a workgroup takes: key heads innermost (neighbouring workgroups go to one XCD in turn, whose L2 then holds few
-// heads' keys), splits outermost, so that those that short blocks do not have come last, and turned by five blocks from split to
-// split, so that they are not always the same XCDs' (32 blocks of 1 to 14 splits: 36 of 238 workgroups on one XCD's 32 compute units, now 30).
-__device__ __forceinline__ void my_block(const CausalParams &P, int *kvh, int *block, int *split)
+// Where item `first + split` of a block parks what it has: N floats a workgroup.
+__device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &it, int split, size_t floats)
 {
-    const int blocks = gridDim.x / (unsigned)(P.kv_heads * P.max_splits), rest = blockIdx.x / P.kv_heads;
-    *kvh = blockIdx.x - rest * P.kv_heads;
-    *split = rest / blocks;
-    *block = (int)((unsigned)(rest - *split * blocks + 5 * *split) % (unsigned)blocks);
+    return P.parts + ((size_t)(it.first + split) * P.kv_heads + it.kvh) * floats;
 }
 
 enum { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };

@@ -179,7 +179,6 @@ cf_status resolve_prompt(const cf_prompt_desc *d, cf::CausalParams *out, bool *n
     p.tokens = (int)d->tokens;
     p.n_seqs = d->n_seqs;
     p.lse_stride = d->tokens;
-    p.max_splits = 1;
     *nothing = d->tokens == 0 || d->n_seqs == 0;
     *out = p;
     return CF_OK;
@@ -220,7 +219,6 @@ cf_status resolve_paged(const cf_cache_desc *cd, const cf_cache *c, const cf_pag
     p.max_pages = d->max_pages;
     const int64_t room = (int64_t)d->max_pages * cd->page_size;
     p.max_kv = p.pool.n_pages == 0 ? 0 : room < d->max_kv ? (int)room : d->max_kv;
-    p.max_splits = 1;
     *nothing = d->total_q == 0 || d->n_seqs == 0 || d->max_q == 0;
     *out = p;
     return CF_OK;

@@ -76,14 +76,17 @@ struct CausalParams {
     const int32_t *kv_len, *table;
     int max_q, max_kv, max_pages;
     // a walk's tiles split over workgroups
-    int chunk = 0;                                  // tiles of a split at the most (0: all, -1: by the work that the tables hold)
-    int max_splits = 1;
-    int num_cu = 0;
+    int items = 0;                                  // workgroups of the launch at the most (0: one for each block and key head)
+    int chunk = 0;                                  // tiles of a split (0: as few as the items allow)
     float *parts = nullptr;
     unsigned *counters = nullptr;
     size_t part_bytes = 0;
     int max_counters = 0;
 };
+// Workgroups of a launch over `blocks` blocks of one key head whose walks are of up to `longest` tiles, and P.items and P.chunk to go with it:
+// as many as fit the compute units the least number of times that leaves a third of them over for splits.  `part`: bytes that one
+// parks.  Without workspace for that, or with more blocks or sequences than are looked at: one workgroup a block.
+int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part, bool counted, int num_cu);
 hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
 hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);
 bool attn_few_takes(const CausalParams &p);         // few rows of a sequence and key head: the kernel that splits keys over waves
