@@ -176,26 +176,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     for (int ks = 0; ks < DS; ++ks)
         qf[ks] = *reinterpret_cast<const bf16x8_t *>(qrow + ks * 16 + lh * 8);
 
-    Keys<SRC> Kk, Kv;
-    if constexpr (SRC == PACKED) {
-        Kk.base = static_cast<const unsigned char *>(P.K) + kvh * P.k_head * 2;
-        Kv.base = static_cast<const unsigned char *>(P.V) + kvh * P.v_head * 2;
-        Kk.row_bytes = P.k_token * 2;
-        Kv.row_bytes = P.v_token * 2;
-    } else {
-        constexpr int E = SRC == PAGED_E4M3 ? 1 : 2;
-        Kk.base = static_cast<const unsigned char *>(P.pool.k) + kvh * P.pool.head_stride * E;
-        Kk.row_bytes = P.pool.token_stride * E;
-        Kk.table = table;
-        Kk.exps = SRC == PAGED_E4M3 ? P.pool.k_exp + ((int64_t)kvh << P.pool.page_shift) : nullptr;
-        Kk.page_bytes = P.pool.page_stride * E;
-        Kk.n_pages = P.pool.n_pages;
-        Kk.exp_page = (int64_t)P.pool.kv_heads << P.pool.page_shift;
-        Kk.shift = P.pool.page_shift;
-        Kv = Kk;
-        Kv.base = static_cast<const unsigned char *>(P.pool.v) + kvh * P.pool.head_stride * E;
-        Kv.exps = SRC == PAGED_E4M3 ? P.pool.v_exp + ((int64_t)kvh << P.pool.page_shift) : nullptr;
-    }
+    constexpr int E = SRC == PAGED_E4M3 ? 1 : 2;
+    const int k_row = (int)(SRC == PACKED ? P.k_token : P.pool.token_stride) * E, v_row = (int)(SRC == PACKED ? P.v_token : P.pool.token_stride) * E;   // bytes
+    const unsigned char *kb = static_cast<const unsigned char *>(SRC == PACKED ? P.K : P.pool.k) + kvh * (SRC == PACKED ? P.k_head : P.pool.head_stride) * E;
+    const unsigned char *vb = static_cast<const unsigned char *>(SRC == PACKED ? P.V : P.pool.v) + kvh * (SRC == PACKED ? P.v_head : P.pool.head_stride) * E;
+    const int shift = P.pool.page_shift, n_pages = (int)P.pool.n_pages;
+    const int64_t page_bytes = P.pool.page_stride * E, exp_page = (int64_t)P.pool.kv_heads << shift;
+    const uint8_t *ke = P.pool.k_exp + ((int64_t)kvh << shift), *ve = P.pool.v_exp + ((int64_t)kvh << shift);       // (e4m3)
     const unsigned lds_base = lds_address(smem);
 
     // Paged: the page table by windows of 64 entries, one a lane; `bad`: which of a window's pages do not exist.  The walk asks for V of
@@ -203,15 +190,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // window or in the one before.
     int window = -1, entry = 0;
     unsigned long long bad = 0, bad_before = 0;
-    auto window_of = [&](int kt) __attribute__((always_inline)) { return ((kt * BKV) >> Kk.shift) >> 6; };
-    auto page_of = [&](int key) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(entry, (key >> Kk.shift) & 63); };
+    auto window_of = [&](int kt) __attribute__((always_inline)) { return ((kt * BKV) >> shift) >> 6; };
+    auto page_of = [&](int key) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(entry, (key >> shift) & 63); };
     auto turn_to = [&](int kt) __attribute__((always_inline)) {
         const int w = window_of(kt);
         if (w != window) {
             const int i = w * 64 + lane;
             entry = i < P.max_pages ? table[i] : -1;
             bad_before = w == window + 1 ? bad : 0;
-            bad = __builtin_amdgcn_ballot_w64((unsigned)entry >= (unsigned)Kk.n_pages);
+            bad = __builtin_amdgcn_ballot_w64((unsigned)entry >= (unsigned)n_pages);
             window = w;
         }
     };
@@ -222,23 +209,24 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // and those of pages that do not exist, read as zero and move no data.
     static_assert(NW * 4 % 16 == 0, "key rows of a wave-load");
     const int ld_row = wave * 4 + (lane >> 4), ld_cp = lane & 15;
-    const unsigned k_off = (unsigned)((lane >> 4) * (int)Kk.row_bytes + ((ld_cp ^ (ld_row & 15)) << 4));
-    const unsigned v_off = (unsigned)((lane >> 4) * (int)Kv.row_bytes + (((ld_cp >> 2) ^ (ld_row & 3)) << 6) + ((ld_cp & 3) << 4));
-    auto issue = [&](int kt, const Keys<SRC> &from, unsigned off, unsigned lds) __attribute__((always_inline)) {
+    const unsigned k_off = (unsigned)((SRC == PACKED ? ld_row : lane >> 4) * k_row + ((ld_cp ^ (ld_row & 15)) << 4));
+    const unsigned v_off = (unsigned)((SRC == PACKED ? ld_row : lane >> 4) * v_row + (((ld_cp >> 2) ^ (ld_row & 3)) << 6) + ((ld_cp & 3) << 4));
+    auto issue = [&](int kt, const unsigned char *from, int row_bytes, unsigned off, unsigned lds) __attribute__((always_inline)) {
+        if constexpr (SRC == PACKED) {                               // one buffer a tile
+            const int key = lo + kt * BKV, left = hi - key < BKV ? hi - key : BKV;
+            const i32x4_t rsrc = make_rsrc(from + (int64_t)key * row_bytes, left > 0 ? (unsigned)left * (unsigned)row_bytes : 0u);
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int row = wave * 4 + j * NW * 4, key = lo + kt * BKV + row;
-            const int left = hi - key < 4 ? hi - key : 4;
-            unsigned bytes = left > 0 ? (unsigned)(left * (int)from.row_bytes) : 0u;
-            const unsigned char *at;
-            if constexpr (SRC == PACKED) {
-                at = from.base + (int64_t)key * from.row_bytes;
-            } else {
-                const int page = page_of(key);
-                bytes = (unsigned)page < (unsigned)from.n_pages ? bytes : 0u;
-                at = from.base + (int64_t)page * from.page_bytes + (int64_t)(key & ((1 << from.shift) - 1)) * from.row_bytes;
+            for (int j = 0; j < LOADS; ++j)
+                direct_load_16(rsrc, off + (unsigned)(j * NW * 4) * (unsigned)row_bytes, lds + wave * 1024 + j * NW * 1024);
+        } else {                                                     // one a wave-load, whose rows lie in one page
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int key = kt * BKV + wave * 4 + j * NW * 4, page = page_of(key);
+                const int left = hi - key < 4 ? hi - key : 4;
+                const bool some = left > 0 && (unsigned)page < (unsigned)n_pages;
+                const unsigned char *at = from + (int64_t)page * page_bytes + (key & ((1 << shift) - 1)) * row_bytes;
+                direct_load_16(make_rsrc(at, some ? (unsigned)(left * row_bytes) : 0u), off, lds + wave * 1024 + j * NW * 1024);
             }
-            direct_load_16(make_rsrc(at, bytes), off, lds + wave * 1024 + j * NW * 1024);
         }
     };
     // e4m3: a lane fetches 16 codes of a row (eight lanes a row, eight rows a wave-load) and the row's exponent into registers, and
@@ -246,15 +234,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     const int ld_row8 = wave * 8 + (lane >> 3), ld_c8 = lane & 7;
     u32x4_t code_k[LOADS8], code_v[LOADS8];
     int exp_k[LOADS8], exp_v[LOADS8];
-    auto issue8 = [&](int kt, const Keys<SRC> &from, u32x4_t (&code)[LOADS8], int (&ex)[LOADS8]) __attribute__((always_inline)) {
+    auto issue8 = [&](int kt, const unsigned char *from, const uint8_t *exponents, int row_bytes, u32x4_t (&code)[LOADS8], int (&ex)[LOADS8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < LOADS8; ++j) {
             const int key = kt * BKV + wave * 8 + j * NW * 8;
-            const int left = hi - key < 8 ? hi - key : 8, page = page_of(key), in_page = key & ((1 << from.shift) - 1);
-            const bool some = left > 0 && (unsigned)page < (unsigned)from.n_pages;
-            const auto rows = plain_rsrc(from.base + (int64_t)page * from.page_bytes + (int64_t)in_page * from.row_bytes, some ? left * (int)from.row_bytes : 0);
-            const auto exps = plain_rsrc(from.exps + page * from.exp_page + in_page, some ? left : 0);
-            code[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, (lane >> 3) * (int)from.row_bytes + ld_c8 * 16, 0, 0);
+            const int left = hi - key < 8 ? hi - key : 8, page = page_of(key), in_page = key & ((1 << shift) - 1);
+            const bool some = left > 0 && (unsigned)page < (unsigned)n_pages;
+            const auto rows = plain_rsrc(from + (int64_t)page * page_bytes + in_page * row_bytes, some ? left * row_bytes : 0);
+            const auto exps = plain_rsrc(exponents + page * exp_page + in_page, some ? left : 0);
+            code[j] = __builtin_amdgcn_raw_buffer_load_b128(rows, (lane >> 3) * row_bytes + ld_c8 * 16, 0, 0);
             ex[j] = __builtin_amdgcn_raw_buffer_load_b8(exps, lane >> 3, 0, 0);
         }
     };
@@ -293,8 +281,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 
     f32x16_t oacc[DT];
     float m_run = -3.402823466e38f;      // (finite: against -inf a tile whose scores are all -inf would give NaN)
-    float l_run = 0.0f, l_pair = 0.0f;   // of the rounded probabilities of this lane's keys; of a pair of tiles
-    float e_run = 0.0f, e_pair = 0.0f;   // LSE: of the probabilities before rounding
+    // Row sums of this lane's keys, and of a pair of tiles: of the rounded probabilities, which multiply V, so that the roundings of a row's
+    // dominant key cancel; LSE: of the probabilities before rounding (rounded, the log-sum-exp of a row with one dominant key would be
+    // off by up to 2^-9).  Both sums cost 16 vector instructions more a tile, of about 130: 10 % of the time of a full chip.
+    float l_run = 0.0f, l_pair = 0.0f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -361,7 +351,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                 for (int j = 0; j < KT; ++j)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if (none >> (((key0 + j * 32 + 8 * (e >> 2) + (e & 3)) >> Kk.shift) & 63) & 1)
+                        if (none >> (((key0 + j * 32 + 8 * (e >> 2) + (e & 3)) >> shift) & 63) & 1)
                             sn[j][e] = -INFINITY;
                 mx = maximum(sn);
             }
@@ -374,10 +364,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             m_run = m_new;
             l_run *= alpha;
             l_pair *= alpha;
-            if constexpr (LSE) {
-                e_run *= alpha;
-                e_pair *= alpha;
-            }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -389,15 +375,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         if constexpr (SRC != PACKED)
             turn_to(kt + 1);
         if constexpr (SRC == PAGED_E4M3)
-            issue8(kt + 1, Kv, code_v, exp_v);
+            issue8(kt + 1, vb, ve, v_row, code_v, exp_v);
         else
-            issue(kt + 1, Kv, v_off, lds_base + V_BASE + (1 - b) * TILE_BYTES);
+            issue(kt + 1, vb, v_row, v_off, lds_base + V_BASE + (1 - b) * TILE_BYTES);
         if constexpr (SRC != PACKED)
             turn_to(kt + 2);
         if constexpr (SRC == PAGED_E4M3)
-            issue8(kt + 2, Kk, code_k, exp_k);
+            issue8(kt + 2, kb, ke, k_row, code_k, exp_k);
         else
-            issue(kt + 2, Kk, k_off, lds_base + b * TILE_BYTES);
+            issue(kt + 2, kb, k_row, k_off, lds_base + b * TILE_BYTES);
     };
     auto finish = [&](int b) __attribute__((always_inline)) {        // V of tile kt+1 and K of tile kt+2 have landed
         if constexpr (SRC == PAGED_E4M3) {
@@ -408,8 +394,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         }
         __syncthreads();                                             // ... for every wave, and V of kt, K of kt+1 are read by all
     };
-    // One tile: probabilities P = exp2(S - m) rounded to bf16, their row sums (of the rounded values that multiply V, two to a dot
-    // product with ones), O^T += V^T P^T; and under it, with `next`, the scores of tile kt+1 and their maximum.  Thirty-two segments
+    // One tile: probabilities P = exp2(S - m) rounded to bf16, their row sums, O^T += V^T P^T; and under it, with `next`, the scores of tile kt+1 and their maximum.  Thirty-two segments
     // of one MFMA each -- sixteen of the scores, sixteen of V's product --, the fragment of the third segment ahead requested in each,
     // the 32 exponentials spread over segments 0 .. 22 and the maximum over the last eight.
     bf16x2_t ones;
@@ -439,17 +424,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             for (int i = 0; i < 2; ++i) {                            // bare v_exp_f32: arguments below -126 give 0
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 4][(e & 15) + i], sl2, nm));
                 if constexpr (LSE)
-                    e_pair = (e == 0 && i == 0 && B == 0 ? 0.0f : e_pair) + p;
+                    l_pair = (e == 0 && i == 0 && B == 0 ? 0.0f : l_pair) + p;
                 two[i] = (__bf16)p;
             }
             pf[e >> 3][(e & 7)] = two[0];
             pf[e >> 3][(e & 7) + 1] = two[1];
-            l_pair = __builtin_amdgcn_fdot2_f32_bf16(two, ones, e == 0 && B == 0 ? 0.0f : l_pair, false);
-            if constexpr (e == 30 && (B == 1 || !NEXT)) {
+            if constexpr (!LSE)
+                l_pair = __builtin_amdgcn_fdot2_f32_bf16(two, ones, e == 0 && B == 0 ? 0.0f : l_pair, false);
+            if constexpr (e == 30 && (B == 1 || !NEXT))
                 l_run += l_pair;
-                if constexpr (LSE)
-                    e_run += e_pair;
-            }
         };
         float mx = -INFINITY;
         auto segment = [&](auto s_tag) __attribute__((always_inline)) {
@@ -497,21 +480,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         if constexpr (SRC != PACKED)
             turn_to(kt0);
         if constexpr (SRC == PAGED_E4M3) {
-            issue8(kt0, Kk, code_k, exp_k);
-            issue8(kt0, Kv, code_v, exp_v);
+            issue8(kt0, kb, ke, k_row, code_k, exp_k);
+            issue8(kt0, vb, ve, v_row, code_v, exp_v);
             put8(code_k, exp_k, 0, false);
         } else {
-            issue(kt0, Kk, k_off, lds_base);
-            issue(kt0, Kv, v_off, lds_base + V_BASE);
+            issue(kt0, kb, k_row, k_off, lds_base);
+            issue(kt0, vb, v_row, v_off, lds_base + V_BASE);
         }
         if constexpr (SRC != PACKED)
             turn_to(kt0 + 1);
         if constexpr (SRC == PAGED_E4M3) {
-            issue8(kt0 + 1, Kk, code_k, exp_k);
+            issue8(kt0 + 1, kb, ke, k_row, code_k, exp_k);
             put8(code_v, exp_v, V_BASE, true);
             put8(code_k, exp_k, TILE_BYTES, false);
         } else {
-            issue(kt0 + 1, Kk, k_off, lds_base + TILE_BYTES);
+            issue(kt0 + 1, kb, k_row, k_off, lds_base + TILE_BYTES);
             wait_vmcnt<0>();
         }
         __syncthreads();
@@ -552,15 +535,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         }
     }
     l_run = sum_of_halves(l_run);                                    // the whole row sums, in both lanes of the row
-    if constexpr (LSE)
-        e_run = sum_of_halves(e_run);
 
     // Key split: park (m, l, O) in the workspace, thread-major so that every access is a coalesced 4 bytes per lane; the
     // workgroup that arrives last merges all splits in split order.  Device-coherent cache policy on exactly these accesses, relaxed
     // agent-scope atomics on the counter.
     if (splits > 1) {
         constexpr int COHERENT = 1 | 16;
-        constexpr int NV = DT * 16 + (LSE ? 3 : 2);                  // floats per thread
+        constexpr int NV = DT * 16 + 2;                              // floats per thread
         const size_t part = (size_t)NV * NT;
         const int group = it.block * P.kv_heads + kvh;
         auto part_rsrc = [&](int sp) {
@@ -581,8 +562,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                     park(oacc[d][e], d * 16 + e);
             park(m_run, DT * 16);
             park(l_run, DT * 16 + 1);
-            if constexpr (LSE)
-                park(e_run, DT * 16 + 2);
         }
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -607,7 +586,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             for (int i = 0; i < 8; ++i)
                 m_all = fmaxf(m_all, m[i]);
         }
-        l_run = e_run = 0.0f;
+        l_run = 0.0f;
         m_run = m_all;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -616,7 +595,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                 oacc[d][e] = 0.0f;
         for (int sp = 0; sp < splits; ++sp) {
             __amdgpu_buffer_rsrc_t rs = part_rsrc(sp);
-            const float m = ld(rs, DT * 16), l = ld(rs, DT * 16 + 1), x = LSE ? ld(rs, DT * 16 + 2) : 0.0f;
+            const float m = ld(rs, DT * 16), l = ld(rs, DT * 16 + 1);
             float v[DT][16];
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -625,7 +604,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                     v[d][e] = ld(rs, d * 16 + e);
             const float f = exp2f(m - m_all);                        // (a row that sees no key of a split: nothing times a factor)
             l_run += l * f;
-            e_run += x * f;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -658,17 +636,30 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                 *reinterpret_cast<u32x2_t *>(orow + d * 32 + 8 * gq + 4 * lh) = __builtin_bit_cast(u32x2_t, h);
             }
         if (LSE && lh == 0)
-            P.lse[(int64_t)head * P.lse_stride + t] = e_run == 0.0f ? -INFINITY : (m_run + __log2f(e_run)) * LN2;
+            P.lse[(int64_t)head * P.lse_stride + t] = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * LN2;
     }
     unsigned long long again = __builtin_amdgcn_ballot_w64(there && odd != 0.0f);
     again = (again | again >> 32) & 0xFFFFFFFFull;
     if (again != 0) {
+        Keys<SRC> K, V;
+        K.base = kb;
+        K.row_bytes = k_row;
+        K.table = table;
+        K.exps = ke;
+        K.page_bytes = page_bytes;
+        K.n_pages = n_pages;
+        K.exp_page = exp_page;
+        K.shift = shift;
+        V = K;
+        V.base = vb;
+        V.row_bytes = v_row;
+        V.exps = ve;
         __builtin_amdgcn_s_waitcnt(0);                               // the row's first result is written before its second
         for (; again != 0; again &= again - 1) {
             const int at = __builtin_ctzll(again);
             const int64_t tr = __shfl(t, at);
             const int hr = __shfl(head, at);
-            careful_row_called<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
+            careful_row_called<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
                              static_cast<__bf16 *>(P.out) + tr * P.o_token + hr * P.o_head, __shfl(first, at), __shfl(last, at), sl2);
         }
     }
@@ -686,7 +677,7 @@ hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t part_bytes(int waves) { return (size_t)(64 + 3) * (64 * waves) * sizeof(float); }
+size_t part_bytes(int waves) { return (size_t)(64 + 2) * (64 * waves) * sizeof(float); }
 
 // Four waves (128 rows) or eight; the launch's workgroups.
 int choose_blocks(CausalParams &p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu, int64_t *wgs)

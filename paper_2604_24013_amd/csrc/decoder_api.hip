@@ -123,8 +123,8 @@ cf_status check_tokens(int64_t tokens, int64_t rows_of_a_token)
     return CF_OK;
 }
 
-// Rows of K or V in a direct load's 32-bit offsets.
-constexpr int64_t MAX_TOKEN_STRIDE = (int64_t)1 << 27;
+// A tile of 64 rows is addressed with 32-bit offsets from its first.
+constexpr int64_t MAX_TOKEN_STRIDE = (int64_t)1 << 23;
 
 cf_status check_scale(float scale)
 {
