@@ -21,7 +21,7 @@
 namespace cf {
 namespace {
 
-constexpr int LEAST_TILES = 4;           // of a split: less than that its hand-over takes
+constexpr int LEAST_TILES = 8;           // of a split: as long as a workgroup's start and hand-over take
 
 // (a call: inlined, its loops would have the walk's registers spilled)
 template <int SRC>
@@ -93,7 +93,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     };
     Item it;
     const int all_blocks = SRC == PACKED ? blocks : blocks * P.n_seqs;
-    if (!my_item(P, all_blocks, LEAST_TILES, [&](int block) {
+    const int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
+    if (!my_item(P, all_blocks, LEAST_TILES, bound, [&](int block) {
             Walk w = walk_of(block);
             if constexpr (SRC == PACKED) {
                 int end;
@@ -680,10 +681,13 @@ hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
 size_t part_bytes(int waves) { return (size_t)(64 + 2) * (64 * waves) * sizeof(float); }
 
 // Four waves (128 rows) or eight; the launch's workgroups.
-int choose_blocks(CausalParams &p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu, int64_t *wgs)
+int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, int64_t tiles, int num_cu, int64_t *wgs)
 {
     const Tuning tn = tuning();
-    const int waves = tn.causal_waves ? tn.causal_waves : 4;
+    // Eight waves share a tile's loads, and its conversion from e4m3; four make twice as many blocks.  us, four / eight: 8192 tokens x 32 heads
+    // 545 / 525, 4096 x 4 in pieces of 20 and 12 tiles 33.5 / 38; 2381 tokens x 8 over 5 to 8 thousand in e4m3 106 / 81.
+    const bool many = (rows + 255) / 256 * p.kv_heads * sequences >= 4 * num_cu;
+    const int waves = tn.causal_waves ? tn.causal_waves : many || (paged && rows >= 256) ? 8 : 4;
     *wgs = plan_items(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, part_bytes(waves), true, num_cu);
     return waves;
 }
@@ -695,7 +699,8 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part
     const Tuning tn = tuning();
     const int64_t all = blocks * p.kv_heads;
     p.items = p.chunk = 0;
-    if (p.parts == nullptr || blocks > 512 || p.n_seqs > 64 || (counted && all > p.max_counters) || longest < 2)
+    p.num_cu = num_cu;
+    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || p.n_seqs > 64 || (counted && all > p.max_counters) || longest < 2)
         return all;
     const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);
     int64_t items = tn.causal_chunk ? all * ((longest + tn.causal_chunk - 1) / tn.causal_chunk) : (rounds > 1 ? rounds : 1) * num_cu / p.kv_heads * p.kv_heads;
@@ -715,7 +720,7 @@ hipError_t launch_attn_prompt(const CausalParams &p_in, hipStream_t s, int num_c
 {
     CausalParams p = p_in;
     int64_t wgs;
-    const int waves = choose_blocks(p, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu, &wgs);
+    const int waves = choose_blocks(p, false, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu, &wgs);
     return waves == 8 ? launch<8, PACKED>(p, wgs, s) : launch<4, PACKED>(p, wgs, s);
 }
 
@@ -723,7 +728,7 @@ hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int
 {
     CausalParams p = p_in;
     int64_t wgs;
-    const int waves = choose_blocks(p, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu, &wgs);
+    const int waves = choose_blocks(p, true, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu, &wgs);
     if (p.pool.e4m3)
         return waves == 8 ? launch<8, PAGED_E4M3>(p, wgs, s) : launch<4, PAGED_E4M3>(p, wgs, s);
     return waves == 8 ? launch<8, PAGED_BF16>(p, wgs, s) : launch<4, PAGED_BF16>(p, wgs, s);
@@ -731,25 +736,25 @@ hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int
 
 namespace {
 // (as if any workspace were there)
-size_t part_bytes_of(CausalParams p, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
+size_t part_bytes_of(CausalParams p, bool paged, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
 {
     p.parts = reinterpret_cast<float *>(256);
     p.part_bytes = (size_t)1 << 48;
     p.max_counters = 1 << 30;
     int64_t wgs;
-    const int waves = choose_blocks(p, rows, sequences, tiles, num_cu, &wgs);
+    const int waves = choose_blocks(p, paged, rows, sequences, tiles, num_cu, &wgs);
     return p.items > 0 ? (size_t)p.items * part_bytes(waves) : 0;
 }
 }  // namespace
 
 size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu)
 {
-    return part_bytes_of(p, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
+    return part_bytes_of(p, true, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
 }
 
 size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu)
 {
-    const size_t f = part_bytes_of(p, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu), g = attn_grad_part_bytes(p, num_cu);
+    const size_t f = part_bytes_of(p, false, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu), g = attn_grad_part_bytes(p, num_cu);
     return f > g ? f : g;
 }
 

@@ -14,7 +14,7 @@
 namespace cf {
 namespace {
 
-constexpr int LEAST_TILES = 4;           // of a split: less than that its hand-over takes
+constexpr int LEAST_TILES = 8;           // of a split: as long as a workgroup's start and hand-over take
 constexpr int DS = DH / 16;              // 16-wide feature slices
 constexpr int DT = DH / 32;              // 32-wide feature tiles
 
@@ -268,6 +268,7 @@ struct RowBlock {
         return from < to ? (to - from + BKV - 1) / BKV : 0;
     }
     __device__ __forceinline__ RowBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((int)(((int64_t)C.tokens * C.group + DQ_ROWS - 1) / DQ_ROWS)) {}
+    __device__ __forceinline__ int bound(const CausalParams &C) const { return C.items > 0 ? (seqs.longest() + DQ_ROWS / C.group + 2 * BKV) / BKV : 0; }
     // the rows and the walk of it.block; false: nothing to do
     __device__ __forceinline__ bool look(const CausalParams &C)
     {
@@ -304,15 +305,15 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
     constexpr int NW = DQ_WAVES, NT = 64 * NW;
-    constexpr int LOADS = TILE_BYTES / 1024 / NW;                    // wave-loads per wave of a K or V tile: four rows each
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_BYTES];    // K, K, V, V
+    constexpr int UNIT_BYTES = TILE_BYTES;                           // 32 rows of K, then of V
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * UNIT_BYTES];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lh = lane >> 5;
 
     RowBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -340,22 +341,28 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
         }
     }
 
-    // Tile loads, straight into LDS
+    // Loads of a unit, 32 keys, straight into LDS: K and V into one of four places.  Wave-load j covers rows 4 wave + 16 j + 0 .. 3; rows
+    // behind the walk read as zero.
     const unsigned lds_base = lds_address(smem);
-    const int ld_row = wave * 4 + (lane >> 4);
+    const int ld_row = wave * 4 + (lane >> 4), k_row = (int)C.k_token * 2, v_row = (int)C.v_token * 2;
     const unsigned swizzled = ((lane & 15) ^ spread(ld_row)) << 4;
-    const unsigned k_off = (unsigned)((lane >> 4) * (int)(C.k_token * 2)) + swizzled, v_off = (unsigned)((lane >> 4) * (int)(C.v_token * 2)) + swizzled;
+    const unsigned k_off = (unsigned)(ld_row * k_row) + swizzled, v_off = (unsigned)(ld_row * v_row) + swizzled;
     const unsigned char *kb = static_cast<const unsigned char *>(C.K) + kvh * C.k_head * 2, *vb = static_cast<const unsigned char *>(C.V) + kvh * C.v_head * 2;
-    auto issue = [&](int kt, const unsigned char *base, int64_t row_bytes, unsigned off, unsigned lds) __attribute__((always_inline)) {
+    auto issue = [&](int unit) __attribute__((always_inline)) {
+        const int key = lo + unit * 32, left = hi - key < 32 ? hi - key : 32;
+        const unsigned rows = left > 0 ? (unsigned)left : 0u, lds = lds_base + (unit & 3) * UNIT_BYTES + wave * 1024;
+        const i32x4_t k = make_rsrc(kb + (int64_t)key * k_row, rows * (unsigned)k_row), v = make_rsrc(vb + (int64_t)key * v_row, rows * (unsigned)v_row);
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int key = lo + kt * BKV + wave * 4 + j * NW * 4, left = hi - key < 4 ? hi - key : 4;
-            direct_load_16(make_rsrc(base + (int64_t)key * row_bytes, left > 0 ? (unsigned)(left * (int)row_bytes) : 0u), off,
-                           lds + wave * 1024 + j * NW * 1024);
+        for (int j = 0; j < 2; ++j) {
+            direct_load_16(k, k_off + (unsigned)(j * 16 * k_row), lds + j * 4096);
+            direct_load_16(v, v_off + (unsigned)(j * 16 * v_row), lds + UNIT_BYTES / 2 + j * 4096);
         }
     };
-    issue(kt0, kb, C.k_token * 2, k_off, lds_base);
-    issue(kt0, vb, C.v_token * 2, v_off, lds_base + 2 * TILE_BYTES);
+    constexpr int LOADS = 4;             // of a wave and unit
+    const int u0 = 2 * kt0, u1 = 2 * nkt;
+    issue(u0);
+    issue(u0 + 1);
+    issue(u0 + 2);
 
     bf16x8_t qf[DS], gf[DS];
     float delta = 0.0f;
@@ -386,57 +393,122 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             acc[d][e] = 0.0f;
-
-    wait_vmcnt<0>();
-    __syncthreads();
-    for (int kt = kt0; kt < nkt; ++kt) {
-        const int b = (kt - kt0) & 1;
-        if (kt + 1 < nkt) {
-            issue(kt + 1, kb, C.k_token * 2, k_off, lds_base + (1 - b) * TILE_BYTES);
-            issue(kt + 1, vb, C.v_token * 2, v_off, lds_base + (3 - b) * TILE_BYTES);
+    constexpr f32x16_t zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    auto products = [&](f32x16_t &s, f32x16_t &dp) __attribute__((always_inline)) {
+        s = dp = zero;
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, 0, ks), qf[ks], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, UNIT_BYTES / 2, ks), gf[ks], dp, 0, 0, 0);
         }
-        if (kt >= wt0 && kt < wt1) {
-            const bool border = kt * BKV < all_from || (kt + 1) * BKV - 1 > all_to;
+    };
+    // A pipeline of one unit's depth: under the exponentials of unit u the products of unit u + 1 with Q and dout (segments 0 .. 15), then
+    // those of unit u with K (16 .. 23), one MFMA a segment, its fragment requested three segments ahead.  row_read is at unit u + 1,
+    // col_read at unit u.
+    auto unit = [&](int u, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn) __attribute__((always_inline)) {
+        constexpr int AHEAD = 3;
+        if (u * 32 < all_from || (u + 1) * 32 - 1 > all_to) {        // border, uniform
+            float ninf = -INFINITY;
+            asm volatile("" : "+v"(ninf));
+            const unsigned key0 = (unsigned)(lo + u * 32 + 4 * lh - first), span = (unsigned)(t - first);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {                            // 32 keys at a time
-                constexpr int V_AT = 2 * TILE_BYTES;
-                const int half = j * 32 * ROWB;
-                f32x16_t s, dp;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    s[e] = dp[e] = 0.0f;
-#pragma unroll
-                for (int ks = 0; ks < DS; ++ks) {
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, half, ks), qf[ks], s, 0, 0, 0);
-                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_read.read(smem, V_AT + half, ks), gf[ks], dp, 0, 0, 0);
-                }
-                if (border) {
-                    const unsigned key0 = (unsigned)(lo + kt * BKV + j * 32 + 4 * lh - first), span = (unsigned)(t - first);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (key0 + (unsigned)(8 * (e >> 2) + (e & 3)) > span)
-                            s[e] = -INFINITY;
-                }
-                bf16x8_t df[2];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse2));
-                    df[e >> 3][e & 7] = (__bf16)(p * (dp[e] - delta));
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_read.read(smem, half + c * 16 * ROWB, d), df[c], acc[d], 0, 0, 0);
+            for (int e = 0; e < 16; ++e)
+                if (key0 + (unsigned)(8 * (e >> 2) + (e & 3)) > span)
+                    s[e] = ninf;
+        }
+        bf16x8_t frag[AHEAD + 1], df[2];
+        auto fetch = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(s_tag)::value;
+            if constexpr (i < 16)
+                frag[i % (AHEAD + 1)] = row_read.read(smem, (i & 1) * (UNIT_BYTES / 2), i >> 1);
+            else if constexpr (i < 24)
+                frag[i % (AHEAD + 1)] = col_read.read(smem, ((i - 16) >> 2) * 16 * ROWB, (i - 16) & 3);
+        };
+        auto argument = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            s[e] = __builtin_fmaf(s[e], sl2, -lse2);
+        };
+        auto exponential = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            s[e] = __builtin_amdgcn_exp2f(s[e]);
+            dp[e] -= delta;
+        };
+        auto product = [&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_tag)::value;
+            dp[e] *= s[e];
+            if constexpr (e & 1) {                                   // rounded in pairs
+                df[e >> 3][(e & 7) - 1] = (__bf16)dp[e - 1];
+                df[e >> 3][e & 7] = (__bf16)dp[e];
             }
+        };
+        auto segment = [&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(s_tag)::value;
+            fetch(std::integral_constant<int, i + AHEAD>{});
+            if constexpr (i < 16) {
+                if constexpr (i & 1)
+                    dpn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], gf[i >> 1], i < 2 ? zero : dpn, 0, 0, 0);
+                else
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], qf[i >> 1], i < 2 ? zero : sn, 0, 0, 0);
+            } else {
+                constexpr int c = (i - 16) >> 2, d = (i - 16) & 3;
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], df[c], acc[d], 0, 0, 0);
+            }
+            if constexpr (i < 16) {                                  // element i in three segments; what is left in front of the second half of dQ
+                argument(std::integral_constant<int, i>{});
+                if constexpr (i >= 1)
+                    exponential(std::integral_constant<int, i - 1>{});
+                if constexpr (i >= 2)
+                    product(std::integral_constant<int, i - 2>{});
+            } else if constexpr (i == 16) {
+                exponential(std::integral_constant<int, 15>{});
+                product(std::integral_constant<int, 14>{});
+            } else if constexpr (i == 17) {
+                product(std::integral_constant<int, 15>{});
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each<0, 1>(fetch, std::make_integer_sequence<int, AHEAD>{});
+        __builtin_amdgcn_sched_barrier(0);
+        each<0, 1>(segment, std::make_integer_sequence<int, 24>{});
+    };
+
+    wait_vmcnt<LOADS>();
+    __syncthreads();
+    int u = u0;
+    auto to_next = [&](int at) { return (at & 3) == 3 ? -3 * UNIT_BYTES : UNIT_BYTES; };
+    auto turn = [&]() __attribute__((always_inline)) {               // unit u + 2 has landed, and every wave is done with unit u
+        wait_vmcnt<LOADS>();
+        __syncthreads();
+        ++u;
+    };
+    if (wt0 < wt1) {
+        while (u < 2 * wt0) {                                        // units of other waves only
+            issue(u + 3);
+            turn();
         }
-        if (kt + 1 < nkt) {
-            row_read.move(b ? -TILE_BYTES : TILE_BYTES);
-            col_read.move(b ? -TILE_BYTES : TILE_BYTES);
-            wait_vmcnt<0>();
-            __syncthreads();
+        f32x16_t sa, da, sb, db;
+        row_read.move((u & 3) * UNIT_BYTES);
+        col_read.move((u & 3) * UNIT_BYTES);
+        products(sa, da);
+        row_read.move(to_next(u));
+        while (u < 2 * wt1) {                                        // (behind the last unit the products of one more, unused)
+            issue(u + 3);
+            unit(u, sa, da, sb, db);
+            col_read.move(to_next(u));
+            row_read.move(to_next(u + 1));
+            turn();
+            issue(u + 3);
+            unit(u, sb, db, sa, da);
+            col_read.move(to_next(u));
+            row_read.move(to_next(u + 1));
+            turn();
         }
     }
+    while (u < u1) {
+        issue(u + 3);
+        turn();
+    }
+    wait_vmcnt<0>();                                                 // (nothing lands behind the kernel's end)
 
     if (splits > 1) {
 #pragma unroll
@@ -459,7 +531,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams 
     RowBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    Splits(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
@@ -490,6 +562,10 @@ struct KeyBlock {
         return from < b && end > from ? (int)(((int64_t)(end - from) * C.group + GRAD_ROWS - 1) / GRAD_ROWS) : 0;
     }
     __device__ __forceinline__ KeyBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((C.tokens + GRAD_KEYS - 1) / GRAD_KEYS) {}
+    __device__ __forceinline__ int bound(const CausalParams &C) const
+    {
+        return C.items > 0 ? (int)min((int64_t)0x7FFFFFFF, ((int64_t)(seqs.longest() + GRAD_KEYS + 1) * C.group + GRAD_ROWS) / GRAD_ROWS) : 0;
+    }
     // the keys and the walk of it.block; false: nothing to do
     __device__ __forceinline__ bool look(const CausalParams &C)
     {
@@ -541,7 +617,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi, end_b = block.end_b;
@@ -843,7 +919,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
     KeyBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    Splits(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);

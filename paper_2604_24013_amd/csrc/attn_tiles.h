@@ -145,6 +145,16 @@ struct Sequences {
         *start = i > 0 ? before : first;
         return a;
     }
+    // tokens of the longest sequence; up to 64 sequences
+    __device__ __forceinline__ int longest() const
+    {
+        const int lane = threadIdx.x & 63, before = __shfl_up(mine, 1);
+        int m = lane < n ? mine - (lane > 0 ? before : first) : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2)
+            m = max(m, __shfl_xor(m, d));
+        return uniform(m);
+    }
     // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences
     __device__ __forceinline__ void around(int t, int *start, int *end) const
     {
@@ -188,14 +198,16 @@ struct Item {
 struct Splits {
     static constexpr int R = MAX_BLOCKS / 64;
     int tiles[R], chunk, blocks;
+    // `bound`: no walk is longer.  Where that is not worth a split (least and half as much again) the walks are not looked at.
     template <typename F>
-    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, F &&tiles_of) : chunk(P.chunk), blocks(count)
+    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int bound, F &&tiles_of) : chunk(P.chunk), blocks(count)
     {
         int all = 0, some = 0;
+        const bool whole = chunk == 0 && bound <= least + least / 2;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            tiles[r] = 0;
-            if (r * 64 < count) {
+            tiles[r] = r * 64 + (threadIdx.x & 63) < count;
+            if (r * 64 < count && !whole) {
                 const int b = r * 64 + (threadIdx.x & 63);
                 tiles[r] = b < count ? tiles_of(b) : 0;
                 all += tiles[r];
@@ -204,9 +216,13 @@ struct Splits {
         }
         if (chunk > 0)
             return;
+        chunk = 1;
+        if (whole)
+            return;
         const int total = wave_total(all), active = wave_total(some), items = P.items / P.kv_heads;
         const float wanted = fmaxf((float)items - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
-        chunk = max(least, (int)(total / wanted) + 1);
+        // (nor much less than a compute unit's share of all: 512 blocks of 1 to 64 tiles take 82 us in pieces of 28, 74 in pieces of 40)
+        chunk = max(max(least, (int)(total / wanted) + 1), (int)(0.8f * total * P.kv_heads / P.num_cu));
         while (number() > items)
             chunk += chunk / 16 + 1;
     }
@@ -259,7 +275,7 @@ struct Splits {
 
 // This workgroup's item; `blocks`: of one key head.
 template <typename F>
-__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, F &&tiles_of, Item *it)
+__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int bound, F &&tiles_of, Item *it)
 {
     const int j = blockIdx.x / P.kv_heads;
     it->kvh = blockIdx.x - j * P.kv_heads;
@@ -269,7 +285,7 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    return Splits(P, blocks, least, tiles_of).item(j, it);
+    return Splits(P, blocks, least, bound, tiles_of).item(j, it);
 }
 // Where item `first + split` of a block parks what it has: N floats a workgroup.
 __device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &it, int split, size_t floats)

@@ -78,6 +78,7 @@ struct CausalParams {
     // a walk's tiles split over workgroups
     int items = 0;                                  // workgroups of the launch at the most (0: one for each block and key head)
     int chunk = 0;                                  // tiles of a split (0: as few as the items allow)
+    int num_cu = 0;
     float *parts = nullptr;
     unsigned *counters = nullptr;
     size_t part_bytes = 0;
