@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int lh = lane >> 5;
 
     RowBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams 
     RowBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    Splits(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi, end_b = block.end_b;
@@ -919,7 +919,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
     KeyBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    Splits(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);

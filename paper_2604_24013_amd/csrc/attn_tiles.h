@@ -198,9 +198,9 @@ struct Item {
 struct Splits {
     static constexpr int R = MAX_BLOCKS / 64;
     int tiles[R], chunk, blocks;
-    // `bound`: no walk is longer.  Where that is not worth a split (least and half as much again) the walks are not looked at.
+    // `grain`: a split takes a multiple of it, where a workgroup's waves take tiles in turn.  `bound`: no walk is longer.  Where that is not worth a split (least and half as much again) the walks are not looked at.
     template <typename F>
-    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int bound, F &&tiles_of) : chunk(P.chunk), blocks(count)
+    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int grain, int bound, F &&tiles_of) : chunk(P.chunk), blocks(count)
     {
         int all = 0, some = 0;
         const bool whole = chunk == 0 && bound <= least + least / 2;
@@ -223,8 +223,9 @@ struct Splits {
         const float wanted = fmaxf((float)items - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
         // (nor much less than a compute unit's share of all: 512 blocks of 1 to 64 tiles take 82 us in pieces of 28, 74 in pieces of 40)
         chunk = max(max(least, (int)(total / wanted) + 1), (int)(0.8f * total * P.kv_heads / P.num_cu));
+        chunk = (chunk + grain - 1) / grain * grain;
         while (number() > items)
-            chunk += chunk / 16 + 1;
+            chunk += chunk / 16 / grain * grain + grain;
     }
     __device__ __forceinline__ int of(int t) const { return t <= 0 ? 0 : (int)((float)(t + chunk - 1) * __builtin_amdgcn_rcpf((float)chunk) * 1.0000002f); }
     __device__ __forceinline__ int number() const
@@ -275,7 +276,7 @@ struct Splits {
 
 // This workgroup's item; `blocks`: of one key head.
 template <typename F>
-__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int bound, F &&tiles_of, Item *it)
+__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, F &&tiles_of, Item *it)
 {
     const int j = blockIdx.x / P.kv_heads;
     it->kvh = blockIdx.x - j * P.kv_heads;
@@ -285,7 +286,7 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    return Splits(P, blocks, least, bound, tiles_of).item(j, it);
+    return Splits(P, blocks, least, grain, bound, tiles_of).item(j, it);
 }
 // Where item `first + split` of a block parks what it has: N floats a workgroup.
 __device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &it, int split, size_t floats)
