@@ -569,8 +569,10 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
  *        empty).  Rows of no sequence (in front of seq_start[0], behind seq_start[n_seqs]) are left as they were.
  * Scores, softmax and sums in fp32; probabilities are rounded to bf16 for the product with V.  What a token does not see has no
  * influence on its result, infinities and NaN included.  With a registered workspace (commfuse_set_workspace; size that lets
- * every choice be used: commfuse_attn_prompt_workspace_bytes) long rows of keys are split over several workgroups.
- * head_dim must be 128 (CF_ERR_UNSUPPORTED otherwise). */
+ * every choice be used, here and for the gradient: commfuse_attn_prompt_workspace_bytes) the keys of long sequences are split
+ * over several workgroups where rows are too few to fill the chip (up to 64 sequences); without one, or with a smaller one, they are
+ * not, or less.  Calls that overlap in time must not share a workspace.  The bits of a result depend on the split.
+ * head_dim must be 128, token strides at most 2^23 elements (CF_ERR_UNSUPPORTED otherwise). */
 typedef struct {
     int64_t tokens;
     int32_t n_seqs;
@@ -589,7 +591,7 @@ size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc);
  * (dK, dV summed over the query heads of a key head).  out and lse as the forward call left them; dout bf16 with the strides of
  * out; dQ, dK, dV bf16 with the strides of Q, K, V; delta fp32 [heads][tokens], scratch of the caller's.  P and dS are rounded to
  * bf16 for their products, sums are fp32, no atomics: the same call gives the same bits.  Rows of no sequence are left as they
- * were.  None of dQ, dK, dV may overlap an operand. */
+ * were.  None of dQ, dK, dV may overlap an operand.  Workspace as above. */
 cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const void *out,
                                     const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK,
                                     void *dV, void *hip_stream);

@@ -15,7 +15,7 @@
 // but zero times an infinite or NaN V is NaN: a row whose result is not finite is computed once more, key by key
 // (`careful_row`), which reads visible keys only.
 // Packed prompts: a workgroup takes consecutive rows whatever sequences they belong to; keys of the walk that belong to another
-// sequence are masked like any others.  Bound: the matrix pipe; see choose_prompt for the split of the keys.
+// sequence are masked like any others.
 #include "attn_tiles.h"
 
 namespace cf {
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         } else {
             const int seq = block % P.n_seqs, nth = blocks - 1 - block / P.n_seqs;
             const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
-            const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens, m = to - from;
+            const int from = clamped(q0, P.tokens), m = clamped(q1, P.tokens) - from;
             int n = P.kv_len[seq];
             n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
             const int rows = m < P.max_q ? m : P.max_q;              // rows behind max_q are left as they were
@@ -700,7 +700,7 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part
     const int64_t all = blocks * p.kv_heads;
     p.items = p.chunk = 0;
     p.num_cu = num_cu;
-    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || p.n_seqs > 64 || (counted && all > p.max_counters) || longest < 2)
+    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (p.table == nullptr && p.n_seqs > 64) || (counted && all > p.max_counters) || longest < 2)
         return all;
     const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);
     int64_t items = tn.causal_chunk ? all * ((longest + tn.causal_chunk - 1) / tn.causal_chunk) : (rounds > 1 ? rounds : 1) * num_cu / p.kv_heads * p.kv_heads;

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     // Keys that a sequence's last row sees, over all of which its waves walk
     auto keys_of = [&](int seq) {
         const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
-        const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens, m = to - from, some = m < P.max_q ? m : P.max_q;
+        const int m = clamped(q1, P.tokens) - clamped(q0, P.tokens), some = m < P.max_q ? m : P.max_q;
         int n = P.kv_len[seq];
         n = (n < 0 ? 0 : n < P.max_kv ? n : P.max_kv) - m + some;
         return some <= 0 ? -1 : n > 0 ? n : 0;
@@ -58,8 +58,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     const int group = seq * P.kv_heads + kvh;
 
     const int q0 = P.starts[seq], q1 = P.starts[seq + 1];
-    const int from = q0 < 0 ? 0 : q0, to = q1 < P.tokens ? q1 : P.tokens;
-    const int m = to - from;                                         // rows of the sequence
+    const int from = clamped(q0, P.tokens), m = clamped(q1, P.tokens) - from;     // rows of the sequence
     int n = P.kv_len[seq];
     n = n < 0 ? 0 : n < P.max_kv ? n : P.max_kv;
     const int rows = (m < P.max_q ? m : P.max_q) * G;                // at most 16 QT

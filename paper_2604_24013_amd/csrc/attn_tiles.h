@@ -98,6 +98,9 @@ __device__ __forceinline__ float sum_of_halves(float x)
     return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
+// A start that a table holds, as a row of the tensor or the one behind its last, whatever it is.
+__device__ __forceinline__ int clamped(int start, int tokens) { return start < 0 ? 0 : start < tokens ? start : tokens; }
+
 // The packed sequences' starts, as every wave needs them: up to 64 sequences from one load, a start a lane; more from memory.
 struct Sequences {
     const int32_t *starts;

@@ -127,7 +127,8 @@ __device__ __forceinline__ void store_unit(T *row, const Unit &at, const float (
     store<T, W>(row + at.b, b);
 }
 
-// The rotated unit: x holds features a .. a + W - 1, then b .. b + W - 1.
+// The rotated unit: x holds features a .. a + W - 1, then b .. b + W - 1.  (Which product is rounded is written down: left to the compiler,
+// a row that the cache's writer rotates and one rotated by itself came out a bit apart now and then.)
 template <int W>
 __device__ __forceinline__ void turn_unit(float (&x)[2 * W], const float (&c)[W], const float (&s)[W], bool interleaved)
 {
@@ -135,15 +136,15 @@ __device__ __forceinline__ void turn_unit(float (&x)[2 * W], const float (&c)[W]
 #pragma unroll
         for (int e = 0; e < W; ++e) {
             const float p = x[2 * e], q = x[2 * e + 1];
-            x[2 * e] = p * c[e] - q * s[e];
-            x[2 * e + 1] = q * c[e] + p * s[e];
+            x[2 * e] = __builtin_fmaf(p, c[e], -(q * s[e]));
+            x[2 * e + 1] = __builtin_fmaf(q, c[e], p * s[e]);
         }
     } else {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
             const float p = x[e], q = x[W + e];
-            x[e] = p * c[e] - q * s[e];
-            x[W + e] = q * c[e] + p * s[e];
+            x[e] = __builtin_fmaf(p, c[e], -(q * s[e]));
+            x[W + e] = __builtin_fmaf(q, c[e], p * s[e]);
         }
     }
 }
