@@ -23,6 +23,8 @@ namespace {
 
 constexpr int LEAST_TILES = 8;           // of a split: as long as a workgroup's start and hand-over take
 
+constexpr int PARKED = DH / 32 * 16 + 4; // floats that a thread parks: its part of O, and m and l
+
 // (a call: inlined, its loops would have the walk's registers spilled)
 template <int SRC>
 __device__ __noinline__ void careful_row_called(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     Item it;
     const int all_blocks = SRC == PACKED ? blocks : blocks * P.n_seqs;
     const int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
-    if (!my_item(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
+    if (!my_item<NT>(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
             Walk w = walk_of(block);
             if constexpr (SRC == PACKED) {
                 int end;
@@ -127,8 +129,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 
     // This workgroup's key tiles: [kt0, nkt) of the block's
     const int tiles = (hi - lo + BKV - 1) / BKV;
-    const int kt0 = (int)(((int64_t)tiles * split) / splits);
-    const int nkt = (int)(((int64_t)tiles * (split + 1)) / splits);
+    int kt0, nkt;
+    it.share(tiles, &kt0, &nkt);
 
     // The lane's row
     const int r = row0 + wave * 32 + lq;
@@ -151,19 +153,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // `all_to` or earlier
     int wt0 = kt0, wt1 = kt0, all_from = 0, all_to = 0;
     {
-        int f_min = there ? first : 0x7FFFFFFF, f_max = there ? first : 0, l_min = there ? last : 0x7FFFFFFF, l_max = there ? last : -1;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            f_min = min(f_min, __shfl_xor(f_min, d));
-            f_max = max(f_max, __shfl_xor(f_max, d));
-            l_min = min(l_min, __shfl_xor(l_min, d));
-            l_max = max(l_max, __shfl_xor(l_max, d));
-        }
-        f_min = uniform(f_min);
-        l_max = uniform(l_max);
-        all_from = uniform(f_max) - lo;
-        all_to = uniform(l_min) - lo;
-        if (l_max >= f_min) {
+        int f_min, f_max, l_min, l_max;
+        if (edges(there, first, last, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+            all_from = f_max - lo;
+            all_to = l_min - lo;
             wt0 = max(kt0, (f_min - lo) / BKV);
             wt0 -= (wt0 - kt0) & 1;                  // (buffers and registers alternate together)
             wt1 = min(nkt, (l_max - lo) / BKV + 1);
@@ -537,32 +530,27 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     }
     l_run = sum_of_halves(l_run);                                    // the whole row sums, in both lanes of the row
 
-    // Key split: park (m, l, O) in the workspace, thread-major so that every access is a coalesced 4 bytes per lane; the
-    // workgroup that arrives last merges all splits in split order.  Device-coherent cache policy on exactly these accesses, relaxed
-    // agent-scope atomics on the counter.
+    // Key split: park (m, l, O) in the workspace, thread-major, sixteen bytes a lane; the workgroup that arrives last merges all
+    // splits in split order, its own from its registers.  Device-coherent cache policy on exactly these accesses, relaxed agent-scope
+    // atomics on the counter.
     if (splits > 1) {
         constexpr int COHERENT = 1 | 16;
-        constexpr int NV = DT * 16 + 2;                              // floats per thread
-        const size_t part = (size_t)NV * NT;
+        const size_t part = (size_t)PARKED * NT;
         const int group = it.block * P.kv_heads + kvh;
         auto part_rsrc = [&](int sp) {
             return __builtin_amdgcn_make_buffer_rsrc(parked_at(P, it, sp, part), 0, (int)(part * 4), 0x00020000);
         };
         {
             __amdgpu_buffer_rsrc_t rs = part_rsrc(split);
-            auto park = [&](float x, int i) __attribute__((always_inline)) {
-                // (through a plain VGPR: storing the accumulator elements straight from their AGPRs
-                // came out of this compiler as sixteen stores of element 0)
-                asm volatile("" : "+v"(x));
-                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), rs, (i * NT + tid) * 4, 0, COHERENT);
+            auto park = [&](f32x4_t x, int i) __attribute__((always_inline)) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), rs, (i * NT + tid) * 16, 0, COHERENT);
             };
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    park(oacc[d][e], d * 16 + e);
-            park(m_run, DT * 16);
-            park(l_run, DT * 16 + 1);
+                for (int e = 0; e < 16; e += 4)
+                    park(f32x4_t{oacc[d][e], oacc[d][e + 1], oacc[d][e + 2], oacc[d][e + 3]}, d * 4 + e / 4);
+            park(f32x4_t{m_run, l_run, 0.0f, 0.0f}, DT * 4);
         }
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -574,43 +562,51 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             return;
         if (tid == 0)
             __hip_atomic_store(&P.counters[group], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        auto ld = [&](__amdgpu_buffer_rsrc_t rs, int i) {
-            return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (i * NT + tid) * 4, 0, COHERENT));
-        };
-        float m_all = -INFINITY;
-        for (int sp0 = 0; sp0 < splits; sp0 += 8) {                  // eight maxima in flight (beyond the last: the last once more)
-            float m[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                m[i] = ld(part_rsrc(sp0 + i < splits ? sp0 + i : splits - 1), DT * 16);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                m_all = fmaxf(m_all, m[i]);
-        }
-        l_run = 0.0f;
-        m_run = m_all;
+        f32x16_t sum[DT];
+        float m_all = -3.402823466e38f, l_all = 0.0f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                oacc[d][e] = 0.0f;
+                sum[d][e] = 0.0f;
+#pragma unroll 1
         for (int sp = 0; sp < splits; ++sp) {
-            __amdgpu_buffer_rsrc_t rs = part_rsrc(sp);
-            const float m = ld(rs, DT * 16), l = ld(rs, DT * 16 + 1);
-            float v[DT][16];
+            f32x16_t v[DT];
+            float m = m_run, l = l_run;
+            if (sp == split) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+                    v[d] = oacc[d];
+            } else {
+                __amdgpu_buffer_rsrc_t rs = part_rsrc(sp);
+                auto ld = [&](int i) { return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (i * NT + tid) * 16, 0, COHERENT)); };
+                const f32x4_t ml = ld(DT * 4);
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const f32x4_t x = ld(d * 4 + e / 4);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[d][e + k] = x[k];
+                    }
+                m = ml[0];
+                l = ml[1];
+            }
+            const float m_new = fmaxf(m_all, m), back = exp2f(m_all - m_new), f = exp2f(m - m_new);   // (a row that sees no key of a split: nothing times a factor)
+            m_all = m_new;
+            l_all = l_all * back + l * f;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    v[d][e] = ld(rs, d * 16 + e);
-            const float f = exp2f(m - m_all);                        // (a row that sees no key of a split: nothing times a factor)
-            l_run += l * f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    oacc[d][e] += f * v[d][e];
+                    sum[d][e] = sum[d][e] * back + v[d][e] * f;
         }
+        m_run = m_all;
+        l_run = l_all;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            oacc[d] = sum[d];
     }
 
     // O = O^T / l, rounded to bf16; a row without a visible key is 0 and its log-sum-exp -inf.
@@ -678,7 +674,7 @@ hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t part_bytes(int waves) { return (size_t)(64 + 2) * (64 * waves) * sizeof(float); }
+size_t part_bytes(int waves) { return (size_t)PARKED * (64 * waves) * sizeof(float); }
 
 // Four waves (128 rows) or eight; the launch's workgroups.
 int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, int64_t tiles, int num_cu, int64_t *wgs)

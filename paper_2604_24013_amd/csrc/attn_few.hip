@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         return some <= 0 ? -1 : n > 0 ? n : 0;
     };
     Item it;
-    if (!my_item(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
+    if (!my_item<NT>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
             const int keys = keys_of(seq);
             return keys < 0 ? 0 : max(1, (keys + FEW_KEYS - 1) / FEW_KEYS);
         }, &it))
@@ -66,7 +66,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         return;
     const int hi = n - m + (rows - 1) / G + 1 > 0 ? n - m + (rows - 1) / G + 1 : 0;   // keys that the last row sees
     const int tiles = (hi + FEW_KEYS - 1) / FEW_KEYS;
-    const int t0 = (int)(((int64_t)tiles * split) / splits), t1 = (int)(((int64_t)tiles * (split + 1)) / splits);
+    int t0, t1;
+    it.share(tiles, &t0, &t1);
 
     const int32_t *table = P.table + (int64_t)seq * P.max_pages;
     const int shift = P.pool.page_shift, n_pages = (int)P.pool.n_pages;

@@ -313,29 +313,21 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int lh = lane >> 5;
 
     RowBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
-    const int kt0 = (int)(((int64_t)block.tiles * split) / splits), nkt = (int)(((int64_t)block.tiles * (split + 1)) / splits);
+    int kt0, nkt;
+    block.it.share(block.tiles, &kt0, &nkt);
     const DqRow row(C, block, kvh);
     const int t = row.t, head = row.head, first = row.first;
     const bool there = row.there;
-    int wt0 = kt0, wt1 = kt0, all_from, all_to;
+    int wt0 = kt0, wt1 = kt0, all_from = 0, all_to = 0;
     {
-        int f_min = there ? first : 0x7FFFFFFF, f_max = there ? first : 0, l_min = there ? t : 0x7FFFFFFF, l_max = there ? t : -1;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            f_min = min(f_min, __shfl_xor(f_min, d));
-            f_max = max(f_max, __shfl_xor(f_max, d));
-            l_min = min(l_min, __shfl_xor(l_min, d));
-            l_max = max(l_max, __shfl_xor(l_max, d));
-        }
-        f_min = uniform(f_min);
-        l_max = uniform(l_max);
-        all_from = uniform(f_max) - lo;
-        all_to = uniform(l_min) - lo;
-        if (l_max >= f_min) {
+        int f_min, f_max, l_min, l_max;
+        if (edges(there, first, t, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+            all_from = f_max - lo;
+            all_to = l_min - lo;
             wt0 = max(kt0, (f_min - lo) / BKV);
             wt1 = min(nkt, (l_max - lo) / BKV + 1);
         }
@@ -531,7 +523,8 @@ __global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams 
     RowBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    __shared__ int looked_at[MAX_BLOCKS];
+    Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
@@ -617,30 +610,22 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock block(C);
-    if (!my_item(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi, end_b = block.end_b;
-    const int rt0 = (int)(((int64_t)block.tiles * split) / splits), nrt = (int)(((int64_t)block.tiles * (split + 1)) / splits);
+    int rt0, nrt;
+    block.it.share(block.tiles, &rt0, &nrt);
     const GradKey mine(C, block);
     const int kk = mine.key, end = mine.end;
     const bool there = mine.there;
     const int from = kk * G, to = there ? end * G : from;            // the rows that see it
-    int wr0 = rt0, wr1 = rt0, all_from, all_to;
+    int wr0 = rt0, wr1 = rt0, all_from = 0, all_to = 0;
     {
-        int f_min = there ? from : 0x7FFFFFFF, f_max = there ? from : 0, l_min = there ? to : 0x7FFFFFFF, l_max = there ? to : 0;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            f_min = min(f_min, __shfl_xor(f_min, d));
-            f_max = max(f_max, __shfl_xor(f_max, d));
-            l_min = min(l_min, __shfl_xor(l_min, d));
-            l_max = max(l_max, __shfl_xor(l_max, d));
-        }
-        f_min = uniform(f_min);
-        l_max = uniform(l_max);
-        all_from = uniform(f_max) - lo;
-        all_to = uniform(l_min) - lo;
-        if (l_max > f_min) {
+        int f_min, f_max, l_min, l_max;
+        if (edges(there, from, to, &f_min, &f_max, &l_min, &l_max) && l_max > f_min) {
+            all_from = f_max - lo;
+            all_to = l_min - lo;
             wr0 = max(rt0, (f_min - lo) / ROWS);
             wr1 = min(nrt, (l_max - lo + ROWS - 1) / ROWS);
         }
@@ -919,7 +904,8 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
     KeyBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }).of_block(block.it.block, &block.it);
+    __shared__ int looked_at[MAX_BLOCKS];
+    Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);

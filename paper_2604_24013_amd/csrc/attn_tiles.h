@@ -101,6 +101,30 @@ __device__ __forceinline__ float sum_of_halves(float x)
 // A start that a table holds, as a row of the tensor or the one behind its last, whatever it is.
 __device__ __forceinline__ int clamped(int start, int tokens) { return start < 0 ? 0 : start < tokens ? start : tokens; }
 
+// Inclusive sums over the wave's lanes.
+__device__ __forceinline__ int scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below in a row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // rows 1 and 3: the last lane of the row below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // rows 2 and 3: lane 31
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan(x), 63); }
+// The largest of the lanes' values, and zero.
+__device__ __forceinline__ int wave_most(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // The packed sequences' starts, as every wave needs them: up to 64 sequences from one load, a start a lane; more from memory.
 struct Sequences {
     const int32_t *starts;
@@ -152,37 +176,33 @@ struct Sequences {
     __device__ __forceinline__ int longest() const
     {
         const int lane = threadIdx.x & 63, before = __shfl_up(mine, 1);
-        int m = lane < n ? mine - (lane > 0 ? before : first) : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2)
-            m = max(m, __shfl_xor(m, d));
-        return uniform(m);
+        return wave_most(lane < n ? mine - (lane > 0 ? before : first) : 0);
     }
-    // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences
+    // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences.  Every
+    // lane takes part.
     __device__ __forceinline__ void around(int t, int *start, int *end) const
     {
-        *start = first;
-        *end = 0x7FFFFFFF;
-        for (int i = 0; i < n; ++i) {
-            const int e = __builtin_amdgcn_readlane(mine, i);
-            *start = e <= t ? e : *start;
-            *end = e > t && e < *end ? e : *end;
+        if (n <= 8) {
+            *start = first;
+            *end = 0x7FFFFFFF;
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const int e = __builtin_amdgcn_readlane(mine, i);
+                *start = e <= t ? e : *start;
+                *end = e > t && e < *end ? e : *end;
+            }
+        } else {
+            int i = 0;                   // how many are <= t
+#pragma unroll 1
+            for (int step = 32; step > 0; step /= 2)
+                i += __shfl(mine, i + step - 1) <= t ? step : 0;
+            i += __shfl(mine, i) <= t;
+            const int before = __shfl(mine, (i - 1) & 63), e = __shfl(mine, i & 63);
+            *start = i > 0 ? before : first;
+            *end = i < n ? e : 0x7FFFFFFF;
         }
     }
 };
-
-// Inclusive sums over the wave's lanes.
-__device__ __forceinline__ int scan(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // from 1, 2, 4, 8 lanes below in a row of 16
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // rows 1 and 3: the last lane of the row below
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // rows 2 and 3: lane 31
-    return x;
-}
-__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan(x), 63); }
 
 // What a workgroup works on.  Walks under a causal mask are of all lengths, which only the tables on the device know, and a launch takes as
 // long as its fullest compute unit.  So every workgroup looks at the walks of all blocks, a lane a block, and cuts them into splits of at most
@@ -191,42 +211,57 @@ __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readl
 // workgroups each takes 33 us, with a quarter more than fit, 47.)  A grid of all blocks by the largest number of splits needs no
 // search, but three workgroups of four then have nothing to do and hold up the others: dK and dV of 4096 tokens, 8 heads on one key
 // head, took 148 us so.
-constexpr int MAX_BLOCKS = 512;          // of one key head, that are looked at: eight a lane
+constexpr int MAX_BLOCKS = 512;          // of one key head, that are looked at
 struct Item {
     int kvh, block, split, splits;       // key heads innermost: neighbouring workgroups go to one XCD in turn, whose L2 holds few heads' keys
     int first;                           // the block's split 0 is this one of its key head's items
+    // The split's share of `tiles`: [*from, *to)
+    __device__ __forceinline__ void share(int tiles, int *from, int *to) const
+    {
+        const unsigned each = (unsigned)tiles / (unsigned)splits;
+        const int over = tiles - (int)each * splits;
+        *from = (int)each * split + (split < over ? split : over);
+        *to = *from + (int)each + (split < over);
+    }
 };
 
-// The splits of all blocks.  tiles_of(block): tiles of a lane's block (0: nothing to do), in the order of dispatch.
+// The splits of all blocks, by a workgroup of NT threads.  tiles_of(block): tiles of a lane's block (0: nothing to do), in the order of
+// dispatch.  They lie in LDS and all loops are loops: unrolled, eight blocks a lane in registers, the same took 1 us more, much of it
+// for fetching 14 KiB of instructions.
+template <int NT>
 struct Splits {
-    static constexpr int R = MAX_BLOCKS / 64;
-    int tiles[R], chunk, blocks;
-    // `grain`: a split takes a multiple of it, where a workgroup's waves take tiles in turn.  `bound`: no walk is longer.  Where that is not worth a split (least and half as much again) the walks are not looked at.
+    const int *tiles;
+    int chunk, blocks;
+    // `grain`: a split takes a multiple of it, where a workgroup's waves take tiles in turn.  `bound`: no walk is longer.  Where that is not
+    // worth a split (least and half as much again) the walks are not looked at.
     template <typename F>
-    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int grain, int bound, F &&tiles_of) : chunk(P.chunk), blocks(count)
+    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int grain, int bound, F &&tiles_of, int *lds) : tiles(lds), chunk(P.chunk), blocks(count)
     {
-        int all = 0, some = 0;
         const bool whole = chunk == 0 && bound <= least + least / 2;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            tiles[r] = r * 64 + (threadIdx.x & 63) < count;
-            if (r * 64 < count && !whole) {
-                const int b = r * 64 + (threadIdx.x & 63);
-                tiles[r] = b < count ? tiles_of(b) : 0;
-                all += tiles[r];
-                some += tiles[r] > 0;
-            }
+        const int lane = threadIdx.x & 63, up = (count + 63) & ~63;
+#pragma unroll 1
+        for (int b = threadIdx.x; b < up; b += NT) {                 // (whole waves)
+            const int t = whole ? 1 : tiles_of(b < count ? b : count - 1);
+            lds[b] = b < count ? t : 0;
         }
+        __syncthreads();
         if (chunk > 0)
             return;
         chunk = 1;
         if (whole)
             return;
+        int all = 0, some = 0;
+#pragma unroll 1
+        for (int b = lane; b < up; b += 64) {
+            all += lds[b];
+            some += lds[b] > 0;
+        }
         const int total = wave_total(all), active = wave_total(some), items = P.items / P.kv_heads;
         const float wanted = fmaxf((float)items - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
         // (nor much less than a compute unit's share of all: 512 blocks of 1 to 64 tiles take 82 us in pieces of 28, 74 in pieces of 40)
         chunk = max(max(least, (int)(total / wanted) + 1), (int)(0.8f * total * P.kv_heads / P.num_cu));
         chunk = (chunk + grain - 1) / grain * grain;
+#pragma unroll 1
         while (number() > items)
             chunk += chunk / 16 / grain * grain + grain;
     }
@@ -234,53 +269,50 @@ struct Splits {
     __device__ __forceinline__ int number() const
     {
         int n = 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 64 < blocks)
-                n += of(tiles[r]);
+#pragma unroll 1
+        for (int b = 0; b < blocks; b += 64)
+            n += of(tiles[b + (threadIdx.x & 63)]);
         return wave_total(n);
     }
     // Item j of a key head: false: there are not so many.
     __device__ __forceinline__ bool item(int j, Item *it) const
     {
         int base = 0;
-        bool found = false;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 64 < blocks && !found) {
-                const int n = of(tiles[r]), end = base + scan(n);
-                const unsigned long long behind = __builtin_amdgcn_ballot_w64(end > j);
-                base = __builtin_amdgcn_readlane(end, 63);
-                if (behind != 0) {
-                    const int lane = __builtin_ctzll(behind);
-                    it->splits = __builtin_amdgcn_readlane(n, lane);
-                    it->first = __builtin_amdgcn_readlane(end, lane) - it->splits;
-                    it->block = r * 64 + lane;
-                    it->split = j - it->first;
-                    found = true;
-                }
+#pragma unroll 1
+        for (int b = 0; b < blocks; b += 64) {
+            const int n = of(tiles[b + (threadIdx.x & 63)]), end = base + scan(n);
+            const unsigned long long behind = __builtin_amdgcn_ballot_w64(end > j);
+            if (behind != 0) {
+                const int lane = __builtin_ctzll(behind);
+                it->splits = __builtin_amdgcn_readlane(n, lane);
+                it->first = __builtin_amdgcn_readlane(end, lane) - it->splits;
+                it->block = b + lane;
+                it->split = j - it->first;
+                return true;
             }
-        return found;
+            base = __builtin_amdgcn_readlane(end, 63);
+        }
+        return false;
     }
     // The splits of a block, and the first of their items.
     __device__ __forceinline__ void of_block(int block, Item *it) const
     {
         int base = 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r * 64 <= block) {
-                const int n = of(tiles[r]), end = base + scan(n);
-                it->splits = __builtin_amdgcn_readlane(n, block & 63);
-                it->first = __builtin_amdgcn_readlane(end, block & 63) - it->splits;
-                base = __builtin_amdgcn_readlane(end, 63);
-            }
+#pragma unroll 1
+        for (int b = 0; b <= block; b += 64) {
+            const int n = of(tiles[b + (threadIdx.x & 63)]), end = base + scan(n);
+            it->splits = __builtin_amdgcn_readlane(n, block & 63);
+            it->first = __builtin_amdgcn_readlane(end, block & 63) - it->splits;
+            base = __builtin_amdgcn_readlane(end, 63);
+        }
     }
 };
 
 // This workgroup's item; `blocks`: of one key head.
-template <typename F>
+template <int NT, typename F>
 __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, F &&tiles_of, Item *it)
 {
+    __shared__ int tiles[MAX_BLOCKS];
     const int j = blockIdx.x / P.kv_heads;
     it->kvh = blockIdx.x - j * P.kv_heads;
     if (P.items == 0) {
@@ -289,7 +321,22 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    return Splits(P, blocks, least, grain, bound, tiles_of).item(j, it);
+    return Splits<NT>(P, blocks, least, grain, bound, tiles_of, tiles).item(j, it);
+}
+
+// Smallest and largest of a wave's `first` and `last`, both of which grow with the row (lanes 0 .. 31, and the same in the others), over
+// the rows that are there.  False: none is.
+__device__ __forceinline__ bool edges(bool there, int first, int last, int *f_min, int *f_max, int *l_min, int *l_max)
+{
+    const unsigned rows = (unsigned)__builtin_amdgcn_ballot_w64(there);
+    if (rows == 0)
+        return false;
+    const int a = __builtin_ctz(rows), b = 31 - __builtin_clz(rows);
+    *f_min = __builtin_amdgcn_readlane(first, a);
+    *f_max = __builtin_amdgcn_readlane(first, b);
+    *l_min = __builtin_amdgcn_readlane(last, a);
+    *l_max = __builtin_amdgcn_readlane(last, b);
+    return true;
 }
 // Where item `first + split` of a block parks what it has: N floats a workgroup.
 __device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &it, int split, size_t floats)
