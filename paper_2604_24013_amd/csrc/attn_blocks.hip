@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     Item it;
     const int all_blocks = SRC == PACKED ? blocks : blocks * P.n_seqs;
     const int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
-    if (!my_item<NT>(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
+    if (!my_item<NT, NW == 4>(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
             Walk w = walk_of(block);
             if constexpr (SRC == PACKED) {
                 int end;

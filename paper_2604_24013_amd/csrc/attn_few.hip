@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         return some <= 0 ? -1 : n > 0 ? n : 0;
     };
     Item it;
-    if (!my_item<NT>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
+    if (!my_item<NT, false>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
             const int keys = keys_of(seq);
             return keys < 0 ? 0 : max(1, (keys + FEW_KEYS - 1) / FEW_KEYS);
         }, &it))

@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int lh = lane >> 5;
 
     RowBlock block(C);
-    if (!my_item<NT>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -610,7 +610,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock block(C);
-    if (!my_item<NT>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi, end_b = block.end_b;

@@ -231,7 +231,7 @@ struct Item {
 template <int NT>
 struct Splits {
     const int *tiles;
-    int chunk, blocks;
+    int chunk, blocks, items;
     // `grain`: a split takes a multiple of it, where a workgroup's waves take tiles in turn.  `bound`: no walk is longer.  Where that is not
     // worth a split (least and half as much again) the walks are not looked at.
     template <typename F>
@@ -245,24 +245,25 @@ struct Splits {
             lds[b] = b < count ? t : 0;
         }
         __syncthreads();
-        if (chunk > 0)
-            return;
-        chunk = 1;
         if (whole)
+            chunk = 1;
+        if (chunk > 0) {
+            items = number();
             return;
+        }
         int all = 0, some = 0;
 #pragma unroll 1
         for (int b = lane; b < up; b += 64) {
             all += lds[b];
             some += lds[b] > 0;
         }
-        const int total = wave_total(all), active = wave_total(some), items = P.items / P.kv_heads;
-        const float wanted = fmaxf((float)items - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
+        const int total = wave_total(all), active = wave_total(some), most = P.items / P.kv_heads;
+        const float wanted = fmaxf((float)most - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
         // (nor much less than a compute unit's share of all: 512 blocks of 1 to 64 tiles take 82 us in pieces of 28, 74 in pieces of 40)
         chunk = max(max(least, (int)(total / wanted) + 1), (int)(0.8f * total * P.kv_heads / P.num_cu));
         chunk = (chunk + grain - 1) / grain * grain;
 #pragma unroll 1
-        while (number() > items)
+        while ((items = number()) > most)
             chunk += chunk / 16 / grain * grain + grain;
     }
     __device__ __forceinline__ int of(int t) const { return t <= 0 ? 0 : (int)((float)(t + chunk - 1) * __builtin_amdgcn_rcpf((float)chunk) * 1.0000002f); }
@@ -309,19 +310,26 @@ struct Splits {
 };
 
 // This workgroup's item; `blocks`: of one key head.
-template <int NT, typename F>
+// PAIRED: two workgroups share a compute unit, those that are dispatched a whole chip apart.  The second half of the first two rounds is
+// handed out backwards: items become shorter towards the end of a sequence's rows, and two of the same place would share.
+template <int NT, bool PAIRED, typename F>
 __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, F &&tiles_of, Item *it)
 {
     __shared__ int tiles[MAX_BLOCKS];
-    const int j = blockIdx.x / P.kv_heads;
+    int j = blockIdx.x / P.kv_heads;
     it->kvh = blockIdx.x - j * P.kv_heads;
+    auto paired = [&](int number) {
+        const int round = P.num_cu / P.kv_heads, end = number < 2 * round ? number : 2 * round;
+        return PAIRED && j >= round && j < end ? round + end - 1 - j : j;
+    };
     if (P.items == 0) {
-        it->block = it->first = j;
+        it->block = it->first = paired(gridDim.x / P.kv_heads);
         it->split = 0;
         it->splits = 1;
         return true;
     }
-    return Splits<NT>(P, blocks, least, grain, bound, tiles_of, tiles).item(j, it);
+    const Splits<NT> splits(P, blocks, least, grain, bound, tiles_of, tiles);
+    return splits.item(paired(splits.items), it);
 }
 
 // Smallest and largest of a wave's `first` and `last`, both of which grow with the row (lanes 0 .. 31, and the same in the others), over
