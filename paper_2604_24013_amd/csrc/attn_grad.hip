@@ -106,7 +106,7 @@ __device__ __forceinline__ void stages(F1 &&argument, F2 &&exponential, F3 &&pro
         argument(std::integral_constant<int, e1>{});
 }
 
-// A split's sums, N registers of every thread of the workgroup, sixteen (a feature tile) after sixteen; a launch of their own adds them up in
+// A split's sums, `regs` registers of every thread of the workgroup, sixteen (a feature tile) after sixteen; a launch of its own adds them up in
 // split order, eight or four workgroups a block, one a feature tile.  (The last workgroup to arrive adding up all by itself: 4096 tokens, 8
 // heads of one key head, 16 splits of 128 KiB: 575 us instead of TODO for dK and dV.)
 template <int NT>
@@ -516,14 +516,14 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     once_more(odd, [&](int l) { careful_dq(P, __shfl(t, l), __shfl(head, l), __shfl(first, l), -1); });
 }
 
-__global__ __launch_bounds__(64 * DQ_WAVES) void attn_dq_join_kernel(GradParams P)
+// Workgroup `at` of the sums over the splits of dQ: one feature tile of one block.
+__device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked_at)
 {
     const CausalParams &C = P.c;
-    const int tile = blockIdx.x % DT, group = blockIdx.x / DT, kvh = group % C.kv_heads;
+    const int tile = at % DT, group = at / DT, kvh = group % C.kv_heads;
     RowBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    __shared__ int looked_at[MAX_BLOCKS];
     Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
@@ -897,14 +897,14 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     once_more(odd, [&](int l) { careful_key(P, __shfl(kk, l), kvh, __shfl(end, l), -1); });
 }
 
-__global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
+// ... of dK and dV
+__device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looked_at)
 {
     const CausalParams &C = P.c;
-    const int tile = blockIdx.x % (2 * DT), group = blockIdx.x / (2 * DT), kvh = group % C.kv_heads;
+    const int tile = at % (2 * DT), group = at / (2 * DT), kvh = group % C.kv_heads;
     KeyBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    __shared__ int looked_at[MAX_BLOCKS];
     Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
@@ -916,16 +916,30 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(GradParams P)
     once_more(odd, [&](int l) { careful_key(P, __shfl(mine.key, l), kvh, __shfl(mine.end, l), tile); });
 }
 
+// Workgroups below `dkv_wgs`: dK and dV; the others dQ.  (Two launches, 6.3 and 10.1 us for a pack of 4096 tokens and four heads.)
+static_assert(DQ_WAVES == 4, "one shape of workgroup for both");
+__global__ __launch_bounds__(256) void attn_grad_join_kernel(GradParams dkv, GradParams dq, int dkv_wgs)
+{
+    __shared__ int looked_at[MAX_BLOCKS];
+    if ((int)blockIdx.x < dkv_wgs)
+        join_dkv(dkv, blockIdx.x, looked_at);
+    else
+        join_dq(dq, (int)blockIdx.x - dkv_wgs, looked_at);
+}
+
 struct GradLaunches {
     CausalParams dq, dkv;
     int64_t row_blocks, key_blocks;      // of one key head
     int64_t dq_wgs, dkv_wgs;
-    size_t bytes;                        // parked, one launch after the other
+    size_t bytes;                        // parked: a half of the workspace each
 };
 GradLaunches plan_grad(const CausalParams &c, int num_cu)
 {
     GradLaunches g;
     g.dq = g.dkv = c;
+    const size_t half = c.part_bytes / 2 & ~(size_t)255;
+    g.dq.part_bytes = g.dkv.part_bytes = half;
+    g.dkv.parts = c.parts == nullptr ? nullptr : c.parts + half / sizeof(float);
     const int64_t rows = (int64_t)c.tokens * c.group;
     g.row_blocks = (rows + DQ_ROWS - 1) / DQ_ROWS;
     g.key_blocks = (c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
@@ -933,30 +947,31 @@ GradLaunches plan_grad(const CausalParams &c, int num_cu)
     g.dq_wgs = plan_items(g.dq, g.row_blocks, (c.tokens + BKV - 1) / BKV, dq_part, false, num_cu);
     g.dkv_wgs = plan_items(g.dkv, g.key_blocks, (rows + GRAD_ROWS - 1) / GRAD_ROWS, dkv_part, false, num_cu);
     const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)g.dkv.items * dkv_part;
-    g.bytes = a > b ? a : b;
+    g.bytes = 2 * (((a > b ? a : b) + 255) & ~(size_t)255);
     return g;
 }
 
 }  // namespace
 
-hipError_t launch_attn_prompt_grad(const GradParams &p_in, hipStream_t s, int num_cu)
+hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_cu)
 {
-    const GradLaunches g = plan_grad(p_in.c, num_cu);
+    const GradLaunches g = plan_grad(p.c, num_cu);
     const int64_t most = (int64_t)1 << 24;                           // workgroups, of 256 threads
-    if (g.dq_wgs >= most || g.dkv_wgs >= most || g.row_blocks * p_in.c.kv_heads * DT >= most || g.key_blocks * p_in.c.kv_heads * 2 * DT >= most)
+    const int64_t join_dq = g.dq.items > 0 ? g.row_blocks * p.c.kv_heads * DT : 0, join_dkv = g.dkv.items > 0 ? g.key_blocks * p.c.kv_heads * 2 * DT : 0;
+    if (g.dq_wgs >= most || g.dkv_wgs >= most || join_dq + join_dkv >= most)
         return hipErrorInvalidValue;
-    GradParams p = p_in;
-    p.c = g.dq;
-    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)g.dq_wgs), dim3(64 * DQ_WAVES), 0, s, p);
-    if (p.c.items > 0)
-        hipLaunchKernelGGL(attn_dq_join_kernel, dim3((unsigned)(g.row_blocks * p.c.kv_heads * DT)), dim3(64 * DQ_WAVES), 0, s, p);
-    const hipError_t e = hipGetLastError();
+    GradParams dq = p, dkv = p;
+    dq.c = g.dq;
+    dkv.c = g.dkv;
+    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)g.dq_wgs), dim3(64 * DQ_WAVES), 0, s, dq);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    p.c = g.dkv;
-    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)g.dkv_wgs), dim3(256), 0, s, p);
-    if (p.c.items > 0)
-        hipLaunchKernelGGL(attn_dkv_join_kernel, dim3((unsigned)(g.key_blocks * p.c.kv_heads * 2 * DT)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)g.dkv_wgs), dim3(256), 0, s, dkv);
+    e = hipGetLastError();
+    if (e != hipSuccess || join_dq + join_dkv == 0)
+        return e;
+    hipLaunchKernelGGL(attn_grad_join_kernel, dim3((unsigned)(join_dkv + join_dq)), dim3(256), 0, s, dkv, dq, (int)join_dkv);
     return hipGetLastError();
 }
 
