@@ -524,7 +524,7 @@ __device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked
     RowBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
+    Splits<256, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
@@ -905,7 +905,7 @@ __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looke
     KeyBlock block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits<256>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
+    Splits<256, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);

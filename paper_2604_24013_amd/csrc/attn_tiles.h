@@ -228,7 +228,8 @@ struct Item {
 // The splits of all blocks, by a workgroup of NT threads.  tiles_of(block): tiles of a lane's block (0: nothing to do), in the order of
 // dispatch.  They lie in LDS and all loops are loops: unrolled, eight blocks a lane in registers, the same took 1 us more, much of it
 // for fetching 14 KiB of instructions.
-template <int NT>
+// PAIRED: two workgroups share a compute unit.
+template <int NT, bool PAIRED>
 struct Splits {
     const int *tiles;
     int chunk, blocks, items;
@@ -259,8 +260,10 @@ struct Splits {
         }
         const int total = wave_total(all), active = wave_total(some), most = P.items / P.kv_heads;
         const float wanted = fmaxf((float)most - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
-        // (nor much less than a compute unit's share of all: 512 blocks of 1 to 64 tiles take 82 us in pieces of 28, 74 in pieces of 40)
-        chunk = max(max(least, (int)(total / wanted) + 1), (int)(0.8f * total * P.kv_heads / P.num_cu));
+        // (nor much less than a compute unit's share of all, or, paired, than 40 tiles: 512 blocks of 1 to 64 tiles took 82 us in pieces of 28 and
+        // 74 in pieces of 40, 256 of them 52 in pieces of 26 and 49 of 40)
+        const float share = (float)total * P.kv_heads / P.num_cu;
+        chunk = max(max(least, (int)(total / wanted) + 1), PAIRED ? min((int)(1.2f * share), 40) : (int)(0.8f * share));
         chunk = (chunk + grain - 1) / grain * grain;
 #pragma unroll 1
         while ((items = number()) > most)
@@ -328,7 +331,7 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    const Splits<NT> splits(P, blocks, least, grain, bound, tiles_of, tiles);
+    const Splits<NT, PAIRED> splits(P, blocks, least, grain, bound, tiles_of, tiles);
     return splits.item(paired(splits.items), it);
 }
 
