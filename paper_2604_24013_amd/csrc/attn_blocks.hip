@@ -16,6 +16,11 @@
 // (`careful_row`), which reads visible keys only.
 // Packed prompts: a workgroup takes consecutive rows whatever sequences they belong to; keys of the walk that belong to another
 // sequence are masked like any others.
+// Bound: the matrix pipe where rows fill the chip (8192 tokens, 32 heads of 4 key heads: 522 us with lse, 488 without, 1053 and 1128 TFLOP/s, where
+// a library product of 8192 reaches 1232); else that a workgroup takes 10 us beside its tiles of 0.9 to 1.3 us each: 1 until
+// kernel arguments and starts are there, 1.3 for the search of its piece, 1.5 to 2.5 for Q and the first tiles, 1.7 to park, and 4.5 for the
+// last to arrive to merge.  4096 tokens, 4 heads: 32.5 us (529 TFLOP/s); 5 packed prompts of 8192 tokens, 8 heads of one key head: 73 us
+// (719); 2381 new tokens over 13528 in e4m3, 8 heads of one key head: 78 us (654).
 #include "attn_tiles.h"
 
 namespace cf {
@@ -277,7 +282,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     float m_run = -3.402823466e38f;      // (finite: against -inf a tile whose scores are all -inf would give NaN)
     // Row sums of this lane's keys, and of a pair of tiles: of the rounded probabilities, which multiply V, so that the roundings of a row's
     // dominant key cancel; LSE: of the probabilities before rounding (rounded, the log-sum-exp of a row with one dominant key would be
-    // off by up to 2^-9).  Both sums cost 16 vector instructions more a tile, of about 130: 10 % of the time of a full chip.
+    // off by up to 2^-9).  A sum over the rounded ones takes half the instructions (a dot product of two): 7 % of a full chip's time.
     float l_run = 0.0f, l_pair = 0.0f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -388,9 +393,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         }
         __syncthreads();                                             // ... for every wave, and V of kt, K of kt+1 are read by all
     };
-    // One tile: probabilities P = exp2(S - m) rounded to bf16, their row sums, O^T += V^T P^T; and under it, with `next`, the scores of tile kt+1 and their maximum.  Thirty-two segments
-    // of one MFMA each -- sixteen of the scores, sixteen of V's product --, the fragment of the third segment ahead requested in each,
-    // the 32 exponentials spread over segments 0 .. 22 and the maximum over the last eight.
+    // One tile: probabilities P = exp2(S - m) rounded to bf16, their row sums, O^T += V^T P^T; and under it, with NEXT, the scores of tile
+    // kt + 1 and their maximum.  Thirty-two segments of one MFMA each -- sixteen of the scores, sixteen of V's
+    // product --, the fragment of the third segment ahead requested in each, the 32 exponentials spread over segments 0 .. 22 and the
+    // maximum over the last eight.
     bf16x2_t ones;
     ones[0] = ones[1] = (__bf16)1.0f;
     auto tile = [&](int kt, f32x16_t (&sc)[KT], f32x16_t (&sn)[KT], auto b_tag, auto next_tag) __attribute__((always_inline)) {
@@ -692,6 +698,7 @@ int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, 
 
 int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part, bool counted, int num_cu)
 {
+    // (Four blocks a compute unit balance by themselves: 8192 tokens, 8 heads on each of 4 key heads, 522 us unsplit, 603 in pieces.)
     const Tuning tn = tuning();
     const int64_t all = blocks * p.kv_heads;
     p.items = p.chunk = 0;

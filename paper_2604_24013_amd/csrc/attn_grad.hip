@@ -3,7 +3,13 @@
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dout
 // Two launches, each with every sum in one place (no atomics, the same bits every time): one workgroup of the first owns rows and
 // walks over keys (and leaves delta for the second), one of the second owns keys and walks over the rows that see them, all
-// query heads of the key head.  Both multiply the scores anew: seven products where five would do with sums spread over memory.
+// query heads of the key head.  Both multiply the scores anew: seven products where five would do with sums spread over memory.  Walks are
+// cut into splits as in the forward kernel; a third launch adds up what they parked.
+// Bound: the matrix pipe, and beside it LDS: every product's "A" fragment, 1 KiB, comes from LDS for one MFMA of 32 cycles, so that four waves
+// ask for all of its 128 bytes a cycle.  dK and dV hold 256 accumulators and 64 registers of K and V a lane: one wave a SIMD, which
+// has to fill the pipe alone, so both kernels run as pipelines of 32-row units with one MFMA a segment.
+// Measured (us; dQ, dK and dV, sums): 4096 tokens, 8 heads of one key head 70, 91, 12 -- 51 and 69 GFLOP at 730 and 760 TFLOP/s;
+// 2048 + 1365 + 683 tokens, 4 heads of their own 26, 35, 12, of which 11 a launch are start, search, first loads and parking.
 // As in the forward kernel a lane owns one row (or key) and 16 of every 32 keys (rows) of a product's result, which is, rounded to
 // bf16, the "B" operand of the next product as it stands: nothing moves between lanes.  Tiles lie in LDS once and are read both by rows
 // and transposed: 16-byte chunks XOR-ed with (row & 15), which the transposing read can follow lane by lane.
@@ -41,7 +47,8 @@ __device__ __forceinline__ void gather_load_4(const void *at, unsigned lds_addr)
 // row & 15 itself the four rows of a transposing read share four positions.)
 __device__ __forceinline__ int spread(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
 
-// Addresses in such a tile, in registers, so that a read costs no arithmetic: what is added to them is a constant.  `move` takes them to another tile (16 additions instead of one a read).
+// Addresses in such a tile, in registers, so that a read costs no arithmetic: what is added to them is a constant.  `move` takes them to
+// another tile (16 additions instead of one a read).
 struct RowRead {                         // "A" operand: lane (row = lane & 31, half = lane >> 5), chunk 2 ks + half
     int at[DS];
     __device__ __forceinline__ RowRead()
@@ -108,7 +115,8 @@ __device__ __forceinline__ void stages(F1 &&argument, F2 &&exponential, F3 &&pro
 
 // A split's sums, `regs` registers of every thread of the workgroup, sixteen (a feature tile) after sixteen; a launch of its own adds them up in
 // split order, eight or four workgroups a block, one a feature tile.  (The last workgroup to arrive adding up all by itself: 4096 tokens, 8
-// heads of one key head, 16 splits of 128 KiB: 575 us instead of TODO for dK and dV.)
+// heads of one key head, up to 16 splits of 128 KiB: 575 us instead of 92 and 12 for dK and dV.)  That launch reads what was parked, 45 MiB
+// there, at 4 TB/s.
 template <int NT>
 __device__ __forceinline__ float *part_of(const CausalParams &P, int regs, const Item &it, int split, int tile)
 {

@@ -205,7 +205,7 @@ struct Sequences {
 };
 
 // What a workgroup works on.  Walks under a causal mask are of all lengths, which only the tables on the device know, and a launch takes as
-// long as its fullest compute unit.  So every workgroup looks at the walks of all blocks, a lane a block, and cuts them into splits of at most
+// long as its fullest compute unit.  So every workgroup looks at the walks of all blocks, a thread a block, and cuts them into splits of at most
 // `chunk` tiles, the same for all, as few as make no more than P.items workgroups: as many as fit the chip a whole number of times.
 // (Computed for one and eight heads, one sequence and several, workgroups one by one on the compute units: with 256 of 128 to 252
 // workgroups each takes 33 us, with a quarter more than fit, 47.)  A grid of all blocks by the largest number of splits needs no

@@ -1,7 +1,7 @@
 """Rotary positions and the paged cache on the GPU against plain forms in 64 bits.  Needs an MI355X: ``-m gpu``.
 
-Tolerances.  A rotated value y = m (x_a cos - x_b sin) is computed in fp32 from an angle in half turns rounded to fp32 (off by
-2^-25 half turns = 2^-23.3 rad at most), cosines good to a few units of 2^-24 (taken as 2^-22) and three roundings of 2^-24 of the
+Tolerances.  A rotated value y = m (x_a cos - x_b sin) is computed in fp32 from an angle of at most an eighth of a turn rounded to fp32
+(off by 2^-23.3 rad at most), cosines good to a few units of 2^-24 (taken as 2^-22) and three roundings of 2^-24 of the
 products: under 2^-20 m (|x_a| + |x_b|) in all.  Then it is rounded to the type: 2^-24 |y| (fp32), 2^-8 |y| (bf16), to e4m3 2^-4 |y|
 and half of the smallest step, 2^-10 2^e.  What is not rotated is copied, so equal; codes of unrotated rows are equal to those of the
 definition."""
