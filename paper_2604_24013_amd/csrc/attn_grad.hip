@@ -202,6 +202,8 @@ __device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head,
         const float ds = exp2f((s * C.scale - lse) * LOG2E) * (dp - delta);
         a += ds * k[0];
         b += ds * k[1];
+        if (settled(a, b))
+            break;
     }
     put_pair(static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, a * C.scale, b * C.scale, tile);
 }
@@ -224,6 +226,8 @@ __device__ __forceinline__ void careful_key(const GradParams &P, int key, int kv
             kb += ds * q[1];
             va += p * g[0];
             vb += p * g[1];
+            if (settled(ka, kb) && settled(va, vb))
+                t = end, head = (kvh + 1) * C.group;
         }
     if (tile < 4)
         put_pair(static_cast<__bf16 *>(P.dk) + (int64_t)key * C.k_token + kvh * C.k_head, ka * C.scale, kb * C.scale, tile);

@@ -394,6 +394,10 @@ struct Keys {
     }
 };
 
+// Sums that are NaN in every lane stay so.  (Of inputs that are NaN throughout, 8192 keys for every row, one by one, would take some 40 ms by
+// the count of instructions.)
+__device__ __forceinline__ bool settled(float a, float b) { return __builtin_amdgcn_ballot_w64(a == a || b == b) == 0; }
+
 // One row's attention by one wave, key by key, in two passes; lane i holds features 2 i and 2 i + 1.
 template <int SRC>
 __device__ __forceinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
@@ -415,12 +419,16 @@ __device__ __forceinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> 
             s *= sl2;
             if (pass == 0) {
                 m = fmaxf(m, s);
+                if (!(s < INFINITY))                                 // this key's p is NaN, and so is everything
+                    break;
             } else {
                 const float p = exp2f(s - (m == -INFINITY ? 0.0f : m));
                 const f32x2_t v = V.pair(V.row(key, &e), lane, e);
                 l += p;
                 o0 += p * v[0];
                 o1 += p * v[1];
+                if (settled(o0, o1))
+                    break;
             }
         }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;

@@ -322,6 +322,22 @@ def test_more_blocks_than_are_looked_at(case):
         assert bool(((lse[head, rows].double() - want).abs() <= 2.0 ** -17 * size + 2.0 ** -18 * (want.abs() + 1)).all())
 
 
+@pytest.mark.parametrize("what", ["all", "v", "dout"])
+def test_nan_throughout(what):
+    """Rows whose result is not finite are computed key by key: with NaN everywhere that ends with the first key."""
+    x, dout, at = grad.problem(93, [6000, 144], 4, 1)
+    (x if what == "all" else x[:, 5:] if what == "v" else dout).fill_(math.nan)
+    out, lse = prompt.run(x, 4, 1, at, SCALE)
+    assert bool(torch.isnan(out).all()) == (what != "dout") and bool(torch.isnan(lse).all()) == (what == "all")
+    got = grad.forward_and_gradient(x, dout, 4, 1, at, SCALE)
+    for n in ("dq", "dk") if what == "v" else ("dq", "dk", "dv"):
+        assert bool(torch.isnan(got[n]).all()), n
+    for new in (1, 100):
+        b = Batch(94, 4, 1, 16, "bf16", [new], [5000])
+        b.pool[1].fill_(math.nan)
+        assert bool(torch.isnan(b.run()[0]).all())
+
+
 NONSENSE = [[5, -2 ** 31, 2 ** 31 - 1, 7, 3], [2 ** 31 - 1, -2 ** 31, 60, 0, 2 ** 31 - 1], [90, 80, 70, 60, 50], [-9, 1000, -1000, 2 ** 30, 40], [-2 ** 31] * 5]
 
 
