@@ -26,7 +26,9 @@
 namespace cf {
 namespace {
 
-constexpr int LEAST_TILES = 8;           // of a split: as long as a workgroup's start and hand-over take
+// Tiles of a split at the least: about as long as a workgroup's start takes (1024 tokens, 8 heads of one key head 17.8 us; eight tiles 19.0, four
+// 18.6).
+constexpr int LEAST_TILES = 6;
 
 constexpr int PARKED = DH / 32 * 16 + 4; // floats that a thread parks: its part of O, and m and l
 
@@ -690,20 +692,21 @@ int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, 
     // 545 / 525, 4096 x 4 in pieces of 20 and 12 tiles 33.5 / 38; 2381 tokens x 8 over 5 to 8 thousand in e4m3 106 / 81.
     const bool many = (rows + 255) / 256 * p.kv_heads * sequences >= 4 * num_cu;
     const int waves = tn.causal_waves ? tn.causal_waves : many || (paged && rows >= 256) ? 8 : 4;
-    *wgs = plan_items(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, part_bytes(waves), true, num_cu);
+    *wgs = plan_items(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, LEAST_TILES, part_bytes(waves), true, num_cu);
     return waves;
 }
 
 }  // namespace
 
-int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, size_t part, bool counted, int num_cu)
+int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu)
 {
     // (Four blocks a compute unit balance by themselves: 8192 tokens, 8 heads on each of 4 key heads, 522 us unsplit, 603 in pieces.)
     const Tuning tn = tuning();
     const int64_t all = blocks * p.kv_heads;
     p.items = p.chunk = 0;
     p.num_cu = num_cu;
-    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (p.table == nullptr && p.n_seqs > 64) || (counted && all > p.max_counters) || longest < 2)
+    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (p.table == nullptr && p.n_seqs > 64) || (counted && all > p.max_counters) ||
+        longest <= (tn.causal_chunk ? 1 : least + least / 2))
         return all;
     const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);
     int64_t items = tn.causal_chunk ? all * ((longest + tn.causal_chunk - 1) / tn.causal_chunk) : (rounds > 1 ? rounds : 1) * num_cu / p.kv_heads * p.kv_heads;

@@ -461,7 +461,7 @@ int choose_few(CausalParams &p, int num_cu, int64_t *wgs, size_t *part)         
 {
     const int qt = p.max_q * p.group <= 16 ? 1 : 2;
     *part = (size_t)(qt * 16) * (DH + 4) * sizeof(float);
-    *wgs = plan_items(p, p.n_seqs, (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, *part, true, num_cu);
+    *wgs = plan_items(p, p.n_seqs, (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, 8, *part, true, num_cu);
     return qt;
 }
 

@@ -967,8 +967,8 @@ GradLaunches plan_grad(const CausalParams &c, int num_cu)
     g.row_blocks = (rows + DQ_ROWS - 1) / DQ_ROWS;
     g.key_blocks = (c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
     const size_t dq_part = (size_t)64 * 64 * DQ_WAVES * 4, dkv_part = (size_t)128 * 256 * 4;
-    g.dq_wgs = plan_items(g.dq, g.row_blocks, (c.tokens + BKV - 1) / BKV, dq_part, false, num_cu);
-    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, (rows + GRAD_ROWS - 1) / GRAD_ROWS, dkv_part, false, num_cu);
+    g.dq_wgs = plan_items(g.dq, g.row_blocks, (c.tokens + BKV - 1) / BKV, LEAST_TILES, dq_part, false, num_cu);
+    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, (rows + GRAD_ROWS - 1) / GRAD_ROWS, LEAST_TILES, dkv_part, false, num_cu);
     const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)g.dkv.items * dkv_part;
     g.bytes = 2 * (((a > b ? a : b) + 255) & ~(size_t)255);
     return g;
