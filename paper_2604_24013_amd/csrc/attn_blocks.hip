@@ -19,8 +19,8 @@
 // Bound: the matrix pipe where rows fill the chip (8192 tokens, 32 heads of 4 key heads: 522 us with lse, 488 without, 1053 and 1128 TFLOP/s, where
 // a library product of 8192 reaches 1232); else that a workgroup takes 10 us beside its tiles of 0.9 to 1.3 us each: 1 until
 // kernel arguments and starts are there, 1.3 for the search of its piece, 1.5 to 2.5 for Q and the first tiles, 1.7 to park, and 4.5 for the
-// last to arrive to merge.  4096 tokens, 4 heads: 32.5 us (529 TFLOP/s); 5 packed prompts of 8192 tokens, 8 heads of one key head: 73 us
-// (719); 2381 new tokens over 13528 in e4m3, 8 heads of one key head: 78 us (654).
+// last to arrive to merge.  4096 tokens, 4 heads: 33 us (519 TFLOP/s); 5 packed prompts of 8192 tokens, 8 heads of one key head: 74 us
+// (708); 2381 new tokens over 13528 in e4m3, 8 heads of one key head: 78 us (654).
 #include "attn_tiles.h"
 
 namespace cf {
