@@ -482,8 +482,9 @@ cf_status commfuse_run_attn_schedule(const cf_attn_desc *desc, const cf_attn_buf
  *                         that pair j makes over the trained length
  *     CF_ROPE_INDEX       r_j = 1 - clamp((j - j_high) / (j_low - j_high), 0, 1), a ramp over the pair's index between
  *                         the pairs that make `high` and `low` turns: j_high = max(0, floor(d(high))), j_low =
- *                         min(rot_dim / 2 - 1, ceil(d(low))), d(t) = rot_dim * ln(trained_len / (2 pi t)) / (2 ln base),
- *                         a ramp of no width taken as one of 0.001
+ *                         min(rot_dim - 1, ceil(d(low))), d(t) = rot_dim * ln(trained_len / (2 pi t)) / (2 ln base), a ramp
+ *                         of no width taken as one of 0.001.  (j_low is behind the last pair, rot_dim / 2 - 1, where that one
+ *                         makes more than `low` turns.)
  * Positions are int32 of either sign; the angle is exact modulo one turn at any of them: a frequency is kept in turns
  * as a 64-bit binary fraction, whose product with the position wraps at whole turns. */
 typedef enum { CF_ROPE_HALF = 0, CF_ROPE_INTERLEAVED = 1 } cf_rope_layout;

@@ -262,7 +262,7 @@ cf_status commfuse_rope_make(const cf_rope_desc *d, cf_rope *rope)
         first = std::floor(per * std::log(d->trained_len / ((double)two_pi * d->high)));
         last = std::ceil(per * std::log(d->trained_len / ((double)two_pi * d->low)));
         first = first > 0.0 ? first : 0.0;
-        last = last < pairs - 1 ? last : pairs - 1;
+        last = last < d->rot_dim - 1 ? last : d->rot_dim - 1;    // (it may lie behind the last pair)
     }
     for (int j = 0; j < pairs; ++j) {
         const long double f = powl((long double)d->base, -2.0L * j / d->rot_dim);
