@@ -705,7 +705,7 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t lea
     const int64_t all = blocks * p.kv_heads;
     p.items = p.chunk = 0;
     p.num_cu = num_cu;
-    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (p.table == nullptr && p.n_seqs > 64) || (counted && all > p.max_counters) ||
+    if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (!p.paged && p.n_seqs > 64) || (counted && all > p.max_counters) ||
         longest <= (tn.causal_chunk ? 1 : least + least / 2))
         return all;
     const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);

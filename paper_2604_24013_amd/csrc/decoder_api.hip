@@ -187,6 +187,7 @@ cf_status resolve_prompt(const cf_prompt_desc *d, cf::CausalParams *out, bool *n
 cf_status resolve_paged(const cf_cache_desc *cd, const cf_cache *c, const cf_paged_desc *d, cf::CausalParams *out, bool *nothing)
 {
     cf::CausalParams p = {};
+    p.paged = true;
     if (cf_status st = resolve_cache(cd, c, &p.pool))
         return st;
     if (d == nullptr)

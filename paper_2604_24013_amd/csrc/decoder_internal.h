@@ -71,7 +71,7 @@ struct CausalParams {
     int64_t k_token, k_head, v_token, v_head;
     int tokens, n_seqs;
     const int32_t *starts;                          // (paged: of the query rows)
-    // paged
+    bool paged;                                     // keys in a cache; else packed
     CachePool pool;
     const int32_t *kv_len, *table;
     int max_q, max_kv, max_pages;

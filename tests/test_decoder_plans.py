@@ -1,0 +1,32 @@
+"""How many bytes of workspace the causal attention asks for, without a GPU: the sizes with which walks over the keys are split."""
+import pytest
+
+from paper_2604_24013_amd import binding as cf
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    import os
+    if not os.path.exists(cf.LIB_PATH):
+        from paper_2604_24013_amd import build
+        build.build()
+    cf.load()
+
+
+def paged(n, max_q, max_kv=65536, heads=8, kv=1, dtype="bf16", page=16):
+    return cf.attn_paged_workspace_bytes(cf.cache_desc(dtype, 9, page, kv), cf.paged_desc(n, heads, n * max_q, max_q, max_kv, -(-max_kv // page), 0.1))
+
+
+@pytest.mark.parametrize("max_q", [1, 4, 5])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_batches_of_more_than_64_sequences_ask_for_a_workspace(max_q, dtype):
+    """A split's share: rows of 132 floats (16 or 32 of them) of the few-rows kernel, 128 rows' of the other."""
+    for n in (1, 64, 65, 100, 255, 256, 511, 512):
+        assert paged(n, max_q, dtype=dtype) >= 65536 + n * 16 * 132 * 4, n
+    assert paged(513, max_q, dtype=dtype) == 0                                # more blocks than are looked at
+
+
+def test_what_is_asked_for_does_not_fall_as_contexts_grow():
+    for n in (1, 63, 64, 65, 66, 200, 512):
+        sizes = [paged(n, 1, 1 << b) for b in range(4, 20)]
+        assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[-1] > 0
