@@ -706,7 +706,7 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t lea
     p.items = p.chunk = 0;
     p.num_cu = num_cu;
     if (p.parts == nullptr || blocks > 512 || all >= 4 * num_cu || (!p.paged && p.n_seqs > 64) || (counted && all > p.max_counters) ||
-        longest <= (tn.causal_chunk ? 1 : least + least / 2))
+        longest <= (tn.causal_chunk ? 1 : least + least / 2) || blocks * longest > INT32_MAX)    // (the tiles of all walks are added up in 32 bits)
         return all;
     const int64_t rounds = (3 * all + 2 * num_cu - 1) / (2 * num_cu), fit = (int64_t)(p.part_bytes / part);
     int64_t items = tn.causal_chunk ? all * ((longest + tn.causal_chunk - 1) / tn.causal_chunk) : (rounds > 1 ? rounds : 1) * num_cu / p.kv_heads * p.kv_heads;

@@ -87,8 +87,8 @@ struct CausalParams {
 // Workgroups of a launch over `blocks` blocks of one key head whose walks are of up to `longest` tiles, and P.items and P.chunk to go with it:
 // as many as fit the compute units the least number of times that leaves a third of them over for splits.  `least`: tiles of a split at
 // the least (where no walk has half as many more, none is cut); `part`: bytes that a split parks; `counted`: every block needs a counter.
-// Without workspace for that, with blocks enough, or with more blocks (512) or packed sequences (64) than are looked at: one workgroup a
-// block.
+// Without workspace for that, with blocks enough, with more blocks (512) or packed sequences (64) than are looked at, or with walks of more
+// than 2^31 tiles together: one workgroup a block.
 int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu);
 hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
 hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);

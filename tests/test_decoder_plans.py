@@ -30,3 +30,14 @@ def test_what_is_asked_for_does_not_fall_as_contexts_grow():
     for n in (1, 63, 64, 65, 66, 200, 512):
         sizes = [paged(n, 1, 1 << b) for b in range(4, 20)]
         assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[-1] > 0
+
+
+def test_walks_that_32_bits_do_not_count_are_not_split():
+    """The kernels add up the tiles of all walks (of 32 or 64 keys) in 32 bits.  Beyond that a batch is not split: 512 sequences that share pages
+    may see 2^31 tokens each."""
+    for max_q, tile in ((1, 32), (5, 64)):
+        for n in (2, 64, 512):
+            tokens = min((2 ** 31 - 1) // n * tile, 2 ** 31 - 2 ** 14) // 1024 * 1024
+            assert paged(n, max_q, tokens, page=1024) > 0
+            if (2 ** 31 - 1) // n * tile < 2 ** 31 - 2 ** 14:
+                assert paged(n, max_q, tokens + 1024 * tile, page=1024) == 0
