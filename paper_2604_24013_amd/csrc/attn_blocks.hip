@@ -12,8 +12,8 @@
 //                    the keys that the lane holds; V^T comes from the [key x feature] tile by the transposing LDS read.
 // Mask.  A wave multiplies only the tiles from its rows' first key to their last; for the others of the workgroup's walk it moves its
 // share of the loads.  Tiles on the border are masked by a select on the scores, so that what a row does not see has no weight --
-// but zero times an infinite or NaN V is NaN: a row whose result is not finite is computed once more, key by key
-// (`careful_row`), which reads visible keys only.
+// but zero times an infinite or NaN V is NaN: rows whose result is not finite are computed once more where hidden values can have
+// been the reason (`rows_again`).
 // Packed prompts: a workgroup takes consecutive rows whatever sequences they belong to; keys of the walk that belong to another
 // sequence are masked like any others.
 // Bound: the matrix pipe where rows fill the chip (8192 tokens, 32 heads of 4 key heads: 522 us with lse, 488 without, 1053 and 1128 TFLOP/s, where
@@ -31,13 +31,6 @@ namespace {
 constexpr int LEAST_TILES = 6;
 
 constexpr int PARKED = DH / 32 * 16 + 4; // floats that a thread parks: its part of O, and m and l
-
-// (a call: inlined, its loops would have the walk's registers spilled)
-template <int SRC>
-__device__ __noinline__ void careful_row_called(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
-{
-    careful_row<SRC>(K, V, q, out, first, last, sl2);
-}
 
 template <int NW, int SRC, bool LSE>
 __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
@@ -643,9 +636,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         if (LSE && lh == 0)
             P.lse[(int64_t)head * P.lse_stride + t] = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * LN2;
     }
-    unsigned long long again = __builtin_amdgcn_ballot_w64(there && odd != 0.0f);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
-    if (again != 0) {
+    const unsigned long long odd_rows = __builtin_amdgcn_ballot_w64(there && odd != 0.0f && l_run == l_run);   // (l is made of visible scores only)
+    if (odd_rows != 0) {
+        const bool again = (odd_rows | odd_rows >> 32) >> lq & 1;
         Keys<SRC> K, V;
         K.base = kb;
         K.row_bytes = k_row;
@@ -659,13 +652,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         V.base = vb;
         V.row_bytes = v_row;
         V.exps = ve;
-        __builtin_amdgcn_s_waitcnt(0);                               // the row's first result is written before its second
-        for (; again != 0; again &= again - 1) {
-            const int at = __builtin_ctzll(again);
-            const int64_t tr = __shfl(t, at);
-            const int hr = __shfl(head, at);
-            careful_row_called<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + tr * P.q_token + hr * P.q_head,
-                             static_cast<__bf16 *>(P.out) + tr * P.o_token + hr * P.o_head, __shfl(first, at), __shfl(last, at), sl2);
+        // The tiles of this wave, of all splits (the first may be one that no row sees); front .. f_max, l_min .. behind: keys that some rows do not see
+        int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
+        edges(there, first, last, &f_min, &f_max, &l_min, &l_max);
+        const int front = lo + max(0, (f_min - lo) / BKV - 1) * BKV, behind = min(hi, lo + ((l_max - lo) / BKV + 1) * BKV);
+        if (any_large(V, front, min(f_max, hi)) || any_large(V, max(l_min + 1, lo), behind)) {
+            __builtin_amdgcn_s_waitcnt(0);                           // the rows' first results are written before their second
+            int row = token, h = head;
+            asm volatile("" : "+v"(row), "+v"(h));                   // (the row's address anew: kept, it would take registers from the walk)
+            rows_again<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + (int64_t)(t_base + (there ? row : 0)) * P.q_token + h * P.q_head, first, last, again, sl2, 0, 1, oacc, &m_run, &l_run);
+            if (again)
+                store_fours(oacc, l_run == 0.0f ? 0.0f : 1.0f / l_run, orow);
         }
     }
 }

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     const int64_t row_floats = DH + 4;                               // a parked row: O, m, l, e
     float *mine = P.parts == nullptr ? nullptr : parked_at(P, it, split, (size_t)QT * ROWS * row_floats);
     constexpr int COHERENT = 1 | 16;
-    auto finish_row = [&](int r, int c, const f32x4_t &o, float mm, float l, float e) __attribute__((always_inline)) {
+    auto store_row = [&](int r, int c, const f32x4_t &o, float l) __attribute__((always_inline)) {
         const int token = r / G, head = kvh * G + r - token * G;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         bf16x4_t h;
@@ -312,9 +312,36 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
             h[x] = (__bf16)y;
         }
         *reinterpret_cast<u32x2_t *>(static_cast<__bf16 *>(P.out) + (int64_t)(from + token) * P.o_token + head * P.o_head + c * 4) = __builtin_bit_cast(u32x2_t, h);
+        return odd != 0.0f && l == l;                                // (l is made of visible scores only)
+    };
+    auto finish_row = [&](int r, int c, const f32x4_t &o, float mm, float l, float e) __attribute__((always_inline)) {
+        const int token = r / G, head = kvh * G + r - token * G;
+        const bool odd = store_row(r, c, o, l);
         if (c == 0 && P.lse != nullptr)
             P.lse[(int64_t)head * P.lse_stride + from + token] = e == 0.0f ? -INFINITY : (mm + __log2f(e)) * LN2;
-        return odd != 0.0f;
+        return odd;
+    };
+    // Features 4 c .. 4 c + 3 of row r of what the waves parked in LDS.
+    auto of_waves = [&](int r, int c, float *top, float *l, float *e) __attribute__((always_inline)) {
+        float mm = -INFINITY, ll = 0.0f, ee = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            mm = fmaxf(mm, stat_m[w][r]);
+        f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = exp2f(stat_m[w][r] - mm);                // (a wave that saw no key: nothing times a factor)
+            const f32x4_t x = *reinterpret_cast<const f32x4_t *>(parked + (w * ROWS + r) * O_STRIDE + c * 4);
+            ll += stat_l[w][r] * f;
+            ee += stat_e[w][r] * f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                a[k] += x[k] * f;
+        }
+        *top = mm;
+        *l = ll;
+        *e = ee;
+        return a;
     };
     if (tid < QT)
         odd_rows[tid] = 0;
@@ -345,21 +372,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
             const int r = u >> 5, c = u & 31, row = t * ROWS + r;
             if (row >= rows)
                 continue;
-            float mm = -INFINITY, ll = 0.0f, ee = 0.0f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w)
-                mm = fmaxf(mm, stat_m[w][r]);
-            f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const float f = exp2f(stat_m[w][r] - mm);            // (a wave that saw no key: nothing times a factor)
-                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(parked + (w * ROWS + r) * O_STRIDE + c * 4);
-                ll += stat_l[w][r] * f;
-                ee += stat_e[w][r] * f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    a[k] += x[k] * f;
-            }
+            float mm, ll, ee;
+            const f32x4_t a = of_waves(r, c, &mm, &ll, &ee);
             if (splits == 1) {
                 if (finish_row(row, c, a, mm, ll, ee))
                     atomicOr(&odd_rows[t], 1u << r);
@@ -421,9 +435,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
                 atomicOr(&odd_rows[row / ROWS], 1u << (row % ROWS));
         }
     }
-    // Rows whose result is not finite once more, key by key: what they do not see may have been.
+    // Rows whose result is not finite once more where what they do not see can have been the reason: the new tokens behind a row's own (a
+    // single token's row sees all keys), or page 0 in the place of one that does not exist.  The waves share the keys.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+    const unsigned odd = odd_rows[0] | (QT > 1 ? odd_rows[QT - 1] << 16 : 0u);
+    if (odd == 0)
+        return;
     Keys<SRC> Kk, Kv;
     Kk.base = kb;
     Kk.row_bytes = row_bytes;
@@ -436,12 +454,33 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     Kv = Kk;
     Kv.base = vb;
     Kv.exps = ve;
-    for (int r = wave; r < rows; r += NW) {
-        if (!(odd_rows[r / ROWS] >> (r % ROWS) & 1u))
-            continue;
-        const int token = r / G, head = kvh * G + r - token * G;
-        careful_row<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + (int64_t)(from + token) * P.q_token + head * P.q_head,
-                         static_cast<__bf16 *>(P.out) + (int64_t)(from + token) * P.o_token + head * P.o_head, 0, n - m + token, sl2);
+    bool absent = false;
+    for (int page = lane; page < (int)(((unsigned)hi + (1u << shift) - 1) >> shift); page += 64)
+        absent = absent || (unsigned)table[page] >= (unsigned)n_pages;
+    if (__builtin_amdgcn_ballot_w64(absent) == 0 && !any_large(Kv, max(n - m + 1, 0), hi))
+        return;
+    const int lq = lane & 31, lh = lane >> 5, r = lq < rows ? lq : 0, token = r / G;
+    f32x16_t acc[DH / 32];
+    float m_row, l_row;
+    rows_again<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + (int64_t)(from + token) * P.q_token + (kvh * G + r - token * G) * P.q_head, 0, n - m + token,
+                    odd >> lq & 1u, sl2, wave, NW, acc, &m_row, &l_row);
+    for (int t = 0; t < QT; ++t) {
+        __syncthreads();                                             // (the rows before have been read)
+        if (lq >> 4 == t) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                *reinterpret_cast<f32x4_t *>(parked + (wave * ROWS + (lq & 15)) * O_STRIDE + 4 * (8 * (e >> 2) + 4 * lh + (e & 3))) =
+                    f32x4_t{acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+            stat_m[wave][lq & 15] = m_row;
+            stat_l[wave][lq & 15] = l_row;
+        }
+        __syncthreads();
+        for (int u = tid; u < ROWS * DH / 4; u += NT)
+            if (odd >> (t * ROWS + (u >> 5)) & 1u) {
+                float mm, ll, ee;
+                const f32x4_t a = of_waves(u >> 5, u & 31, &mm, &ll, &ee);
+                store_row(t * ROWS + (u >> 5), u & 31, a, ll);
+            }
     }
 }
 

@@ -186,6 +186,10 @@ __device__ __forceinline__ void put_pair(void *row, float a, float b, int tile) 
         static_cast<bf16x2_t *>(row)[lane] = v;
 }
 
+// Sums that are NaN in every lane stay so.  (Of inputs that are NaN throughout, 8192 keys for every row, one by one, would take some 40 ms by
+// the count of instructions.)
+__device__ __forceinline__ bool settled(float a, float b) { return __builtin_amdgcn_ballot_w64(a == a || b == b) == 0; }
+
 // dQ of one row, key by key (all of it, or one feature tile).
 __device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head, int first, int tile)
 {

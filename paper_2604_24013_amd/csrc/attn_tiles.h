@@ -19,6 +19,7 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int DH = 128;                  // head dimension these kernels are written for
 constexpr int BKV = 64;                  // keys per tile
@@ -357,6 +358,19 @@ __device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &i
 
 enum { PACKED = 0, PAGED_BF16 = 1, PAGED_E4M3 = 2 };
 
+// Does a row of bf16 features hold a value that is not finite, or of 2^60 and more?
+__device__ __forceinline__ bool large_row(const __bf16 *row)
+{
+    unsigned most = 0;
+    for (int i = 0; i < DH / 8; ++i) {
+        const u32x4_t w = reinterpret_cast<const u32x4_t *>(row)[i];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            most = max(most, max(w[c] & 0x7FFFu, w[c] >> 16 & 0x7FFFu));
+    }
+    return most >= (127 + 60) << 7;
+}
+
 // Where a sequence's (or the pack's) keys lie, for single rows: the pointer of key `key` (nullptr: its page does not exist), and its
 // scale.
 template <int SRC>
@@ -382,60 +396,266 @@ struct Keys {
             return base + page * page_bytes + in_page * row_bytes;
         }
     }
-    __device__ __forceinline__ f32x2_t pair(const unsigned char *row, int i, int e) const    // features 2 i and 2 i + 1
+    __device__ __forceinline__ bf16x8_t eight(const unsigned char *row, int i, int e) const   // features 8 i .. 8 i + 7
     {
         if constexpr (SRC == PAGED_E4M3) {
-            const f32x2_t v = __builtin_amdgcn_cvt_pk_f32_fp8((int)reinterpret_cast<const unsigned short *>(row)[i], false);
-            return f32x2_t{ldexpf(v[0], e), ldexpf(v[1], e)};
+            const u32x2_t code = reinterpret_cast<const u32x2_t *>(row)[i];
+            const float scale = __builtin_bit_cast(float, (unsigned)(e + 127) << 23);
+            u32x4_t w;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                w[2 * c] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[c], scale, false));
+                w[2 * c + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[c], scale, true));
+            }
+            return __builtin_bit_cast(bf16x8_t, w);
         } else {
-            const bf16x2_t v = reinterpret_cast<const bf16x2_t *>(row)[i];
-            return f32x2_t{(float)v[0], (float)v[1]};
+            return reinterpret_cast<const bf16x8_t *>(row)[i];
+        }
+    }
+    __device__ __forceinline__ u32x2_t four(const unsigned char *row, int i, int e) const     // features 4 i .. 4 i + 3
+    {
+        if constexpr (SRC == PAGED_E4M3) {
+            const unsigned code = reinterpret_cast<const unsigned *>(row)[i];
+            const float scale = __builtin_bit_cast(float, (unsigned)(e + 127) << 23);
+            return u32x2_t{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, scale, false)),
+                           __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, scale, true))};
+        } else {
+            return reinterpret_cast<const u32x2_t *>(row)[i];
+        }
+    }
+    // Does a row hold a value that is not finite, or of 2^60 and more?  (Products of 128 smaller ones do not overflow.)
+    __device__ __forceinline__ bool large(const unsigned char *row, int e) const
+    {
+        if constexpr (SRC == PAGED_E4M3) {
+            unsigned nan = 0;
+            for (int i = 0; i < DH / 16; ++i) {
+                const u32x4_t w = reinterpret_cast<const u32x4_t *>(row)[i];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    nan |= (w[c] & 0x7F7F7F7Fu) + 0x01010101u;       // (0x7F is NaN)
+            }
+            return e > 50 || (nan & 0x80808080u) != 0;
+        } else {
+            return large_row(reinterpret_cast<const __bf16 *>(row));
         }
     }
 };
 
-// Sums that are NaN in every lane stay so.  (Of inputs that are NaN throughout, 8192 keys for every row, one by one, would take some 40 ms by
-// the count of instructions.)
-__device__ __forceinline__ bool settled(float a, float b) { return __builtin_amdgcn_ballot_w64(a == a || b == b) == 0; }
-
-// One row's attention by one wave, key by key, in two passes; lane i holds features 2 i and 2 i + 1.
+// Results that are not finite.  The mask is a select on the scores, so that a hidden key has a probability of 0 -- but 0 times an infinite or
+// NaN value of V is NaN.  Only the tiles on a wave's border hold keys that some of its rows see and others do not.  So a wave that finds a
+// result that is not finite looks at the V rows of those tiles (64 keys a time, a lane each); if one of them is not finite, the wave walks over all keys once
+// more, from memory, with such values taken out of the product and counted for the rows that see them.  Otherwise what is visible is not
+// finite, and the result stays.
+// Is one of the rows [from, to) large?
 template <int SRC>
-__device__ __forceinline__ void careful_row(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, __bf16 *out, int first, int last, float sl2)
+__device__ __forceinline__ bool any_large(const Keys<SRC> &K, int from, int to)
 {
-    const int lane = threadIdx.x & 63;
-    const float q0 = (float)q[2 * lane], q1 = (float)q[2 * lane + 1];
-    float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int pass = 0; pass < 2; ++pass)
-        for (int key = first; key <= last; ++key) {
-            int e = 0;
-            const unsigned char *k = K.row(key, &e);
-            if (k == nullptr)
-                continue;
-            const f32x2_t kv = K.pair(k, lane, e);
-            float s = q0 * kv[0] + q1 * kv[1];
+    for (; from < to; from += 64) {
+        const int key = from + (int)(threadIdx.x & 63);
+        int e = 0;
+        const unsigned char *row = key < to ? K.row(key, &e) : nullptr;
+        if (__builtin_amdgcn_ballot_w64(row != nullptr && K.large(row, e)) != 0)
+            return true;
+    }
+    return false;
+}
+
+// acc[d] += a[d] w (an MFMA's "A" and "B" operands), d the feature tiles, where elements of `a` that are not finite count for the columns that see
+// their index only (bit x of `seen`: slot x): they are taken out of `a`, and products of ones say which results they make +inf, -inf or NaN.
+__device__ __forceinline__ void add_seen(f32x16_t (&acc)[DH / 32], bf16x8_t (&a)[DH / 32], bf16x8_t w, unsigned seen)
+{
+    u16x8_t most = {};
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2)
-                s += __shfl_xor(s, d);
-            s *= sl2;
-            if (pass == 0) {
-                m = fmaxf(m, s);
-                if (!(s < INFINITY))                                 // this key's p is NaN, and so is everything
-                    break;
-            } else {
-                const float p = exp2f(s - (m == -INFINITY ? 0.0f : m));
-                const f32x2_t v = V.pair(V.row(key, &e), lane, e);
-                l += p;
-                o0 += p * v[0];
-                o1 += p * v[1];
-                if (settled(o0, o1))
-                    break;
+    for (int d = 0; d < DH / 32; ++d)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x8_t, a[d]) & (unsigned short)0x7FFF);
+    bool finite = true;
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+        finite = finite && most[x] < 0x7F80;
+    if (__builtin_amdgcn_ballot_w64(!finite) != 0) {
+        constexpr unsigned short ONE = 0x3F80;
+        u16x8_t plus, minus;                                         // what they are multiplied by
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const bool sees = seen >> x & 1, negative = (float)w[x] < 0.0f;
+            plus[x] = sees && !negative ? ONE : 0;
+            minus[x] = sees && negative ? ONE : 0;
+        }
+#pragma unroll 1
+        for (int i = 0; i < 2 * (DH / 32); ++i) {                    // (the code is there once) tile i / 2: what makes it +inf, what makes it -inf
+            u16x8_t bits = __builtin_bit_cast(u16x8_t, a[0]), up, down;
+#pragma unroll
+            for (int d = 1; d < DH / 32; ++d)
+                bits = i >> 1 == d ? __builtin_bit_cast(u16x8_t, a[d]) : bits;
+            const unsigned short sign = i & 1 ? 0x8000 : 0;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const bool nan = (bits[x] & 0x7FFF) > 0x7F80;
+                up[x] = nan || bits[x] == (0x7F80 | sign) ? ONE : 0;
+                down[x] = nan || bits[x] == (0xFF80 ^ sign) ? ONE : 0;
+            }
+            const f32x16_t zero = {};
+            f32x16_t n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, up), __builtin_bit_cast(bf16x8_t, plus), zero, 0, 0, 0);
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, down), __builtin_bit_cast(bf16x8_t, minus), n, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float more = n[e] > 0.0f ? (i & 1 ? -INFINITY : INFINITY) : 0.0f;
+#pragma unroll
+                for (int d = 0; d < DH / 32; ++d)
+                    acc[d][e] += i >> 1 == d ? more : 0.0f;
             }
         }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    bf16x2_t r;
-    r[0] = (__bf16)(o0 * inv);
-    r[1] = (__bf16)(o1 * inv);
-    reinterpret_cast<bf16x2_t *>(out)[lane] = r;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d) {
+            const u16x8_t bits = __builtin_bit_cast(u16x8_t, a[d]);
+            u16x8_t kept;
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                kept[x] = (bits[x] & 0x7FFF) < 0x7F80 ? bits[x] : 0;
+            a[d] = __builtin_bit_cast(bf16x8_t, kept);
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[d], w, acc[d], 0, 0, 0);
+}
+
+__device__ __forceinline__ bool none_finite(const f32x16_t &x)
+{
+    bool finite = false;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        finite = finite || __builtin_isfinite(x[e]);
+    return !finite;
+}
+// Smallest / largest of the wave's values.
+__device__ __forceinline__ int least_of(int x)
+{
+    for (int d = 1; d < 64; d *= 2)
+        x = min(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int most_of(int x) { return -least_of(-x); }
+// What lanes at + 4 (lane / 32) hold, for a constant `at`: of the rows 0 .. 31 that lanes 0 .. 31 look up, those that an MFMA operand's slots stand for.
+__device__ __forceinline__ int of_slot(int x, int at)
+{
+    const int low = __builtin_amdgcn_readlane(x, at), high = __builtin_amdgcn_readlane(x, at + 4);
+    return threadIdx.x & 32 ? high : low;
+}
+template <typename T>
+__device__ __forceinline__ const T *of_slot(const T *p, int at)
+{
+    const unsigned long long u = reinterpret_cast<unsigned long long>(p);
+    const unsigned lo = of_slot((int)(unsigned)u, at), hi = of_slot((int)(unsigned)(u >> 32), at);
+    return reinterpret_cast<const T *>((unsigned long long)hi << 32 | lo);
+}
+
+// "A" operands of the transposed product: four features 4 n .. 4 n + 3 of rows 2 i and 2 i + 1, n = lane & 31, go to slots 2 i and 2 i + 1 of the four
+// feature tiles, so that register e of tile d of the result is feature 4 (8 (e >> 2) + 4 half + (e & 3)) + d.
+__device__ __forceinline__ void put_pair(bf16x8_t (&a)[DH / 32], int i, u32x2_t even, u32x2_t odd)
+{
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d) {
+        u32x4_t w = __builtin_bit_cast(u32x4_t, a[d]);
+        w[i] = __builtin_amdgcn_perm(odd[d >> 1], even[d >> 1], d & 1 ? 0x07060302u : 0x05040100u);
+        a[d] = __builtin_bit_cast(bf16x8_t, w);
+    }
+}
+// A lane's row of such a result, times `factor`, as bf16.
+__device__ __forceinline__ void store_fours(const f32x16_t (&acc)[DH / 32], float factor, __bf16 *row)
+{
+    const int lh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        bf16x4_t h;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+            h[d] = (__bf16)(acc[d][e] * factor);
+        *reinterpret_cast<u32x2_t *>(row + 4 * (8 * (e >> 2) + 4 * lh + (e & 3))) = __builtin_bit_cast(u32x2_t, h);
+    }
+}
+
+// Attention of up to 32 rows by one wave, from memory: lane (row = lane & 31, and the same in the other half) sees keys first .. last; results where
+// `wanted`: m, l, and O^T as `put_pair` has it.  The wave takes units of 32 keys nth, nth + step, ... from the first that is seen on.
+template <int SRC>
+__device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, int first, int last, bool wanted, float sl2, int nth, int step,
+                                           f32x16_t (&acc)[DH / 32], float *max_score, float *sum)
+{
+    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5;
+    const int from = least_of(wanted ? first : 0x7FFFFFFF), to = most_of(wanted ? last : -1);
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            acc[d][i] = 0.0f;
+    float m = -3.402823466e38f, l = 0.0f;
+#pragma unroll 1
+    for (int64_t at0 = (from & ~31) + 32 * (int64_t)nth; at0 <= to; at0 += 32 * step) {
+        const int key0 = (int)at0, mine = key0 + lq < from ? from : key0 + lq < to ? key0 + lq : to;
+        int ek = 0, ev = 0;
+        const unsigned char *kr = K.row(mine, &ek), *vr = V.row(mine, &ev);
+        const unsigned absent = (unsigned)__builtin_amdgcn_ballot_w64(kr == nullptr);
+        if (kr == nullptr) {                                         // (not seen)
+            kr = K.base;
+            vr = V.base;
+        }
+        bf16x8_t v[2][DH / 32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u32x2_t four[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int at = 16 * c + 8 * (i >> 1) + 2 * (i & 1) + x;
+                    four[x] = V.four(of_slot(vr, at), lq, SRC == PAGED_E4M3 ? of_slot(ev, at) : 0);
+                }
+                put_pair(v[c], i, four[0], four[1]);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16_t s = {};
+        asm volatile("" : "+v"(q));                                  // (the row is read in every unit: 32 registers)
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ++ks)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(K.eight(kr, 2 * ks + lh, ek), reinterpret_cast<const bf16x8_t *>(q)[2 * ks + lh], s, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        unsigned seen = 0;                                           // of the lane's sixteen keys
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = 8 * (i >> 2) + 4 * lh + (i & 3), key = key0 + at;
+            const bool sees = key >= first && key <= last && !(absent >> at & 1);
+            seen |= (unsigned)sees << i;
+            s[i] = sees ? s[i] * sl2 : -INFINITY;
+            mx = fmaxf(mx, s[i]);
+        }
+        const float m_new = fmaxf(m, max_of_halves(mx)), alpha = exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
+        bf16x8_t p[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i >> 3][i & 7] = (__bf16)exp2f(s[i] - m);
+            l += (float)p[i >> 3][i & 7];
+        }
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                acc[d][i] *= alpha;
+        add_seen(acc, v[0], p[0], seen);
+        add_seen(acc, v[1], p[1], seen >> 8);
+        if ((key0 & 0xE0) == 0) {                                    // now and then: does anything that follows matter?
+            bool done = true;
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+                done = done && none_finite(acc[d]);
+            if (__builtin_amdgcn_ballot_w64(wanted && !done) == 0)
+                break;
+        }
+    }
+    *max_score = m;
+    *sum = sum_of_halves(l);
 }
 
 }  // namespace

@@ -50,3 +50,157 @@ def test_large_batches_in_the_workspace_that_they_ask_for(n, new, dtype):
     finally:
         torch.cuda.synchronize()
         cf.set_workspace(WORKSPACE)
+
+
+# ---- values that are not finite --------------------------------------------------------------------------------------------------
+# A feature of V that is not finite makes that feature of the rows that see it so, with its sign, and nothing else: the probabilities of these
+# problems are far above 2^-126.  All other elements are those of V with 0 there, up to that key's weight -- so the reference has 0 in the
+# place, and the spoilt feature of the rows that see it is compared by itself.
+SPOILT = [(math.inf, math.inf), (-math.inf, -math.inf), (math.nan, math.nan), ("both", math.nan)]      # value(s), what sees it
+
+
+def _packed_case(lens, h, kv, tokens, value, seed):
+    """(spoilt x, clean x, starts, [(row mask, feature, key head)])"""
+    x = prompt.make(seed, sum(lens), h, kv)
+    at, clean, marks = prompt.starts(lens), x.clone(), []
+    ends = at[1:].tolist()
+    for i, t in enumerate(tokens):
+        head, d = h + kv + i % kv, (37 * i + 5) % D
+        end = next(e for e in ends if e > t)
+        seen = torch.zeros(x.shape[0], dtype=torch.bool, device=DEV)
+        if value == "both":
+            other = max([b for b in [0] + ends if b <= t]) if t + 1 >= end else t + 1
+            x[t, head, d], x[other, head, d] = math.inf, -math.inf
+            clean[t, head, d] = clean[other, head, d] = 0
+            seen[max(t, other):end] = True
+            one = torch.zeros_like(seen)
+            one[min(t, other):max(t, other)] = True                       # see one of them only
+            marks.append((one, d, i % kv, math.inf if t < other else -math.inf))
+            marks.append((seen, d, i % kv, math.nan if other != t else -math.inf))
+        else:
+            x[t, head, d], clean[t, head, d] = value, 0
+            seen[t:end] = True
+            marks.append((seen, d, i % kv, value))
+    return x, clean, at, marks
+
+
+def _expect(out, marks, group):
+    """Looks at the spoilt elements of out [tokens, heads, D] and puts 0 there; a later mark adds to an earlier one of the same feature."""
+    for rows, d, kvh, value in marks:
+        for head in range(kvh * group, (kvh + 1) * group):
+            got = out[rows, head, d].float()
+            want = torch.full_like(got, value)
+            assert torch.equal(got.nan_to_num(7.0, 8.0, 9.0), want.nan_to_num(7.0, 8.0, 9.0)), (d, head, value, got[:5].tolist())
+            out[rows, head, d] = 0
+
+
+@pytest.mark.parametrize("value", [v for v, _ in SPOILT])
+@pytest.mark.parametrize("chunk", [None, "4x1", "8x2", "4x100000"])
+@pytest.mark.parametrize("case", [(4, 2, [150, 81, 160], [100, 190, 391 - 1]), (8, 1, [5, 3, 9, 1, 30, 2], [3, 6, 20, 49]), (1, 1, [300], [0, 130]),
+                                  (6, 2, [1] * 70 + [200] + [2] * 40, [10, 75, 269, 300]), (3, 3, [700], [64, 65, 500])])
+def test_one_feature_of_a_prompts_v(case, chunk, value, monkeypatch):
+    h, kv, lens, tokens = case
+    if chunk:
+        monkeypatch.setenv("COMMFUSE_CAUSAL", chunk)
+    x, clean, at, marks = _packed_case(lens, h, kv, tokens, value, 501)
+    q, k, v = clean[:, :h], clean[:, h:h + kv], clean[:, h + kv:]
+    ref = prompt.definition(q, k, v, at, SCALE)
+    for with_lse in (True, False):
+        out, lse = prompt.run(x, h, kv, at, SCALE, with_lse)
+        for rows, d, kvh, _ in marks:
+            for head in range(kvh * (h // kv), (kvh + 1) * (h // kv)):
+                ref[0][rows, head, d] = 0
+        _expect(out, marks, h // kv)
+        prompt.check(out, lse, ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("chunk", [None, "4x1", "8x3"])
+@pytest.mark.parametrize("case", [(8, 2, 16, [4, 3, 1], [250, 64, 33]), (4, 4, 32, [7, 5], [7, 300]), (8, 1, 16, [60, 5], [700, 5]), (4, 2, 64, [33, 200], [333, 200])])
+def test_one_feature_of_a_caches_v(case, chunk, dtype, monkeypatch):
+    """Of one of the new tokens, and of an old one where there are any.  (e4m3 has NaN only.)"""
+    if chunk:
+        monkeypatch.setenv("COMMFUSE_CAUSAL", chunk)
+    heads, kv, page, new, ctx = case
+    b = Batch(511, heads, kv, page, dtype, new, ctx)
+    marks = []
+    for s, (m, n) in enumerate(zip(new, ctx)):
+        for i, key in enumerate({n - m + m // 2, (n - m) // 2}):
+            d = (29 * s + 50 * i + 3) % D
+            at = (int(b.table[s, key // page]), s % kv, key % page, d)
+            b.pool[1][at] = 127 if dtype == "e4m3" else math.nan
+            b.values[1][at] = 0
+            rows = torch.zeros(b.total, dtype=torch.bool, device=DEV)
+            first = int(b.starts[s]) + max(0, key - (n - m))
+            rows[first:int(b.starts[s + 1])] = True
+            marks.append((rows, d, s % kv, math.nan))
+    ref = b.definition()
+    out, lse = b.run()
+    for rows, d, kvh, _ in marks:
+        for head in range(kvh * (heads // kv), (kvh + 1) * (heads // kv)):
+            ref[0][rows, head, d] = 0
+    _expect(out, marks, heads // kv)
+    check_paged(out, lse, ref)
+
+
+def test_missing_pages_in_front_of_a_page_that_is_not_finite():
+    """Keys of pages that do not exist are not seen, whatever page 0 holds."""
+    for dtype in ("bf16", "e4m3"):
+        for new in (1, 3, 40):
+            b = Batch(521, 8, 2, 16, dtype, [new, new], [600, 90])
+            page = int(b.table[0, 7])
+            for pool in b.pool:                                               # page 0 becomes one of no sequence, NaN throughout
+                pool[page].copy_(pool[0])
+            for values in b.values:
+                values[page].copy_(values[0])
+            for e in b.exps:
+                if e is not None:
+                    e[page].copy_(e[0])
+            b.table[b.table == 0] = page
+            b.table[0, 7] = -1
+            for pool in b.pool:
+                pool[0] = 127 if dtype == "e4m3" else math.nan
+            b.table[1, 2] = b.pages + 5
+            check_paged(*b.run(), b.definition(absent=[(0, 7), (1, 2)]))
+
+
+def _time(f):
+    """Shortest of five, in milliseconds."""
+    best = math.inf
+    for _ in range(6):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+# Time with values that are not finite.  A wave whose results may be spoilt walks over its rows' keys once more, by itself, while others may have
+# shared the first walk: 32 keys take it some five times as long as 64 keys take a workgroup, so a walk takes ten times as long as an unsplit one, and an
+# unsplit one of these problems three times as long as the call.
+SLOWER = 30
+
+
+@pytest.mark.parametrize("tokens", [[100], [5000], list(range(20, 6000, 50))])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_time_of_prompts_with_a_value_that_is_not_finite(tokens, value):
+    x, at = prompt.make(531, 6144, 4, 1), prompt.starts([6000, 144])
+    out, lse, s = torch.empty(6144, 4, D, dtype=torch.bfloat16, device=DEV), torch.empty(4, 6144, device=DEV), x.stride()[:2]
+    call = lambda: cf.attn_prompt(cf.prompt_desc(6144, 2, 4, 1, SCALE, q=s, k=s, v=s), x[:, :4], x[:, 4:5], x[:, 5:], at, out, lse)
+    normal = _time(call)
+    x[tokens, 5, 7] = value
+    assert _time(call) <= SLOWER * normal
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 4, 100])
+def test_time_of_a_cache_with_a_value_that_is_not_finite(new, dtype):
+    b = Batch(541, 8, 1, 16, dtype, [new, new], [6000, 4000])
+    out, lse = torch.empty(b.total, 8, D, dtype=torch.bfloat16, device=DEV), torch.empty(8, b.total, device=DEV)
+    call = lambda: b.run(out=out, lse=lse, stream=torch.cuda.current_stream())
+    normal = _time(call)
+    for key in (70, 6000 - new + new // 2):
+        b.pool[1][int(b.table[0, key // 16]), 0, key % 16, 9] = 127 if dtype == "e4m3" else math.inf
+        assert _time(call) <= SLOWER * normal
