@@ -436,7 +436,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         }
     }
     // Rows whose result is not finite once more where what they do not see can have been the reason: the new tokens behind a row's own (a
-    // single token's row sees all keys), or page 0 in the place of one that does not exist.  The waves share the keys.
+    // single token's row sees all keys), the last key in the place of those behind it, or page 0 in the place of one that does not exist.  The waves
+    // share the keys.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     const unsigned odd = odd_rows[0] | (QT > 1 ? odd_rows[QT - 1] << 16 : 0u);
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     bool absent = false;
     for (int page = lane; page < (int)(((unsigned)hi + (1u << shift) - 1) >> shift); page += 64)
         absent = absent || (unsigned)table[page] >= (unsigned)n_pages;
-    if (__builtin_amdgcn_ballot_w64(absent) == 0 && !any_large(Kv, max(n - m + 1, 0), hi))
+    if (__builtin_amdgcn_ballot_w64(absent) == 0 && !any_large(Kv, max(min(n - m + 1, hi - 1), 0), hi))
         return;
     const int lq = lane & 31, lh = lane >> 5, r = lq < rows ? lq : 0, token = r / G;
     f32x16_t acc[DH / 32];

@@ -13,8 +13,8 @@
 // As in the forward kernel a lane owns one row (or key) and 16 of every 32 keys (rows) of a product's result, which is, rounded to
 // bf16, the "B" operand of the next product as it stands: nothing moves between lanes.  Tiles lie in LDS once and are read both by rows
 // and transposed: 16-byte chunks XOR-ed with (row & 15), which the transposing read can follow lane by lane.
-// Rows behind a walk are read from its last row, or as zero, and masked.  A result that is not finite is computed once more over what is
-// visible only, so that what the mask hides has no influence.
+// Rows behind a walk are read as zero, and masked.  Results that are not finite are computed once more where what the mask
+// hides can have been the reason, so that it has no influence.
 #include "attn_tiles.h"
 
 namespace cf {
@@ -164,81 +164,6 @@ __device__ __forceinline__ f32x16_t sum_of_parts(const CausalParams &P, int regs
     return x;
 }
 
-__device__ __forceinline__ float wave_sum(float x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        x += __shfl_xor(x, d);
-    return x;
-}
-__device__ __forceinline__ f32x2_t pair_at(const void *row)          // features 2 lane, 2 lane + 1
-{
-    const bf16x2_t v = static_cast<const bf16x2_t *>(row)[threadIdx.x & 63];
-    return f32x2_t{(float)v[0], (float)v[1]};
-}
-__device__ __forceinline__ void put_pair(void *row, float a, float b, int tile)     // (of a feature tile, or -1: of all)
-{
-    const int lane = threadIdx.x & 63;
-    bf16x2_t v;
-    v[0] = (__bf16)a;
-    v[1] = (__bf16)b;
-    if (tile < 0 || lane >> 4 == tile)
-        static_cast<bf16x2_t *>(row)[lane] = v;
-}
-
-// Sums that are NaN in every lane stay so.  (Of inputs that are NaN throughout, 8192 keys for every row, one by one, would take some 40 ms by
-// the count of instructions.)
-__device__ __forceinline__ bool settled(float a, float b) { return __builtin_amdgcn_ballot_w64(a == a || b == b) == 0; }
-
-// dQ of one row, key by key (all of it, or one feature tile).
-__device__ __forceinline__ void careful_dq(const GradParams &P, int t, int head, int first, int tile)
-{
-    const CausalParams &C = P.c;
-    const int kvh = head / C.group;
-    const __bf16 *K = static_cast<const __bf16 *>(C.K) + kvh * C.k_head, *V = static_cast<const __bf16 *>(C.V) + kvh * C.v_head;
-    const f32x2_t q = pair_at(static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head);
-    const f32x2_t g = pair_at(static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head);
-    const float lse = C.lse[(int64_t)head * C.lse_stride + t], delta = P.delta[(int64_t)head * C.lse_stride + t];
-    float a = 0.0f, b = 0.0f;
-    for (int key = first; key <= t; ++key) {
-        const f32x2_t k = pair_at(K + (int64_t)key * C.k_token), v = pair_at(V + (int64_t)key * C.v_token);
-        const float s = wave_sum(q[0] * k[0] + q[1] * k[1]), dp = wave_sum(g[0] * v[0] + g[1] * v[1]);
-        const float ds = exp2f((s * C.scale - lse) * LOG2E) * (dp - delta);
-        a += ds * k[0];
-        b += ds * k[1];
-        if (settled(a, b))
-            break;
-    }
-    put_pair(static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, a * C.scale, b * C.scale, tile);
-}
-
-// dK and dV of one key, row by row (all of both, or a feature tile: 0 .. 3 of dK, 4 .. 7 of dV).
-__device__ __forceinline__ void careful_key(const GradParams &P, int key, int kvh, int end, int tile)
-{
-    const CausalParams &C = P.c;
-    const f32x2_t k = pair_at(static_cast<const __bf16 *>(C.K) + (int64_t)key * C.k_token + kvh * C.k_head);
-    const f32x2_t v = pair_at(static_cast<const __bf16 *>(C.V) + (int64_t)key * C.v_token + kvh * C.v_head);
-    float ka = 0.0f, kb = 0.0f, va = 0.0f, vb = 0.0f;
-    for (int head = kvh * C.group; head < (kvh + 1) * C.group; ++head)
-        for (int t = key; t < end; ++t) {
-            const f32x2_t q = pair_at(static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head);
-            const f32x2_t g = pair_at(static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head);
-            const float s = wave_sum(q[0] * k[0] + q[1] * k[1]), dp = wave_sum(g[0] * v[0] + g[1] * v[1]);
-            const int64_t at = (int64_t)head * C.lse_stride + t;
-            const float p = exp2f((s * C.scale - C.lse[at]) * LOG2E), ds = p * (dp - P.delta[at]);
-            ka += ds * q[0];
-            kb += ds * q[1];
-            va += p * g[0];
-            vb += p * g[1];
-            if (settled(ka, kb) && settled(va, vb))
-                t = end, head = (kvh + 1) * C.group;
-        }
-    if (tile < 4)
-        put_pair(static_cast<__bf16 *>(P.dk) + (int64_t)key * C.k_token + kvh * C.k_head, ka * C.scale, kb * C.scale, tile);
-    if (tile < 0 || tile >= 4)
-        put_pair(static_cast<__bf16 *>(P.dv) + (int64_t)key * C.v_token + kvh * C.v_head, va, vb, tile < 0 ? -1 : tile - 4);
-}
-
 // A lane's row of a feature tile of a result X^T, times `factor`, as bf16.  True if a value is not finite.
 __device__ __forceinline__ bool store_tile(const f32x16_t &x, float factor, __bf16 *row, int tile, bool there)
 {
@@ -259,16 +184,107 @@ __device__ __forceinline__ bool store_tile(const f32x16_t &x, float factor, __bf
     return there && odd != 0.0f;
 }
 
-// f(lane) for every row (or key) of the wave that has a value that is not finite, once its first result is written.
-template <typename F>
-__device__ __forceinline__ void once_more(bool odd, F &&f)
+// Rows (or keys) of the wave with a value that is not finite, in both lanes that share one.
+__device__ __forceinline__ bool odd_row(bool odd)
 {
-    unsigned long long again = __builtin_amdgcn_ballot_w64(odd);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
-    if (again != 0) {
-        __builtin_amdgcn_s_waitcnt(0);
-        for (; again != 0; again &= again - 1)
-            f(__builtin_ctzll(again));
+    const unsigned long long rows = __builtin_amdgcn_ballot_w64(odd);
+    return (rows | rows >> 32) >> (threadIdx.x & 31) & 1;
+}
+
+// One of the three results for 32 columns (rows of Q, or keys) by one wave, from memory: as in `rows_again`.  A lane's column (lane & 31) has rows
+// b1, b2 and sees indices [lo, hi): keys, or with KEYS rows (token, head of the group); stored where `wanted`: all features, or (TILES = 1, a quarter of
+// the registers) those of tile `tile`.
+// dQ: sum over keys of dS k; dK: over rows of dS q; dV (`values`): over rows of P dout.
+template <bool KEYS, int TILES>
+__device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const __bf16 *b1, const __bf16 *b2, int lo, int hi, float lse, float delta, bool values,
+                                           bool wanted, __bf16 *out, int tile)
+{
+    const CausalParams &C = P.c;
+    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5;
+    const int from = least_of(wanted ? lo : 0x7FFFFFFF), to = most_of(wanted ? hi : 0);
+    f32x16_t acc[TILES];
+#pragma unroll
+    for (int d = 0; d < TILES; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            acc[d][e] = 0.0f;
+#pragma unroll 1
+    for (int at0 = from & ~31; at0 < to; at0 += 32) {
+        const int mine = at0 + lq < from ? from : at0 + lq < to ? at0 + lq : to - 1;
+        const __bf16 *a1, *a2;
+        float lse_of = 0.0f, delta_of = 0.0f;
+        if constexpr (KEYS) {
+            const int t = mine / C.group, head = kvh * C.group + mine - t * C.group;
+            a1 = static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head;
+            a2 = static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head;
+            lse_of = C.lse[(int64_t)head * C.lse_stride + t];
+            delta_of = P.delta[(int64_t)head * C.lse_stride + t];
+        } else {
+            a1 = static_cast<const __bf16 *>(C.K) + (int64_t)mine * C.k_token + kvh * C.k_head;
+            a2 = static_cast<const __bf16 *>(C.V) + (int64_t)mine * C.v_token + kvh * C.v_head;
+        }
+        bf16x8_t v[2][TILES];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int slot = 16 * c + 8 * (i >> 1) + 2 * (i & 1);
+                const __bf16 *even = of_slot(values ? a2 : a1, slot), *odd = of_slot(values ? a2 : a1, slot + 1);
+                if constexpr (TILES == DT) {
+                    put_pair(v[c], i, reinterpret_cast<const u32x2_t *>(even)[lq], reinterpret_cast<const u32x2_t *>(odd)[lq]);
+                } else {
+                    v[c][0][2 * i] = even[tile * 32 + lq];
+                    v[c][0][2 * i + 1] = odd[tile * 32 + lq];
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16_t s = {}, dp = {};
+        asm volatile("" : "+v"(b1), "+v"(b2));                       // (read in every unit: 64 registers)
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(reinterpret_cast<const bf16x8_t *>(a1)[2 * ks + lh], reinterpret_cast<const bf16x8_t *>(b1)[2 * ks + lh], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(reinterpret_cast<const bf16x8_t *>(a2)[2 * ks + lh], reinterpret_cast<const bf16x8_t *>(b2)[2 * ks + lh], dp, 0, 0, 0);
+            if (TILES == 1 || ks % 4 == 1)
+                __builtin_amdgcn_sched_barrier(0);                   // (fewer registers)
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        unsigned seen = 0;
+        bf16x8_t w[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int slot = 8 * (i >> 2) + (i & 3), at = at0 + slot + 4 * lh;
+            const bool sees = at >= lo && at < hi;
+            seen |= (unsigned)sees << i;
+            const float l = KEYS ? __builtin_bit_cast(float, of_slot(__builtin_bit_cast(int, lse_of), slot)) : lse;
+            const float d = KEYS ? __builtin_bit_cast(float, of_slot(__builtin_bit_cast(int, delta_of), slot)) : delta;
+            const float p = exp2f((s[i] * C.scale - l) * LOG2E);
+            w[i >> 3][i & 7] = (__bf16)(sees ? values ? p : p * (dp[i] - d) : 0.0f);
+            if (i % 4 == 3)
+                __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            add_seen(acc, v[0], w[0], seen);
+            seen >>= 8;
+            w[0] = w[1];
+#pragma unroll
+            for (int d = 0; d < TILES; ++d)
+                v[0][d] = v[1][d];
+        }
+        if ((at0 & 0xE0) == 0) {                                     // now and then: does anything that follows matter?
+            bool done = true;
+#pragma unroll
+            for (int d = 0; d < TILES; ++d)
+                done = done && none_finite(acc[d]);
+            if (__builtin_amdgcn_ballot_w64(wanted && !done) == 0)
+                break;
+        }
+    }
+    if constexpr (TILES == DT) {
+        if (wanted)
+            store_fours(acc, values ? 1.0f : C.scale, out);
+    } else {
+        store_tile(acc[0], values ? 1.0f : C.scale, out, tile, wanted);
     }
 }
 
@@ -327,6 +343,37 @@ struct DqRow {                           // a lane's row: token t sees keys firs
         first = there ? (first < 0 ? 0 : first) : t;                 // (a row of no sequence: any visible key will do, it is not stored)
     }
 };
+
+// Rows whose dQ is not finite once more, where keys that they do not see can have been the reason: by products with 0 (K, V not finite) or by a
+// dP that is infinite.  (A row whose lse or delta is not finite has no other result.)
+template <int TILES>
+__device__ __forceinline__ void dq_again(const GradParams &P, const RowBlock &B, const DqRow &row, int kvh, bool odd, int tile)
+{
+    const CausalParams &C = P.c;
+    odd = odd_row(odd);
+    if (__builtin_amdgcn_ballot_w64(odd) == 0)
+        return;
+    __builtin_amdgcn_s_waitcnt(0);                                   // the first results, and delta, are written
+    int t = row.t, head = row.head;
+    asm volatile("" : "+v"(t), "+v"(head));                          // (addresses anew: kept, they would take registers from the walk)
+    const __bf16 *g = static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head;
+    const float lse = C.lse[(int64_t)head * C.lse_stride + t], delta = P.delta[(int64_t)head * C.lse_stride + t];
+    odd = odd && __builtin_isfinite(lse) && __builtin_isfinite(delta);
+    Keys<PACKED> K, V;
+    K.base = reinterpret_cast<const unsigned char *>(static_cast<const __bf16 *>(C.K) + kvh * C.k_head);
+    K.row_bytes = C.k_token * 2;
+    V.base = reinterpret_cast<const unsigned char *>(static_cast<const __bf16 *>(C.V) + kvh * C.v_head);
+    V.row_bytes = C.v_token * 2;
+    int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
+    edges(row.there, row.first, row.t, &f_min, &f_max, &l_min, &l_max);
+    const int front = B.lo + max(0, (f_min - B.lo) / BKV) * BKV, behind = min(B.hi, B.lo + ((l_max - B.lo) / BKV + 1) * BKV);
+    const int seen_by_all = min(f_max, B.hi), unseen = max(l_min + 1, B.lo);   // front .. seen_by_all, unseen .. behind: keys that some rows do not see
+    if (__builtin_amdgcn_ballot_w64(odd) == 0 || (__builtin_amdgcn_ballot_w64(odd && large_row(g)) == 0 && !any_large(K, front, seen_by_all) &&
+                                                  !any_large(V, front, seen_by_all) && !any_large(K, unseen, behind) && !any_large(V, unseen, behind)))
+        return;
+    grad_again<false, TILES>(P, kvh, static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head, g, row.first, t + 1, lse, delta, false, odd,
+                      static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, tile);
+}
 
 __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 {
@@ -540,7 +587,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 #pragma unroll
     for (int d = 0; d < DT; ++d)
         odd = store_tile(acc[d], C.scale, out, d, there) || odd;
-    once_more(odd, [&](int l) { careful_dq(P, __shfl(t, l), __shfl(head, l), __shfl(first, l), -1); });
+    dq_again<DT>(P, block, row, kvh, odd, 0);
 }
 
 // Workgroup `at` of the sums over the splits of dQ: one feature tile of one block.
@@ -557,7 +604,7 @@ __device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked
     const DqRow row(C, block, kvh);
     const f32x16_t x = sum_of_parts<64 * DQ_WAVES>(C, DT * 16, block.it, tile);
     const bool odd = store_tile(x, C.scale, static_cast<__bf16 *>(P.dq) + (int64_t)row.t * C.q_token + row.head * C.q_head, tile, row.there);
-    once_more(odd, [&](int l) { careful_dq(P, __shfl(row.t, l), __shfl(row.head, l), __shfl(row.first, l), tile); });
+    dq_again<1>(P, block, row, kvh, odd, tile);
 }
 
 constexpr int GRAD_KEYS = 128;           // keys of a workgroup of the second launch: four waves of 32
@@ -623,6 +670,53 @@ struct GradKey {                         // a lane's key, seen by tokens key .. 
     }
 };
 
+// Keys whose dK or dV is not finite once more, where rows that do not see them can have been the reason: by products with 0 (Q, dout not finite), an
+// infinite dP, or an lse or delta that is not finite.
+template <int TILES>
+__device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock &B, const GradKey &mine, int kvh, bool odd_k, bool odd_v, int tile)
+{
+    const CausalParams &C = P.c;
+    odd_k = odd_row(odd_k);
+    odd_v = odd_row(odd_v);
+    if (__builtin_amdgcn_ballot_w64(odd_k || odd_v) == 0)
+        return;
+    __builtin_amdgcn_s_waitcnt(0);                                   // the first results are written
+    const int G = C.group, lo = B.lo, hi = B.hi, first = mine.key * G, end = mine.there ? mine.end * G : first;
+    const __bf16 *k = static_cast<const __bf16 *>(C.K) + (int64_t)mine.key * C.k_token + kvh * C.k_head;
+    const __bf16 *v = static_cast<const __bf16 *>(C.V) + (int64_t)mine.key * C.v_token + kvh * C.v_head;
+    auto any_odd = [&](int from, int to) {                           // of the rows [from, to)
+        for (; from < to; from += 64) {
+            const int r = from + (int)(threadIdx.x & 63);
+            bool odd = false;
+            if (r < to) {
+                const int t = r / G, head = kvh * G + r - t * G;
+                odd = large_row(static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head) ||
+                      large_row(static_cast<const __bf16 *>(P.dout) + (int64_t)t * C.o_token + head * C.o_head) ||
+                      !__builtin_isfinite(C.lse[(int64_t)head * C.lse_stride + t]) || !(fabsf(P.delta[(int64_t)head * C.lse_stride + t]) < 0x1p100f);
+            }
+            if (__builtin_amdgcn_ballot_w64(odd) != 0)
+                return true;
+        }
+        return false;
+    };
+    int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
+    edges(mine.there, first, end, &f_min, &f_max, &l_min, &l_max);
+    const int front = lo + max(0, (f_min - lo) / GRAD_ROWS) * GRAD_ROWS, tiles = (l_max - lo + GRAD_ROWS - 1) / GRAD_ROWS;
+    const int behind = tiles < B.tiles ? lo + tiles * GRAD_ROWS : hi;
+    if (__builtin_amdgcn_ballot_w64((odd_k || odd_v) && large_row(v)) == 0 && !any_odd(front, min(f_max, hi)) && !any_odd(max(l_min, lo), behind))
+        return;
+#pragma unroll 1
+    for (int values = 0; values < 2; ++values) {                     // dK, dV
+        const bool odd = values ? odd_v : odd_k;
+        if (__builtin_amdgcn_ballot_w64(odd) != 0)
+            grad_again<true, TILES>(P, kvh, k, v, first, end, 0.0f, 0.0f, values, odd, values ? static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head
+                                                                                       : static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head, tile);
+    }
+}
+
+// What stands for rows behind a walk: a probability of 0 times anything else of them would be NaN where that is not finite.
+__device__ const __attribute__((aligned(16))) char zero_row[ROWB] = {};
+
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
@@ -640,7 +734,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     if (!my_item<NT, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
-    const int lo = block.lo, hi = block.hi, end_b = block.end_b;
+    const int lo = block.lo, hi = block.hi;
     int rt0, nrt;
     block.it.share(block.tiles, &rt0, &nrt);
     const GradKey mine(C, block);
@@ -706,17 +800,13 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
             q[j] = q_at[j];
             g[j] = g_at[j];
         }
-        if (rows_left < ROWS) {                                      // uniform: rows behind the walk are its last row
-            const int64_t q_last = 2 * ((end_b - 1) * C.q_token + (G - 1) * C.q_head), o_last = 2 * ((end_b - 1) * C.o_token + (G - 1) * C.o_head);
+        if (rows_left < ROWS) {                                      // uniform: rows behind the walk
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (row_in + 4 * j >= rows_left) {
-                    const int chunk = ((lane & 15) ^ spread(j * 4 + (lane >> 4))) * 16;
-                    q[j] = qb + q_last + chunk;
-                    g[j] = gb + o_last + chunk;
-                }
+                if (row_in + 4 * j >= rows_left)
+                    q[j] = g[j] = zero_row + (lane & 15) * 16;
             if (lane >= rows_left)
-                l = lb + 4 * ((int64_t)(end_b - 1) + (G - 1) * C.lse_stride);
+                l = zero_row;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -915,13 +1005,13 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     }
     __bf16 *out_k = static_cast<__bf16 *>(P.dk) + (int64_t)kk * C.k_token + kvh * C.k_head;
     __bf16 *out_v = static_cast<__bf16 *>(P.dv) + (int64_t)kk * C.v_token + kvh * C.v_head;
-    bool odd = false;
+    bool odd_k = false, odd_v = false;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-        odd = store_tile(dk[d], C.scale, out_k, d, there) || odd;
-        odd = store_tile(dv[d], 1.0f, out_v, d, there) || odd;
+        odd_k = store_tile(dk[d], C.scale, out_k, d, there) || odd_k;
+        odd_v = store_tile(dv[d], 1.0f, out_v, d, there) || odd_v;
     }
-    once_more(odd, [&](int l) { careful_key(P, __shfl(kk, l), kvh, __shfl(end, l), -1); });
+    dkv_again<DT>(P, block, mine, kvh, odd_k, odd_v, 0);
 }
 
 // ... of dK and dV
@@ -940,12 +1030,12 @@ __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looke
     __bf16 *out = tile < DT ? static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head
                             : static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head;
     const bool odd = store_tile(x, tile < DT ? C.scale : 1.0f, out, tile & (DT - 1), mine.there);
-    once_more(odd, [&](int l) { careful_key(P, __shfl(mine.key, l), kvh, __shfl(mine.end, l), tile); });
+    dkv_again<1>(P, block, mine, kvh, odd && tile < DT, odd && tile >= DT, tile & (DT - 1));
 }
 
 // Workgroups below `dkv_wgs`: dK and dV; the others dQ.  (Two launches, 6.3 and 10.1 us for a pack of 4096 tokens and four heads.)
 static_assert(DQ_WAVES == 4, "one shape of workgroup for both");
-__global__ __launch_bounds__(256) void attn_grad_join_kernel(GradParams dkv, GradParams dq, int dkv_wgs)
+__global__ __launch_bounds__(256, 4) void attn_grad_join_kernel(GradParams dkv, GradParams dq, int dkv_wgs)
 {
     __shared__ int looked_at[MAX_BLOCKS];
     if ((int)blockIdx.x < dkv_wgs)

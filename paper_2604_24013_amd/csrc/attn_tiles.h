@@ -462,11 +462,12 @@ __device__ __forceinline__ bool any_large(const Keys<SRC> &K, int from, int to)
 
 // acc[d] += a[d] w (an MFMA's "A" and "B" operands), d the feature tiles, where elements of `a` that are not finite count for the columns that see
 // their index only (bit x of `seen`: slot x): they are taken out of `a`, and products of ones say which results they make +inf, -inf or NaN.
-__device__ __forceinline__ void add_seen(f32x16_t (&acc)[DH / 32], bf16x8_t (&a)[DH / 32], bf16x8_t w, unsigned seen)
+template <int TILES>
+__device__ __forceinline__ void add_seen(f32x16_t (&acc)[TILES], bf16x8_t (&a)[TILES], bf16x8_t w, unsigned seen)
 {
     u16x8_t most = {};
 #pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
+    for (int d = 0; d < TILES; ++d)
         most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x8_t, a[d]) & (unsigned short)0x7FFF);
     bool finite = true;
 #pragma unroll
@@ -482,10 +483,10 @@ __device__ __forceinline__ void add_seen(f32x16_t (&acc)[DH / 32], bf16x8_t (&a)
             minus[x] = sees && negative ? ONE : 0;
         }
 #pragma unroll 1
-        for (int i = 0; i < 2 * (DH / 32); ++i) {                    // (the code is there once) tile i / 2: what makes it +inf, what makes it -inf
+        for (int i = 0; i < 2 * (TILES); ++i) {                    // (the code is there once) tile i / 2: what makes it +inf, what makes it -inf
             u16x8_t bits = __builtin_bit_cast(u16x8_t, a[0]), up, down;
 #pragma unroll
-            for (int d = 1; d < DH / 32; ++d)
+            for (int d = 1; d < TILES; ++d)
                 bits = i >> 1 == d ? __builtin_bit_cast(u16x8_t, a[d]) : bits;
             const unsigned short sign = i & 1 ? 0x8000 : 0;
 #pragma unroll
@@ -501,12 +502,12 @@ __device__ __forceinline__ void add_seen(f32x16_t (&acc)[DH / 32], bf16x8_t (&a)
             for (int e = 0; e < 16; ++e) {
                 const float more = n[e] > 0.0f ? (i & 1 ? -INFINITY : INFINITY) : 0.0f;
 #pragma unroll
-                for (int d = 0; d < DH / 32; ++d)
+                for (int d = 0; d < TILES; ++d)
                     acc[d][e] += i >> 1 == d ? more : 0.0f;
             }
         }
 #pragma unroll
-        for (int d = 0; d < DH / 32; ++d) {
+        for (int d = 0; d < TILES; ++d) {
             const u16x8_t bits = __builtin_bit_cast(u16x8_t, a[d]);
             u16x8_t kept;
 #pragma unroll
@@ -516,7 +517,7 @@ __device__ __forceinline__ void add_seen(f32x16_t (&acc)[DH / 32], bf16x8_t (&a)
         }
     }
 #pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
+    for (int d = 0; d < TILES; ++d)
         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[d], w, acc[d], 0, 0, 0);
 }
 

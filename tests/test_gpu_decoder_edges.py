@@ -204,3 +204,88 @@ def test_time_of_a_cache_with_a_value_that_is_not_finite(new, dtype):
     for key in (70, 6000 - new + new // 2):
         b.pool[1][int(b.table[0, key // 16]), 0, key % 16, 9] = 127 if dtype == "e4m3" else math.inf
         assert _time(call) <= SLOWER * normal
+
+
+# The gradient.  What a value that is not finite reaches by the formulas (all probabilities are above 2^-126, no element of Q, K, V or dout is 0):
+#   dout[t, d]   dP and delta of row t: dQ of the row, dK of the keys that it sees; dV of those keys in feature d
+#   V[t, d]      delta of the rows that see t: their dQ, and dK of all keys that those rows see; no dV
+#   Q[t, d]      lse of row t: dQ of the row, dK and dV of the keys that it sees
+#   K[t, d]      lse of the rows that see t: their dQ, dK and dV of all keys that those rows see        (NaN; an infinite score may be -inf)
+# Everything else is as without it.
+def _reached(what, t, a, b):
+    """{result: tokens} of a sequence [a, b)"""
+    row, keys, rows, every = slice(t, t + 1), slice(a, t + 1), slice(t, b), slice(a, b)
+    return {"dout": dict(dq=row, dk=keys, dv=keys), "v": dict(dq=rows, dk=every), "q": dict(dq=row, dk=keys, dv=keys), "k": dict(dq=rows, dk=every, dv=every)}[what]
+
+
+@pytest.mark.parametrize("what, value", [("dout", math.inf), ("dout", -math.inf), ("dout", math.nan), ("v", math.inf), ("v", math.nan), ("q", math.nan), ("k", math.nan)])
+@pytest.mark.parametrize("chunk", [None, "4x1", "4x3", "4x100000"])
+@pytest.mark.parametrize("case", [(4, 2, [150, 81, 160], [100, 151, 390]), (8, 1, [5, 3, 9, 1, 30, 2], [3, 6, 20, 48]), (1, 1, [300], [0, 130]),
+                                  (6, 2, [1] * 70 + [200] + [2] * 40, [10, 75, 269, 300]), (3, 3, [420], [64, 65, 300]), (40, 1, [70], [33])])
+def test_one_feature_of_a_gradients_operand(case, chunk, what, value, monkeypatch):
+    h, kv, lens, tokens = case
+    if chunk:
+        monkeypatch.setenv("COMMFUSE_CAUSAL", chunk)
+    ends = [sum(lens[:i + 1]) for i in range(len(lens))]
+    for i, t in enumerate(tokens):                                            # one at a time
+        x, dout, at = grad.problem(601, lens, h, kv)
+        head, d = (3 * i + 1) % h, (37 * i + 5) % D
+        kvh = head // (h // kv)
+        clean = [y.clone() for y in (x, dout)]
+        spot = dict(dout=(1, head), q=(0, head), k=(0, h + kvh), v=(0, h + kv + kvh))[what]
+        (x, dout)[spot[0]][t, spot[1], d] = value
+        clean[spot[0]][t, spot[1], d] = 0
+        ref = grad.gradient(clean[0][:, :h], clean[0][:, h:h + kv], clean[0][:, h + kv:], clean[1], at, SCALE)
+        got = grad.forward_and_gradient(x, dout, h, kv, at, SCALE)
+        end = next(e for e in ends if e > t)
+        a, group = end - lens[ends.index(end)], slice(kvh * (h // kv), (kvh + 1) * (h // kv))
+        for n, rows in _reached(what, t, a, end).items():
+            heads = kvh if n != "dq" else head if what in ("dout", "q") else group
+            features = d if (what, n) == ("dout", "dv") else slice(None)
+            part = got[n][rows, heads, features].float()
+            if (what, n) == ("dout", "dv"):
+                assert torch.equal(part.nan_to_num(7.0, 8.0, 9.0), torch.full_like(part, value).nan_to_num(7.0, 8.0, 9.0))
+            else:
+                assert not bool(torch.isfinite(part).any()), (n, t)
+            got[n][rows, heads, features] = -7
+            for r in ref:
+                r[n][rows, heads, features] = math.nan
+        grad.check(got, ref)
+
+
+@pytest.mark.parametrize("new, ctx", [([1, 1, 1], [33, 600, 64]), ([2, 3], [50, 1000]), ([30, 50], [45, 700])])
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+def test_infinite_v_of_a_caches_last_keys(new, ctx, value):
+    """Places behind the last key may be read from it: the rows that see it are infinite in that feature, no row is NaN."""
+    b = Batch(551, 8, 2, 16, "bf16", new, ctx)
+    marks = []
+    for s, n in enumerate(ctx):
+        d, at = 11 + 40 * s, (int(b.table[s, (n - 1) // 16]), s % 2, (n - 1) % 16)
+        b.pool[1][at][d], b.values[1][at][d] = value, 0
+        rows = torch.zeros(b.total, dtype=torch.bool, device=DEV)
+        rows[int(b.starts[s + 1]) - 1] = True
+        marks.append((rows, d, s % 2, value))
+    ref = b.definition()
+    out, lse = b.run()
+    for rows, d, kvh, _ in marks:
+        ref[0][rows, kvh * 4:kvh * 4 + 4, d] = 0
+    _expect(out, marks, 4)
+    check_paged(out, lse, ref)
+
+
+@pytest.mark.parametrize("what", ["dout", "v", "q"])
+@pytest.mark.parametrize("tokens", [[100], [4000], [4095], list(range(20, 4096, 50))])
+@pytest.mark.parametrize("h, kv, lens", [(8, 1, [4096]), (4, 4, [3000, 1096])])
+def test_time_of_a_gradient_with_a_value_that_is_not_finite(h, kv, lens, tokens, what):
+    x, dout, at = grad.problem(611, lens, h, kv)
+    out, lse, delta, dx = torch.empty_like(dout), torch.empty(h, 4096, device=DEV), torch.empty(h, 4096, device=DEV), torch.empty_like(x)
+    q, k, v, s = x[:, :h], x[:, h:h + kv], x[:, h + kv:], x.stride()[:2]
+    desc = cf.prompt_desc(4096, len(lens), h, kv, SCALE, q=s, k=s, v=s)
+
+    def call():
+        cf.attn_prompt(desc, q, k, v, at, out, lse)
+        cf.attn_prompt_grad(desc, q, k, v, out, lse, dout, at, delta, dx[:, :h], dx[:, h:h + kv], dx[:, h + kv:])
+
+    normal = _time(call)
+    dict(dout=dout, v=v, q=q)[what][tokens, 0, 7] = math.inf
+    assert _time(call) <= SLOWER * normal
