@@ -163,6 +163,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         }
     }
     const bool busy = wt0 < wt1;
+    const unsigned long long rows_there = __builtin_amdgcn_ballot_w64(there);
 
     const __bf16 *qrow = static_cast<const __bf16 *>(P.Q) + (int64_t)(t_base + (there ? token : 0)) * P.q_token + head * P.q_head;
     bf16x8_t qf[DS];
@@ -611,8 +612,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     }
 
     // O = O^T / l, rounded to bf16; a row without a visible key is 0 and its log-sum-exp -inf.
-    const int64_t t = t_base + token;
-    __bf16 *orow = static_cast<__bf16 *>(P.out) + t * P.o_token + head * P.o_head;
+    int nth = lane, per_token = G;
+    asm volatile("" : "+v"(nth), "+s"(per_token));                   // (found anew: kept, they would take registers from the walk)
+    const bool stored = rows_there >> nth & 1;
+    const int r_out = row0 + wave * 32 + (nth & 31), of_token = r_out / per_token, of_head = kvh * G + r_out - of_token * G;
+    const int64_t t = t_base + of_token;
+    __bf16 *orow = static_cast<__bf16 *>(P.out) + t * P.o_token + of_head * P.o_head;
     const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
     float odd = 0.0f;                                                // NaN if a value is not finite
 #pragma unroll
@@ -622,7 +627,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
             oacc[d][e] *= inv;
             odd = __builtin_fmaf(oacc[d][e], 0.0f, odd);
         }
-    if (there) {
+    if (stored) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -634,9 +639,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
                 *reinterpret_cast<u32x2_t *>(orow + d * 32 + 8 * gq + 4 * lh) = __builtin_bit_cast(u32x2_t, h);
             }
         if (LSE && lh == 0)
-            P.lse[(int64_t)head * P.lse_stride + t] = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * LN2;
+            P.lse[(int64_t)of_head * P.lse_stride + t] = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * LN2;
     }
-    const unsigned long long odd_rows = __builtin_amdgcn_ballot_w64(there && odd != 0.0f && l_run == l_run);   // (l is made of visible scores only)
+    const unsigned long long odd_rows = __builtin_amdgcn_ballot_w64(stored && odd != 0.0f && l_run == l_run);   // (l is made of visible scores only)
     if (odd_rows != 0) {
         const bool again = (odd_rows | odd_rows >> 32) >> lq & 1;
         Keys<SRC> K, V;
@@ -654,13 +659,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         V.exps = ve;
         // The tiles of this wave, of all splits (the first may be one that no row sees); front .. f_max, l_min .. behind: keys that some rows do not see
         int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
-        edges(there, first, last, &f_min, &f_max, &l_min, &l_max);
+        edges(stored, first, last, &f_min, &f_max, &l_min, &l_max);
         const int front = lo + max(0, (f_min - lo) / BKV - 1) * BKV, behind = min(hi, lo + ((l_max - lo) / BKV + 1) * BKV);
         if (any_large(V, front, min(f_max, hi)) || any_large(V, max(l_min + 1, lo), behind)) {
             __builtin_amdgcn_s_waitcnt(0);                           // the rows' first results are written before their second
-            int row = token, h = head;
-            asm volatile("" : "+v"(row), "+v"(h));                   // (the row's address anew: kept, it would take registers from the walk)
-            rows_again<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + (int64_t)(t_base + (there ? row : 0)) * P.q_token + h * P.q_head, first, last, again, sl2, 0, 1, oacc, &m_run, &l_run);
+            rows_again<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + (stored ? t : t_base) * P.q_token + of_head * P.q_head, first, last, again, sl2, 0, 1, oacc,
+                            &m_run, &l_run);
             if (again)
                 store_fours(oacc, l_run == 0.0f ? 0.0f : 1.0f / l_run, orow);
         }

@@ -582,7 +582,9 @@ template <int SRC>
 __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, int first, int last, bool wanted, float sl2, int nth, int step,
                                            f32x16_t (&acc)[DH / 32], float *max_score, float *sum)
 {
-    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                                   // (nothing made of it is kept over the walk before)
+    const int lq = lane & 31, lh = lane >> 5;
     const int from = least_of(wanted ? first : 0x7FFFFFFF), to = most_of(wanted ? last : -1);
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
