@@ -41,3 +41,13 @@ def test_walks_that_32_bits_do_not_count_are_not_split():
             assert paged(n, max_q, tokens, page=1024) > 0
             if (2 ** 31 - 1) // n * tile < 2 ** 31 - 2 ** 14:
                 assert paged(n, max_q, tokens + 1024 * tile, page=1024) == 0
+
+
+@pytest.mark.parametrize("which", ["in_dtype", "out_dtype"])
+def test_e4m3_is_for_cache_pages_only(which):
+    """The projections refuse it."""
+    desc = cf.layer_desc(2, 0, 16, 256, 256, **{which: "e4m3"})
+    for call in (lambda: cf.ag_step(desc, 0, 0x10000, 0x20000, 0x30000), lambda: cf.rs_step(desc, 0, 0x10000, 0x20000, 0x30000, 0x40000)):
+        with pytest.raises(cf.CommFuseError) as refused:
+            call()
+        assert refused.value.status == cf.CF_ERR_UNSUPPORTED

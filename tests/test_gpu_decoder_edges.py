@@ -289,3 +289,25 @@ def test_time_of_a_gradient_with_a_value_that_is_not_finite(h, kv, lens, tokens,
     normal = _time(call)
     dict(dout=dout, v=v, q=q)[what][tokens, 0, 7] = math.inf
     assert _time(call) <= SLOWER * normal
+
+
+@pytest.mark.parametrize("chunk", [None, "4x1", "4x3"])
+@pytest.mark.parametrize("n", [8, 9, 33, 63, 64, 65])
+@pytest.mark.parametrize("h, kv", [(8, 1), (4, 4)])
+def test_numbers_of_packed_sequences(n, h, kv, chunk, monkeypatch):
+    """Up to 64 sequences walks are split by the starts that a wave holds, from nine on by a search over its lanes: uneven ones, empty ones at both
+    ends and between, one long enough to be split, rows before the first and behind the last."""
+    if chunk:
+        monkeypatch.setenv("COMMFUSE_CAUSAL", chunk)
+    lens = [(i * 13) % 40 if i % 5 else 0 for i in range(n)]
+    lens[n // 2] = 1500
+    lens[-2:] = [7, 0]
+    x, dout, at = grad.problem(700 + n, lens, h, kv, 37, 96)
+    for t in (x, dout):
+        t[:37], t[37 + sum(lens):] = math.nan, math.inf
+    q, k, v = x[:, :h], x[:, h:h + kv], x[:, h + kv:]
+    out, lse = prompt.run(x, h, kv, at, SCALE)
+    prompt.check(out, lse, prompt.definition(q, k, v, at, SCALE))
+    for r in (slice(0, 37), slice(37 + sum(lens), None)):
+        assert bool((out[r] == -7).all()) and bool((lse[:, r] == -7).all())
+    grad.check(grad.forward_and_gradient(x, dout, h, kv, at, SCALE), grad.gradient(q, k, v, dout, at, SCALE))

@@ -55,3 +55,12 @@ def test_ramp_over_the_index_may_end_behind_the_last_pair(rot, base, trained, lo
     """Where even the slowest pair makes more than `low` turns over the trained length, the ramp goes on beyond the last pair (up to index
     rot_dim - 1): pairs are between trained and stretched as far as their own turns say."""
     check(rot, base, "index", 4.0, trained, low, high)
+
+
+@pytest.mark.parametrize("rot", [2, 24, 64, 96, 128, 256])
+@pytest.mark.parametrize("base, scaling, factor, trained, low, high", [
+    (1e4, "linear", 1.0, 0, 1.0, 4.0), (1e4, "linear", 2.5, 0, 1.0, 4.0), (1.5, "linear", 1.0, 0, 1.0, 4.0), (1e18, "linear", 1e9, 0, 1.0, 4.0),
+    (5e5, "wavelength", 8.0, 8192, 1.0, 4.0), (1e4, "wavelength", 2.0, 4096, 0.25, 16.0), (1e6, "index", 4.0, 32768, 1.0, 32.0),
+    (1e4, "index", 40.0, 4096, 1.0, 32.0), (2.0, "index", 2.0, 7, 1.0, 1.1)])
+def test_frequencies_in_sixty_digits(rot, base, scaling, factor, trained, low, high):
+    check(rot, base, scaling, factor, trained, low, high)
