@@ -527,8 +527,8 @@ cf_status commfuse_rope(const cf_rope *rope, const cf_rope_rows *rows, const voi
  *   CF_E4M3: one exponent per token and head, and one byte per value (four significant bits): with e the smallest integer
  *     for which the largest finite magnitude of the row is at most 448 * 2^e (e in [-126, 120]; 0 for a row of zeros), a value
  *     is stored as x * 2^-e rounded to nearest even (to 240 at the most where e = 120: no finite value becomes infinite), and
- *     stands for that times 2^e -- which bf16 holds exactly.  Powers of two: scaling itself rounds nothing.  NaN and infinities
- *     become NaN.  k_exp / v_exp hold e + 127. */
+ *     stands for that times 2^e -- which bf16 holds exactly (for e < -124, of rotated rows, but for what is below its smallest step,
+ *     2^-133).  Powers of two: scaling itself rounds nothing.  NaN and infinities become NaN.  k_exp / v_exp hold e + 127. */
 typedef struct {
     int32_t dtype;                       /* CF_BF16 or CF_E4M3                                */
     int32_t page_size;                   /* power of two, 16 .. 1024                          */
@@ -556,8 +556,8 @@ typedef struct {                         /* rows of new tokens                  
 cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const cf_rope *rope,
                                const void *Q, const void *K, const void *V, const int32_t *positions, const int64_t *slots,
                                void *q_out, void *hip_stream);
-/* Reads tokens back as bf16 rows (k_token .. v_head of `rows`; exact): K and V of slot slots[i] into row i.  Rows whose slot is
- * out of range are left as they were.  A slot may be read into several rows. */
+/* Reads tokens back as bf16 rows (k_token .. v_head of `rows`), the values that the cache stands for: K and V of slot slots[i] into row
+ * i.  Rows whose slot is out of range are left as they were.  A slot may be read into several rows. */
 cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const int64_t *slots,
                               void *K, void *V, void *hip_stream);
 

@@ -311,3 +311,33 @@ def test_numbers_of_packed_sequences(n, h, kv, chunk, monkeypatch):
     for r in (slice(0, 37), slice(37 + sum(lens), None)):
         assert bool((out[r] == -7).all()) and bool((lse[:, r] == -7).all())
     grad.check(grad.forward_and_gradient(x, dout, h, kv, at, SCALE), grad.gradient(q, k, v, dout, at, SCALE))
+
+
+@pytest.mark.parametrize("power", [-110, -117, -118, -119, -121, -123, -126])
+def test_rows_of_the_smallest_values_in_e4m3(power):
+    """What a code and its exponent stand for, rounded to bf16: exact from e = -124 on, below that to a multiple of 2^-133, to nearest even.  Rotated
+    rows: their values have more bits than bf16's subnormal numbers."""
+    T, kv = 40, 2
+    g = torch.Generator(device=DEV)
+    g.manual_seed(800 - power)
+    k, v = ((torch.randn(T, kv, D, generator=g, device=DEV).double() * 2.0 ** power).to(torch.bfloat16) for _ in range(2))
+    pools = [torch.zeros(3, kv, 16, D, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    exps = [torch.zeros(3, kv, 16, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    desc, cache = cf.cache_desc("e4m3", 3, 16, kv), cf.make_cache(*pools, *exps)
+    at, slots = torch.arange(T, dtype=torch.int32, device=DEV) * 1000 + 7, torch.arange(T, dtype=torch.int64, device=DEV)
+    cf.cache_write(desc, cache, cf.cache_rows(T), cf.rope_make(D), None, k, v, at, slots, None)
+    back = [torch.empty_like(k) for _ in range(2)]
+    cf.cache_read(desc, cache, cf.cache_rows(T), slots, *back)
+    torch.cuda.synchronize()
+    exact = 0
+    for pool, exp, got in zip(pools, exps, back):
+        codes = pool.view(torch.float8_e4m3fn).double().permute(0, 2, 1, 3).reshape(48, kv, D)[:T].cpu()
+        e = exp.permute(0, 2, 1).reshape(48, kv)[:T, :, None].double().cpu() - 127
+        stands_for = codes * torch.exp2(e)                                    # in 64 bits: exact
+        step = torch.clamp(torch.floor(torch.log2(stands_for.abs().clamp(min=2.0 ** -140))) - 7, min=-133.0)
+        want = torch.exp2(step) * torch.round(stands_for * torch.exp2(-step))
+        assert torch.equal(got.double().cpu(), want)
+        assert bool((want == stands_for)[(e >= -124).expand_as(want)].all())
+        assert int(e.min()) >= -126
+        exact += int((want == stands_for).all())
+    assert exact >= (1 if power <= -118 else 2)                               # V is not rotated: exact at any size
