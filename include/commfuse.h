@@ -572,7 +572,8 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
  * influence on its result, infinities and NaN included.  With a registered workspace (commfuse_set_workspace; size that lets
  * every choice be used, here and for the gradient: commfuse_attn_prompt_workspace_bytes) the keys of long sequences are split
  * over several workgroups where rows are too few to fill the chip (up to 64 sequences); without one, or with a smaller one, they are
- * not, or less.  Calls that overlap in time must not share a workspace.  The bits of a result depend on the split.
+ * not, or less.  Calls that overlap in time must not share a workspace.  The bits of a result depend on the split, and on whether lse is
+ * asked for: with it the output is divided by the sum of the probabilities before rounding, without it by that of the rounded ones.
  * head_dim must be 128, token strides at most 2^23 elements (CF_ERR_UNSUPPORTED otherwise). */
 typedef struct {
     int64_t tokens;

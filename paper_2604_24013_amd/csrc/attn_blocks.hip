@@ -278,7 +278,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     float m_run = -3.402823466e38f;      // (finite: against -inf a tile whose scores are all -inf would give NaN)
     // Row sums of this lane's keys, and of a pair of tiles: of the rounded probabilities, which multiply V, so that the roundings of a row's
     // dominant key cancel; LSE: of the probabilities before rounding (rounded, the log-sum-exp of a row with one dominant key would be
-    // off by up to 2^-9).  A sum over the rounded ones takes half the instructions (a dot product of two): 7 % of a full chip's time.
+    // off by up to 2^-9), and the output is divided by that.  Both sums would bring the output of a call with lse from 0.00212 to 0.00207 from 64
+    // bits (scores of sigma 4: 0.00208 to 0.00183; rounded once, 0.0016), and cost 3 % of a full chip's time (504 to 520 us), 7 % of small launches'
+    // (32.9 to 35.1 us, 74.2 to 79.5), as much as the sum over the rounded ones alone saves: a dot product of two, half the instructions.
     float l_run = 0.0f, l_pair = 0.0f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
