@@ -341,3 +341,34 @@ def test_rows_of_the_smallest_values_in_e4m3(power):
         assert int(e.min()) >= -126
         exact += int((want == stands_for).all())
     assert exact >= (1 if power <= -118 else 2)                               # V is not rotated: exact at any size
+
+
+@pytest.mark.parametrize("what", ["v", "dout"])
+@pytest.mark.parametrize("chunk", [None, "4x1", "4x100000"])
+@pytest.mark.parametrize("h, kv, lens, t", [(4, 2, [150, 81, 160], 180), (8, 1, [5, 30, 9, 60], 20), (1, 1, [300], 130)])
+def test_finite_values_whose_products_overflow(h, kv, lens, t, what, chunk, monkeypatch):
+    """One token's V (of 2^110) or dout (of 2^120): dP and delta overflow for what sees it, nothing else changes."""
+    if chunk:
+        monkeypatch.setenv("COMMFUSE_CAUSAL", chunk)
+    x, dout, at = grad.problem(621, lens, h, kv)
+    if what == "v":
+        dout *= 2.0 ** 30
+        part, factor = x[t, h + kv], 2.0 ** 110
+    else:
+        x[:, h + kv:] *= 2.0 ** 12
+        part, factor = dout[t, 0], 2.0 ** 120
+    clean_x, clean_g = x.clone(), dout.clone()
+    (clean_x[t, h + kv] if what == "v" else clean_g[t, 0]).zero_()
+    part *= factor
+    ref = grad.gradient(clean_x[:, :h], clean_x[:, h:h + kv], clean_x[:, h + kv:], clean_g, at, SCALE)
+    got = grad.forward_and_gradient(x, dout, h, kv, at, SCALE)
+    ends = [sum(lens[:i + 1]) for i in range(len(lens))]
+    end = next(e for e in ends if e > t)
+    for n, rows in _reached(what, t, end - lens[ends.index(end)], end).items():
+        heads = 0 if n != "dq" or what == "dout" else slice(0, h // kv)
+        if n != "dv":
+            assert not bool(torch.isfinite(got[n][rows, heads].float()).any()), n
+        got[n][rows, heads] = -7
+        for r in ref:
+            r[n][rows, heads] = math.nan
+    grad.check(got, ref)
