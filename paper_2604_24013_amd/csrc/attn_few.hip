@@ -455,10 +455,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     Kv = Kk;
     Kv.base = vb;
     Kv.exps = ve;
-    bool absent = false;
+    bool unseen = false;                                             // values that no row sees may have been in the products
     for (int page = lane; page < (int)(((unsigned)hi + (1u << shift) - 1) >> shift); page += 64)
-        absent = absent || (unsigned)table[page] >= (unsigned)n_pages;
-    if (__builtin_amdgcn_ballot_w64(absent) == 0 && !any_large(Kv, max(min(n - m + 1, hi - 1), 0), hi))
+        unseen = unseen || (unsigned)table[page] >= (unsigned)n_pages;
+    if (SRC == PAGED_BF16 && hi % FEW_KEYS != 0) {                   // (the last key's V: NaN would be so in all rows that see it, infinite becomes NaN)
+        int e;
+        const unsigned char *row = Kv.row(hi - 1, &e);
+        const unsigned w = row != nullptr ? reinterpret_cast<const unsigned *>(row)[lane] : 0;
+        unseen = unseen || (w & 0x7FFFu) == 0x7F80 || (w >> 16 & 0x7FFFu) == 0x7F80;
+    }
+    if (__builtin_amdgcn_ballot_w64(unseen) == 0 && !any_large(Kv, max(n - m + 1, 0), hi))
         return;
     const int lq = lane & 31, lh = lane >> 5, r = lq < rows ? lq : 0, token = r / G;
     f32x16_t acc[DH / 32];

@@ -443,9 +443,10 @@ struct Keys {
 
 // Results that are not finite.  The mask is a select on the scores, so that a hidden key has a probability of 0 -- but 0 times an infinite or
 // NaN value of V is NaN.  Only the tiles on a wave's border hold keys that some of its rows see and others do not.  So a wave that finds a
-// result that is not finite looks at the V rows of those tiles (64 keys a time, a lane each); if one of them is not finite, the wave walks over all keys once
-// more, from memory, with such values taken out of the product and counted for the rows that see them.  Otherwise what is visible is not
-// finite, and the result stays.
+// result that is not finite looks at the V rows of those tiles (64 keys at a time, a lane each).  If one of them is not finite, the wave walks over
+// all keys once more, from memory, with such values taken out of the product and counted for the rows that see them; otherwise what is
+// visible is not finite, and the result stays.  Bound by the latency of its loads: 3 us for 32 keys, about three times as long as an unsplit
+// walk of the kernels takes.  6144 tokens, 4 heads of one key head: 70 us, with one infinite feature of V in an early token too, in a late one 572.
 // Is one of the rows [from, to) large?
 template <int SRC>
 __device__ __forceinline__ bool any_large(const Keys<SRC> &K, int from, int to)
@@ -602,19 +603,12 @@ __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &
             kr = K.base;
             vr = V.base;
         }
-        bf16x8_t v[2][DH / 32];
+        u32x2_t four[16];                                            // of the keys that a lane's sixteen slots stand for
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                u32x2_t four[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int at = 16 * c + 8 * (i >> 1) + 2 * (i & 1) + x;
-                    four[x] = V.four(of_slot(vr, at), lq, SRC == PAGED_E4M3 ? of_slot(ev, at) : 0);
-                }
-                put_pair(v[c], i, four[0], four[1]);
-            }
+        for (int x = 0; x < 16; ++x) {
+            const int at = 8 * (x >> 2) + (x & 3);
+            four[x] = V.four(of_slot(vr, at), lq, SRC == PAGED_E4M3 ? of_slot(ev, at) : 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
         f32x16_t s = {};
         asm volatile("" : "+v"(q));                                  // (the row is read in every unit: 32 registers)
@@ -638,7 +632,7 @@ __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &
         bf16x8_t p[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            p[i >> 3][i & 7] = (__bf16)exp2f(s[i] - m);
+            p[i >> 3][i & 7] = (__bf16)__builtin_amdgcn_exp2f(s[i] - m);
             l += (float)p[i >> 3][i & 7];
         }
 #pragma unroll
@@ -646,8 +640,14 @@ __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 acc[d][i] *= alpha;
-        add_seen(acc, v[0], p[0], seen);
-        add_seen(acc, v[1], p[1], seen >> 8);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            bf16x8_t v[DH / 32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                put_pair(v, i, four[8 * c + 2 * i], four[8 * c + 2 * i + 1]);
+            add_seen(acc, v, p[c], seen >> 8 * c);
+        }
         if ((key0 & 0xE0) == 0) {                                    // now and then: does anything that follows matter?
             bool done = true;
 #pragma unroll
