@@ -13,6 +13,10 @@
 // As in the forward kernel a lane owns one row (or key) and 16 of every 32 keys (rows) of a product's result, which is, rounded to
 // bf16, the "B" operand of the next product as it stands: nothing moves between lanes.  Tiles lie in LDS once and are read both by rows
 // and transposed: 16-byte chunks XOR-ed with a permutation of (row & 15), which the transposing read can follow lane by lane.
+// Precision: P and dS are rounded to bf16 for their products, and delta is made of the bf16 `out`.  From 64 bits dQ is 0.0026 off (2048 + 1365 + 683 tokens, 4
+// heads; up to 0.0033 in packs of ten tokens a sequence, where the rounding of `out` weighs most), dK 0.0025, dV 0.0023; rounding exact
+// results once gives 0.0017, with dS alone rounded before its products 0.0024.  dS as the sum of two bf16 numbers, a product more each for dQ and dK,
+// gives 0.0019 and 0.0018 and takes 97 us instead of 90 with the forward call (4096 tokens, 8 heads of one key head 239 instead of 207): not worth it.
 // Rows behind a walk are read as zero, and masked.  Results that are not finite are computed once more where what the mask
 // hides can have been the reason, so that it has no influence.
 #include "attn_tiles.h"
