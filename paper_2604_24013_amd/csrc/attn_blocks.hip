@@ -16,11 +16,11 @@
 // been the reason (`rows_again`).
 // Packed prompts: a workgroup takes consecutive rows whatever sequences they belong to; keys of the walk that belong to another
 // sequence are masked like any others.
-// Bound: the matrix pipe where rows fill the chip (8192 tokens, 32 heads of 4 key heads: 522 us with lse, 488 without, 1053 and 1128 TFLOP/s, where
-// a library product of 8192 reaches 1232); else that a workgroup takes 10 us beside its tiles of 0.9 to 1.3 us each: 1 until
+// Bound: the matrix pipe where rows fill the chip (8192 tokens, 32 heads of 4 key heads: 489 to 505 us with lse, 478 to 493 without, 1090 to 1120 and
+// 1120 to 1150 TFLOP/s, where a library product of 8192 reaches 1232); else that a workgroup takes 10 us beside its tiles of 0.9 to 1.3 us each: 1 until
 // kernel arguments and starts are there, 1.3 for the search of its piece, 1.5 to 2.5 for Q and the first tiles, 1.7 to park, and 4.5 for the
-// last to arrive to merge.  4096 tokens, 4 heads: 33 us (519 TFLOP/s); 5 packed prompts of 8192 tokens, 8 heads of one key head: 74 us
-// (708); 2381 new tokens over 13528 in e4m3, 8 heads of one key head: 78 us (654).
+// last to arrive to merge.  4096 tokens, 4 heads: 33.6 us (511 TFLOP/s); 5 packed prompts of 8192 tokens, 8 heads of one key head: 73.4 us
+// (712); 2381 new tokens over 13528 in e4m3, 8 heads of one key head: 76.6 us (668).
 #include "attn_tiles.h"
 
 namespace cf {

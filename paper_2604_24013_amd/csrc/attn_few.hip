@@ -15,7 +15,7 @@
 // every address is inside the pool.  The waves' (m, l, O) are merged in LDS, those of workgroups that share a sequence's keys in
 // the workspace by the one that finishes last.
 // Measured: 62 sequences of 33 to 4096 tokens, 4 heads of their own, bf16: 50 us, 4.4 TB/s of cache (a sum over memory reaches 4.0, a copy 4.7);
-// eight contexts of 12 to 65 thousand, 8 heads of one key head, e4m3: 27 us, 3.7 TB/s; one of 1003: 9 us, of which 6 are the launch, the
+// eight contexts of 12 to 65 thousand, 8 heads of one key head, e4m3: 26.8 us, 3.7 TB/s; one of 1003: 8.9 us, of which 6 are the launch, the
 // search and the merge.
 #include "attn_tiles.h"
 

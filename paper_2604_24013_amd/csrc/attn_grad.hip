@@ -8,8 +8,8 @@
 // Bound: the matrix pipe, and beside it LDS: every product's "A" fragment, 1 KiB, comes from LDS for one MFMA of 32 cycles, so that four waves
 // ask for all of its 128 bytes a cycle.  dK and dV hold 128 sums, 64 scores and 64 registers of K and V a lane: one wave a SIMD, which
 // has to fill the pipe alone, so both kernels run as pipelines of 32-row units with one MFMA a segment.
-// Measured (us; dQ, dK and dV, sums): 4096 tokens, 8 heads of one key head 70, 91, 12 -- 51 and 69 GFLOP at 730 and 760 TFLOP/s;
-// 2048 + 1365 + 683 tokens, 4 heads of their own 26, 35, 12, of which 11 a launch are start, search, first loads and parking.
+// Measured (us, traced; dQ, dK and dV, sums): 4096 tokens, 8 heads of one key head 69 to 73, 92 to 96, 12 to 14 -- 51 and 69 GFLOP at 730 and 750
+// TFLOP/s; 2048 + 1365 + 683 tokens, 4 heads of their own 26, 36, 11, of which 11 a launch are start, search, first loads and parking.
 // As in the forward kernel a lane owns one row (or key) and 16 of every 32 keys (rows) of a product's result, which is, rounded to
 // bf16, the "B" operand of the next product as it stands: nothing moves between lanes.  Tiles lie in LDS once and are read both by rows
 // and transposed: 16-byte chunks XOR-ed with a permutation of (row & 15), which the transposing read can follow lane by lane.
