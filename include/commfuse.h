@@ -520,6 +520,63 @@ typedef struct {
 cf_status commfuse_rope(const cf_rope *rope, const cf_rope_rows *rows, const void *x, const int32_t *positions, void *out,
                         int gradient, void *hip_stream);
 
+/* Rotary positions on several axes (time, height and width of images and video): every pair of a head turns by its axis' position.  With
+ * n_axes axes of sections[a] pairs each, rot_dim / 2 together,
+ *     CF_AXES_SECTIONS     the first sections[0] pairs are axis 0's, the next sections[1] axis 1's, and so on
+ *     CF_AXES_INTERLEAVED  pair j is axis (j mod n_axes)'s where j / n_axes (rounded down) < sections[j mod n_axes], else axis 0's
+ *                          (sections[a] at most rot_dim / 2 / n_axes, rounded down, for a > 0)
+ *     CF_SPECTRUM_SHARED   pair j has the frequency that it has on one axis
+ *     CF_SPECTRUM_OWN      the i-th pair of axis a has that of pair i of a head with rot_dim = 2 sections[a]
+ * All else as commfuse_rope_make has it.  Positions are [n_axes] rows of int32 [tokens], `position_axis` elements apart (0: one row, the
+ * same position on every axis, as for text). */
+typedef enum { CF_AXES_SECTIONS = 0, CF_AXES_INTERLEAVED = 1 } cf_axes_order;
+typedef enum { CF_SPECTRUM_SHARED = 0, CF_SPECTRUM_OWN = 1 } cf_spectrum;
+typedef struct {
+    int32_t n_axes;         /* 1 .. 4                                                         */
+    int32_t order;          /* cf_axes_order                                                  */
+    int32_t spectrum;       /* cf_spectrum                                                    */
+    int32_t sections[4];    /* pairs of each axis, at least 1                                 */
+} cf_axes_desc;
+typedef struct {            /* HOST struct that commfuse_rope_axes_make fills in; the caller keeps it */
+    cf_rope rope;
+    int32_t n_axes;
+    uint8_t axis[128];      /* of each pair                                                   */
+} cf_rope_axes;
+/* Host-only arithmetic. */
+cf_status commfuse_rope_axes_make(const cf_rope_desc *desc, const cf_axes_desc *axes, cf_rope_axes *rope);
+
+/* Norms of queries and keys, head by head, and their rotation, in one pass: for every head x of Q (K) with weights w = wq (wk)
+ *     r = (mean of x^2 + eps)^(-1/2),   y = rotation of x * r * (offset + w)
+ * norm NULL: the rotation alone.  rope NULL: no rotation (positions unused).  Not both.  wq, wk [head_dim], shared by the heads; NULL:
+ * a factor of 1.  heads or kv_heads may be 0 (its pointers are unused).  q_out may be Q itself, and k_out K itself, with the same
+ * strides (in place); they may not overlap otherwise.  All arithmetic in fp32, results rounded once. */
+typedef struct {
+    int32_t weight_dtype;   /* CF_BF16 or CF_F32, of wq and wk                                */
+    float eps;              /* >= 1e-30                                                       */
+    float offset;           /* 0, or 1 for weights that are kept as what they exceed 1 by     */
+    int32_t reserved;       /* 0                                                              */
+} cf_head_norm;
+typedef struct {
+    int64_t tokens;
+    int32_t heads, kv_heads;             /* of Q, of K                                        */
+    int32_t head_dim;                    /* multiple of 8, at most 256                        */
+    int32_t dtype;                       /* CF_BF16 or CF_F32, of Q, K, q_out, k_out          */
+    int64_t q_token, q_head, k_token, k_head, oq_token, oq_head, ok_token, ok_head;   /* oq, ok: of q_out, k_out */
+} cf_head_rows;
+cf_status commfuse_norm_rope(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *Q, const void *K,
+                             const void *wq, const void *wk, const int32_t *positions, int64_t position_axis, void *q_out, void *k_out,
+                             void *hip_stream);
+/* Its gradient: with g = dq_out (dk_out) rotated back, n = x * r and h = g * (offset + w),
+ *     dQ (dK) = r * (h - n * mean of h * n),   dwq (dwk) = sum over tokens and heads of g * n
+ * Q and K as the forward call read them (norm NULL: unused).  dq_out, dk_out with the strides of q_out, k_out; dQ, dK with those of Q, K,
+ * and possibly dq_out, dk_out or Q, K themselves with the same strides.  dwq, dwk fp32 [head_dim], written, not added to; NULL: not
+ * wanted.  scratch: commfuse_norm_rope_scratch_bytes(rows) of device memory, 16-byte aligned, for dwq and dwk (else NULL).  Sums
+ * in fp32, no atomics: the same call gives the same bits. */
+size_t commfuse_norm_rope_scratch_bytes(const cf_head_rows *rows);
+cf_status commfuse_norm_rope_grad(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *Q, const void *K,
+                                  const void *wq, const void *wk, const int32_t *positions, int64_t position_axis, const void *dq_out,
+                                  const void *dk_out, void *dQ, void *dK, float *dwq, float *dwk, void *scratch, void *hip_stream);
+
 /* A paged cache: K and V in pages of `page_size` tokens, [n_pages][kv_heads][page_size][head_dim] with the strides below
  * (of pages, heads and tokens, in elements; 0, 0, 0 = packed in that order).  Slot s stands for token s % page_size of page
  * s / page_size.
@@ -556,10 +613,51 @@ typedef struct {                         /* rows of new tokens                  
 cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const cf_rope *rope,
                                const void *Q, const void *K, const void *V, const int32_t *positions, const int64_t *slots,
                                void *q_out, void *hip_stream);
+/* The same with normed heads and positions on several axes, in one launch: K on its way into the cache and Q on its way into q_out as
+ * commfuse_norm_rope has them (its norm, rope, wq, wk, positions and position_axis), V as it is.  rot_dim a multiple of 16. */
+cf_status commfuse_cache_write_norm(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const cf_rope_axes *rope,
+                                    const cf_head_norm *norm, const void *Q, const void *K, const void *V, const void *wq, const void *wk,
+                                    const int32_t *positions, int64_t position_axis, const int64_t *slots, void *q_out, void *hip_stream);
+
 /* Reads tokens back as bf16 rows (k_token .. v_head of `rows`), the values that the cache stands for: K and V of slot slots[i] into row
  * i.  Rows whose slot is out of range are left as they were.  A slot may be read into several rows. */
 cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const int64_t *slots,
                               void *K, void *V, void *hip_stream);
+
+/* A serving step's tables, built from the lengths of its requests.  Place s of the batch (an idle one brings no token) holds held[s] tokens in
+ * the cache and brings new_tokens[s] more; its row of the page table names its pages, in order.
+ *     back_from, back_to  entries [back_from[s], back_to[s]) of row s that name a page are put onto the stack of free pages first, in the
+ *                 order of the batch (NULL, NULL: none): all of a finished request's, or those that have left a window.  The row itself
+ *                 stays as it is.
+ *     q_start     [n_seqs + 1]: q_start[0] = 0, q_start[s+1] = min(max_tokens, sum of new_tokens[0 .. s]); m_s = q_start[s+1] - q_start[s]
+ *     kv_len      [n_seqs]: held[s] + m_s
+ *     page_table  [n_seqs][max_pages]: entries ceil(held[s] / page_size) .. ceil(kv_len[s] / page_size) - 1 of row s that it has are written:
+ *                 the i-th of all of them (in the order of the batch) is the i-th page from the top of the stack, or -1 where that is
+ *                 empty.  The others stay as they are.
+ *     free_left   [1]: pages that are left; below 0: so many were missing.  The stack is free_pages[0 .. count), its top the last.
+ *     positions   int32 [max_tokens]: held[s] + i of token q_start[s] + i
+ *     slots       int64 [max_tokens]: where that position's page, by the table, has it; -1 where the row has no such entry or that is no page
+ *                 Behind the last token positions are 0 and slots -1 (padding, as commfuse_cache_write takes it).
+ * These are what commfuse_cache_write, commfuse_cache_write_norm and the paged attention calls take.  free_left may be free_count itself, for
+ * the next step.  Values below 0 of held, new_tokens, back_from and free_count count as 0, a free_count or a pushed page beyond n_pages is
+ * dropped, and lengths end at 2^31 - 1.  A page that is on the stack twice is handed out twice.  n_seqs at most 4096
+ * (CF_ERR_UNSUPPORTED otherwise). */
+typedef struct {
+    int32_t n_seqs;
+    int32_t page_size;                   /* power of two, 16 .. 1024                          */
+    int32_t max_pages;                   /* entries of a row of the page table                */
+    int32_t reserved;                    /* 0                                                 */
+    int64_t n_pages;                     /* of the cache; entries of free_pages               */
+    int64_t max_tokens;                  /* entries of slots and positions                    */
+} cf_tables_desc;
+typedef struct {                         /* HOST struct of DEVICE pointers                    */
+    const int32_t *held, *new_tokens;    /* [n_seqs]                                          */
+    const int32_t *back_from, *back_to;  /* [n_seqs]; may be NULL                             */
+    const int32_t *free_count;           /* [1]                                               */
+    int32_t *page_table, *free_pages, *free_left, *q_start, *kv_len, *positions;
+    int64_t *slots;
+} cf_tables;
+cf_status commfuse_step_tables(const cf_tables_desc *desc, const cf_tables *tables, void *hip_stream);
 
 /* Causal attention over packed prompts, query heads sharing key heads: with g = heads / kv_heads, query head h reads key head
  * h / g, and token t of a sequence sees the tokens of its sequence up to itself:

@@ -27,6 +27,10 @@ KINDS = {"rs": CF_KIND_RS, "ag": CF_KIND_AG, "dp": CF_KIND_DP, "rs_pair": CF_KIN
 DTYPES = {"bf16": CF_BF16, "f32": CF_F32, "e4m3": CF_E4M3}
 CF_ROPE_HALF, CF_ROPE_INTERLEAVED = 0, 1
 CF_ROPE_LINEAR, CF_ROPE_WAVELENGTH, CF_ROPE_INDEX = 0, 1, 2
+CF_AXES_SECTIONS, CF_AXES_INTERLEAVED = 0, 1
+CF_SPECTRUM_SHARED, CF_SPECTRUM_OWN = 0, 1
+AXES_ORDERS = {"sections": CF_AXES_SECTIONS, "interleaved": CF_AXES_INTERLEAVED}
+SPECTRA = {"shared": CF_SPECTRUM_SHARED, "own": CF_SPECTRUM_OWN}
 ROPE_LAYOUTS = {"half": CF_ROPE_HALF, "interleaved": CF_ROPE_INTERLEAVED}
 ROPE_SCALINGS = {"linear": CF_ROPE_LINEAR, "wavelength": CF_ROPE_WAVELENGTH, "index": CF_ROPE_INDEX}
 
@@ -35,6 +39,7 @@ EXPORTS = [
     "commfuse_run_attn_schedule", "commfuse_rs_step", "commfuse_rs_step_noalloc", "commfuse_ag_step", "commfuse_dp_reduce_step",
     "commfuse_run_schedule", "commfuse_last_error", "commfuse_workspace_bytes", "commfuse_set_workspace",
     "commfuse_device_status", "commfuse_rope_make", "commfuse_rope", "commfuse_cache_write", "commfuse_cache_read",
+    "commfuse_rope_axes_make", "commfuse_norm_rope", "commfuse_norm_rope_scratch_bytes", "commfuse_norm_rope_grad", "commfuse_cache_write_norm", "commfuse_step_tables",
     "commfuse_attn_prompt", "commfuse_attn_prompt_workspace_bytes", "commfuse_attn_prompt_grad", "commfuse_attn_paged", "commfuse_attn_paged_workspace_bytes",
     "commfuse_destroy_cache", "commfuse_version",
 ]
@@ -93,6 +98,32 @@ class RopeDesc(ctypes.Structure):
 class Rope(ctypes.Structure):
     _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
                 ("turn", ctypes.c_uint64 * 128)]
+
+
+class AxesDesc(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("order", ctypes.c_int32), ("spectrum", ctypes.c_int32), ("sections", ctypes.c_int32 * 4)]
+
+
+class RopeAxes(ctypes.Structure):
+    _fields_ = [("rope", Rope), ("n_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 128)]
+
+
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("offset", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class HeadRows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype")] + [
+        (n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "oq_token", "oq_head", "ok_token", "ok_head")]
+
+
+class TablesDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "page_size", "max_pages", "reserved")] + [("n_pages", ctypes.c_int64), ("max_tokens", ctypes.c_int64)]
+
+
+class Tables(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("held", "new_tokens", "back_from", "back_to", "free_count", "page_table", "free_pages", "free_left",
+                                               "q_start", "kv_len", "positions", "slots")]
 
 
 class RopeRows(ctypes.Structure):
@@ -203,6 +234,19 @@ def load():
     lib.commfuse_attn_paged.restype = i32
     lib.commfuse_attn_paged_workspace_bytes.argtypes = [ref(CacheDesc), ref(PagedDesc)]
     lib.commfuse_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.commfuse_rope_axes_make.argtypes = [ref(RopeDesc), ref(AxesDesc), ref(RopeAxes)]
+    lib.commfuse_rope_axes_make.restype = i32
+    heads = [ref(RopeAxes), ref(HeadNorm), ref(HeadRows), vp, vp, vp, vp, vp, i64]
+    lib.commfuse_norm_rope.argtypes = heads + [vp] * 3
+    lib.commfuse_norm_rope.restype = i32
+    lib.commfuse_norm_rope_scratch_bytes.argtypes = [ref(HeadRows)]
+    lib.commfuse_norm_rope_scratch_bytes.restype = ctypes.c_size_t
+    lib.commfuse_norm_rope_grad.argtypes = heads + [vp] * 8
+    lib.commfuse_norm_rope_grad.restype = i32
+    lib.commfuse_cache_write_norm.argtypes = [ref(CacheDesc), ref(Cache), ref(CacheRows), ref(RopeAxes), ref(HeadNorm)] + [vp] * 6 + [i64] + [vp] * 3
+    lib.commfuse_cache_write_norm.restype = i32
+    lib.commfuse_step_tables.argtypes = [ref(TablesDesc), ref(Tables), vp]
+    lib.commfuse_step_tables.restype = i32
     lib.commfuse_destroy_cache.argtypes = []
     lib.commfuse_destroy_cache.restype = None
     lib.commfuse_version.argtypes = []
@@ -512,3 +556,62 @@ def attn_paged(cache_desc_: CacheDesc, cache: Cache, desc: PagedDesc, Q, q_start
 
 def attn_paged_workspace_bytes(cache_desc_: CacheDesc, desc: PagedDesc) -> int:
     return int(load().commfuse_attn_paged_workspace_bytes(cache_desc_, desc))
+
+
+def rope_axes_make(head_dim: int, rot_dim: int = 0, layout="half", base: float = 10000.0, scaling="linear", factor: float = 1.0,
+                   trained_len: int = 0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0, sections: Optional[Sequence] = None,
+                   order="sections", spectrum="shared") -> RopeAxes:
+    """``sections``: pairs of each axis (None: one axis)."""
+    d = RopeDesc(head_dim, rot_dim or head_dim, ROPE_LAYOUTS[layout] if isinstance(layout, str) else layout,
+                 ROPE_SCALINGS[scaling] if isinstance(scaling, str) else scaling, trained_len, base, factor, low, high, magnitude)
+    sections = [(rot_dim or head_dim) // 2] if sections is None else list(sections)
+    a = AxesDesc(len(sections), AXES_ORDERS[order] if isinstance(order, str) else order, SPECTRA[spectrum] if isinstance(spectrum, str) else spectrum)
+    for i, pairs in enumerate(sections[:4]):
+        a.sections[i] = pairs
+    r = RopeAxes()
+    _check(load().commfuse_rope_axes_make(ctypes.byref(d), ctypes.byref(a), ctypes.byref(r)))
+    return r
+
+
+def head_norm(eps: float, offset: float = 0.0, weight_dtype="bf16") -> HeadNorm:
+    return HeadNorm(DTYPES[weight_dtype] if isinstance(weight_dtype, str) else weight_dtype, eps, offset, 0)
+
+
+def head_rows(tokens: int, heads: int, kv_heads: int, head_dim: int = 128, dtype="bf16", q=(0, 0), k=(0, 0), oq=(0, 0), ok=(0, 0)) -> HeadRows:
+    return HeadRows(tokens, heads, kv_heads, head_dim, DTYPES[dtype] if isinstance(dtype, str) else dtype, *q, *k, *oq, *ok)
+
+
+def norm_rope(rope_: Optional[RopeAxes], norm: Optional[HeadNorm], rows: HeadRows, Q, K, wq, wk, positions, position_axis: int, q_out, k_out,
+              stream=None) -> None:
+    _check((_lib or load()).commfuse_norm_rope(rope_, norm, rows, _ptr(Q), _ptr(K), _ptr(wq), _ptr(wk), _ptr(positions), position_axis, _ptr(q_out),
+                                               _ptr(k_out), _stream(stream)))
+
+
+def norm_rope_scratch_bytes(rows: HeadRows) -> int:
+    return int(load().commfuse_norm_rope_scratch_bytes(rows))
+
+
+def norm_rope_grad(rope_: Optional[RopeAxes], norm: Optional[HeadNorm], rows: HeadRows, Q, K, wq, wk, positions, position_axis: int, dq_out, dk_out,
+                   dQ, dK, dwq=None, dwk=None, scratch=None, stream=None) -> None:
+    _check((_lib or load()).commfuse_norm_rope_grad(rope_, norm, rows, _ptr(Q), _ptr(K), _ptr(wq), _ptr(wk), _ptr(positions), position_axis,
+                                                    _ptr(dq_out), _ptr(dk_out), _ptr(dQ), _ptr(dK), _ptr(dwq), _ptr(dwk), _ptr(scratch),
+                                                    _stream(stream)))
+
+
+def cache_write_norm(desc: CacheDesc, cache: Cache, rows: CacheRows, rope_: Optional[RopeAxes], norm: Optional[HeadNorm], Q, K, V, wq, wk, positions,
+                     position_axis: int, slots, q_out, stream=None) -> None:
+    _check((_lib or load()).commfuse_cache_write_norm(desc, cache, rows, rope_, norm, _ptr(Q), _ptr(K), _ptr(V), _ptr(wq), _ptr(wk), _ptr(positions),
+                                                      position_axis, _ptr(slots), _ptr(q_out), _stream(stream)))
+
+
+def tables_desc(n_seqs: int, page_size: int, n_pages: int, max_pages: int, max_tokens: int) -> TablesDesc:
+    return TablesDesc(n_seqs, page_size, max_pages, 0, n_pages, max_tokens)
+
+
+def make_tables(held, new_tokens, page_table, free_pages, free_count, free_left, q_start, kv_len, positions, slots, back_from=None, back_to=None) -> Tables:
+    """The caller keeps the tensors alive."""
+    return Tables(*map(_ptr, (held, new_tokens, back_from, back_to, free_count, page_table, free_pages, free_left, q_start, kv_len, positions, slots)))
+
+
+def step_tables(desc: TablesDesc, tables: Tables, stream=None) -> None:
+    _check((_lib or load()).commfuse_step_tables(desc, tables, _stream(stream)))

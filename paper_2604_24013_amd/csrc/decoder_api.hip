@@ -142,6 +142,186 @@ void use_workspace(cf::CausalParams &p, hipStream_t s)
     p.max_counters = v.max_counters;
 }
 
+// The strides of the rows that go into the cache.  `nothing`: no token.
+cf_status resolve_cache_rows(const cf::CachePool &c, const cf_cache_rows *rows, bool q_given, cf::CacheRows *out, bool *nothing)
+{
+    if (rows == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "rows is NULL");
+    if (rows->heads < 0 || rows->reserved != 0)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "heads = %d, reserved = %d", rows->heads, rows->reserved);
+    if (cf_status st = check_tokens(rows->tokens, (int64_t)rows->heads + 2 * c.kv_heads))
+        return st;
+    cf::CacheRows r = {};
+    r.q_token = rows->q_token, r.q_head = rows->q_head, r.k_token = rows->k_token, r.k_head = rows->k_head;
+    r.v_token = rows->v_token, r.v_head = rows->v_head, r.o_token = rows->o_token, r.o_head = rows->o_head;
+    if (cf_status st = resolve_rows("K", &r.k_token, &r.k_head, rows->tokens, c.kv_heads, c.head_dim, 8))
+        return st;
+    if (cf_status st = resolve_rows("V", &r.v_token, &r.v_head, rows->tokens, c.kv_heads, c.head_dim, 8))
+        return st;
+    if (q_given && rows->heads > 0) {
+        if (cf_status st = resolve_rows("Q", &r.q_token, &r.q_head, rows->tokens, rows->heads, c.head_dim, 8))
+            return st;
+        if (cf_status st = resolve_rows("q_out", &r.o_token, &r.o_head, rows->tokens, rows->heads, c.head_dim, 8))
+            return st;
+    }
+    *nothing = rows->tokens == 0;
+    *out = r;
+    return CF_OK;
+}
+
+// ... and their pointers.
+cf_status take_cache_rows(const void *Q, const void *K, const void *V, bool rotated, const int32_t *positions, const int64_t *slots, void *q_out,
+                          const cf_cache_rows *rows, cf::CacheRows *r)
+{
+    const bool with_q = Q != nullptr && rows->heads > 0;
+    if (K == nullptr || V == nullptr || slots == nullptr || (rotated && positions == nullptr) || (with_q && q_out == nullptr))
+        return CF_FAIL(CF_ERR_NULL_PTR, "K, V, slots, with rope positions, with Q q_out must not be NULL");
+    if (!aligned(K, 16) || !aligned(V, 16) || (with_q && (!aligned(Q, 16) || !aligned(q_out, 16))) || !aligned(slots, 8) || (rotated && !aligned(positions, 4)))
+        return CF_FAIL(CF_ERR_MISALIGNED, "tensor pointers must be 16-byte aligned, slots 8-byte, positions 4-byte");
+    if (with_q && Q == q_out && (r->q_token != r->o_token || r->q_head != r->o_head))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "in place, Q and q_out must have the same strides");
+    r->q = with_q ? Q : nullptr;
+    r->k = K;
+    r->v = V;
+    r->q_out = q_out;
+    r->tokens = (unsigned)rows->tokens;
+    r->heads = (unsigned)rows->heads;
+    r->positions = positions;
+    r->slots = slots;
+    return CF_OK;
+}
+
+// Turns per position, in units of 2^-64, of pair j of a spectrum over `dim` features.
+uint64_t turns_of(const cf_rope_desc &d, int dim, int j)
+{
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    const long double f = powl((long double)d.base, -2.0L * j / dim);
+    double r = 0.0;
+    if (d.scaling == CF_ROPE_WAVELENGTH) {
+        r = ((double)(d.trained_len * f / two_pi) - d.low) / (d.high - d.low);
+    } else if (d.scaling == CF_ROPE_INDEX) {
+        const double per = dim / (2.0 * std::log(d.base));           // the ramp's ends
+        double first = std::floor(per * std::log(d.trained_len / ((double)two_pi * d.high)));
+        double last = std::ceil(per * std::log(d.trained_len / ((double)two_pi * d.low)));
+        first = first > 0.0 ? first : 0.0;
+        last = last < dim - 1 ? last : dim - 1;                      // (it may lie behind the last pair)
+        r = 1.0 - (j - first) / (last - first > 0.001 ? last - first : 0.001);
+    }
+    r = r < 0.0 ? 0.0 : r > 1.0 ? 1.0 : r;
+    const long double turns = f * (r + (1.0L - r) / d.factor) / two_pi;              // below 0.16
+    return (uint64_t)(turns * 18446744073709551616.0L + 0.5L);
+}
+
+// What the kernels take of a rotation by several axes (nullptr: none).
+cf_status resolve_axes(const cf_rope_axes *rope, int head_dim, int64_t tokens, int64_t position_axis, cf::AxesRotation *out)
+{
+    cf::AxesRotation r = {};
+    if (rope != nullptr) {
+        if (cf_status st = check_rope(&rope->rope))
+            return st;
+        if (rope->n_axes < 1 || rope->n_axes > 4)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "rope was not filled in by commfuse_rope_axes_make");
+        if (rope->rope.head_dim != head_dim)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "rope turns heads of %d features, these have %d", rope->rope.head_dim, head_dim);
+        if (position_axis < 0 || (position_axis > 0 && position_axis < tokens && rope->n_axes > 1))
+            return CF_FAIL(CF_ERR_INVALID_ARG, "position_axis = %lld: 0, or at least the %lld tokens", (long long)position_axis, (long long)tokens);
+        if (position_axis > INT64_MAX / 32)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "position_axis = %lld", (long long)position_axis);
+        memcpy(r.turn, rope->rope.turn, sizeof(r.turn));
+        for (int j = 0; j < rope->rope.rot_dim / 2; ++j) {
+            if (rope->axis[j] >= rope->n_axes)
+                return CF_FAIL(CF_ERR_INVALID_ARG, "rope was not filled in by commfuse_rope_axes_make");
+            r.axis_bits[j / 16] |= (uint32_t)rope->axis[j] << 2 * (j % 16);
+        }
+        r.n_axes = rope->n_axes;
+        r.rot_dim = rope->rope.rot_dim;
+        r.interleaved = rope->rope.layout == CF_ROPE_INTERLEAVED;
+        r.magnitude = rope->rope.magnitude;
+        r.position_axis = position_axis;
+    }
+    *out = r;
+    return CF_OK;
+}
+
+cf_status resolve_norm(const cf_head_norm *norm, const void *wq, const void *wk, cf::NormParams *out)
+{
+    cf::NormParams n = {};
+    if (norm != nullptr) {
+        if (norm->weight_dtype != CF_BF16 && norm->weight_dtype != CF_F32)
+            return CF_FAIL(CF_ERR_UNSUPPORTED, "weight dtype %d", norm->weight_dtype);
+        if (norm->reserved != 0)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "reserved = %d", norm->reserved);
+        if (!(norm->eps >= 1e-30f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset))
+            return CF_FAIL(CF_ERR_INVALID_ARG, "need a finite eps of at least 1e-30 and a finite offset");
+        const uintptr_t to = norm->weight_dtype == CF_BF16 ? 2 : 4;
+        if (!aligned(wq, to) || !aligned(wk, to))
+            return CF_FAIL(CF_ERR_MISALIGNED, "weights must be aligned to their type");
+        n.on = true;
+        n.wq = wq;
+        n.wk = wk;
+        n.weight_bf16 = norm->weight_dtype == CF_BF16;
+        n.eps = norm->eps;
+        n.offset = norm->offset;
+    }
+    *out = n;
+    return CF_OK;
+}
+
+// The rows of commfuse_norm_rope and its gradient.  `nothing`: no row.
+cf_status resolve_heads(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *wq, const void *wk, int64_t position_axis,
+                        cf::HeadParams *out, bool *nothing)
+{
+    if (rows == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "rows is NULL");
+    if (rope == nullptr && norm == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "neither rope nor norm is given");
+    if (rows->dtype != CF_BF16 && rows->dtype != CF_F32)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "dtype %d", rows->dtype);
+    if (rows->head_dim < 8 || rows->head_dim > 256 || rows->head_dim % 8)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "head_dim %d: multiples of 8 up to 256", rows->head_dim);
+    if (rows->heads < 0 || rows->kv_heads < 0)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "heads = %d, kv_heads = %d", rows->heads, rows->kv_heads);
+    if (cf_status st = check_tokens(rows->tokens, (int64_t)rows->heads + rows->kv_heads))
+        return st;
+    cf::HeadParams p = {};
+    if (cf_status st = resolve_axes(rope, rows->head_dim, rows->tokens, position_axis, &p.rot))
+        return st;
+    if (cf_status st = resolve_norm(norm, wq, wk, &p.norm))
+        return st;
+    p.q_token = rows->q_token, p.q_head = rows->q_head, p.k_token = rows->k_token, p.k_head = rows->k_head;
+    p.oq_token = rows->oq_token, p.oq_head = rows->oq_head, p.ok_token = rows->ok_token, p.ok_head = rows->ok_head;
+    const int64_t mult = rows->dtype == CF_BF16 ? 8 : 4;
+    if (cf_status st = resolve_rows("Q", &p.q_token, &p.q_head, rows->tokens, rows->heads, rows->head_dim, mult))
+        return st;
+    if (cf_status st = resolve_rows("K", &p.k_token, &p.k_head, rows->tokens, rows->kv_heads, rows->head_dim, mult))
+        return st;
+    if (cf_status st = resolve_rows("q_out", &p.oq_token, &p.oq_head, rows->tokens, rows->heads, rows->head_dim, mult))
+        return st;
+    if (cf_status st = resolve_rows("k_out", &p.ok_token, &p.ok_head, rows->tokens, rows->kv_heads, rows->head_dim, mult))
+        return st;
+    p.head_dim = rows->head_dim;
+    p.tokens = (unsigned)rows->tokens;
+    p.heads = (unsigned)rows->heads;
+    p.kv_heads = (unsigned)rows->kv_heads;
+    *nothing = rows->tokens == 0 || rows->heads + rows->kv_heads == 0;
+    *out = p;
+    return CF_OK;
+}
+
+// Pointers of the rows of some heads: all there and aligned, and in place only with the same strides.
+cf_status check_rows(const char *what, int heads, const void *in, int64_t in_token, int64_t in_head, const void *out, int64_t out_token, int64_t out_head)
+{
+    if (heads == 0)
+        return CF_OK;
+    if (in == nullptr || out == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "%s must not be NULL", what);
+    if (!aligned(in, 16) || !aligned(out, 16))
+        return CF_FAIL(CF_ERR_MISALIGNED, "%s must be 16-byte aligned", what);
+    if (in == out && (in_token != out_token || in_head != out_head))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "%s: in place, both must have the same strides", what);
+    return CF_OK;
+}
+
 // The packed prompts' geometry.  `nothing`: no row to compute.
 cf_status resolve_prompt(const cf_prompt_desc *d, cf::CausalParams *out, bool *nothing)
 {
@@ -250,32 +430,58 @@ cf_status commfuse_rope_make(const cf_rope_desc *d, cf_rope *rope)
         return CF_FAIL(CF_ERR_INVALID_ARG, "need base in (1, 1e18], factor in [1, 1e9], magnitude in (0, 1e9]");
     if (d->scaling != CF_ROPE_LINEAR && (d->trained_len < 1 || !(d->low > 0.0) || !(d->high > d->low) || !std::isfinite(d->high)))
         return CF_FAIL(CF_ERR_INVALID_ARG, "the ramp needs trained_len >= 1 and 0 < low < high");
-    const int pairs = d->rot_dim / 2;
-    const long double two_pi = 6.283185307179586476925286766559005768L;
     memset(rope, 0, sizeof(*rope));
     rope->head_dim = d->head_dim;
     rope->rot_dim = d->rot_dim;
     rope->layout = d->layout;
     rope->magnitude = (float)d->magnitude;
-    double first = 0.0, last = 0.0;                              // CF_ROPE_INDEX: the ramp's ends
-    if (d->scaling == CF_ROPE_INDEX) {
-        const double per = d->rot_dim / (2.0 * std::log(d->base));
-        first = std::floor(per * std::log(d->trained_len / ((double)two_pi * d->high)));
-        last = std::ceil(per * std::log(d->trained_len / ((double)two_pi * d->low)));
-        first = first > 0.0 ? first : 0.0;
-        last = last < d->rot_dim - 1 ? last : d->rot_dim - 1;    // (it may lie behind the last pair)
+    for (int j = 0; j < d->rot_dim / 2; ++j)
+        rope->turn[j] = turns_of(*d, d->rot_dim, j);
+    return CF_OK;
+}
+
+cf_status commfuse_rope_axes_make(const cf_rope_desc *d, const cf_axes_desc *axes, cf_rope_axes *rope)
+{
+    if (axes == nullptr || rope == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "axes or rope is NULL");
+    if (axes->n_axes < 1 || axes->n_axes > 4)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "n_axes = %d must be in [1, 4]", axes->n_axes);
+    if (axes->order != CF_AXES_SECTIONS && axes->order != CF_AXES_INTERLEAVED)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "order %d", axes->order);
+    if (axes->spectrum != CF_SPECTRUM_SHARED && axes->spectrum != CF_SPECTRUM_OWN)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "spectrum %d", axes->spectrum);
+    cf_rope_axes r;
+    memset(&r, 0, sizeof(r));
+    if (cf_status st = commfuse_rope_make(d, &r.rope))
+        return st;
+    const int pairs = d->rot_dim / 2, n = axes->n_axes;
+    int64_t all = 0;
+    for (int a = 0; a < n; ++a) {
+        if (axes->sections[a] < 1)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "section %d has %d pairs", a, axes->sections[a]);
+        if (a > 0 && axes->order == CF_AXES_INTERLEAVED && axes->sections[a] > pairs / n)
+            return CF_FAIL(CF_ERR_INVALID_ARG, "section %d: of %d pairs that %d axes take in turn it cannot have %d", a, pairs, n, axes->sections[a]);
+        all += axes->sections[a];
     }
-    for (int j = 0; j < pairs; ++j) {
-        const long double f = powl((long double)d->base, -2.0L * j / d->rot_dim);
-        double r = 0.0;
-        if (d->scaling == CF_ROPE_WAVELENGTH)
-            r = ((double)(d->trained_len * f / two_pi) - d->low) / (d->high - d->low);
-        else if (d->scaling == CF_ROPE_INDEX)
-            r = 1.0 - (j - first) / (last - first > 0.001 ? last - first : 0.001);
-        r = r < 0.0 ? 0.0 : r > 1.0 ? 1.0 : r;
-        const long double turns = f * (r + (1.0L - r) / d->factor) / two_pi;         // below 0.16
-        rope->turn[j] = (uint64_t)(turns * 18446744073709551616.0L + 0.5L);
+    if (all != pairs)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "the sections have %lld pairs, rot_dim %d has %d", (long long)all, d->rot_dim, pairs);
+    r.n_axes = n;
+    int used[4] = {};
+    for (int j = 0, section = 0; j < pairs; ++j) {
+        int a = 0;
+        if (axes->order == CF_AXES_INTERLEAVED) {
+            a = j / n < axes->sections[j % n] ? j % n : 0;
+        } else {
+            while (used[section] == axes->sections[section])
+                ++section;
+            a = section;
+        }
+        r.axis[j] = (uint8_t)a;
+        if (axes->spectrum == CF_SPECTRUM_OWN)
+            r.rope.turn[j] = turns_of(*d, 2 * axes->sections[a], used[a]);
+        ++used[a];
     }
+    *rope = r;
     return CF_OK;
 }
 
@@ -329,13 +535,9 @@ cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache,
                                void *q_out, void *hip_stream)
 {
     cf::CachePool c;
+    cf::CacheRows r;
+    bool nothing;
     if (cf_status st = resolve_cache(desc, cache, &c))
-        return st;
-    if (rows == nullptr)
-        return CF_FAIL(CF_ERR_NULL_PTR, "rows is NULL");
-    if (rows->heads < 0 || rows->reserved != 0)
-        return CF_FAIL(CF_ERR_INVALID_ARG, "heads = %d, reserved = %d", rows->heads, rows->reserved);
-    if (cf_status st = check_tokens(rows->tokens, (int64_t)rows->heads + 2 * c.kv_heads))
         return st;
     if (rope != nullptr) {
         if (cf_status st = check_rope(rope))
@@ -345,39 +547,14 @@ cf_status commfuse_cache_write(const cf_cache_desc *desc, const cf_cache *cache,
         if (rope->rot_dim % 16)
             return CF_FAIL(CF_ERR_UNSUPPORTED, "rot_dim %d: the cache's writer takes multiples of 16 (rotate with commfuse_rope first)", rope->rot_dim);
     }
-    const bool with_q = Q != nullptr && rows->heads > 0;
-    if (with_q && rope == nullptr)
+    if (cf_status st = resolve_cache_rows(c, rows, Q != nullptr, &r, &nothing))
+        return st;
+    if (Q != nullptr && rows->heads > 0 && rope == nullptr)
         return CF_FAIL(CF_ERR_NULL_PTR, "Q is given, but no rope to rotate it by");
-    cf::CacheRows r = {};
-    r.q_token = rows->q_token, r.q_head = rows->q_head, r.k_token = rows->k_token, r.k_head = rows->k_head;
-    r.v_token = rows->v_token, r.v_head = rows->v_head, r.o_token = rows->o_token, r.o_head = rows->o_head;
-    if (cf_status st = resolve_rows("K", &r.k_token, &r.k_head, rows->tokens, c.kv_heads, c.head_dim, 8))
-        return st;
-    if (cf_status st = resolve_rows("V", &r.v_token, &r.v_head, rows->tokens, c.kv_heads, c.head_dim, 8))
-        return st;
-    if (with_q) {
-        if (cf_status st = resolve_rows("Q", &r.q_token, &r.q_head, rows->tokens, rows->heads, c.head_dim, 8))
-            return st;
-        if (cf_status st = resolve_rows("q_out", &r.o_token, &r.o_head, rows->tokens, rows->heads, c.head_dim, 8))
-            return st;
-    }
-    if (rows->tokens == 0)
+    if (nothing)
         return CF_OK;
-    if (K == nullptr || V == nullptr || slots == nullptr || (rope != nullptr && positions == nullptr) || (with_q && q_out == nullptr))
-        return CF_FAIL(CF_ERR_NULL_PTR, "K, V, slots, with rope positions, with Q q_out must not be NULL");
-    if (!aligned(K, 16) || !aligned(V, 16) || (with_q && (!aligned(Q, 16) || !aligned(q_out, 16))) || !aligned(slots, 8) ||
-        (rope != nullptr && !aligned(positions, 4)))
-        return CF_FAIL(CF_ERR_MISALIGNED, "tensor pointers must be 16-byte aligned, slots 8-byte, positions 4-byte");
-    if (with_q && Q == q_out && (r.q_token != r.o_token || r.q_head != r.o_head))
-        return CF_FAIL(CF_ERR_INVALID_ARG, "in place, Q and q_out must have the same strides");
-    r.q = with_q ? Q : nullptr;
-    r.k = K;
-    r.v = V;
-    r.q_out = q_out;
-    r.tokens = (unsigned)rows->tokens;
-    r.heads = (unsigned)rows->heads;
-    r.positions = positions;
-    r.slots = slots;
+    if (cf_status st = take_cache_rows(Q, K, V, rope != nullptr, positions, slots, q_out, rows, &r))
+        return st;
     if (rope != nullptr) {
         r.rot_dim = rope->rot_dim;
         r.interleaved = rope->layout == CF_ROPE_INTERLEAVED;
@@ -414,6 +591,149 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
     r.tokens = (unsigned)rows->tokens;
     r.slots = slots;
     return launched(cf::launch_cache_read(c, r, K, V, static_cast<hipStream_t>(hip_stream)), "cache read launch");
+}
+
+cf_status commfuse_norm_rope(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *Q, const void *K, const void *wq,
+                             const void *wk, const int32_t *positions, int64_t position_axis, void *q_out, void *k_out, void *hip_stream)
+{
+    cf::HeadParams p;
+    bool nothing;
+    if (cf_status st = resolve_heads(rope, norm, rows, wq, wk, position_axis, &p, &nothing))
+        return st;
+    if (nothing)
+        return CF_OK;
+    if (rope != nullptr && (positions == nullptr || !aligned(positions, 4)))
+        return CF_FAIL(positions == nullptr ? CF_ERR_NULL_PTR : CF_ERR_MISALIGNED, "positions must not be NULL, and 4-byte aligned");
+    if (cf_status st = check_rows("Q and q_out", rows->heads, Q, p.q_token, p.q_head, q_out, p.oq_token, p.oq_head))
+        return st;
+    if (cf_status st = check_rows("K and k_out", rows->kv_heads, K, p.k_token, p.k_head, k_out, p.ok_token, p.ok_head))
+        return st;
+    p.q = Q;
+    p.k = K;
+    p.q_out = q_out;
+    p.k_out = k_out;
+    p.positions = positions;
+    return launched(cf::launch_norm_rope(p, rows->dtype == CF_BF16, static_cast<hipStream_t>(hip_stream), cf::num_cu()), "norm and rotation launch");
+}
+
+size_t commfuse_norm_rope_scratch_bytes(const cf_head_rows *rows)
+{
+    return rows == nullptr || rows->head_dim < 8 || rows->head_dim > 256 ? 0 : cf::norm_rope_scratch_bytes(rows->head_dim);
+}
+
+cf_status commfuse_norm_rope_grad(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *Q, const void *K, const void *wq,
+                                  const void *wk, const int32_t *positions, int64_t position_axis, const void *dq_out, const void *dk_out, void *dQ, void *dK,
+                                  float *dwq, float *dwk, void *scratch, void *hip_stream)
+{
+    cf::HeadParams p;
+    bool nothing;
+    if (cf_status st = resolve_heads(rope, norm, rows, wq, wk, position_axis, &p, &nothing))
+        return st;
+    if (norm == nullptr && (dwq != nullptr || dwk != nullptr))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "without norm there are no weights: dwq and dwk must be NULL");
+    if (!aligned(dwq, 4) || !aligned(dwk, 4) || !aligned(scratch, 16))
+        return CF_FAIL(CF_ERR_MISALIGNED, "dwq and dwk must be 4-byte aligned, scratch 16-byte");
+    if ((dwq != nullptr || dwk != nullptr) && scratch == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "dwq and dwk need scratch");
+    if (dwq != nullptr && dwq == dwk)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "dwq and dwk may not alias each other");
+    if (nothing && dwq == nullptr && dwk == nullptr)
+        return CF_OK;
+    if (!nothing) {
+        if (rope != nullptr && (positions == nullptr || !aligned(positions, 4)))
+            return CF_FAIL(positions == nullptr ? CF_ERR_NULL_PTR : CF_ERR_MISALIGNED, "positions must not be NULL, and 4-byte aligned");
+        if (cf_status st = check_rows("dq_out and dQ", rows->heads, dq_out, p.oq_token, p.oq_head, dQ, p.q_token, p.q_head))
+            return st;
+        if (cf_status st = check_rows("dk_out and dK", rows->kv_heads, dk_out, p.ok_token, p.ok_head, dK, p.k_token, p.k_head))
+            return st;
+        if (norm != nullptr) {
+            if (cf_status st = check_rows("Q and dQ", rows->heads, Q, p.q_token, p.q_head, dQ, p.q_token, p.q_head))
+                return st;
+            if (cf_status st = check_rows("K and dK", rows->kv_heads, K, p.k_token, p.k_head, dK, p.k_token, p.k_head))
+                return st;
+        }
+    }
+    p.q = Q;
+    p.k = K;
+    p.positions = positions;
+    return launched(cf::launch_norm_rope_grad(p, dq_out, dk_out, dQ, dK, dwq, dwk, static_cast<float *>(scratch), rows->dtype == CF_BF16,
+                                              static_cast<hipStream_t>(hip_stream), cf::num_cu()), "norm and rotation gradient launch");
+}
+
+cf_status commfuse_cache_write_norm(const cf_cache_desc *desc, const cf_cache *cache, const cf_cache_rows *rows, const cf_rope_axes *rope,
+                                    const cf_head_norm *norm, const void *Q, const void *K, const void *V, const void *wq, const void *wk,
+                                    const int32_t *positions, int64_t position_axis, const int64_t *slots, void *q_out, void *hip_stream)
+{
+    cf::CachePool c;
+    cf::CacheRows r;
+    bool nothing;
+    if (cf_status st = resolve_cache(desc, cache, &c))
+        return st;
+    if (rope == nullptr && norm == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "neither rope nor norm is given");
+    if (cf_status st = resolve_cache_rows(c, rows, Q != nullptr, &r, &nothing))
+        return st;
+    cf::AxesRotation a;
+    cf::NormParams n;
+    if (cf_status st = resolve_axes(rope, c.head_dim, rows->tokens, position_axis, &a))
+        return st;
+    if (a.rot_dim % 16)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "rot_dim %d: the cache's writer takes multiples of 16 (rotate with commfuse_norm_rope first)", a.rot_dim);
+    if (cf_status st = resolve_norm(norm, wq, wk, &n))
+        return st;
+    if (nothing)
+        return CF_OK;
+    if (cf_status st = take_cache_rows(Q, K, V, rope != nullptr, positions, slots, q_out, rows, &r))
+        return st;
+    return launched(cf::launch_cache_write_norm(c, r, a, n, static_cast<hipStream_t>(hip_stream), cf::num_cu()), "cache write launch");
+}
+
+cf_status commfuse_step_tables(const cf_tables_desc *d, const cf_tables *t, void *hip_stream)
+{
+    if (d == nullptr || t == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "descriptor or tables is NULL");
+    if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "page_size = %d must be a power of two in [16, 1024]", d->page_size);
+    if (d->n_seqs < 0 || d->max_pages < 0 || d->reserved != 0 || d->n_pages < 0 || d->n_pages > INT32_MAX || d->max_tokens < 0 || d->max_tokens > INT32_MAX - 1024)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "n_seqs = %d, max_pages = %d, reserved = %d, n_pages = %lld, max_tokens = %lld", d->n_seqs, d->max_pages, d->reserved,
+                       (long long)d->n_pages, (long long)d->max_tokens);
+    if (d->n_seqs > cf::MAX_TABLE_SEQS)
+        return CF_FAIL(CF_ERR_UNSUPPORTED, "n_seqs = %d: the kernel keeps the sums of up to %d sequences", d->n_seqs, cf::MAX_TABLE_SEQS);
+    const bool seqs = d->n_seqs > 0, table = seqs && d->max_pages > 0;
+    if (t->free_count == nullptr || t->free_left == nullptr || t->q_start == nullptr || (seqs && (t->held == nullptr || t->new_tokens == nullptr || t->kv_len == nullptr)) ||
+        (table && t->page_table == nullptr) || (d->n_pages > 0 && t->free_pages == nullptr) || (d->max_tokens > 0 && (t->slots == nullptr || t->positions == nullptr)))
+        return CF_FAIL(CF_ERR_NULL_PTR, "tables must not be NULL but for back_from and back_to");
+    if ((t->back_from == nullptr) != (t->back_to == nullptr))
+        return CF_FAIL(CF_ERR_NULL_PTR, "back_from and back_to go together");
+    for (const void *x : {static_cast<const void *>(t->held), static_cast<const void *>(t->new_tokens), static_cast<const void *>(t->back_from),
+                          static_cast<const void *>(t->back_to), static_cast<const void *>(t->page_table), static_cast<const void *>(t->free_pages),
+                          static_cast<const void *>(t->free_count), static_cast<const void *>(t->free_left), static_cast<const void *>(t->q_start),
+                          static_cast<const void *>(t->kv_len), static_cast<const void *>(t->positions)})
+        if (!aligned(x, 4))
+            return CF_FAIL(CF_ERR_MISALIGNED, "tables must be 4-byte aligned, slots 8-byte");
+    if (!aligned(t->slots, 8))
+        return CF_FAIL(CF_ERR_MISALIGNED, "tables must be 4-byte aligned, slots 8-byte");
+    if (seqs && (t->kv_len == t->held || t->kv_len == t->new_tokens || t->q_start == t->held || t->q_start == t->new_tokens))
+        return CF_FAIL(CF_ERR_INVALID_ARG, "q_start and kv_len may not alias held or new_tokens");
+    cf::TableParams p;
+    p.n_seqs = d->n_seqs;
+    p.page_shift = __builtin_ctz((unsigned)d->page_size);
+    p.max_pages = d->max_pages;
+    p.n_pages = (int)d->n_pages;
+    p.max_tokens = (int)d->max_tokens;
+    p.held = t->held;
+    p.new_tokens = t->new_tokens;
+    p.back_from = t->back_from;
+    p.back_to = t->back_to;
+    p.free_count = t->free_count;
+    p.page_table = t->page_table;
+    p.free_pages = t->free_pages;
+    p.free_left = t->free_left;
+    p.q_start = t->q_start;
+    p.kv_len = t->kv_len;
+    p.positions = t->positions;
+    p.slots = t->slots;
+    return launched(cf::launch_step_tables(p, static_cast<hipStream_t>(hip_stream)), "tables launch");
 }
 
 cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *seq_start,

@@ -56,6 +56,49 @@ struct CacheRows {
 hipError_t launch_cache_write(const CachePool &c, const CacheRows &r, hipStream_t s, int num_cu);
 hipError_t launch_cache_read(const CachePool &c, const CacheRows &r, void *K, void *V, hipStream_t s);
 
+// Positions on up to four axes, and the weights of heads that are divided by their root mean square.
+struct AxesRotation {
+    uint64_t turn[128];
+    uint32_t axis_bits[8];                          // of pair j: bits 2 (j % 16), .. + 1 of word j / 16
+    int n_axes;
+    int rot_dim;                                    // 0: no rotation
+    bool interleaved;
+    float magnitude;
+    int64_t position_axis;                          // between two axes' positions of a token
+};
+struct NormParams {
+    const void *wq, *wk;                            // null: a factor of 1
+    bool on, weight_bf16;
+    float eps, offset;
+};
+struct HeadParams {
+    AxesRotation rot;
+    NormParams norm;
+    int head_dim;
+    unsigned tokens, heads, kv_heads;
+    unsigned lanes, groups;                         // lanes of a head; a thread takes rows g, g + groups, ... of its token
+    const void *q, *k;
+    void *q_out, *k_out;
+    const int32_t *positions;
+    int64_t q_token, q_head, k_token, k_head, oq_token, oq_head, ok_token, ok_head;
+};
+hipError_t launch_norm_rope(const HeadParams &p, bool bf16, hipStream_t s, int num_cu);
+// dq_out, dk_out with the strides of q_out, k_out; dq, dk with those of q, k; dwq, dwk: null = not wanted
+hipError_t launch_norm_rope_grad(const HeadParams &p, const void *dq_out, const void *dk_out, void *dq, void *dk, float *dwq, float *dwk, float *scratch,
+                                 bool bf16, hipStream_t s, int num_cu);
+size_t norm_rope_scratch_bytes(int head_dim);
+hipError_t launch_cache_write_norm(const CachePool &c, const CacheRows &r, const AxesRotation &a, const NormParams &n, hipStream_t s, int num_cu);
+
+// A serving step's tables (cf_tables, with the counts resolved).
+constexpr int MAX_TABLE_SEQS = 4096;
+struct TableParams {
+    int n_seqs, page_shift, max_pages, n_pages, max_tokens;
+    const int32_t *held, *new_tokens, *back_from, *back_to, *free_count;
+    int32_t *page_table, *free_pages, *free_left, *q_start, *kv_len, *positions;
+    int64_t *slots;
+};
+hipError_t launch_step_tables(const TableParams &p, hipStream_t s);
+
 // Causal attention of rows (token, query head of one key head's group) over keys that lie packed (a prompt's own) or in a
 // paged cache.  Strides in elements.
 struct CausalParams {
