@@ -722,6 +722,27 @@ cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *c
                               void *hip_stream);
 size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc);
 
+/* The same three with a sliding window: a token sees the last `window` tokens of its sequence up to itself, and of those before them the first
+ * `sinks` of the sequence, which stay visible: token i (from 0 on) sees j <= i where j > i - window or j < sinks.  The formulas, operands,
+ * strides, limits and guarantees of commfuse_attn_prompt, commfuse_attn_prompt_grad and commfuse_attn_paged; what a token does not see costs no
+ * time but in the tiles (64 keys, 32 for few rows) on its window's ends.  In the paged call i counts the sequence's cached tokens, the new ones
+ * among them, and the table's entries for pages that no new token sees are not read (they may name no page, or one that another
+ * sequence has by now).  Where window + sinks covers all tokens (max_kv for the paged call) the results are those of the calls above, bit for bit. */
+typedef struct {
+    int32_t window;                      /* >= 1                                              */
+    int32_t sinks;                       /* >= 0                                              */
+} cf_window;
+cf_status commfuse_attn_prompt_window(const cf_prompt_desc *desc, const cf_window *window, const void *Q, const void *K, const void *V,
+                                      const int32_t *seq_start, void *out, float *lse, void *hip_stream);
+cf_status commfuse_attn_prompt_window_grad(const cf_prompt_desc *desc, const cf_window *window, const void *Q, const void *K, const void *V,
+                                           const void *out, const float *lse, const void *dout, const int32_t *seq_start, float *delta,
+                                           void *dQ, void *dK, void *dV, void *hip_stream);
+size_t commfuse_attn_prompt_window_workspace_bytes(const cf_prompt_desc *desc, const cf_window *window);
+cf_status commfuse_attn_paged_window(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const cf_window *window,
+                                     const void *Q, const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out,
+                                     float *lse, void *hip_stream);
+size_t commfuse_attn_paged_window_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc, const cf_window *window);
+
 /* Synchronises `hip_stream` and reports whether any step kernel since the last call gave up a
  * bounded device-side wait (CF_DEVICE_WAIT; CF_ERR_HIP, the status word in the workspace is cleared).  CF_OK if none did
  * or no workspace is registered.  This is the one entry point that synchronises. */

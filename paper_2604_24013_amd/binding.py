@@ -41,7 +41,8 @@ EXPORTS = [
     "commfuse_device_status", "commfuse_rope_make", "commfuse_rope", "commfuse_cache_write", "commfuse_cache_read",
     "commfuse_rope_axes_make", "commfuse_norm_rope", "commfuse_norm_rope_scratch_bytes", "commfuse_norm_rope_grad", "commfuse_cache_write_norm", "commfuse_step_tables",
     "commfuse_attn_prompt", "commfuse_attn_prompt_workspace_bytes", "commfuse_attn_prompt_grad", "commfuse_attn_paged", "commfuse_attn_paged_workspace_bytes",
-    "commfuse_destroy_cache", "commfuse_version",
+    "commfuse_attn_prompt_window", "commfuse_attn_prompt_window_grad", "commfuse_attn_prompt_window_workspace_bytes", "commfuse_attn_paged_window",
+    "commfuse_attn_paged_window_workspace_bytes", "commfuse_destroy_cache", "commfuse_version",
 ]
 
 
@@ -115,6 +116,10 @@ class HeadNorm(ctypes.Structure):
 class HeadRows(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype")] + [
         (n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "oq_token", "oq_head", "ok_token", "ok_head")]
+
+
+class Window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class TablesDesc(ctypes.Structure):
@@ -245,6 +250,16 @@ def load():
     lib.commfuse_norm_rope_grad.restype = i32
     lib.commfuse_cache_write_norm.argtypes = [ref(CacheDesc), ref(Cache), ref(CacheRows), ref(RopeAxes), ref(HeadNorm)] + [vp] * 6 + [i64] + [vp] * 3
     lib.commfuse_cache_write_norm.restype = i32
+    lib.commfuse_attn_prompt_window.argtypes = [ref(PromptDesc), ref(Window)] + [vp] * 7
+    lib.commfuse_attn_prompt_window.restype = i32
+    lib.commfuse_attn_prompt_window_grad.argtypes = [ref(PromptDesc), ref(Window)] + [vp] * 12
+    lib.commfuse_attn_prompt_window_grad.restype = i32
+    lib.commfuse_attn_prompt_window_workspace_bytes.argtypes = [ref(PromptDesc), ref(Window)]
+    lib.commfuse_attn_prompt_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.commfuse_attn_paged_window.argtypes = [ref(CacheDesc), ref(Cache), ref(PagedDesc), ref(Window)] + [vp] * 7
+    lib.commfuse_attn_paged_window.restype = i32
+    lib.commfuse_attn_paged_window_workspace_bytes.argtypes = [ref(CacheDesc), ref(PagedDesc), ref(Window)]
+    lib.commfuse_attn_paged_window_workspace_bytes.restype = ctypes.c_size_t
     lib.commfuse_step_tables.argtypes = [ref(TablesDesc), ref(Tables), vp]
     lib.commfuse_step_tables.restype = i32
     lib.commfuse_destroy_cache.argtypes = []
@@ -615,3 +630,29 @@ def make_tables(held, new_tokens, page_table, free_pages, free_count, free_left,
 
 def step_tables(desc: TablesDesc, tables: Tables, stream=None) -> None:
     _check((_lib or load()).commfuse_step_tables(desc, tables, _stream(stream)))
+
+
+def window(window_: int, sinks: int = 0) -> Window:
+    return Window(window_, sinks)
+
+
+def attn_prompt_window(desc: PromptDesc, window_: Window, Q, K, V, seq_start, out, lse=None, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_prompt_window(desc, window_, _ptr(Q), _ptr(K), _ptr(V), _ptr(seq_start), _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def attn_prompt_window_grad(desc: PromptDesc, window_: Window, Q, K, V, out, lse, dout, seq_start, delta, dQ, dK, dV, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_prompt_window_grad(desc, window_, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(lse), _ptr(dout), _ptr(seq_start),
+                                                             _ptr(delta), _ptr(dQ), _ptr(dK), _ptr(dV), _stream(stream)))
+
+
+def attn_prompt_window_workspace_bytes(desc: PromptDesc, window_: Window) -> int:
+    return int(load().commfuse_attn_prompt_window_workspace_bytes(desc, window_))
+
+
+def attn_paged_window(cache_desc_: CacheDesc, cache: Cache, desc: PagedDesc, window_: Window, Q, q_start, kv_len, page_table, out, lse=None, stream=None) -> None:
+    _check((_lib or load()).commfuse_attn_paged_window(cache_desc_, cache, desc, window_, _ptr(Q), _ptr(q_start), _ptr(kv_len), _ptr(page_table),
+                                                       _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def attn_paged_window_workspace_bytes(cache_desc_: CacheDesc, desc: PagedDesc, window_: Window) -> int:
+    return int(load().commfuse_attn_paged_window_workspace_bytes(cache_desc_, desc, window_))

@@ -32,7 +32,7 @@ constexpr int LEAST_TILES = 6;
 
 constexpr int PARKED = DH / 32 * 16 + 4; // floats that a thread parks: its part of O, and m and l
 
-template <int NW, int SRC, bool LSE>
+template <int NW, int SRC, bool LSE, bool WIN>
 __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
 {
     constexpr int NT = 64 * NW;          // threads per workgroup
@@ -93,17 +93,25 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         }
         return w;
     };
+    // the gap of a walk whose first row's last key is `last`
+    auto gap_of = [&](int lo, int hi, int last) { return WIN ? Gap<BKV>(P.sinks, lo, hi, window_from(P, lo, last)) : Gap<BKV>(); };
     Item it;
     const int all_blocks = SRC == PACKED ? blocks : blocks * P.n_seqs;
-    const int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
+    int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
+    if constexpr (WIN)
+        bound = (int)min((int64_t)bound, ((int64_t)P.window + P.sinks + BQ / G + 4 * BKV) / BKV);
     if (!my_item<NT, NW == 4>(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
             Walk w = walk_of(block);
             if constexpr (SRC == PACKED) {
                 int end;
                 seqs.around(w.t_base, &w.lo, &end);
                 w.lo = w.lo < 0 ? 0 : w.lo;
+                if constexpr (WIN)
+                    return w.lo < w.hi ? gap_of(w.lo, w.hi, w.t_base).tiles(w.lo, w.hi) : 0;
                 return w.lo < w.hi ? (w.hi - w.lo + BKV - 1) / BKV : 0;
             } else {
+                if constexpr (WIN)
+                    return w.any ? max(1, gap_of(0, w.hi, w.shown).tiles(0, w.hi)) : 0;
                 return w.any ? max(1, (w.hi + BKV - 1) / BKV) : 0;
             }
         }, &it))
@@ -128,7 +136,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     }
 
     // This workgroup's key tiles: [kt0, nkt) of the block's
-    const int tiles = (hi - lo + BKV - 1) / BKV;
+    const Gap<BKV> gap = gap_of(lo, hi, SRC == PACKED ? t_base : shown);
+    auto place_of = [&](int kt) __attribute__((always_inline)) { return WIN ? gap.key(kt) : kt * BKV; };   // a tile's first key, from lo on
+    const int tiles = WIN ? gap.tiles(lo, hi) : (hi - lo + BKV - 1) / BKV;
     int kt0, nkt;
     it.share(tiles, &kt0, &nkt);
 
@@ -151,10 +161,27 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     }
     // ... and its wave's: tiles [wt0, wt1) have keys that a row of it sees; all see tiles that start at `all_from` or later and end at
     // `all_to` or earlier
+    using Sees = std::conditional_t<WIN, SeesWindow, SeesUpTo>;
+    const Sees sees = [&]() {
+        if constexpr (WIN)
+            return SeesWindow(P, first, last);
+        else
+            return SeesUpTo{first, last};
+    }();
     int wt0 = kt0, wt1 = kt0, all_from = 0, all_to = 0;
     {
         int f_min, f_max, l_min, l_max;
-        if (edges(there, first, last, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+        if constexpr (WIN) {
+            int low, unused;                         // (rows that see first keys see those of their sequence, so that the lowest grows with the row)
+            if (edges(there, sees.from, last, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+                edges(there, P.sinks > 0 ? first : sees.from, last, &low, &unused, &unused, &unused);
+                all_from = f_max - lo;
+                all_to = l_min - lo;
+                wt0 = max(kt0, gap.tile(low - lo));
+                wt0 -= (wt0 - kt0) & 1;
+                wt1 = min(nkt, gap.tile(l_max - lo) + 1);
+            }
+        } else if (edges(there, first, last, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
             all_from = f_max - lo;
             all_to = l_min - lo;
             wt0 = max(kt0, (f_min - lo) / BKV);
@@ -185,14 +212,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // window or in the one before.
     int window = -1, entry = 0;
     unsigned long long bad = 0, bad_before = 0;
-    auto window_of = [&](int kt) __attribute__((always_inline)) { return ((kt * BKV) >> shift) >> 6; };
+    auto window_of = [&](int kt) __attribute__((always_inline)) { return (place_of(kt) >> shift) >> 6; };
     auto page_of = [&](int key) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(entry, (key >> shift) & 63); };
     auto turn_to = [&](int kt) __attribute__((always_inline)) {
         const int w = window_of(kt);
         if (w != window) {
             const int i = w * 64 + lane;
             entry = i < P.max_pages ? table[i] : -1;
-            bad_before = w == window + 1 ? bad : 0;
+            bad_before = WIN || w == window + 1 ? bad : 0;           // (a gap may leave windows out)
             bad = __builtin_amdgcn_ballot_w64((unsigned)entry >= (unsigned)n_pages);
             window = w;
         }
@@ -208,7 +235,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     const unsigned v_off = (unsigned)((SRC == PACKED ? ld_row : lane >> 4) * v_row + (((ld_cp >> 2) ^ (ld_row & 3)) << 6) + ((ld_cp & 3) << 4));
     auto issue = [&](int kt, const unsigned char *from, int row_bytes, unsigned off, unsigned lds) __attribute__((always_inline)) {
         if constexpr (SRC == PACKED) {                               // one buffer a tile
-            const int key = lo + kt * BKV, left = hi - key < BKV ? hi - key : BKV;
+            const int key = lo + place_of(kt), left = hi - key < BKV ? hi - key : BKV;
             const i32x4_t rsrc = make_rsrc(from + (int64_t)key * row_bytes, left > 0 ? (unsigned)left * (unsigned)row_bytes : 0u);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j)
@@ -216,7 +243,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         } else {                                                     // one a wave-load, whose rows lie in one page
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
-                const int key = kt * BKV + wave * 4 + j * NW * 4, page = page_of(key);
+                const int key = place_of(kt) + wave * 4 + j * NW * 4, page = page_of(key);
                 const int left = hi - key < 4 ? hi - key : 4;
                 const bool some = left > 0 && (unsigned)page < (unsigned)n_pages;
                 const unsigned char *at = from + (int64_t)page * page_bytes + (key & ((1 << shift) - 1)) * row_bytes;
@@ -232,7 +259,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     auto issue8 = [&](int kt, const unsigned char *from, const uint8_t *exponents, int row_bytes, u32x4_t (&code)[LOADS8], int (&ex)[LOADS8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < LOADS8; ++j) {
-            const int key = kt * BKV + wave * 8 + j * NW * 8;
+            const int key = place_of(kt) + wave * 8 + j * NW * 8;
             const int left = hi - key < 8 ? hi - key : 8, page = page_of(key), in_page = key & ((1 << shift) - 1);
             const bool some = left > 0 && (unsigned)page < (unsigned)n_pages;
             const auto rows = plain_rsrc(from + (int64_t)page * page_bytes + in_page * row_bytes, some ? left * row_bytes : 0);
@@ -318,11 +345,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     // of the accumulators is rare and sits in a wave-uniform branch.
     constexpr float RAISE = 8.0f;
     auto settle = [&](int kt, f32x16_t (&sn)[KT], float mx) __attribute__((always_inline)) {
-        if (kt * BKV < all_from || (kt + 1) * BKV - 1 > all_to) {    // uniform
+        if (place_of(kt) < all_from || place_of(kt) + BKV - 1 > all_to) {    // uniform
             float ninf = -INFINITY;
             asm volatile("" : "+v"(ninf));                           // (keeps this a branch: not 32 selects in every tile)
-            const int key0 = lo + kt * BKV + 4 * lh;
-            if constexpr (SRC == PACKED) {
+            const int key0 = lo + place_of(kt) + 4 * lh;
+            if constexpr (WIN) {
+#pragma unroll
+                for (int j = 0; j < KT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!sees(key0 + j * 32 + 8 * (e >> 2) + (e & 3)))
+                            sn[j][e] = ninf;
+            } else if constexpr (SRC == PACKED) {
                 const unsigned at = (unsigned)(key0 - first), span = (unsigned)(last - first);
 #pragma unroll
                 for (int j = 0; j < KT; ++j)
@@ -343,7 +377,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         if constexpr (SRC != PACKED) {
             const unsigned long long none = window_of(kt) == window ? bad : bad_before;
             if (none != 0) {                                         // uniform
-                const int key0 = kt * BKV + 4 * lh;
+                const int key0 = place_of(kt) + 4 * lh;
 #pragma unroll
                 for (int j = 0; j < KT; ++j)
 #pragma unroll
@@ -661,11 +695,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
         V.exps = ve;
         // The tiles of this wave, of all splits (the first may be one that no row sees); front .. f_max, l_min .. behind: keys that some rows do not see
         int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
-        edges(stored, first, last, &f_min, &f_max, &l_min, &l_max);
-        const int front = lo + max(0, (f_min - lo) / BKV - 1) * BKV, behind = min(hi, lo + ((l_max - lo) / BKV + 1) * BKV);
-        if (any_large(V, front, min(f_max, hi)) || any_large(V, max(l_min + 1, lo), behind)) {
+        int sinks_end = lo;                                          // (with a window the tiles with first keys too, of which rows see some)
+        if constexpr (WIN) {
+            edges(stored, sees.from, last, &f_min, &f_max, &l_min, &l_max);
+            sinks_end = (int)min((int64_t)hi, lo + (int64_t)gap.front * BKV);
+        } else {
+            edges(stored, first, last, &f_min, &f_max, &l_min, &l_max);
+        }
+        const int front = lo + (WIN ? gap.key(gap.front) : max(0, (f_min - lo) / BKV - 1) * BKV), behind = min(hi, lo + ((l_max - lo) / BKV + 1) * BKV);
+        if (any_large(V, front, min(f_max, hi)) || any_large(V, max(l_min + 1, lo), behind) || (WIN && any_large(V, lo, sinks_end))) {
             __builtin_amdgcn_s_waitcnt(0);                           // the rows' first results are written before their second
-            rows_again<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + (stored ? t : t_base) * P.q_token + of_head * P.q_head, first, last, again, sl2, 0, 1, oacc,
+            rows_again<SRC>(K, V, static_cast<const __bf16 *>(P.Q) + (stored ? t : t_base) * P.q_token + of_head * P.q_head, sees, again, sl2, 0, 1, oacc,
                             &m_run, &l_run);
             if (again)
                 store_fours(oacc, l_run == 0.0f ? 0.0f : 1.0f / l_run, orow);
@@ -673,15 +713,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     }
 }
 
-template <int NW, int SRC>
+template <int NW, int SRC, bool WIN>
 hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
 {
     if (wgs * 64 * NW >= ((int64_t)1 << 32))
         return hipErrorInvalidValue;
     if (p.lse != nullptr)
-        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, true>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, true, WIN>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
     else
-        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, false>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+        hipLaunchKernelGGL((attn_blocks_kernel<NW, SRC, false, WIN>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
     return hipGetLastError();
 }
 
@@ -729,45 +769,70 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t lea
     return items;
 }
 
+namespace {
+// Tiles of a walk at the most, of `keys` keys.
+int64_t longest_walk(const CausalParams &p, int64_t keys, int64_t rows)
+{
+    const int64_t all = (keys + BKV - 1) / BKV;
+    if (p.window == 0)
+        return all;
+    const int64_t some = ((int64_t)p.window + p.sinks + (rows < 256 ? rows : 256) + 3 * BKV) / BKV;
+    return some < all ? some : all;
+}
+
+template <int SRC>
+hipError_t launch_as(const CausalParams &p, int waves, int64_t wgs, hipStream_t s)
+{
+    if (p.window > 0)
+        return waves == 8 ? launch<8, SRC, true>(p, wgs, s) : launch<4, SRC, true>(p, wgs, s);
+    return waves == 8 ? launch<8, SRC, false>(p, wgs, s) : launch<4, SRC, false>(p, wgs, s);
+}
+
+int choose_prompt(CausalParams &p, int num_cu, int64_t *wgs)
+{
+    const int64_t rows = (int64_t)p.tokens * p.group;
+    return choose_blocks(p, false, rows, 1, longest_walk(p, p.tokens, rows), num_cu, wgs);
+}
+int choose_paged(CausalParams &p, int num_cu, int64_t *wgs)
+{
+    const int64_t rows = (int64_t)p.max_q * p.group;
+    return choose_blocks(p, true, rows, p.n_seqs, longest_walk(p, p.max_kv, rows), num_cu, wgs);
+}
+}  // namespace
+
 hipError_t launch_attn_prompt(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
     int64_t wgs;
-    const int waves = choose_blocks(p, false, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu, &wgs);
-    return waves == 8 ? launch<8, PACKED>(p, wgs, s) : launch<4, PACKED>(p, wgs, s);
+    const int waves = choose_prompt(p, num_cu, &wgs);
+    return launch_as<PACKED>(p, waves, wgs, s);
 }
 
 hipError_t launch_attn_paged_blocks(const CausalParams &p_in, hipStream_t s, int num_cu)
 {
     CausalParams p = p_in;
     int64_t wgs;
-    const int waves = choose_blocks(p, true, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu, &wgs);
-    if (p.pool.e4m3)
-        return waves == 8 ? launch<8, PAGED_E4M3>(p, wgs, s) : launch<4, PAGED_E4M3>(p, wgs, s);
-    return waves == 8 ? launch<8, PAGED_BF16>(p, wgs, s) : launch<4, PAGED_BF16>(p, wgs, s);
+    const int waves = choose_paged(p, num_cu, &wgs);
+    return p.pool.e4m3 ? launch_as<PAGED_E4M3>(p, waves, wgs, s) : launch_as<PAGED_BF16>(p, waves, wgs, s);
 }
 
 namespace {
-// (as if any workspace were there)
-size_t part_bytes_of(CausalParams p, bool paged, int64_t rows, int64_t sequences, int64_t tiles, int num_cu)
+size_t part_bytes_of(CausalParams p, int (*choose)(CausalParams &, int, int64_t *), int num_cu)
 {
-    p.parts = reinterpret_cast<float *>(256);
+    p.parts = reinterpret_cast<float *>(256);                        // as if any workspace were there
     p.part_bytes = (size_t)1 << 48;
     p.max_counters = 1 << 30;
     int64_t wgs;
-    const int waves = choose_blocks(p, paged, rows, sequences, tiles, num_cu, &wgs);
+    const int waves = choose(p, num_cu, &wgs);
     return p.items > 0 ? (size_t)p.items * part_bytes(waves) : 0;
 }
 }  // namespace
 
-size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu)
-{
-    return part_bytes_of(p, true, (int64_t)p.max_q * p.group, p.n_seqs, (p.max_kv + BKV - 1) / BKV, num_cu);
-}
+size_t attn_paged_blocks_part_bytes(const CausalParams &p, int num_cu) { return part_bytes_of(p, choose_paged, num_cu); }
 
 size_t attn_prompt_part_bytes(const CausalParams &p, int num_cu)
 {
-    const size_t f = part_bytes_of(p, false, (int64_t)p.tokens * p.group, 1, (p.tokens + BKV - 1) / BKV, num_cu), g = attn_grad_part_bytes(p, num_cu);
+    const size_t f = part_bytes_of(p, choose_prompt, num_cu), g = attn_grad_part_bytes(p, num_cu);
     return f > g ? f : g;
 }
 

@@ -25,7 +25,7 @@ namespace {
 constexpr int FEW_KEYS = 32;             // keys of a tile
 constexpr int O_STRIDE = DH + 4;         // floats between rows of a parked O in LDS (the 16 rows of a store on different banks)
 
-template <int NW, int QT, int SRC>
+template <int NW, int QT, int SRC, bool WIN>
 __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
 {
     constexpr int NT = 64 * NW;
@@ -51,9 +51,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         n = (n < 0 ? 0 : n < P.max_kv ? n : P.max_kv) - m + some;
         return some <= 0 ? -1 : n > 0 ? n : 0;
     };
+    // ... of which, with a window, some in the middle are seen by none: `rows` rows see `keys` keys, the last of them all
+    auto gap_of = [&](int keys, int tokens) { return Gap<FEW_KEYS>(P.sinks, 0, keys, window_from(P, 0, keys - tokens)); };
     Item it;
     if (!my_item<NT, false>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
             const int keys = keys_of(seq);
+            if constexpr (WIN) {
+                const int m = clamped(P.starts[seq + 1], P.tokens) - clamped(P.starts[seq], P.tokens);
+                return keys < 0 ? 0 : max(1, gap_of(keys, m < P.max_q ? m : P.max_q).tiles(0, keys));
+            }
             return keys < 0 ? 0 : max(1, (keys + FEW_KEYS - 1) / FEW_KEYS);
         }, &it))
         return;
@@ -68,7 +74,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     if (rows <= 0)
         return;
     const int hi = n - m + (rows - 1) / G + 1 > 0 ? n - m + (rows - 1) / G + 1 : 0;   // keys that the last row sees
-    const int tiles = (hi + FEW_KEYS - 1) / FEW_KEYS;
+    const Gap<FEW_KEYS> gap = WIN ? gap_of(hi, (rows - 1) / G + 1) : Gap<FEW_KEYS>();
+    auto place_of = [&](int tile) __attribute__((always_inline)) { return WIN ? gap.key(tile) : tile * FEW_KEYS; };      // a tile's first key
+    const int tiles = WIN ? gap.tiles(0, hi) : (hi + FEW_KEYS - 1) / FEW_KEYS;
     int t0, t1;
     it.share(tiles, &t0, &t1);
 
@@ -117,7 +125,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     struct Pages {
         int k, v;
     };
-    auto key_of = [&](int tile, int eight) { const int key = tile * FEW_KEYS + eight; return key < hi ? key : hi - 1; };
+    auto key_of = [&](int tile, int eight) { const int key = place_of(tile) + eight; return key < hi ? key : hi - 1; };
     auto pages_of = [&](int tile) __attribute__((always_inline)) {
         Pages p;
         p.k = table[key_of(tile, k_eight) >> shift];
@@ -208,8 +216,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
             bf16x8_t pf[QT];
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                const int key = tile * FEW_KEYS + v_eight;
-                if (__builtin_amdgcn_ballot_w64(none || key + 7 > last[t]) != 0) {
+                const int key = place_of(tile) + v_eight;
+                if constexpr (WIN) {
+                    const SeesWindow sees(P, 0, last[t]);
+                    if (__builtin_amdgcn_ballot_w64(none || key + 7 > last[t] || key < sees.from) != 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (none || !sees(key + e))
+                                sc[t][e >> 2][e & 3] = -INFINITY;
+                    }
+                } else if (__builtin_amdgcn_ballot_w64(none || key + 7 > last[t]) != 0) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (none || key + e > last[t])
@@ -253,8 +269,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
             }
 
             if constexpr (E4M3) {                                    // exponents behind the last key may be anything
-                const int real = hi - tile * FEW_KEYS - v_eight;
-                if ((tile + 1) * FEW_KEYS > hi) {
+                const int real = hi - place_of(tile) - v_eight;
+                if (place_of(tile) + FEW_KEYS > hi) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int have = real - 4 * c;
@@ -464,12 +480,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
         const unsigned w = row != nullptr ? reinterpret_cast<const unsigned *>(row)[lane] : 0;
         unseen = unseen || (w & 0x7FFFu) == 0x7F80 || (w >> 16 & 0x7FFFu) == 0x7F80;
     }
-    if (__builtin_amdgcn_ballot_w64(unseen) == 0 && !any_large(Kv, max(n - m + 1, 0), hi))
+    // Keys from here on are hidden from some rows; with a window those of the tiles with first keys, and from the first tile behind the gap on.
+    const int hidden = WIN ? min(max(n - m + 1, 0), place_of(gap.front)) : max(n - m + 1, 0);
+    if (__builtin_amdgcn_ballot_w64(unseen) == 0 && !any_large(Kv, hidden, hi) && !(WIN && any_large(Kv, 0, min(hi, gap.front * FEW_KEYS))))
         return;
     const int lq = lane & 31, lh = lane >> 5, r = lq < rows ? lq : 0, token = r / G;
     f32x16_t acc[DH / 32];
     float m_row, l_row;
-    rows_again<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + (int64_t)(from + token) * P.q_token + (kvh * G + r - token * G) * P.q_head, 0, n - m + token,
+    const auto sees = [&]() {
+        if constexpr (WIN)
+            return SeesWindow(P, 0, n - m + token);
+        else
+            return SeesUpTo{0, n - m + token};
+    }();
+    rows_again<SRC>(Kk, Kv, static_cast<const __bf16 *>(P.Q) + (int64_t)(from + token) * P.q_token + (kvh * G + r - token * G) * P.q_head, sees,
                     odd >> lq & 1u, sl2, wave, NW, acc, &m_row, &l_row);
     for (int t = 0; t < QT; ++t) {
         __syncthreads();                                             // (the rows before have been read)
@@ -491,15 +515,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     }
 }
 
-template <int NW, int QT>
+template <int NW, int QT, bool WIN>
 hipError_t launch(const CausalParams &p, int64_t wgs, hipStream_t s)
 {
     if (wgs * 64 * NW >= ((int64_t)1 << 32))
         return hipErrorInvalidValue;
     if (p.pool.e4m3)
-        hipLaunchKernelGGL((attn_few_kernel<NW, QT, PAGED_E4M3>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+        hipLaunchKernelGGL((attn_few_kernel<NW, QT, PAGED_E4M3, WIN>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
     else
-        hipLaunchKernelGGL((attn_few_kernel<NW, QT, PAGED_BF16>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
+        hipLaunchKernelGGL((attn_few_kernel<NW, QT, PAGED_BF16, WIN>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, p);
     return hipGetLastError();
 }
 
@@ -507,7 +531,10 @@ int choose_few(CausalParams &p, int num_cu, int64_t *wgs, size_t *part)         
 {
     const int qt = p.max_q * p.group <= 16 ? 1 : 2;
     *part = (size_t)(qt * 16) * (DH + 4) * sizeof(float);
-    *wgs = plan_items(p, p.n_seqs, (p.max_kv + FEW_KEYS - 1) / FEW_KEYS, 8, *part, true, num_cu);
+    int64_t longest = (p.max_kv + FEW_KEYS - 1) / FEW_KEYS;
+    if (p.window > 0 && ((int64_t)p.window + p.sinks + p.max_q + 3 * FEW_KEYS) / FEW_KEYS < longest)
+        longest = ((int64_t)p.window + p.sinks + p.max_q + 3 * FEW_KEYS) / FEW_KEYS;
+    *wgs = plan_items(p, p.n_seqs, longest, 8, *part, true, num_cu);
     return qt;
 }
 
@@ -520,7 +547,10 @@ hipError_t launch_attn_few(const CausalParams &p_in, hipStream_t s, int num_cu)
     CausalParams p = p_in;
     int64_t wgs;
     size_t part;
-    return choose_few(p, num_cu, &wgs, &part) == 1 ? launch<8, 1>(p, wgs, s) : launch<8, 2>(p, wgs, s);
+    const bool one = choose_few(p, num_cu, &wgs, &part) == 1;
+    if (p.window > 0)
+        return one ? launch<8, 1, true>(p, wgs, s) : launch<8, 2, true>(p, wgs, s);
+    return one ? launch<8, 1, false>(p, wgs, s) : launch<8, 2, false>(p, wgs, s);
 }
 
 size_t attn_few_part_bytes(const CausalParams &p_in, int num_cu)

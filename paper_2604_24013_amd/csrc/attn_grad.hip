@@ -21,6 +21,8 @@
 // hides can have been the reason, so that it has no influence.
 #include "attn_tiles.h"
 
+#include <algorithm>
+
 namespace cf {
 namespace {
 
@@ -196,17 +198,17 @@ __device__ __forceinline__ bool odd_row(bool odd)
 }
 
 // One of the three results for 32 columns (rows of Q, or keys) by one wave, from memory: as in `rows_again`.  A lane's column (lane & 31) has rows
-// b1, b2 and sees indices [lo, hi): keys, or with KEYS rows (token, head of the group); stored where `wanted`: all features, or (TILES = 1, a quarter of
+// b1, b2 and sees the indices that `sees` says: keys, or with KEYS rows (token, head of the group); stored where `wanted`: all features, or (TILES = 1, a quarter of
 // the registers) those of tile `tile`.
 // dQ: sum over keys of dS k; dK: over rows of dS q; dV (`values`): over rows of P dout.  6144 tokens, 4 heads of one key head: 0.19 ms, with an
 // infinite element of dout in their middle 1.8.
-template <bool KEYS, int TILES>
-__device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const __bf16 *b1, const __bf16 *b2, int lo, int hi, float lse, float delta, bool values,
+template <bool KEYS, int TILES, typename S>
+__device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const __bf16 *b1, const __bf16 *b2, const S &sees, float lse, float delta, bool values,
                                            bool wanted, __bf16 *out, int tile)
 {
     const CausalParams &C = P.c;
     const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5;
-    const int from = least_of(wanted ? lo : 0x7FFFFFFF), to = most_of(wanted ? hi : 0);
+    const int from = least_of(wanted ? sees.lowest() : 0x7FFFFFFF), to = most_of(wanted ? sees.last + 1 : 0);
     f32x16_t acc[TILES];
 #pragma unroll
     for (int d = 0; d < TILES; ++d)
@@ -216,6 +218,9 @@ __device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const _
 #pragma unroll 1
     for (int at0 = from & ~31; at0 < to; at0 += 32) {
         const int mine = at0 + lq < from ? from : at0 + lq < to ? at0 + lq : to - 1;
+        if constexpr (!std::is_same_v<S, SeesUpTo>)
+            if (__builtin_amdgcn_ballot_w64(wanted && !sees.none_of(at0, at0 + 32)) == 0)
+                continue;
         const __bf16 *a1, *a2;
         float lse_of = 0.0f, delta_of = 0.0f;
         if constexpr (KEYS) {
@@ -254,12 +259,12 @@ __device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const _
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int slot = 8 * (i >> 2) + (i & 3), at = at0 + slot + 4 * lh;
-            const bool sees = at >= lo && at < hi;
-            seen |= (unsigned)sees << i;
+            const bool visible = sees(at);
+            seen |= (unsigned)visible << i;
             const float l = KEYS ? __builtin_bit_cast(float, of_slot(__builtin_bit_cast(int, lse_of), slot)) : lse;
             const float d = KEYS ? __builtin_bit_cast(float, of_slot(__builtin_bit_cast(int, delta_of), slot)) : delta;
             const float p = __builtin_amdgcn_exp2f((s[i] * C.scale - l) * LOG2E);
-            w[i >> 3][i & 7] = (__bf16)(sees ? values ? p : p * (dp[i] - d) : 0.0f);
+            w[i >> 3][i & 7] = (__bf16)(visible ? values ? p : p * (dp[i] - d) : 0.0f);
             if (i % 4 == 3)
                 __builtin_amdgcn_sched_barrier(0);
         }
@@ -301,11 +306,13 @@ __device__ __forceinline__ void grad_again(const GradParams &P, int kvh, const _
 
 // A workgroup's rows and walk, as in the forward kernel.
 constexpr int DQ_WAVES = 4, DQ_ROWS = DQ_WAVES * 32;
+template <bool WIN>
 struct RowBlock {
     const Sequences seqs;
     int blocks;                          // of one key head
     Item it;
     int t_base, t_last, row0, seq_a, seq_b, lo, hi, tiles;
+    Gap<BKV> gap;
     __device__ __forceinline__ void rows_of(const CausalParams &C, int block, int *base, int *row, int *last) const
     {
         const int64_t r0 = (int64_t)(blocks - 1 - block) * DQ_ROWS, all = (int64_t)C.tokens * C.group, r1 = r0 + DQ_ROWS < all ? r0 + DQ_ROWS : all;   // long blocks first
@@ -319,10 +326,17 @@ struct RowBlock {
         rows_of(C, block, &base, &row, &last);
         seqs.around(base, &start, &end);
         const int stop = seqs.end_of(C.n_seqs - 1), from = start < 0 ? 0 : start, to = last + 1 < stop ? last + 1 : stop;
+        if constexpr (WIN)
+            return from < to ? Gap<BKV>(C.sinks, from, to, window_from(C, from, base)).tiles(from, to) : 0;
         return from < to ? (to - from + BKV - 1) / BKV : 0;
     }
     __device__ __forceinline__ RowBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((int)(((int64_t)C.tokens * C.group + DQ_ROWS - 1) / DQ_ROWS)) {}
-    __device__ __forceinline__ int bound(const CausalParams &C) const { return C.items > 0 ? (seqs.longest() + DQ_ROWS / C.group + 2 * BKV) / BKV : 0; }
+    __device__ __forceinline__ int bound(const CausalParams &C) const
+    {
+        const int all = C.items > 0 ? (seqs.longest() + DQ_ROWS / C.group + 2 * BKV) / BKV : 0;
+        return WIN ? (int)min((int64_t)all, ((int64_t)C.window + C.sinks + DQ_ROWS / C.group + 4 * BKV) / BKV) : all;
+    }
+    __device__ __forceinline__ int place_of_unit(int u) const { return WIN ? u * 32 + (u >= 2 * gap.front ? gap.keys : 0) : u * 32; }      // its first key, from lo on
     // the rows and the walk of it.block; false: nothing to do
     __device__ __forceinline__ bool look(const CausalParams &C)
     {
@@ -334,14 +348,17 @@ struct RowBlock {
         const int begin = seqs.start_of(seq_a), stop = seqs.end_of(C.n_seqs - 1);
         lo = begin < 0 ? 0 : begin;
         hi = t_last + 1 < stop ? t_last + 1 : stop;
-        tiles = (hi - lo + BKV - 1) / BKV;
+        if constexpr (WIN)
+            gap = Gap<BKV>(C.sinks, lo, hi, window_from(C, lo, t_base));
+        tiles = WIN ? gap.tiles(lo, hi) : (hi - lo + BKV - 1) / BKV;
         return lo < hi;
     }
 };
 struct DqRow {                           // a lane's row: token t sees keys first .. t
     int t, head, first;
     bool there;
-    __device__ __forceinline__ DqRow(const CausalParams &C, const RowBlock &B, int kvh)
+    template <bool WIN>
+    __device__ __forceinline__ DqRow(const CausalParams &C, const RowBlock<WIN> &B, int kvh)
     {
         const int r = B.row0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31), rt = r / C.group;
         head = kvh * C.group + r - rt * C.group;
@@ -355,10 +372,19 @@ struct DqRow {                           // a lane's row: token t sees keys firs
     }
 };
 
+template <bool WIN>
+__device__ __forceinline__ std::conditional_t<WIN, SeesWindow, SeesUpTo> seen_by(const CausalParams &C, const DqRow &row)
+{
+    if constexpr (WIN)
+        return SeesWindow(C, row.first, row.t);
+    else
+        return SeesUpTo{row.first, row.t};
+}
+
 // Rows whose dQ is not finite once more, where keys that they do not see can have been the reason: by products with 0 (K, V not finite) or by a
 // dP that is infinite.  (A row whose lse or delta is not finite has no other result.)
-template <int TILES>
-__device__ __forceinline__ void dq_again(const GradParams &P, const RowBlock &B, const DqRow &row, int kvh, bool odd, int tile)
+template <int TILES, bool WIN>
+__device__ __forceinline__ void dq_again(const GradParams &P, const RowBlock<WIN> &B, const DqRow &row, int kvh, bool odd, int tile)
 {
     const CausalParams &C = P.c;
     odd = odd_row(odd);
@@ -376,16 +402,25 @@ __device__ __forceinline__ void dq_again(const GradParams &P, const RowBlock &B,
     V.base = reinterpret_cast<const unsigned char *>(static_cast<const __bf16 *>(C.V) + kvh * C.v_head);
     V.row_bytes = C.v_token * 2;
     int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
-    edges(row.there, row.first, row.t, &f_min, &f_max, &l_min, &l_max);
-    const int front = B.lo + max(0, (f_min - B.lo) / BKV) * BKV, behind = min(B.hi, B.lo + ((l_max - B.lo) / BKV + 1) * BKV);
+    const auto sees = seen_by<WIN>(C, row);
+    int sinks_end = B.lo;                                            // (with a window the tiles with first keys too, of which rows see some)
+    if constexpr (WIN) {
+        edges(row.there, sees.from, row.t, &f_min, &f_max, &l_min, &l_max);
+        sinks_end = (int)min((int64_t)B.hi, B.lo + (int64_t)B.gap.front * BKV);
+    } else {
+        edges(row.there, row.first, row.t, &f_min, &f_max, &l_min, &l_max);
+    }
+    const int front = B.lo + (WIN ? B.gap.key(B.gap.front) : max(0, (f_min - B.lo) / BKV) * BKV), behind = min(B.hi, B.lo + ((l_max - B.lo) / BKV + 1) * BKV);
     const int seen_by_all = min(f_max, B.hi), unseen = max(l_min + 1, B.lo);   // front .. seen_by_all, unseen .. behind: keys that some rows do not see
     if (__builtin_amdgcn_ballot_w64(odd) == 0 || (__builtin_amdgcn_ballot_w64(odd && large_row(g)) == 0 && !any_large(K, front, seen_by_all) &&
-                                                  !any_large(V, front, seen_by_all) && !any_large(K, unseen, behind) && !any_large(V, unseen, behind)))
+                                                  !any_large(V, front, seen_by_all) && !any_large(K, unseen, behind) && !any_large(V, unseen, behind) &&
+                                                  !(WIN && (any_large(K, B.lo, sinks_end) || any_large(V, B.lo, sinks_end)))))
         return;
-    grad_again<false, TILES>(P, kvh, static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head, g, row.first, t + 1, lse, delta, false, odd,
+    grad_again<false, TILES>(P, kvh, static_cast<const __bf16 *>(C.Q) + (int64_t)t * C.q_token + head * C.q_head, g, sees, lse, delta, false, odd,
                       static_cast<__bf16 *>(P.dq) + (int64_t)t * C.q_token + head * C.q_head, tile);
 }
 
+template <bool WIN>
 __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
@@ -397,7 +432,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lh = lane >> 5;
 
-    RowBlock block(C);
+    RowBlock<WIN> block(C);
     if (!my_item<NT, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
@@ -408,9 +443,19 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int t = row.t, head = row.head, first = row.first;
     const bool there = row.there;
     int wt0 = kt0, wt1 = kt0, all_from = 0, all_to = 0;
+    const auto sees = seen_by<WIN>(C, row);
     {
         int f_min, f_max, l_min, l_max;
-        if (edges(there, first, t, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+        if constexpr (WIN) {
+            int low, unused;
+            if (edges(there, sees.from, t, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
+                edges(there, C.sinks > 0 ? first : sees.from, t, &low, &unused, &unused, &unused);
+                all_from = f_max - lo;
+                all_to = l_min - lo;
+                wt0 = max(kt0, block.gap.tile(low - lo));
+                wt1 = min(nkt, block.gap.tile(l_max - lo) + 1);
+            }
+        } else if (edges(there, first, t, &f_min, &f_max, &l_min, &l_max) && l_max >= f_min) {
             all_from = f_max - lo;
             all_to = l_min - lo;
             wt0 = max(kt0, (f_min - lo) / BKV);
@@ -426,7 +471,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const unsigned k_off = (unsigned)(ld_row * k_row) + swizzled, v_off = (unsigned)(ld_row * v_row) + swizzled;
     const unsigned char *kb = static_cast<const unsigned char *>(C.K) + kvh * C.k_head * 2, *vb = static_cast<const unsigned char *>(C.V) + kvh * C.v_head * 2;
     auto issue = [&](int unit) __attribute__((always_inline)) {
-        const int key = lo + unit * 32, left = hi - key < 32 ? hi - key : 32;
+        const int key = lo + block.place_of_unit(unit), left = hi - key < 32 ? hi - key : 32;
         const unsigned rows = left > 0 ? (unsigned)left : 0u, lds = lds_base + (unit & 3) * UNIT_BYTES + wave * 1024;
         const i32x4_t k = make_rsrc(kb + (int64_t)key * k_row, rows * (unsigned)k_row), v = make_rsrc(vb + (int64_t)key * v_row, rows * (unsigned)v_row);
 #pragma unroll
@@ -484,14 +529,23 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     // col_read at unit u.
     auto unit = [&](int u, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn) __attribute__((always_inline)) {
         constexpr int AHEAD = 3;
-        if (u * 32 < all_from || (u + 1) * 32 - 1 > all_to) {        // border, uniform
+        const int place = block.place_of_unit(u);
+        if (place < all_from || place + 31 > all_to) {               // border, uniform
             float ninf = -INFINITY;
             asm volatile("" : "+v"(ninf));
-            const unsigned key0 = (unsigned)(lo + u * 32 + 4 * lh - first), span = (unsigned)(t - first);
+            if constexpr (WIN) {
+                const int key0 = lo + place + 4 * lh;
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (key0 + (unsigned)(8 * (e >> 2) + (e & 3)) > span)
-                    s[e] = ninf;
+                for (int e = 0; e < 16; ++e)
+                    if (!sees(key0 + 8 * (e >> 2) + (e & 3)))
+                        s[e] = ninf;
+            } else {
+                const unsigned key0 = (unsigned)(lo + place + 4 * lh - first), span = (unsigned)(t - first);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (key0 + (unsigned)(8 * (e >> 2) + (e & 3)) > span)
+                        s[e] = ninf;
+            }
         }
         bf16x8_t frag[AHEAD + 1], df[2];
         auto fetch = [&](auto s_tag) __attribute__((always_inline)) {
@@ -598,15 +652,16 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
 #pragma unroll
     for (int d = 0; d < DT; ++d)
         odd = store_tile(acc[d], C.scale, out, d, there) || odd;
-    dq_again<DT>(P, block, row, kvh, odd, 0);
+    dq_again<DT, WIN>(P, block, row, kvh, odd, 0);
 }
 
 // Workgroup `at` of the sums over the splits of dQ: one feature tile of one block.
+template <bool WIN>
 __device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked_at)
 {
     const CausalParams &C = P.c;
     const int tile = at % DT, group = at / DT, kvh = group % C.kv_heads;
-    RowBlock block(C);
+    RowBlock<WIN> block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
     Splits<256, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
@@ -615,12 +670,13 @@ __device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked
     const DqRow row(C, block, kvh);
     const f32x16_t x = sum_of_parts<64 * DQ_WAVES>(C, DT * 16, block.it, tile);
     const bool odd = store_tile(x, C.scale, static_cast<__bf16 *>(P.dq) + (int64_t)row.t * C.q_token + row.head * C.q_head, tile, row.there);
-    dq_again<1>(P, block, row, kvh, odd, tile);
+    dq_again<1, WIN>(P, block, row, kvh, odd, tile);
 }
 
 constexpr int GRAD_KEYS = 128;           // keys of a workgroup of the second launch: four waves of 32
 constexpr int GRAD_ROWS = 64;            // rows per tile
 // Its keys [begin, k1), and the walk over rows [lo, hi) = (token, head of the group), tokens [begin, end_b)
+template <bool WIN>
 struct KeyBlock {
     const Sequences seqs;
     int blocks;                          // of one key head
@@ -631,18 +687,28 @@ struct KeyBlock {
         const int last = seqs.end_of(C.n_seqs - 1);
         return last < C.tokens ? last : C.tokens;
     }
+    // Where the rows end that see any key of the block; the last key, `last`, is of the sequence [start, end), `from` the block's first.  With a window only
+    // a sequence's first keys are seen to its end (and of the sequences that end in the block no row lies behind it).
+    __device__ __forceinline__ int rows_end(const CausalParams &C, int from, int last, int start, int end) const
+    {
+        if constexpr (WIN)
+            return max(from - start, 0) < C.sinks || end - last < C.window ? end : last + C.window;
+        return end;
+    }
     __device__ __forceinline__ int tiles_of(const CausalParams &C, int block) const
     {
         const int a = block * GRAD_KEYS, s = seqs.start_of(0), b = a + GRAD_KEYS < stop(C) ? a + GRAD_KEYS : stop(C), from = s > a ? s : a;
         int start, end;
         seqs.around(b - 1, &start, &end);
         end = end < C.tokens ? end : C.tokens;
+        end = rows_end(C, from, b - 1, start, end);
         return from < b && end > from ? (int)(((int64_t)(end - from) * C.group + GRAD_ROWS - 1) / GRAD_ROWS) : 0;
     }
     __device__ __forceinline__ KeyBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((C.tokens + GRAD_KEYS - 1) / GRAD_KEYS) {}
     __device__ __forceinline__ int bound(const CausalParams &C) const
     {
-        return C.items > 0 ? (int)min((int64_t)0x7FFFFFFF, ((int64_t)(seqs.longest() + GRAD_KEYS + 1) * C.group + GRAD_ROWS) / GRAD_ROWS) : 0;
+        const int seen = C.items > 0 ? seqs.longest() : 0, tokens = WIN && C.sinks == 0 && C.window < seen ? C.window : seen;
+        return C.items > 0 ? (int)min((int64_t)0x7FFFFFFF, ((int64_t)(tokens + GRAD_KEYS + 1) * C.group + GRAD_ROWS) / GRAD_ROWS) : 0;
     }
     // the keys and the walk of it.block; false: nothing to do
     __device__ __forceinline__ bool look(const CausalParams &C)
@@ -659,6 +725,7 @@ struct KeyBlock {
         end_b = seqs.end_of(seq_b) < C.tokens ? seqs.end_of(seq_b) : C.tokens;
         if (end_b <= begin)
             return false;
+        end_b = rows_end(C, begin, k1 - 1, seqs.start_of(seq_b), end_b);
         lo = begin * C.group;
         hi = end_b * C.group;
         tiles = (int)(((int64_t)hi - lo + GRAD_ROWS - 1) / GRAD_ROWS);
@@ -668,7 +735,20 @@ struct KeyBlock {
 struct GradKey {                         // a lane's key, seen by tokens key .. end - 1 of its sequence
     int key, end;
     bool there;
-    __device__ __forceinline__ GradKey(const CausalParams &C, const KeyBlock &B)
+    // the wave's edges of rows [first, last); with a window a sequence's first keys are seen by more rows than those behind them
+    template <bool WIN>
+    __device__ __forceinline__ bool wave_edges(int first, int last, int *f_min, int *f_max, int *l_min, int *l_max) const
+    {
+        if (!edges(there, first, last, f_min, f_max, l_min, l_max))
+            return false;
+        if constexpr (WIN) {
+            *l_min = least_of(there ? last : 0x7FFFFFFF);
+            *l_max = most_of(there ? last : -1);
+        }
+        return true;
+    }
+    template <bool WIN>
+    __device__ __forceinline__ GradKey(const CausalParams &C, const KeyBlock<WIN> &B)
     {
         const int k = B.k0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
         there = k >= B.begin && k < B.k1;
@@ -677,14 +757,16 @@ struct GradKey {                         // a lane's key, seen by tokens key .. 
         const int a = B.seqs.between(B.seq_a, B.seq_b, key, &start, &end);
         end = a < C.n_seqs ? end : 0;
         end = end < B.end_b ? end : B.end_b;
+        if constexpr (WIN)
+            end = key - start < C.sinks || end - key <= C.window ? end : key + C.window;
         there = there && end > key;
     }
 };
 
 // Keys whose dK or dV is not finite once more, where rows that do not see them can have been the reason: by products with 0 (Q, dout not finite), an
 // infinite dP, or an lse or delta that is not finite.
-template <int TILES>
-__device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock &B, const GradKey &mine, int kvh, bool odd_k, bool odd_v, int tile)
+template <int TILES, bool WIN>
+__device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock<WIN> &B, const GradKey &mine, int kvh, bool odd_k, bool odd_v, int tile)
 {
     const CausalParams &C = P.c;
     odd_k = odd_row(odd_k);
@@ -711,7 +793,7 @@ __device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock &B
         return false;
     };
     int f_min = 0, f_max = 0, l_min = 0, l_max = 0;
-    edges(mine.there, first, end, &f_min, &f_max, &l_min, &l_max);
+    mine.wave_edges<WIN>(first, end, &f_min, &f_max, &l_min, &l_max);
     const int front = lo + max(0, (f_min - lo) / GRAD_ROWS) * GRAD_ROWS, tiles = (l_max - lo + GRAD_ROWS - 1) / GRAD_ROWS;
     const int behind = tiles < B.tiles ? lo + tiles * GRAD_ROWS : hi;
     if (__builtin_amdgcn_ballot_w64((odd_k || odd_v) && large_row(v)) == 0 && !any_odd(front, min(f_max, hi)) && !any_odd(max(l_min, lo), behind))
@@ -720,7 +802,7 @@ __device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock &B
     for (int values = 0; values < 2; ++values) {                     // dK, dV
         const bool odd = values ? odd_v : odd_k;
         if (__builtin_amdgcn_ballot_w64(odd) != 0)
-            grad_again<true, TILES>(P, kvh, k, v, first, end, 0.0f, 0.0f, values, odd, values ? static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head
+            grad_again<true, TILES>(P, kvh, k, v, SeesUpTo{first, end - 1}, 0.0f, 0.0f, values, odd, values ? static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head
                                                                                        : static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head, tile);
     }
 }
@@ -728,6 +810,7 @@ __device__ __forceinline__ void dkv_again(const GradParams &P, const KeyBlock &B
 // What stands for rows behind a walk: a probability of 0 times anything else of them would be NaN where that is not finite.
 __device__ const __attribute__((aligned(16))) char zero_row[ROWB] = {};
 
+template <bool WIN>
 __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
 {
     const CausalParams &C = P.c;
@@ -741,7 +824,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int lh = lane >> 5;
     const int G = C.group;
 
-    KeyBlock block(C);
+    KeyBlock<WIN> block(C);
     if (!my_item<NT, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
@@ -755,7 +838,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     int wr0 = rt0, wr1 = rt0, all_from = 0, all_to = 0;
     {
         int f_min, f_max, l_min, l_max;
-        if (edges(there, from, to, &f_min, &f_max, &l_min, &l_max) && l_max > f_min) {
+        if (mine.wave_edges<WIN>(from, to, &f_min, &f_max, &l_min, &l_max) && l_max > f_min) {
             all_from = f_max - lo;
             all_to = l_min - lo;
             wr0 = max(rt0, (f_min - lo) / ROWS);
@@ -1022,15 +1105,16 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
         odd_k = store_tile(dk[d], C.scale, out_k, d, there) || odd_k;
         odd_v = store_tile(dv[d], 1.0f, out_v, d, there) || odd_v;
     }
-    dkv_again<DT>(P, block, mine, kvh, odd_k, odd_v, 0);
+    dkv_again<DT, WIN>(P, block, mine, kvh, odd_k, odd_v, 0);
 }
 
 // ... of dK and dV
+template <bool WIN>
 __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looked_at)
 {
     const CausalParams &C = P.c;
     const int tile = at % (2 * DT), group = at / (2 * DT), kvh = group % C.kv_heads;
-    KeyBlock block(C);
+    KeyBlock<WIN> block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
     Splits<256, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
@@ -1041,18 +1125,19 @@ __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looke
     __bf16 *out = tile < DT ? static_cast<__bf16 *>(P.dk) + (int64_t)mine.key * C.k_token + kvh * C.k_head
                             : static_cast<__bf16 *>(P.dv) + (int64_t)mine.key * C.v_token + kvh * C.v_head;
     const bool odd = store_tile(x, tile < DT ? C.scale : 1.0f, out, tile & (DT - 1), mine.there);
-    dkv_again<1>(P, block, mine, kvh, odd && tile < DT, odd && tile >= DT, tile & (DT - 1));
+    dkv_again<1, WIN>(P, block, mine, kvh, odd && tile < DT, odd && tile >= DT, tile & (DT - 1));
 }
 
 // Workgroups below `dkv_wgs`: dK and dV; the others dQ.  (Two launches, 6.3 and 10.1 us for a pack of 4096 tokens and four heads.)
 static_assert(DQ_WAVES == 4, "one shape of workgroup for both");
+template <bool WIN>
 __global__ __launch_bounds__(256, 4) void attn_grad_join_kernel(GradParams dkv, GradParams dq, int dkv_wgs)
 {
     __shared__ int looked_at[MAX_BLOCKS];
     if ((int)blockIdx.x < dkv_wgs)
-        join_dkv(dkv, blockIdx.x, looked_at);
+        join_dkv<WIN>(dkv, blockIdx.x, looked_at);
     else
-        join_dq(dq, (int)blockIdx.x - dkv_wgs, looked_at);
+        join_dq<WIN>(dq, (int)blockIdx.x - dkv_wgs, looked_at);
 }
 
 struct GradLaunches {
@@ -1072,16 +1157,22 @@ GradLaunches plan_grad(const CausalParams &c, int num_cu)
     g.row_blocks = (rows + DQ_ROWS - 1) / DQ_ROWS;
     g.key_blocks = (c.tokens + GRAD_KEYS - 1) / GRAD_KEYS;
     const size_t dq_part = (size_t)64 * 64 * DQ_WAVES * 4, dkv_part = (size_t)128 * 256 * 4;
-    g.dq_wgs = plan_items(g.dq, g.row_blocks, (c.tokens + BKV - 1) / BKV, LEAST_TILES, dq_part, false, num_cu);
-    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, (rows + GRAD_ROWS - 1) / GRAD_ROWS, LEAST_TILES, dkv_part, false, num_cu);
+    // walks at the longest
+    int64_t keys = (c.tokens + BKV - 1) / BKV, seen = (rows + GRAD_ROWS - 1) / GRAD_ROWS;
+    if (c.window > 0) {
+        keys = std::min(keys, ((int64_t)c.window + c.sinks + DQ_ROWS + 3 * BKV) / BKV);
+        if (c.sinks == 0)
+            seen = std::min(seen, ((int64_t)(c.window + GRAD_KEYS + 1) * c.group + GRAD_ROWS) / GRAD_ROWS);
+    }
+    g.dq_wgs = plan_items(g.dq, g.row_blocks, keys, LEAST_TILES, dq_part, false, num_cu);
+    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, seen, LEAST_TILES, dkv_part, false, num_cu);
     const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)g.dkv.items * dkv_part;
     g.bytes = 2 * (((a > b ? a : b) + 255) & ~(size_t)255);
     return g;
 }
 
-}  // namespace
-
-hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_cu)
+template <bool WIN>
+hipError_t launch(const GradParams &p, hipStream_t s, int num_cu)
 {
     const GradLaunches g = plan_grad(p.c, num_cu);
     const int64_t most = (int64_t)1 << 24;                           // workgroups, of 256 threads
@@ -1091,17 +1182,21 @@ hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_c
     GradParams dq = p, dkv = p;
     dq.c = g.dq;
     dkv.c = g.dkv;
-    hipLaunchKernelGGL(attn_dq_kernel, dim3((unsigned)g.dq_wgs), dim3(64 * DQ_WAVES), 0, s, dq);
+    hipLaunchKernelGGL((attn_dq_kernel<WIN>), dim3((unsigned)g.dq_wgs), dim3(64 * DQ_WAVES), 0, s, dq);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(attn_dkv_kernel, dim3((unsigned)g.dkv_wgs), dim3(256), 0, s, dkv);
+    hipLaunchKernelGGL((attn_dkv_kernel<WIN>), dim3((unsigned)g.dkv_wgs), dim3(256), 0, s, dkv);
     e = hipGetLastError();
     if (e != hipSuccess || join_dq + join_dkv == 0)
         return e;
-    hipLaunchKernelGGL(attn_grad_join_kernel, dim3((unsigned)(join_dkv + join_dq)), dim3(256), 0, s, dkv, dq, (int)join_dkv);
+    hipLaunchKernelGGL((attn_grad_join_kernel<WIN>), dim3((unsigned)(join_dkv + join_dq)), dim3(256), 0, s, dkv, dq, (int)join_dkv);
     return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_attn_prompt_grad(const GradParams &p, hipStream_t s, int num_cu) { return p.c.window > 0 ? launch<true>(p, s, num_cu) : launch<false>(p, s, num_cu); }
 
 size_t attn_grad_part_bytes(const CausalParams &p_in, int num_cu)
 {

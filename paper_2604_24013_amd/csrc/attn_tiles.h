@@ -350,6 +350,51 @@ __device__ __forceinline__ bool edges(bool there, int first, int last, int *f_mi
     *l_max = __builtin_amdgcn_readlane(last, b);
     return true;
 }
+// A window: a row whose last key is `last` sees keys last - window + 1 .. last, and the first `sinks` of its sequence.  So a walk goes over the tiles
+// with the first keys, leaves out `gap` keys (whole tiles of KEYS, counted from the walk's first key on), and goes on with the first tile that has
+// keys of its first row's window.
+template <int KEYS>
+struct Gap {
+    int front = 0, keys = 0;             // tiles in front of the gap; what is left out
+    Gap() = default;
+    // a walk over keys [lo, hi) whose first row sees keys window_from and more
+    __device__ __forceinline__ Gap(int sinks, int lo, int hi, int window_from)
+    {
+        const int whole = window_from > lo && hi > lo ? ((window_from < hi ? window_from : hi) - lo) / KEYS : 0;
+        const int some = sinks < hi - lo ? sinks : hi - lo;
+        front = some > 0 ? (int)(((unsigned)some + KEYS - 1) / KEYS) : 0;
+        keys = whole > front ? (whole - front) * KEYS : 0;
+    }
+    __device__ __forceinline__ int key(int tile) const { return tile * KEYS + (tile >= front ? keys : 0); }      // of a tile's first, from the walk's on
+    __device__ __forceinline__ int tile(int key) const { return (key / KEYS) - (key / KEYS >= front ? keys / KEYS : 0); }
+    __device__ __forceinline__ int tiles(int lo, int hi) const { return (hi - lo - keys + KEYS - 1) / KEYS; }
+};
+// The first key of a row's window; `first`: of its sequence.
+__device__ __forceinline__ int window_from(const CausalParams &P, int first, int last)
+{
+    const int from = (last > -1 ? last : -1) - P.window + 1;
+    return from > first ? from : first;
+}
+// What a lane's row sees.
+struct SeesUpTo {
+    int first, last;
+    __device__ __forceinline__ bool operator()(int key) const { return key >= first && key <= last; }
+    __device__ __forceinline__ int lowest() const { return first; }
+    __device__ __forceinline__ bool none_of(int, int) const { return false; }        // (not worth a look)
+};
+struct SeesWindow {
+    int first, last, from;               // of the sequence; of the row; of the window
+    unsigned sinks, window;              // how many: keys first .. and from ..
+    __device__ __forceinline__ SeesWindow(const CausalParams &P, int first_, int last_) : first(first_), last(last_), from(window_from(P, first_, last_))
+    {
+        window = last >= from ? (unsigned)(last - from) + 1 : 0;
+        sinks = last >= first ? min((unsigned)P.sinks, (unsigned)(last - first) + 1) : 0;
+    }
+    __device__ __forceinline__ bool operator()(int key) const { return (unsigned)(key - from) < window || (unsigned)(key - first) < sinks; }
+    __device__ __forceinline__ int lowest() const { return sinks > 0 ? first : from; }
+    __device__ __forceinline__ bool none_of(int a, int b) const { return a > last || (b <= from && a - first >= (int)sinks); }   // keys a .. b - 1
+};
+
 // Where item `first + split` of a block parks what it has: N floats a workgroup.
 __device__ __forceinline__ float *parked_at(const CausalParams &P, const Item &it, int split, size_t floats)
 {
@@ -577,16 +622,16 @@ __device__ __forceinline__ void store_fours(const f32x16_t (&acc)[DH / 32], floa
     }
 }
 
-// Attention of up to 32 rows by one wave, from memory: lane (row = lane & 31, and the same in the other half) sees keys first .. last; results where
+// Attention of up to 32 rows by one wave, from memory: lane (row = lane & 31, and the same in the other half) sees what `sees` says; results where
 // `wanted`: m, l, and O^T as `put_pair` has it.  The wave takes units of 32 keys nth, nth + step, ... from the first that is seen on.
-template <int SRC>
-__device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, int first, int last, bool wanted, float sl2, int nth, int step,
+template <int SRC, typename S>
+__device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &V, const __bf16 *q, const S &sees, bool wanted, float sl2, int nth, int step,
                                            f32x16_t (&acc)[DH / 32], float *max_score, float *sum)
 {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));                                   // (nothing made of it is kept over the walk before)
     const int lq = lane & 31, lh = lane >> 5;
-    const int from = least_of(wanted ? first : 0x7FFFFFFF), to = most_of(wanted ? last : -1);
+    const int from = least_of(wanted ? sees.lowest() : 0x7FFFFFFF), to = most_of(wanted ? sees.last : -1);
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -596,6 +641,9 @@ __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &
 #pragma unroll 1
     for (int64_t at0 = (from & ~31) + 32 * (int64_t)nth; at0 <= to; at0 += 32 * step) {
         const int key0 = (int)at0, mine = key0 + lq < from ? from : key0 + lq < to ? key0 + lq : to;
+        if constexpr (!std::is_same_v<S, SeesUpTo>)
+            if (__builtin_amdgcn_ballot_w64(wanted && !sees.none_of(key0, key0 + 32)) == 0)
+                continue;
         int ek = 0, ev = 0;
         const unsigned char *kr = K.row(mine, &ek), *vr = V.row(mine, &ev);
         const unsigned absent = (unsigned)__builtin_amdgcn_ballot_w64(kr == nullptr);
@@ -621,9 +669,9 @@ __device__ __forceinline__ void rows_again(const Keys<SRC> &K, const Keys<SRC> &
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int at = 8 * (i >> 2) + 4 * lh + (i & 3), key = key0 + at;
-            const bool sees = key >= first && key <= last && !(absent >> at & 1);
-            seen |= (unsigned)sees << i;
-            s[i] = sees ? s[i] * sl2 : -INFINITY;
+            const bool visible = sees(key) && !(absent >> at & 1);
+            seen |= (unsigned)visible << i;
+            s[i] = visible ? s[i] * sl2 : -INFINITY;
             mx = fmaxf(mx, s[i]);
         }
         const float m_new = fmaxf(m, max_of_halves(mx)), alpha = exp2f(m - m_new);

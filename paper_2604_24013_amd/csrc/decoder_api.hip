@@ -405,6 +405,19 @@ cf_status resolve_paged(const cf_cache_desc *cd, const cf_cache *c, const cf_pag
     return CF_OK;
 }
 
+// The window (nullptr: none) of sequences of up to `longest` tokens; where it hides none of them, the kernels without one.
+cf_status resolve_window(const cf_window *w, int64_t longest, cf::CausalParams *p)
+{
+    if (w == nullptr)
+        return CF_FAIL(CF_ERR_NULL_PTR, "window is NULL");
+    if (w->window < 1 || w->sinks < 0)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "window = %d must be at least 1, sinks = %d at least 0", w->window, w->sinks);
+    const bool hides = (int64_t)w->window + w->sinks < longest;
+    p->window = hides ? w->window : 0;
+    p->sinks = hides ? w->sinks : 0;
+    return CF_OK;
+}
+
 cf_status launched(hipError_t e, const char *what)
 {
     return e == hipSuccess ? CF_OK : CF_FAIL(CF_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -736,13 +749,19 @@ cf_status commfuse_step_tables(const cf_tables_desc *d, const cf_tables *t, void
     return launched(cf::launch_step_tables(p, static_cast<hipStream_t>(hip_stream)), "tables launch");
 }
 
-cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *seq_start,
-                               void *out, float *lse, void *hip_stream)
+namespace {
+
+// Packed prompts, with a window or without.
+cf_status attn_prompt(const cf_prompt_desc *desc, bool with_window, const cf_window *window, const void *Q, const void *K, const void *V, const int32_t *seq_start,
+                      void *out, float *lse, void *hip_stream)
 {
     cf::CausalParams p;
     bool nothing;
     if (cf_status st = resolve_prompt(desc, &p, &nothing))
         return st;
+    if (with_window)
+        if (cf_status st = resolve_window(window, p.tokens, &p))
+            return st;
     if (nothing)
         return CF_OK;
     if (Q == nullptr || K == nullptr || V == nullptr || seq_start == nullptr || out == nullptr)
@@ -762,14 +781,16 @@ cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const 
     return launched(cf::launch_attn_prompt(p, s, cf::num_cu()), "attention launch");
 }
 
-cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const void *out,
-                                    const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK,
-                                    void *dV, void *hip_stream)
+cf_status attn_prompt_grad(const cf_prompt_desc *desc, bool with_window, const cf_window *window, const void *Q, const void *K, const void *V, const void *out,
+                           const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK, void *dV, void *hip_stream)
 {
     cf::GradParams p = {};
     bool nothing;
     if (cf_status st = resolve_prompt(desc, &p.c, &nothing))
         return st;
+    if (with_window)
+        if (cf_status st = resolve_window(window, p.c.tokens, &p.c))
+            return st;
     if (nothing)
         return CF_OK;
     const void *const in[] = {Q, K, V, out, lse, dout, seq_start};
@@ -809,24 +830,26 @@ cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, c
     return launched(cf::launch_attn_prompt_grad(p, s, cf::num_cu()), "attention gradient launch");
 }
 
-size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc)
+size_t attn_prompt_workspace_bytes(const cf_prompt_desc *desc, bool with_window, const cf_window *window)
 {
     cf::CausalParams p;
     bool nothing;
-    if (resolve_prompt(desc, &p, &nothing) != CF_OK || nothing)
+    if (resolve_prompt(desc, &p, &nothing) != CF_OK || nothing || (with_window && resolve_window(window, p.tokens, &p) != CF_OK))
         return 0;
     const size_t parts = cf::attn_prompt_part_bytes(p, cf::num_cu());
     return parts > 0 ? cf::WORKSPACE_HEAD_BYTES + parts : 0;
 }
 
-cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const void *Q,
-                              const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out, float *lse,
-                              void *hip_stream)
+cf_status attn_paged(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, bool with_window, const cf_window *window, const void *Q,
+                     const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out, float *lse, void *hip_stream)
 {
     cf::CausalParams p;
     bool nothing;
     if (cf_status st = resolve_paged(cache_desc, cache, desc, &p, &nothing))
         return st;
+    if (with_window)
+        if (cf_status st = resolve_window(window, p.max_kv, &p))
+            return st;
     if (nothing)
         return CF_OK;
     if (Q == nullptr || q_start == nullptr || kv_len == nullptr || (page_table == nullptr && desc->max_pages > 0) || out == nullptr)
@@ -846,16 +869,67 @@ cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *c
     return launched(cf::attn_few_takes(p) ? cf::launch_attn_few(p, s, cf::num_cu()) : cf::launch_attn_paged_blocks(p, s, cf::num_cu()), "attention launch");
 }
 
-size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc)
+size_t attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc, bool with_window, const cf_window *window)
 {
     cf_cache any = {};
     any.k = any.v = any.k_exp = any.v_exp = reinterpret_cast<uint8_t *>(256);      // (of the pool's geometry, addresses are not looked at)
     cf::CausalParams p;
     bool nothing;
-    if (resolve_paged(cache_desc, &any, desc, &p, &nothing) != CF_OK || nothing)
+    if (resolve_paged(cache_desc, &any, desc, &p, &nothing) != CF_OK || nothing || (with_window && resolve_window(window, p.max_kv, &p) != CF_OK))
         return 0;
     const size_t parts = cf::attn_few_takes(p) ? cf::attn_few_part_bytes(p, cf::num_cu()) : cf::attn_paged_blocks_part_bytes(p, cf::num_cu());
     return parts > 0 ? cf::WORKSPACE_HEAD_BYTES + parts : 0;
+}
+
+}  // namespace
+
+cf_status commfuse_attn_prompt(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *seq_start, void *out, float *lse, void *hip_stream)
+{
+    return attn_prompt(desc, false, nullptr, Q, K, V, seq_start, out, lse, hip_stream);
+}
+
+cf_status commfuse_attn_prompt_window(const cf_prompt_desc *desc, const cf_window *window, const void *Q, const void *K, const void *V, const int32_t *seq_start,
+                                      void *out, float *lse, void *hip_stream)
+{
+    return attn_prompt(desc, true, window, Q, K, V, seq_start, out, lse, hip_stream);
+}
+
+cf_status commfuse_attn_prompt_grad(const cf_prompt_desc *desc, const void *Q, const void *K, const void *V, const void *out, const float *lse, const void *dout,
+                                    const int32_t *seq_start, float *delta, void *dQ, void *dK, void *dV, void *hip_stream)
+{
+    return attn_prompt_grad(desc, false, nullptr, Q, K, V, out, lse, dout, seq_start, delta, dQ, dK, dV, hip_stream);
+}
+
+cf_status commfuse_attn_prompt_window_grad(const cf_prompt_desc *desc, const cf_window *window, const void *Q, const void *K, const void *V, const void *out,
+                                           const float *lse, const void *dout, const int32_t *seq_start, float *delta, void *dQ, void *dK, void *dV, void *hip_stream)
+{
+    return attn_prompt_grad(desc, true, window, Q, K, V, out, lse, dout, seq_start, delta, dQ, dK, dV, hip_stream);
+}
+
+size_t commfuse_attn_prompt_workspace_bytes(const cf_prompt_desc *desc) { return attn_prompt_workspace_bytes(desc, false, nullptr); }
+
+size_t commfuse_attn_prompt_window_workspace_bytes(const cf_prompt_desc *desc, const cf_window *window) { return attn_prompt_workspace_bytes(desc, true, window); }
+
+cf_status commfuse_attn_paged(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const void *Q, const int32_t *q_start,
+                              const int32_t *kv_len, const int32_t *page_table, void *out, float *lse, void *hip_stream)
+{
+    return attn_paged(cache_desc, cache, desc, false, nullptr, Q, q_start, kv_len, page_table, out, lse, hip_stream);
+}
+
+cf_status commfuse_attn_paged_window(const cf_cache_desc *cache_desc, const cf_cache *cache, const cf_paged_desc *desc, const cf_window *window, const void *Q,
+                                     const int32_t *q_start, const int32_t *kv_len, const int32_t *page_table, void *out, float *lse, void *hip_stream)
+{
+    return attn_paged(cache_desc, cache, desc, true, window, Q, q_start, kv_len, page_table, out, lse, hip_stream);
+}
+
+size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc)
+{
+    return attn_paged_workspace_bytes(cache_desc, desc, false, nullptr);
+}
+
+size_t commfuse_attn_paged_window_workspace_bytes(const cf_cache_desc *cache_desc, const cf_paged_desc *desc, const cf_window *window)
+{
+    return attn_paged_workspace_bytes(cache_desc, desc, true, window);
 }
 
 }  // extern "C"

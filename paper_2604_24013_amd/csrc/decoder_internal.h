@@ -118,6 +118,7 @@ struct CausalParams {
     CachePool pool;
     const int32_t *kv_len, *table;
     int max_q, max_kv, max_pages;
+    int window = 0, sinks = 0;                      // a row sees the last `window` keys up to its own and the first `sinks` (0: all up to its own)
     // a walk's tiles split over workgroups
     int items = 0;                                  // workgroups of the launch at the most (0: one for each block and key head)
     int chunk = 0;                                  // tiles of a split (0: as few as the items allow)
