@@ -253,9 +253,8 @@ cf_status resolve_norm(const cf_head_norm *norm, const void *wq, const void *wk,
             return CF_FAIL(CF_ERR_INVALID_ARG, "reserved = %d", norm->reserved);
         if (!(norm->eps >= 1e-30f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset))
             return CF_FAIL(CF_ERR_INVALID_ARG, "need a finite eps of at least 1e-30 and a finite offset");
-        const uintptr_t to = norm->weight_dtype == CF_BF16 ? 2 : 4;
-        if (!aligned(wq, to) || !aligned(wk, to))
-            return CF_FAIL(CF_ERR_MISALIGNED, "weights must be aligned to their type");
+        if (!aligned(wq, 16) || !aligned(wk, 16))
+            return CF_FAIL(CF_ERR_MISALIGNED, "weights must be 16-byte aligned");
         n.on = true;
         n.wq = wq;
         n.wk = wk;
@@ -631,7 +630,9 @@ cf_status commfuse_norm_rope(const cf_rope_axes *rope, const cf_head_norm *norm,
 
 size_t commfuse_norm_rope_scratch_bytes(const cf_head_rows *rows)
 {
-    return rows == nullptr || rows->head_dim < 8 || rows->head_dim > 256 ? 0 : cf::norm_rope_scratch_bytes(rows->head_dim);
+    if (rows == nullptr || rows->head_dim < 8 || rows->head_dim > 256 || rows->heads < 0 || rows->kv_heads < 0)
+        return 0;
+    return cf::norm_rope_scratch_bytes(rows->head_dim, (unsigned)rows->heads + (unsigned)rows->kv_heads);
 }
 
 cf_status commfuse_norm_rope_grad(const cf_rope_axes *rope, const cf_head_norm *norm, const cf_head_rows *rows, const void *Q, const void *K, const void *wq,

@@ -76,7 +76,7 @@ struct HeadParams {
     NormParams norm;
     int head_dim;
     unsigned tokens, heads, kv_heads;
-    unsigned lanes, groups;                         // lanes of a head; a thread takes rows g, g + groups, ... of its token
+    unsigned lanes, groups, subs_shift;             // lanes of a head; workgroups that share out the heads of some tokens; jobs of a head (their logarithm)
     const void *q, *k;
     void *q_out, *k_out;
     const int32_t *positions;
@@ -86,7 +86,7 @@ hipError_t launch_norm_rope(const HeadParams &p, bool bf16, hipStream_t s, int n
 // dq_out, dk_out with the strides of q_out, k_out; dq, dk with those of q, k; dwq, dwk: null = not wanted
 hipError_t launch_norm_rope_grad(const HeadParams &p, const void *dq_out, const void *dk_out, void *dq, void *dk, float *dwq, float *dwk, float *scratch,
                                  bool bf16, hipStream_t s, int num_cu);
-size_t norm_rope_scratch_bytes(int head_dim);
+size_t norm_rope_scratch_bytes(int head_dim, unsigned heads);
 hipError_t launch_cache_write_norm(const CachePool &c, const CacheRows &r, const AxesRotation &a, const NormParams &n, hipStream_t s, int num_cu);
 
 // A serving step's tables (cf_tables, with the counts resolved).

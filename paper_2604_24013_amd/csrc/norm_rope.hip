@@ -6,49 +6,52 @@
 // Bound by HBM: forward every feature is read and written once, backward x and dy are read and dx is written.  A thread owns a unit of one
 // head (W rotated pairs, or 2 W features that are copied), the lanes of a head are neighbours, a power of two of them, and add up its
 // squares by moves inside the wave.  Nothing is kept for the gradient: r costs less to compute again than to read, since x is read in any
-// case.  Weights, angles and the weights' gradients of a unit stay in its thread's registers over the heads and tokens that it takes.
-// The gradients of the weights are sums over all tokens: every workgroup leaves one for each of its columns in the caller's scratch
-// memory, and a second launch adds those up in order.  No atomics: the same call gives the same bits.
+// case.
+// A workgroup takes some tokens, and its waves share out jobs of one head of as many tokens as fill a wave, each with two jobs on their way from memory:
+// nine heads of sixteen tokens are nine jobs a wave.  Cosines and sines of its tokens are computed once by all threads together and come from
+// LDS: for every wave anew they took more than half of the vector instructions (64-bit products and two series a pair).  So do the weights.
+// The gradients of the weights are sums over all tokens: every workgroup leaves one row of them in the caller's scratch memory, and a second
+// launch adds those up in order.  No atomics: the same call gives the same bits.
 #include "rope_units.h"
 
 namespace cf {
 namespace {
 
-// Cosine and sine of the W pairs from `j` on, of which each has an axis of its own: two bits of `axis`.
-template <int W>
-__device__ __forceinline__ void angles_of_axes(const AxesRotation &R, int j, const int32_t *positions, unsigned token, float sign, float (&c)[W], float (&s)[W])
-{
-    int32_t p[4];
-#pragma unroll
-    for (int a = 0; a < 4; ++a)
-        p[a] = a < R.n_axes ? positions[a * R.position_axis + token] : 0;
-    const unsigned which = R.axis_bits[j >> 4] >> 2 * (j & 15);      // (W divides 16: a unit's pairs lie in one word)
-    const float factor = R.magnitude;
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const unsigned a = which >> 2 * e & 3;
-        const int32_t position = a & 2 ? (a & 1 ? p[3] : p[2]) : (a & 1 ? p[1] : p[0]);
-        float ce[1], se[1];
-        angles<1>(R.turn, j + e, position, factor, sign * factor, ce, se);
-        c[e] = ce[0];
-        s[e] = se[0];
+constexpr unsigned WAVES = THREADS / 64;
+constexpr int MAX_DIM = 256;             // features of a head
+
+// Cosines and sines of the tokens of a workgroup, [tokens][pairs] of each, found by all its threads.  (64 lanes hold the heads of a job, so that there are 64 W PER
+// pairs of its tokens at the most.)  Two buffers: the next tokens' are written while the last ones' may still be read.
+constexpr int MAX_SUBS = 4;              // jobs of a head
+template <int W, int PER>
+struct AngleTable {
+    static constexpr int SIZE = MAX_SUBS * 64 * W * PER;
+    float c[2][SIZE] __attribute__((aligned(16))), s[2][SIZE] __attribute__((aligned(16)));
+    __device__ __forceinline__ void fill(int buf, const AxesRotation &R, const int32_t *positions, unsigned first, unsigned per_block, unsigned tokens, float sign)
+    {
+        const unsigned pairs = (unsigned)R.rot_dim / 2;
+        for (unsigned i = threadIdx.x; i < per_block * pairs; i += THREADS) {
+            const unsigned t = i / pairs, j = i - t * pairs, axis = R.axis_bits[j >> 4] >> 2 * (j & 15) & 3;
+            const unsigned token = first + t < tokens ? first + t : tokens - 1;
+            cos_sin(phase_of(R.turn[j], positions[axis * R.position_axis + token]), R.magnitude, sign * R.magnitude, &c[buf][i], &s[buf][i]);
+        }
     }
-}
+};
+
+template <int CONTROL>
+__device__ __forceinline__ float moved(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true)); }
 
 // Sum over the `lanes` neighbouring lanes (a power of two) of a head; every one of them gets it.
 __device__ __forceinline__ float sum_of_lanes(float x, unsigned lanes)
 {
-    auto moved = [](float y, auto control) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), decltype(control)::value, 0xf, 0xf, true));
-    };
     if (lanes > 1)
-        x += moved(x, std::integral_constant<int, 0xB1>{});          // from the other lane of a pair
+        x += moved<0xB1>(x);                                         // from the other lane of a pair
     if (lanes > 2)
-        x += moved(x, std::integral_constant<int, 0x4E>{});          // ... pair of four
+        x += moved<0x4E>(x);                                         // ... pair of four
     if (lanes > 4)
-        x += moved(x, std::integral_constant<int, 0x141>{});         // ... four of eight (mirrored)
+        x += moved<0x141>(x);                                        // ... four of eight (mirrored)
     if (lanes > 8)
-        x += moved(x, std::integral_constant<int, 0x140>{});         // ... eight of sixteen (mirrored)
+        x += moved<0x140>(x);                                        // ... eight of sixteen (mirrored)
     if (lanes > 16)
         x += __shfl_xor(x, 16);
     if (lanes > 32)
@@ -56,43 +59,7 @@ __device__ __forceinline__ float sum_of_lanes(float x, unsigned lanes)
     return x;
 }
 
-// One over the root mean square of a head's features, of which a lane holds N.  Squares of more than 2^128 together: scaled down first.
-template <int N>
-__device__ __forceinline__ float inverse_root(const float (&x)[N], unsigned lanes, int head_dim, float eps)
-{
-    float ss = 0.0f;
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-        ss = __builtin_fmaf(x[e], x[e], ss);
-    ss = sum_of_lanes(ss, lanes);
-    const float inv_dim = 1.0f / head_dim;
-    float r = 1.0f / sqrtf(__builtin_fmaf(ss, inv_dim, eps));
-    if (ss == INFINITY) {                                            // (the same in all lanes of a head)
-        float small = 0.0f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float y = x[e] * 0x1p-70f;
-            small = __builtin_fmaf(y, y, small);
-        }
-        r = 0x1p-70f / sqrtf(sum_of_lanes(small, lanes) * inv_dim);
-    }
-    return r;
-}
-
-// The weights of a thread's units, as factors: (offset + w), or 1 without weights.
-template <int W, int PER>
-__device__ __forceinline__ void load_factors(const NormParams &N, const void *w, const Unit (&at)[PER], const bool (&mine)[PER], float (&f)[PER][2 * W])
-{
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-#pragma unroll
-        for (int e = 0; e < 2 * W; ++e) {
-            const int i = e < W ? at[k].a + e : at[k].b + e - W;
-            f[k][e] = !mine[k] ? 0.0f : w == nullptr ? 1.0f : N.offset + (N.weight_bf16 ? (float)static_cast<const __bf16 *>(w)[i] : static_cast<const float *>(w)[i]);
-        }
-}
-
-// What every kernel here has of its thread: the lane of a head, and its units (PER, `lanes` apart; those behind the head's last are not there).
+// What a thread has of a head: the lane, and its units (PER, `lanes` apart; those behind the head's last are not there).
 template <int W, int PER>
 struct HeadLane {
     unsigned lanes, u;
@@ -106,21 +73,62 @@ struct HeadLane {
             at[k] = unit_at<W>(mine[k] ? u + k * lanes : 0, rot_dim, interleaved);
         }
     }
+    __device__ __forceinline__ int feature(int k, int e) const { return e < W ? at[k].a + e : at[k].b + e - W; }
 };
 
-template <typename T, int W, int PER>
-__device__ __forceinline__ void load_units(const T *row, const HeadLane<W, PER> &L, float (&v)[PER][2 * W])
+// One over the root mean square of a head, of which a lane's units hold PER times N features.  Squares of more than 2^128 together: scaled down first.
+template <int W, int PER>
+__device__ __forceinline__ float inverse_root(const HeadLane<W, PER> &L, const float (&x)[PER][2 * W], float inv_dim, float eps)
 {
+    float all = 0.0f, most = 0.0f;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        if (L.mine[k])
-            load_unit<T, W>(row, L.at[k], v[k]);
-        else
+        float ss = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2 * W; ++e)
-                v[k][e] = 0.0f;
+        for (int e = 0; e < 2 * W; ++e)
+            ss = __builtin_fmaf(x[k][e], x[k][e], ss);
+        all += L.mine[k] ? ss : 0.0f;
     }
+    const float ss = sum_of_lanes(all, L.lanes);
+    float r = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, inv_dim, eps));
+    if (__builtin_amdgcn_ballot_w64(ss == INFINITY) != 0) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int e = 0; e < 2 * W; ++e) {
+                const float y = x[k][e] * 0x1p-70f;
+                most = L.mine[k] ? __builtin_fmaf(y, y, most) : most;
+            }
+        r = ss == INFINITY ? 0x1p-70f * __builtin_amdgcn_rsqf(sum_of_lanes(most, L.lanes) * inv_dim) : r;
+    }
+    return r;
 }
+
+// A thread's part of a head as it comes from memory.
+template <typename T, int W, int PER>
+struct Raw {
+    typedef T V __attribute__((ext_vector_type(W)));
+    V a[PER], b[PER];
+    __device__ __forceinline__ void load(const T *row, const HeadLane<W, PER> &L)
+    {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {                              // (a unit that is not there: the head's first)
+            a[k] = *reinterpret_cast<const V *>(row + L.at[k].a);
+            b[k] = *reinterpret_cast<const V *>(row + L.at[k].b);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[PER][2 * W]) const
+    {
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                v[k][e] = (float)a[k][e];
+                v[k][W + e] = (float)b[k][e];
+            }
+    }
+};
+
 template <typename T, int W, int PER>
 __device__ __forceinline__ void store_units(T *row, const HeadLane<W, PER> &L, const float (&v)[PER][2 * W])
 {
@@ -129,14 +137,38 @@ __device__ __forceinline__ void store_units(T *row, const HeadLane<W, PER> &L, c
         if (L.mine[k])
             store_unit<T, W>(row, L.at[k], v[k]);
 }
+
+// The weights of Q and of K as factors (offset + w), or 1 without weights: in LDS, from where a head takes sixteen at a time (in registers, of both, they
+// would cost a wave's neighbours their place).
 template <int W, int PER>
-__device__ __forceinline__ void find_angles(const AxesRotation &R, const HeadLane<W, PER> &L, const int32_t *positions, unsigned token, float sign, float (&c)[PER][W],
-                                            float (&s)[PER][W])
+struct FactorTable {
+    float f[2][MAX_DIM] __attribute__((aligned(16)));
+    __device__ __forceinline__ void fill(const NormParams &N, int head_dim)
+    {
+        for (int i = threadIdx.x; i < 2 * head_dim; i += THREADS) {
+            const int k = i >= head_dim, at = k ? i - head_dim : i;
+            const void *w = k ? N.wk : N.wq;
+            f[k][at] = w == nullptr ? 1.0f : N.offset + (N.weight_bf16 ? (float)static_cast<const __bf16 *>(w)[at] : static_cast<const float *>(w)[at]);
+        }
+    }
+    __device__ __forceinline__ void read(int of, const HeadLane<W, PER> &L, float (&x)[PER][2 * W]) const
+    {
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            load_unit<float, W>(f[of], L.at[k], x[k]);
+    }
+};
+
+// A thread's cosines and sines of token `t` of the workgroup's.
+template <int W, int PER>
+__device__ __forceinline__ void read_angles(const AngleTable<W, PER> &T, int buf, const HeadLane<W, PER> &L, unsigned t, unsigned pairs, float (&c)[PER][W], float (&s)[PER][W])
 {
 #pragma unroll
     for (int k = 0; k < PER; ++k)
-        if (L.mine[k] && L.at[k].rotated)
-            angles_of_axes<W>(R, L.at[k].pair, positions, token, sign, c[k], s[k]);
+        if (L.mine[k] && L.at[k].rotated) {
+            load<float, W>(&T.c[buf][t * pairs + L.at[k].pair], c[k]);
+            load<float, W>(&T.s[buf][t * pairs + L.at[k].pair], s[k]);
+        }
 }
 template <int W, int PER>
 __device__ __forceinline__ void turn_units(const HeadLane<W, PER> &L, float (&v)[PER][2 * W], const float (&c)[PER][W], const float (&s)[PER][W], bool interleaved)
@@ -148,10 +180,11 @@ __device__ __forceinline__ void turn_units(const HeadLane<W, PER> &L, float (&v)
 }
 // x becomes (offset + w) x / root(mean x^2 + eps)
 template <int W, int PER>
-__device__ __forceinline__ void norm_units(const NormParams &N, unsigned lanes, int head_dim, float (&v)[PER][2 * W], const float (&f)[PER][2 * W])
+__device__ __forceinline__ void norm_units(const HeadLane<W, PER> &L, float inv_dim, float eps, float (&v)[PER][2 * W], const FactorTable<W, PER> &factors, int of)
 {
-    float (&flat)[PER * 2 * W] = reinterpret_cast<float (&)[PER * 2 * W]>(v);
-    const float r = inverse_root(flat, lanes, head_dim, N.eps);
+    float f[PER][2 * W];
+    factors.read(of, L, f);
+    const float r = inverse_root(L, v, inv_dim, eps);
 #pragma unroll
     for (int k = 0; k < PER; ++k)
 #pragma unroll
@@ -159,202 +192,343 @@ __device__ __forceinline__ void norm_units(const NormParams &N, unsigned lanes, 
             v[k][e] = v[k][e] * r * f[k][e];
 }
 
-template <typename T, int W, int PER>
-__global__ __launch_bounds__(THREADS) void norm_rope_kernel(HeadParams P)
+// use(i, what load(i) asked for) for i = first, first + step, .. below count with two of them on their way; `before` behind the first two loads.
+template <typename F1, typename F2, typename F3>
+__device__ __forceinline__ void over_jobs(unsigned first, unsigned count, unsigned step, F1 &&load, F2 &&before, F3 &&use)
 {
-    const HeadLane<W, PER> L(P.lanes, P.head_dim, P.rot.rot_dim, P.rot.interleaved);
-    const unsigned per_block = THREADS / L.lanes, rows = P.heads + P.kv_heads;
-    float fq[PER][2 * W], fk[PER][2 * W];
-    if (P.norm.on) {
-        load_factors<W, PER>(P.norm, P.norm.wq, L.at, L.mine, fq);
-        load_factors<W, PER>(P.norm, P.norm.wk, L.at, L.mine, fk);
-    }
-    for (unsigned item = blockIdx.x * per_block + threadIdx.x / L.lanes; item < P.tokens * P.groups; item += gridDim.x * per_block) {
-        const unsigned token = item / P.groups, group = item - token * P.groups;
-        float c[PER][W], s[PER][W];
-        find_angles<W, PER>(P.rot, L, P.positions, token, 1.0f, c, s);
-        for (unsigned row = group; row < rows; row += P.groups) {
-            const bool is_k = row >= P.heads;
-            const unsigned h = is_k ? row - P.heads : row;
-            const T *x = is_k ? static_cast<const T *>(P.k) + (int64_t)token * P.k_token + h * P.k_head : static_cast<const T *>(P.q) + (int64_t)token * P.q_token + h * P.q_head;
-            T *out = is_k ? static_cast<T *>(P.k_out) + (int64_t)token * P.ok_token + h * P.ok_head : static_cast<T *>(P.q_out) + (int64_t)token * P.oq_token + h * P.oq_head;
-            float v[PER][2 * W];
-            load_units<T, W, PER>(x, L, v);
-            if (P.norm.on) {
-                if (is_k)
-                    norm_units<W, PER>(P.norm, L.lanes, P.head_dim, v, fk);
-                else
-                    norm_units<W, PER>(P.norm, L.lanes, P.head_dim, v, fq);
-            }
-            turn_units<W, PER>(L, v, c, s, P.rot.interleaved);
-            store_units<T, W, PER>(out, L, v);
-        }
+    const unsigned last = count - 1;
+    auto next = load(first < count ? first : last), then = load(first + step < count ? first + step : last);
+    before();
+#pragma unroll 1
+    for (unsigned i = first; i < count; i += step) {
+        const auto now = next;
+        next = then;
+        if (i + 2 * step < count)
+            then = load(i + 2 * step);
+        use(i, now);
     }
 }
 
-// dQ, dK; and of every workgroup the sums for dwq and dwk, [2][head_dim] floats.
-template <typename T, int W, int PER>
-__global__ __launch_bounds__(THREADS) void norm_rope_grad_kernel(HeadParams P, const void *dq_out, const void *dk_out, void *dq, void *dk, float *sums)
-{
-    const HeadLane<W, PER> L(P.lanes, P.head_dim, P.rot.rot_dim, P.rot.interleaved);
-    const unsigned per_block = THREADS / L.lanes, rows = P.heads + P.kv_heads, slot = threadIdx.x / L.lanes;
-    const float inv_dim = 1.0f / P.head_dim;
-    float fq[PER][2 * W], fk[PER][2 * W], aq[PER][2 * W] = {}, ak[PER][2 * W] = {};
-    if (P.norm.on) {
-        load_factors<W, PER>(P.norm, P.norm.wq, L.at, L.mine, fq);
-        load_factors<W, PER>(P.norm, P.norm.wk, L.at, L.mine, fk);
+// Which jobs a wave takes: first, first + step, .. of the (head, part of the workgroup's tokens) pairs; heads are Q's, then K's (and V's).
+struct Jobs {
+    unsigned first, step, per_job, in_job, sub_shift;
+    unsigned block, rounds, per_block;
+    __device__ __forceinline__ Jobs(unsigned groups, unsigned lanes, unsigned subs_shift)
+    {
+        const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        first = blockIdx.x % groups * WAVES + wave;
+        step = groups * WAVES;
+        block = blockIdx.x / groups;
+        rounds = gridDim.x / groups;
+        per_job = 64 / lanes;
+        in_job = (threadIdx.x & 63) / lanes;
+        sub_shift = subs_shift;
+        per_block = per_job << subs_shift;
     }
-    for (unsigned item = blockIdx.x * per_block + slot; item < P.tokens * P.groups; item += gridDim.x * per_block) {
-        const unsigned token = item / P.groups, group = item - token * P.groups;
-        float c[PER][W], s[PER][W];
-        find_angles<W, PER>(P.rot, L, P.positions, token, -1.0f, c, s);
-        for (unsigned row = group; row < rows; row += P.groups) {
-            const bool is_k = row >= P.heads;
-            const unsigned h = is_k ? row - P.heads : row;
-            const int64_t in = is_k ? (int64_t)token * P.k_token + h * P.k_head : (int64_t)token * P.q_token + h * P.q_head;
-            const int64_t from = is_k ? (int64_t)token * P.ok_token + h * P.ok_head : (int64_t)token * P.oq_token + h * P.oq_head;
-            float g[PER][2 * W], n[PER][2 * W];
-            load_units<T, W, PER>(static_cast<const T *>(is_k ? dk_out : dq_out) + from, L, g);
-            if (P.norm.on)
-                load_units<T, W, PER>(static_cast<const T *>(is_k ? P.k : P.q) + in, L, n);
-            turn_units<W, PER>(L, g, c, s, P.rot.interleaved);
-            if (P.norm.on) {
-                auto norm_grad = [&](const float (&f)[PER][2 * W], float (&a)[PER][2 * W]) __attribute__((always_inline)) {
-                    const float r = inverse_root(reinterpret_cast<float (&)[PER * 2 * W]>(n), L.lanes, P.head_dim, P.norm.eps);
-                    float hn = 0.0f;
+    __device__ __forceinline__ unsigned head(unsigned job) const { return job >> sub_shift; }
+    __device__ __forceinline__ unsigned from(unsigned job) const { return (job & ((1u << sub_shift) - 1)) * per_job; }     // the first token, in the workgroup's
+};
+
+// (INTER, the layout of pairs, is known when the kernels are built: with a branch on it the units came to lie in scratch memory.)
+template <typename T, int W, int PER, bool INTER>
+__global__ __launch_bounds__(THREADS) void norm_rope_kernel(HeadParams P)
+{
+    __shared__ AngleTable<W, PER> table;
+    __shared__ FactorTable<W, PER> factors;
+    const HeadLane<W, PER> L(P.lanes, P.head_dim, P.rot.rot_dim, INTER);
+    const Jobs J(P.groups, P.lanes, P.subs_shift);
+    const unsigned heads = P.heads + P.kv_heads, pairs = P.rot.rot_dim / 2;
+    const float inv_dim = 1.0f / P.head_dim;
+    // (addresses: of a job in scalar registers, and the lane's token behind the first)
+    const int64_t q_in = J.in_job * P.q_token, k_in = J.in_job * P.k_token, q_to = J.in_job * P.oq_token, k_to = J.in_job * P.ok_token;
+    int buf = 0;
+    bool filled = false;                                             // (the weights, once)
+    for (unsigned t0 = J.block * J.per_block; t0 < P.tokens; t0 += J.rounds * J.per_block, buf ^= 1) {
+        over_jobs(
+            J.first, heads << J.sub_shift, J.step,
+            [&](unsigned job) __attribute__((always_inline)) {
+                Raw<T, W, PER> raw;
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                if (t + J.in_job < P.tokens) {
+                    if (i < P.heads)
+                        raw.load(static_cast<const T *>(P.q) + (t * P.q_token + i * P.q_head) + q_in, L);
+                    else
+                        raw.load(static_cast<const T *>(P.k) + (t * P.k_token + (i - P.heads) * P.k_head) + k_in, L);
+                }
+                return raw;
+            },
+            [&]() __attribute__((always_inline)) {
+                if (P.norm.on && !filled)
+                    factors.fill(P.norm, P.head_dim);
+                if (pairs > 0)
+                    table.fill(buf, P.rot, P.positions, t0, J.per_block, P.tokens, 1.0f);
+                if (pairs > 0 || !filled)
+                    __syncthreads();
+                filled = true;
+            },
+            [&](unsigned job, const Raw<T, W, PER> &raw) __attribute__((always_inline)) {
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                if (t + J.in_job >= P.tokens)
+                    return;
+                const bool is_k = i >= P.heads;                      // (uniform)
+                float v[PER][2 * W], c[PER][W], s[PER][W];
+                raw.get(v);
+                if (P.norm.on)
+                    norm_units<W, PER>(L, inv_dim, P.norm.eps, v, factors, is_k);
+                read_angles<W, PER>(table, buf, L, J.from(job) + J.in_job, pairs, c, s);
+                turn_units<W, PER>(L, v, c, s, INTER);
+                if (is_k)
+                    store_units<T, W, PER>(static_cast<T *>(P.k_out) + (t * P.ok_token + (i - P.heads) * P.ok_head) + k_to, L, v);
+                else
+                    store_units<T, W, PER>(static_cast<T *>(P.q_out) + (t * P.oq_token + i * P.oq_head) + q_to, L, v);
+            });
+    }
+}
+
+// dQ, dK; and of every workgroup a row of sums for the weights of both, [2][head_dim] floats.
+template <typename T, int W, int PER, bool INTER>
+__global__ __launch_bounds__(THREADS, 4) void norm_rope_grad_kernel(HeadParams P, const void *dq_out, const void *dk_out, void *dq, void *dk, float *sums)
+{
+    __shared__ AngleTable<W, PER> table;
+    __shared__ FactorTable<W, PER> factors;
+    const HeadLane<W, PER> L(P.lanes, P.head_dim, P.rot.rot_dim, INTER);
+    const Jobs J(P.groups, P.lanes, P.subs_shift);
+    const unsigned heads = P.heads + P.kv_heads, pairs = P.rot.rot_dim / 2;
+    const float inv_dim = 1.0f / P.head_dim;
+    const int64_t q_in = J.in_job * P.q_token, k_in = J.in_job * P.k_token, q_from = J.in_job * P.oq_token, k_from = J.in_job * P.ok_token;
+    // The sums of the tensor that the wave is at; what its tokens have of a tensor goes to LDS when it turns to the other one (in registers, both took
+    // the place of every second wave).
+    __shared__ float parts[2][WAVES][MAX_DIM];
+    const unsigned wave = threadIdx.x >> 6;
+    float sum[PER][2 * W] = {};
+    bool of_k = false;
+    for (int i = threadIdx.x & 63; i < P.head_dim; i += 64)
+        parts[0][wave][i] = parts[1][wave][i] = 0.0f;
+    auto put_away = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                    for (int k = 0; k < PER; ++k)
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int e = 0; e < 2 * W; ++e) {
+                float y = sum[k][e];
+                for (unsigned d = P.lanes; d < 64; d *= 2)
+                    y += __shfl_xor(y, (int)d);
+                if (L.mine[k] && J.in_job == 0)
+                    parts[of_k][wave][L.feature(k, e)] += y;
+                sum[k][e] = 0.0f;
+            }
+    };
+    struct Both {
+        Raw<T, W, PER> g, x;
+    };
+    int buf = 0;
+    bool filled = false;
+    for (unsigned t0 = J.block * J.per_block; t0 < P.tokens; t0 += J.rounds * J.per_block, buf ^= 1) {
+        auto at_q = [&](unsigned t, unsigned i) __attribute__((always_inline)) { return (t * P.q_token + i * P.q_head) + q_in; };
+        auto at_k = [&](unsigned t, unsigned i) __attribute__((always_inline)) { return (t * P.k_token + (i - P.heads) * P.k_head) + k_in; };
+        over_jobs(
+            J.first, heads << J.sub_shift, J.step,
+            [&](unsigned job) __attribute__((always_inline)) {
+                Both raw;
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                if (t + J.in_job < P.tokens) {
+                    if (i < P.heads) {
+                        raw.g.load(static_cast<const T *>(dq_out) + (t * P.oq_token + i * P.oq_head) + q_from, L);
+                        if (P.norm.on)
+                            raw.x.load(static_cast<const T *>(P.q) + at_q(t, i), L);
+                    } else {
+                        raw.g.load(static_cast<const T *>(dk_out) + (t * P.ok_token + (i - P.heads) * P.ok_head) + k_from, L);
+                        if (P.norm.on)
+                            raw.x.load(static_cast<const T *>(P.k) + at_k(t, i), L);
+                    }
+                }
+                return raw;
+            },
+            [&]() __attribute__((always_inline)) {
+                if (P.norm.on && !filled)
+                    factors.fill(P.norm, P.head_dim);
+                if (pairs > 0)
+                    table.fill(buf, P.rot, P.positions, t0, J.per_block, P.tokens, -1.0f);
+                if (pairs > 0 || !filled)
+                    __syncthreads();
+                filled = true;
+            },
+            [&](unsigned job, const Both &raw) __attribute__((always_inline)) {
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                const bool is_k = i >= P.heads;                      // (uniform)
+                if (is_k != of_k) {
+                    if (P.norm.on)
+                        put_away();
+                    of_k = is_k;
+                }
+                if (t + J.in_job >= P.tokens)
+                    return;
+                float g[PER][2 * W], n[PER][2 * W], c[PER][W], s[PER][W];
+                raw.g.get(g);
+                read_angles<W, PER>(table, buf, L, J.from(job) + J.in_job, pairs, c, s);
+                turn_units<W, PER>(L, g, c, s, INTER);
+                if (P.norm.on) {
+                    raw.x.get(n);
+                    const float r = inverse_root(L, n, inv_dim, P.norm.eps);
+                    float hn = 0.0f;
+                    float f[PER][2 * W];
+                    factors.read(is_k, L, f);
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) {
+                        float part = 0.0f;
 #pragma unroll
                         for (int e = 0; e < 2 * W; ++e) {
                             n[k][e] *= r;
-                            a[k][e] = __builtin_fmaf(g[k][e], n[k][e], a[k][e]);
+                            sum[k][e] = __builtin_fmaf(g[k][e], n[k][e], sum[k][e]);
                             g[k][e] *= f[k][e];
-                            hn = __builtin_fmaf(g[k][e], n[k][e], hn);
+                            part = __builtin_fmaf(g[k][e], n[k][e], part);
                         }
-                    hn = sum_of_lanes(hn, L.lanes) * inv_dim;
+                        hn += L.mine[k] ? part : 0.0f;
+                    }
+                    hn = sum_of_lanes(hn, P.lanes) * inv_dim;
 #pragma unroll
                     for (int k = 0; k < PER; ++k)
 #pragma unroll
                         for (int e = 0; e < 2 * W; ++e)
                             g[k][e] = r * __builtin_fmaf(-n[k][e], hn, g[k][e]);
-                };
+                }
                 if (is_k)
-                    norm_grad(fk, ak);
+                    store_units<T, W, PER>(static_cast<T *>(dk) + at_k(t, i), L, g);
                 else
-                    norm_grad(fq, aq);
-            }
-            store_units<T, W, PER>(static_cast<T *>(is_k ? dk : dq) + in, L, g);
-        }
+                    store_units<T, W, PER>(static_cast<T *>(dq) + at_q(t, i), L, g);
+            });
     }
     if (sums == nullptr)
         return;
-    // [slots of the workgroup][2][head_dim] in LDS, then a column a thread
-    __shared__ float parts[THREADS * 4 * W * PER];                         // (a slot's lanes hold 2 W PER features each)
-    const unsigned columns = 2 * P.head_dim;
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if (L.mine[k])
-#pragma unroll
-            for (int e = 0; e < 2 * W; ++e) {
-                const int i = e < W ? L.at[k].a + e : L.at[k].b + e - W;
-                parts[slot * columns + i] = aq[k][e];
-                parts[slot * columns + P.head_dim + i] = ak[k][e];
-            }
+    put_away();
     __syncthreads();
-    for (unsigned i = threadIdx.x; i < columns; i += THREADS) {
+    for (int i = threadIdx.x; i < 2 * P.head_dim; i += THREADS) {
+        const int k = i >= P.head_dim, at = k ? i - P.head_dim : i;
         float total = 0.0f;
-        for (unsigned j = 0; j < per_block; ++j)
-            total += parts[j * columns + i];
-        sums[(size_t)blockIdx.x * columns + i] = total;
+#pragma unroll
+        for (unsigned w = 0; w < WAVES; ++w)
+            total += parts[k][w][at];
+        sums[(size_t)blockIdx.x * 2 * P.head_dim + i] = total;
     }
 }
 
-// dwq and dwk: sixteen columns a workgroup, each added up by sixteen threads and those by the first.
-constexpr unsigned SUM_COLUMNS = 16;
-__global__ __launch_bounds__(THREADS) void norm_weights_kernel(const float *sums, unsigned count, unsigned head_dim, float *dwq, float *dwk)
+// dwq and dwk from `count` rows of sums: sixteen columns a workgroup, sixty-four threads for each of them, which have eight loads on their way (one by
+// one by sixteen threads: 20 us).
+constexpr unsigned SUM_THREADS = 1024, SUM_COLUMNS = 16, SUM_ROWS = SUM_THREADS / SUM_COLUMNS;
+__global__ __launch_bounds__(SUM_THREADS) void norm_weights_kernel(const float *sums, unsigned count, unsigned head_dim, float *dwq, float *dwk)
 {
-    __shared__ float parts[THREADS];
-    const unsigned columns = 2 * head_dim, i = blockIdx.x * SUM_COLUMNS + threadIdx.x % SUM_COLUMNS, first = threadIdx.x / SUM_COLUMNS;
+    __shared__ float parts[SUM_ROWS][SUM_COLUMNS + 1];
+    const unsigned column = threadIdx.x % SUM_COLUMNS, i = blockIdx.x * SUM_COLUMNS + column, row = threadIdx.x / SUM_COLUMNS, columns = 2 * head_dim;
     float total = 0.0f;
     if (i < columns)
-        for (unsigned j = first; j < count; j += THREADS / SUM_COLUMNS)
-            total += sums[(size_t)j * columns + i];
-    parts[threadIdx.x] = total;
+        for (unsigned j0 = row; j0 < count; j0 += 8 * SUM_ROWS) {
+            float x[8];
+#pragma unroll
+            for (unsigned u = 0; u < 8; ++u) {
+                const unsigned j = j0 + u * SUM_ROWS;
+                x[u] = sums[(size_t)(j < count ? j : j0) * columns + i];
+            }
+#pragma unroll
+            for (unsigned u = 0; u < 8; ++u)
+                total += j0 + u * SUM_ROWS < count ? x[u] : 0.0f;
+        }
+    parts[row][column] = total;
     __syncthreads();
-    if (first == 0 && i < columns) {
-        for (unsigned j = 1; j < THREADS / SUM_COLUMNS; ++j)
-            total += parts[j * SUM_COLUMNS + threadIdx.x];
-        float *to = i < head_dim ? dwq : dwk;
-        if (to != nullptr)
-            to[i < head_dim ? i : i - head_dim] = total;
+    if (threadIdx.x < SUM_COLUMNS * 16) {                            // sixteen threads a column
+        const unsigned mine = threadIdx.x / 16, part = threadIdx.x % 16, to = blockIdx.x * SUM_COLUMNS + mine;
+        float all = 0.0f;
+#pragma unroll
+        for (unsigned j = 0; j < SUM_ROWS / 16; ++j)
+            all += parts[part * (SUM_ROWS / 16) + j][mine];
+        all = sum_of_lanes(all, 16);
+        float *dw = to < head_dim ? dwq : dwk;
+        if (part == 0 && to < columns && dw != nullptr)
+            dw[to < head_dim ? to : to - head_dim] = all;
     }
 }
 
-// The cache's writer with normed heads: `lanes` neighbouring lanes share a row, its squares and, in e4m3, its largest magnitude.
-template <bool E4M3>
-__global__ __launch_bounds__(THREADS) void cache_write_norm_kernel(CachePool C, CacheRows R, AxesRotation A, NormParams N)
+// The cache's writer with normed heads: of every token the heads of Q, K and V; the lanes of a row share its squares and, in e4m3, its largest
+// magnitude.
+template <bool E4M3, bool INTER>
+__global__ __launch_bounds__(THREADS) void cache_write_norm_kernel(CachePool C, CacheRows R, AxesRotation A, NormParams N, unsigned lanes, unsigned subs_shift)
 {
     constexpr int W = 8;
-    unsigned lanes = 1;
-    while (lanes * 16 < (unsigned)C.head_dim)
-        lanes *= 2;
-    const HeadLane<W, 1> L(lanes, C.head_dim, A.rot_dim, A.interleaved);
-    const unsigned per_block = THREADS / lanes, total = R.tokens * R.groups;
-    const unsigned heads = R.q != nullptr ? R.heads : 0, rows = heads + 2 * C.kv_heads;
-    float fq[1][2 * W], fk[1][2 * W];
-    if (N.on) {
-        load_factors<W, 1>(N, heads > 0 ? N.wq : nullptr, L.at, L.mine, fq);
-        load_factors<W, 1>(N, N.wk, L.at, L.mine, fk);
-    }
-    for (unsigned item = blockIdx.x * per_block + threadIdx.x / lanes; item < total; item += gridDim.x * per_block) {
-        const unsigned token = item / R.groups, group = item - token * R.groups;
-        float c[1][W], s[1][W];
-        if (group < heads + C.kv_heads)
-            find_angles<W, 1>(A, L, R.positions, token, 1.0f, c, s);
-        const int64_t slot = R.slots[token];
-        const bool stored = slot >= 0 && (slot >> C.page_shift) < C.n_pages;
-        const int64_t page = stored ? slot >> C.page_shift : 0;
-        const int in_page = (int)(slot & ((1 << C.page_shift) - 1));
-        for (unsigned row = group; row < rows; row += R.groups) {    // (the lanes of a row together)
-            const bool is_q = row < heads, is_v = row >= heads + C.kv_heads;
-            const unsigned h = is_q ? row : is_v ? row - heads - C.kv_heads : row - heads;
-            float v[1][2 * W];
-            load_units<__bf16, W, 1>(is_q ? static_cast<const __bf16 *>(R.q) + (int64_t)token * R.q_token + h * R.q_head
-                                     : is_v ? static_cast<const __bf16 *>(R.v) + (int64_t)token * R.v_token + h * R.v_head
-                                            : static_cast<const __bf16 *>(R.k) + (int64_t)token * R.k_token + h * R.k_head, L, v);
-            if (!is_v) {
-                if (N.on) {
-                    if (is_q)
-                        norm_units<W, 1>(N, lanes, C.head_dim, v, fq);
+    __shared__ AngleTable<W, 1> table;
+    __shared__ FactorTable<W, 1> factors;
+    __shared__ int64_t slots[2][MAX_SUBS * 64];
+    const HeadLane<W, 1> L(lanes, C.head_dim, A.rot_dim, INTER);
+    const Jobs J(R.groups, lanes, subs_shift);
+    const unsigned q_heads = R.q != nullptr ? R.heads : 0, v_from = q_heads + C.kv_heads, heads = v_from + C.kv_heads, pairs = A.rot_dim / 2;
+    const float inv_dim = 1.0f / C.head_dim;
+    const int64_t q_in = J.in_job * R.q_token, k_in = J.in_job * R.k_token, v_in = J.in_job * R.v_token, q_to = J.in_job * R.o_token;
+    int buf = 0;
+    bool filled = false;
+    for (unsigned t0 = J.block * J.per_block; t0 < R.tokens; t0 += J.rounds * J.per_block, buf ^= 1) {
+        over_jobs(
+            J.first, heads << J.sub_shift, J.step,
+            [&](unsigned job) __attribute__((always_inline)) {
+                Raw<__bf16, W, 1> raw;
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                if (t + J.in_job < R.tokens) {
+                    if (i < q_heads)
+                        raw.load(static_cast<const __bf16 *>(R.q) + (t * R.q_token + i * R.q_head) + q_in, L);
+                    else if (i < v_from)
+                        raw.load(static_cast<const __bf16 *>(R.k) + (t * R.k_token + (i - q_heads) * R.k_head) + k_in, L);
                     else
-                        norm_units<W, 1>(N, lanes, C.head_dim, v, fk);
+                        raw.load(static_cast<const __bf16 *>(R.v) + (t * R.v_token + (i - v_from) * R.v_head) + v_in, L);
                 }
-                turn_units<W, 1>(L, v, c, s, A.interleaved);
-            }
-            const int64_t place = page * C.page_stride + h * C.head_stride + in_page * C.token_stride;
-            if (is_q) {
-                store_units<__bf16, W, 1>(static_cast<__bf16 *>(R.q_out) + (int64_t)token * R.o_token + h * R.o_head, L, v);
-                continue;
-            }
-            if constexpr (!E4M3) {
-                if (stored)
-                    store_units<__bf16, W, 1>(static_cast<__bf16 *>(is_v ? C.v : C.k) + place, L, v);
-            } else {
-                float top = 0.0f;
+                return raw;
+            },
+            [&]() __attribute__((always_inline)) {
+                if (N.on && !filled)
+                    factors.fill(N, C.head_dim);
+                for (unsigned i = threadIdx.x; i < J.per_block; i += THREADS)
+                    slots[buf][i] = t0 + i < R.tokens ? R.slots[t0 + i] : -1;
+                if (pairs > 0)
+                    table.fill(buf, A, R.positions, t0, J.per_block, R.tokens, 1.0f);
+                __syncthreads();
+                filled = true;
+            },
+            [&](unsigned job, const Raw<__bf16, W, 1> &raw) __attribute__((always_inline)) {
+                const unsigned i = J.head(job), t = t0 + J.from(job);
+                if (t + J.in_job >= R.tokens)
+                    return;
+                const bool is_q = i < q_heads, is_v = i >= v_from;   // (uniform)
+                float v[1][2 * W];
+                raw.get(v);
+                if (!is_v) {
+                    float c[1][W], s[1][W];
+                    if (N.on)
+                        norm_units<W, 1>(L, inv_dim, N.eps, v, factors, !is_q);
+                    read_angles<W, 1>(table, buf, L, J.from(job) + J.in_job, pairs, c, s);
+                    turn_units<W, 1>(L, v, c, s, INTER);
+                }
+                const unsigned h = is_v ? i - v_from : i - q_heads;
+                const int64_t to = slots[buf][J.from(job) + J.in_job];
+                const bool stored = to >= 0 && (to >> C.page_shift) < C.n_pages;
+                const int64_t page = stored ? to >> C.page_shift : 0;
+                const int in_page = (int)(to & ((1 << C.page_shift) - 1));
+                const int64_t place = page * C.page_stride + h * C.head_stride + in_page * C.token_stride;
+                if (is_q) {
+                    store_units<__bf16, W, 1>(static_cast<__bf16 *>(R.q_out) + (t * R.o_token + i * R.o_head) + q_to, L, v);
+                } else if constexpr (!E4M3) {
+                    if (stored)
+                        store_units<__bf16, W, 1>(static_cast<__bf16 *>(is_v ? C.v : C.k) + place, L, v);
+                } else {
+                    float top = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 2 * W; ++i)
-                    top = fmaxf(top, __builtin_isfinite(v[0][i]) ? fabsf(v[0][i]) : 0.0f);
-                for (unsigned d = 1; d < lanes; d *= 2)
-                    top = fmaxf(top, __shfl_xor(top, (int)d));
-                const int e = exponent_of(top);
-                if (stored && L.mine[0]) {
-                    unsigned char *dst = static_cast<unsigned char *>(is_v ? C.v : C.k) + place;
-                    store_codes(dst, L.at[0], codes(v[0], e));
-                    if (L.u == 0)
-                        (is_v ? C.v_exp : C.k_exp)[((page * C.kv_heads + h) << C.page_shift) + in_page] = (uint8_t)(e + 127);
+                    for (int e = 0; e < 2 * W; ++e)
+                        top = fmaxf(top, __builtin_isfinite(v[0][e]) ? fabsf(v[0][e]) : 0.0f);
+                    top = L.mine[0] ? top : 0.0f;
+                    for (unsigned d = 1; d < lanes; d *= 2)
+                        top = fmaxf(top, __shfl_xor(top, (int)d));
+                    const int e = exponent_of(top);
+                    if (stored && L.mine[0]) {
+                        store_codes(static_cast<unsigned char *>(is_v ? C.v : C.k) + place, L.at[0], codes(v[0], e));
+                        if (L.u == 0)
+                            (is_v ? C.v_exp : C.k_exp)[((page * C.kv_heads + h) << C.page_shift) + in_page] = (uint8_t)(e + 127);
+                    }
                 }
-            }
-        }
+            });
     }
 }
 
@@ -366,78 +540,122 @@ unsigned lanes_of(int units)                                         // of a hea
     return lanes;
 }
 
-// Whole 16-byte accesses where a unit's two parts start on them.
-bool wide_units(const HeadParams &p, bool bf16)
+
+// Whole accesses where a unit's two parts start on them.
+bool wide_units(const HeadParams &p, int w)
 {
-    const int w = bf16 ? 8 : 4;
     return p.head_dim % (2 * w) == 0 && p.rot.rot_dim % (2 * w) == 0;
 }
 
-// Workgroups of the gradient at the most, each of which leaves sums.
+// f(type, W, PER, layout) of the kernel that takes p, whose units of bf16 are of W pairs where that gives whole accesses
+template <int W_BF16, typename F>
+void for_kind(const HeadParams &p, bool bf16, F &&f)
+{
+    auto by_layout = [&](auto t, auto w, auto per) {
+        if (p.rot.interleaved)
+            f(t, w, per, std::true_type{});
+        else
+            f(t, w, per, std::false_type{});
+    };
+    using one = std::integral_constant<int, 1>;
+    using two = std::integral_constant<int, 2>;
+    if (bf16 && wide_units(p, W_BF16))
+        by_layout((__bf16)0.0f, std::integral_constant<int, W_BF16>{}, one{});
+    else if (bf16)
+        by_layout((__bf16)0.0f, one{}, two{});
+    else if (wide_units(p, 4))
+        by_layout(0.0f, std::integral_constant<int, 4>{}, one{});
+    else
+        by_layout(0.0f, one{}, two{});
+}
+
+// Jobs of a head and workgroup (1 << subs_shift), and workgroups that share out the heads of its tokens: as few jobs of a head, up to MAX_SUBS, as make four
+// workgroups or less for every compute unit, which it holds at once; where tokens alone do not make those, heads are shared out, with a job for every wave at the least.
+struct Shape {
+    unsigned subs_shift, groups;
+    uint64_t blocks;                     // of tokens
+};
+Shape shape_of(uint64_t tokens, unsigned lanes, unsigned heads, int num_cu)
+{
+    const uint64_t per_job = 64 / lanes, jobs = (tokens + per_job - 1) / per_job;
+    Shape s;
+    s.subs_shift = 0;
+    while (1 << s.subs_shift < MAX_SUBS && (jobs + (1u << s.subs_shift) - 1) >> s.subs_shift > 4 * (uint64_t)num_cu)
+        ++s.subs_shift;
+    s.blocks = (jobs + (1u << s.subs_shift) - 1) >> s.subs_shift;
+    const uint64_t want = (4 * (uint64_t)num_cu + s.blocks - 1) / s.blocks, most = ((uint64_t)heads + WAVES - 1) / WAVES;
+    s.groups = s.subs_shift > 0 ? 1 : (unsigned)(want < most ? want : most);
+    return s;
+}
+
+// Workgroups of the gradient at the most, each of which leaves a row of sums.
 constexpr unsigned GRAD_BLOCKS = 1024;
+
+// The launch's shape: workgroups of at most `most` / groups rounds of tokens (more tokens: one after the other).
+unsigned choose_heads(HeadParams &p, int width, unsigned most, int num_cu)
+{
+    p.lanes = lanes_of(p.head_dim / (wide_units(p, width) ? 2 * width : 2));
+    const Shape s = shape_of(p.tokens, p.lanes, p.heads + p.kv_heads, num_cu);
+    p.groups = s.groups;
+    p.subs_shift = s.subs_shift;
+    const uint64_t rounds = most / p.groups > 1 ? most / p.groups : 1;
+    return (unsigned)(s.blocks < rounds ? s.blocks : rounds) * p.groups;
+}
 
 }  // namespace
 
 hipError_t launch_norm_rope(const HeadParams &p_in, bool bf16, hipStream_t s, int num_cu)
 {
     HeadParams p = p_in;
-    const bool wide = wide_units(p, bf16);
-    p.lanes = lanes_of(p.head_dim / (!wide ? 2 : bf16 ? 16 : 8));
-    p.groups = groups_of(p.tokens, p.lanes, p.heads + p.kv_heads, num_cu);
-    const dim3 grid(blocks_of((uint64_t)p.tokens * p.groups, THREADS / p.lanes));
-    if (bf16 && wide)
-        hipLaunchKernelGGL((norm_rope_kernel<__bf16, 8, 1>), grid, dim3(THREADS), 0, s, p);
-    else if (bf16)
-        hipLaunchKernelGGL((norm_rope_kernel<__bf16, 1, 2>), grid, dim3(THREADS), 0, s, p);
-    else if (wide)
-        hipLaunchKernelGGL((norm_rope_kernel<float, 4, 1>), grid, dim3(THREADS), 0, s, p);
-    else
-        hipLaunchKernelGGL((norm_rope_kernel<float, 1, 2>), grid, dim3(THREADS), 0, s, p);
+    const dim3 grid(choose_heads(p, bf16 ? 8 : 4, 1u << 20, num_cu));
+    for_kind<8>(p, bf16, [&](auto t, auto w, auto per, auto inter) {
+        hipLaunchKernelGGL((norm_rope_kernel<decltype(t), decltype(w)::value, decltype(per)::value, decltype(inter)::value>), grid, dim3(THREADS), 0, s, p);
+    });
     return hipGetLastError();
 }
 
-size_t norm_rope_scratch_bytes(int head_dim) { return (size_t)GRAD_BLOCKS * 2 * head_dim * sizeof(float); }
+// (a group takes WAVES heads at the least)
+static size_t grad_rows(unsigned heads) { return heads / WAVES + 1 > GRAD_BLOCKS ? heads / WAVES + 1 : GRAD_BLOCKS; }
+size_t norm_rope_scratch_bytes(int head_dim, unsigned heads) { return grad_rows(heads) * 2 * head_dim * sizeof(float); }
 
 hipError_t launch_norm_rope_grad(const HeadParams &p_in, const void *dq_out, const void *dk_out, void *dq, void *dk, float *dwq, float *dwk, float *scratch,
                                  bool bf16, hipStream_t s, int num_cu)
 {
     HeadParams p = p_in;
-    const bool wide = wide_units(p, bf16);
-    p.lanes = lanes_of(p.head_dim / (!wide ? 2 : bf16 ? 16 : 8));
-    const bool nothing = p.tokens == 0 || p.heads + p.kv_heads == 0; // (the sums over nothing are zeros)
-    p.groups = nothing ? 1 : groups_of(p.tokens, p.lanes, p.heads + p.kv_heads, num_cu);
-    unsigned blocks = nothing ? 0 : blocks_of((uint64_t)p.tokens * p.groups, THREADS / p.lanes);
     float *sums = dwq != nullptr || dwk != nullptr ? scratch : nullptr;
-    if (sums != nullptr && blocks > GRAD_BLOCKS)
-        blocks = GRAD_BLOCKS;
-    const dim3 grid(blocks);
-    if (nothing)
-        ;
-    else if (bf16 && wide)
-        hipLaunchKernelGGL((norm_rope_grad_kernel<__bf16, 8, 1>), grid, dim3(THREADS), 0, s, p, dq_out, dk_out, dq, dk, sums);
-    else if (bf16)
-        hipLaunchKernelGGL((norm_rope_grad_kernel<__bf16, 1, 2>), grid, dim3(THREADS), 0, s, p, dq_out, dk_out, dq, dk, sums);
-    else if (wide)
-        hipLaunchKernelGGL((norm_rope_grad_kernel<float, 4, 1>), grid, dim3(THREADS), 0, s, p, dq_out, dk_out, dq, dk, sums);
-    else
-        hipLaunchKernelGGL((norm_rope_grad_kernel<float, 1, 2>), grid, dim3(THREADS), 0, s, p, dq_out, dk_out, dq, dk, sums);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || sums == nullptr)
-        return e;
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((2 * p.head_dim + SUM_COLUMNS - 1) / SUM_COLUMNS), dim3(THREADS), 0, s, sums, blocks, (unsigned)p.head_dim, dwq, dwk);
+    unsigned blocks = 0;
+    if (p.tokens > 0 && p.heads + p.kv_heads > 0) {                  // (else the sums over nothing are zeros)
+        blocks = choose_heads(p, 4, sums != nullptr ? GRAD_BLOCKS : 1u << 20, num_cu);
+        const dim3 grid(blocks);
+        for_kind<4>(p, bf16, [&](auto t, auto w, auto per, auto inter) {
+            hipLaunchKernelGGL((norm_rope_grad_kernel<decltype(t), decltype(w)::value, decltype(per)::value, decltype(inter)::value>), grid, dim3(THREADS), 0, s, p, dq_out,
+                               dk_out, dq, dk, sums);
+        });
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    if (sums == nullptr)
+        return hipSuccess;
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((2 * p.head_dim + SUM_COLUMNS - 1) / SUM_COLUMNS), dim3(SUM_THREADS), 0, s, sums, blocks, (unsigned)p.head_dim, dwq, dwk);
     return hipGetLastError();
 }
 
 hipError_t launch_cache_write_norm(const CachePool &c, const CacheRows &r_in, const AxesRotation &a, const NormParams &n, hipStream_t s, int num_cu)
 {
     CacheRows r = r_in;
-    const unsigned lanes = lanes_of(c.head_dim / 16);
-    r.groups = groups_of(r.tokens, lanes, (r.q != nullptr ? r.heads : 0) + 2 * c.kv_heads, num_cu);
-    const dim3 grid(blocks_of((uint64_t)r.tokens * r.groups, THREADS / lanes));
+    const unsigned lanes = lanes_of(c.head_dim / 16), heads = (r.q != nullptr ? r.heads : 0) + 2 * c.kv_heads;
+    const Shape shape = shape_of(r.tokens, lanes, heads, num_cu);
+    r.groups = shape.groups;
+    const uint64_t rounds = (1u << 20) / r.groups > 1 ? (1u << 20) / r.groups : 1;
+    const dim3 grid((unsigned)(shape.blocks < rounds ? shape.blocks : rounds) * r.groups);
+    auto launch = [&](auto e4m3, auto inter) { hipLaunchKernelGGL((cache_write_norm_kernel<decltype(e4m3)::value, decltype(inter)::value>), grid, dim3(THREADS), 0, s, c, r, a, n, lanes, shape.subs_shift); };
+    using yes = std::true_type;
+    using no = std::false_type;
     if (c.e4m3)
-        hipLaunchKernelGGL((cache_write_norm_kernel<true>), grid, dim3(THREADS), 0, s, c, r, a, n);
+        a.interleaved ? launch(yes{}, yes{}) : launch(yes{}, no{});
     else
-        hipLaunchKernelGGL((cache_write_norm_kernel<false>), grid, dim3(THREADS), 0, s, c, r, a, n);
+        a.interleaved ? launch(no{}, yes{}) : launch(no{}, no{});
     return hipGetLastError();
 }
 

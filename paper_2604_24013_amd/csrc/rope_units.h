@@ -67,23 +67,33 @@ __device__ __forceinline__ void store(T *p, const float (&x)[N])
     }
 }
 
-// Cosine and sine of a position's angles with the W pairs from `j` on.  The phase's two upper bits and the next one say which quarter turn is
+// Position times turn, modulo one turn, in units of 2^-64.  (By two products of 32 bits: the sign of a position takes the turn's lower half off the upper.)
+__device__ __forceinline__ uint64_t phase_of(uint64_t turn, int32_t position)
+{
+    const unsigned lo = (unsigned)turn, hi = (unsigned)(turn >> 32), u = (unsigned)position;
+    const uint64_t low = (uint64_t)u * lo;
+    return low + ((uint64_t)(u * hi - (position < 0 ? lo : 0u)) << 32);
+}
+
+// Cosine and sine of a phase.  Its two upper bits and the next one say which quarter turn is
 // nearest, the bits below how far it is from there, exactly: at most an eighth of a turn, where Taylor's series of both to the tenth
 // power are good to 2^-28.  (An angle rounded to 32 bits as a whole is off by up to 2^-23.3; so it is by 2^-24 of at most pi / 4.)
+__device__ __forceinline__ void cos_sin(uint64_t phase, float cos_factor, float sin_factor, float *c, float *s)
+{
+    const unsigned quarter = (unsigned)(phase >> 62) + ((unsigned)(phase >> 61) & 1u);
+    const float x = (float)(int32_t)(unsigned)(phase >> 30) * (6.283185307179586f * 0x1p-34f), x2 = x * x;
+    const float sine = __builtin_fmaf(x * x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+    const float cosine = __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    const float cs = quarter & 1 ? sine : cosine, sn = quarter & 1 ? cosine : sine;
+    *c = (quarter + 1 & 2 ? -cs : cs) * cos_factor;
+    *s = (quarter & 2 ? -sn : sn) * sin_factor;
+}
 template <int W>
 __device__ __forceinline__ void angles(const uint64_t *turn, int j, int32_t position, float cos_factor, float sin_factor, float (&c)[W], float (&s)[W])
 {
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const uint64_t phase = (uint64_t)(int64_t)position * turn[j + e];
-        const unsigned quarter = (unsigned)(phase >> 62) + ((unsigned)(phase >> 61) & 1u);
-        const float x = (float)(int32_t)(unsigned)(phase >> 30) * (6.283185307179586f * 0x1p-34f), x2 = x * x;
-        const float sine = __builtin_fmaf(x * x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
-        const float cosine = __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
-        const float cs = quarter & 1 ? sine : cosine, sn = quarter & 1 ? cosine : sine;
-        c[e] = (quarter + 1 & 2 ? -cs : cs) * cos_factor;
-        s[e] = (quarter & 2 ? -sn : sn) * sin_factor;
-    }
+    for (int e = 0; e < W; ++e)
+        cos_sin(phase_of(turn[j + e], position), cos_factor, sin_factor, &c[e], &s[e]);
 }
 
 // Where the 2 W features of unit u lie: the first W (or all) at `a`, the others at `b`.
