@@ -735,7 +735,7 @@ int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, 
     // 545 / 525, 4096 x 4 in pieces of 20 and 12 tiles 33.5 / 38; 2381 tokens x 8 over 5 to 8 thousand in e4m3 106 / 81.
     const bool many = (rows + 255) / 256 * p.kv_heads * sequences >= 4 * num_cu;
     const int waves = tn.causal_waves ? tn.causal_waves : many || (paged && rows >= 256) ? 8 : 4;
-    *wgs = plan_items(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, LEAST_TILES, part_bytes(waves), true, num_cu);
+    *wgs = plan_alike(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, LEAST_TILES, part_bytes(waves), true, num_cu, (int64_t)num_cu * 8 / waves);
     return waves;
 }
 
@@ -767,6 +767,18 @@ int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t lea
     p.items = (int)items;
     p.chunk = tn.causal_chunk;
     return items;
+}
+
+int64_t plan_alike(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu, int64_t resident)
+{
+    // (8192 tokens, 8 heads of one key head, window 1024, forward and gradient: 512 blocks of rows left whole 221 us, in pieces 228.  128 of them, window
+    // 512: in pieces 83, whole 88.  256 blocks of keys, 32768 tokens, the gradient: whole 530, in pieces 626.)
+    const int64_t all = blocks * p.kv_heads;
+    if (p.window == 0 || tuning().causal_chunk || 4 * all < 3 * resident)
+        return plan_items(p, blocks, longest, least, part, counted, num_cu);
+    p.items = p.chunk = 0;
+    p.num_cu = num_cu;
+    return all;
 }
 
 namespace {

@@ -699,7 +699,7 @@ struct KeyBlock {
     {
         const int a = block * GRAD_KEYS, s = seqs.start_of(0), b = a + GRAD_KEYS < stop(C) ? a + GRAD_KEYS : stop(C), from = s > a ? s : a;
         int start, end;
-        seqs.around(b - 1, &start, &end);
+        seqs.template around<WIN>(b - 1, &start, &end);
         end = end < C.tokens ? end : C.tokens;
         end = rows_end(C, from, b - 1, start, end);
         return from < b && end > from ? (int)(((int64_t)(end - from) * C.group + GRAD_ROWS - 1) / GRAD_ROWS) : 0;
@@ -707,7 +707,7 @@ struct KeyBlock {
     __device__ __forceinline__ KeyBlock(const CausalParams &C) : seqs(C.starts, C.n_seqs), blocks((C.tokens + GRAD_KEYS - 1) / GRAD_KEYS) {}
     __device__ __forceinline__ int bound(const CausalParams &C) const
     {
-        const int seen = C.items > 0 ? seqs.longest() : 0, tokens = WIN && C.sinks == 0 && C.window < seen ? C.window : seen;
+        const int seen = C.items > 0 ? (WIN && C.n_seqs > 64 ? C.tokens : seqs.longest()) : 0, tokens = WIN && C.sinks == 0 && C.window < seen ? C.window : seen;
         return C.items > 0 ? (int)min((int64_t)0x7FFFFFFF, ((int64_t)(tokens + GRAD_KEYS + 1) * C.group + GRAD_ROWS) / GRAD_ROWS) : 0;
     }
     // the keys and the walk of it.block; false: nothing to do
@@ -825,7 +825,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock<WIN> block(C);
-    if (!my_item<NT, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -1117,7 +1117,7 @@ __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looke
     KeyBlock<WIN> block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits<256, false>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
+    Splits<256, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);
@@ -1133,11 +1133,33 @@ static_assert(DQ_WAVES == 4, "one shape of workgroup for both");
 template <bool WIN>
 __global__ __launch_bounds__(256, 4) void attn_grad_join_kernel(GradParams dkv, GradParams dq, int dkv_wgs)
 {
-    __shared__ int looked_at[MAX_BLOCKS];
+    __shared__ int looked_at[WIN ? MAX_SINK_BLOCKS : MAX_BLOCKS];
     if ((int)blockIdx.x < dkv_wgs)
         join_dkv<WIN>(dkv, blockIdx.x, looked_at);
     else
         join_dq<WIN>(dq, (int)blockIdx.x - dkv_wgs, looked_at);
+}
+
+// plan_items for keys with a window.  A sequence's first keys are seen to its end, the others by `window` tokens: whatever the number of blocks, those walks
+// have to be cut, and they are few: a workgroup a compute unit more than there are blocks, and parked results of those alone.  (The gradient of 32768
+// tokens, 32 heads of 4 key heads, window 1024, 4 first tokens: 8850 us unsplit, 2380 so.)
+int64_t plan_window_keys(CausalParams &p, int64_t blocks, int64_t longest, size_t part, int num_cu)
+{
+    const int64_t all = blocks * p.kv_heads, usual = ((int64_t)(p.window + GRAD_KEYS + 1) * p.group + GRAD_ROWS) / GRAD_ROWS;
+    const Tuning tn = tuning();
+    const int64_t wgs = plan_alike(p, blocks, longest, LEAST_TILES, part, false, num_cu, num_cu);
+    p.slots = p.items;
+    if (p.items > 0 || p.sinks == 0 || p.parts == nullptr || blocks > MAX_SINK_BLOCKS || longest < 2 * usual || blocks * longest > INT32_MAX || tn.causal_chunk)
+        return wgs;
+    const int64_t more = (num_cu + p.kv_heads - 1) / p.kv_heads * p.kv_heads;
+    int64_t slots = (int64_t)(p.part_bytes / part);
+    slots = (slots < 2 * more ? slots : 2 * more) / p.kv_heads * p.kv_heads;
+    if (slots == 0)
+        return wgs;
+    p.items = (int)(all + more);
+    p.chunk = 0;
+    p.slots = (int)slots;
+    return p.items;
 }
 
 struct GradLaunches {
@@ -1164,9 +1186,9 @@ GradLaunches plan_grad(const CausalParams &c, int num_cu)
         if (c.sinks == 0)
             seen = std::min(seen, ((int64_t)(c.window + GRAD_KEYS + 1) * c.group + GRAD_ROWS) / GRAD_ROWS);
     }
-    g.dq_wgs = plan_items(g.dq, g.row_blocks, keys, LEAST_TILES, dq_part, false, num_cu);
-    g.dkv_wgs = plan_items(g.dkv, g.key_blocks, seen, LEAST_TILES, dkv_part, false, num_cu);
-    const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)g.dkv.items * dkv_part;
+    g.dq_wgs = plan_alike(g.dq, g.row_blocks, keys, LEAST_TILES, dq_part, false, num_cu, 2 * num_cu);
+    g.dkv_wgs = c.window > 0 ? plan_window_keys(g.dkv, g.key_blocks, seen, dkv_part, num_cu) : plan_items(g.dkv, g.key_blocks, seen, LEAST_TILES, dkv_part, false, num_cu);
+    const size_t a = (size_t)g.dq.items * dq_part, b = (size_t)(c.window > 0 ? g.dkv.slots : g.dkv.items) * dkv_part;
     g.bytes = 2 * (((a > b ? a : b) + 255) & ~(size_t)255);
     return g;
 }

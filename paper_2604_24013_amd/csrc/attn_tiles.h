@@ -179,10 +179,26 @@ struct Sequences {
         const int lane = threadIdx.x & 63, before = __shfl_up(mine, 1);
         return wave_most(lane < n ? mine - (lane > 0 ? before : first) : 0);
     }
-    // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences.  Every
+    // where the sequence of the lane's token t begins, and where it ends (2^31 - 1: t is behind the last); up to 64 sequences, MANY: any number.  Every
     // lane takes part.
+    template <bool MANY = false>
     __device__ __forceinline__ void around(int t, int *start, int *end) const
     {
+        if (MANY && n > 64) {
+            int i = 0, hi = n;           // how many are <= t
+            while (__builtin_amdgcn_ballot_w64(i < hi) != 0) {
+                const int mid = (i + hi) >> 1, s = starts[1 + (mid < n ? mid : n - 1)];
+                if (i < hi) {
+                    if (s <= t)
+                        i = mid + 1;
+                    else
+                        hi = mid;
+                }
+            }
+            *start = i > 0 ? starts[i] : first;
+            *end = i < n ? starts[1 + (i < n ? i : n - 1)] : 0x7FFFFFFF;
+            return;
+        }
         if (n <= 8) {
             *start = first;
             *end = 0x7FFFFFFF;
@@ -213,9 +229,10 @@ struct Sequences {
 // search, but three workgroups of four then have nothing to do and hold up the others: dK and dV of 4096 tokens, 8 heads on one key
 // head, took 148 us so.
 constexpr int MAX_BLOCKS = 512;          // of one key head, that are looked at
+constexpr int MAX_SINK_BLOCKS = 2048;    // ... where a sequence's first keys are seen to its end and the others are not
 struct Item {
     int kvh, block, split, splits;       // key heads innermost: neighbouring workgroups go to one XCD in turn, whose L2 holds few heads' keys
-    int first;                           // the block's split 0 is this one of its key head's items
+    int first;                           // the block's split 0 is this one of its key head's items, or (FEW) of those that park
     // The split's share of `tiles`: [*from, *to)
     __device__ __forceinline__ void share(int tiles, int *from, int *to) const
     {
@@ -229,8 +246,9 @@ struct Item {
 // The splits of all blocks, by a workgroup of NT threads.  tiles_of(block): tiles of a lane's block (0: nothing to do), in the order of
 // dispatch.  They lie in LDS and all loops are loops: unrolled, eight blocks a lane in registers, the same took 1 us more, much of it
 // for fetching 14 KiB of instructions.
-// PAIRED: two workgroups share a compute unit.
-template <int NT, bool PAIRED>
+// PAIRED: two workgroups share a compute unit.  FEW: only some walks are long; parked results are numbered among those of the blocks that are cut, of which
+// no more than P.slots are parked.
+template <int NT, bool PAIRED, bool FEW = false>
 struct Splits {
     const int *tiles;
     int chunk, blocks, items;
@@ -267,8 +285,18 @@ struct Splits {
         chunk = max(max(least, (int)(total / wanted) + 1), PAIRED ? min((int)(1.2f * share), 40) : (int)(0.8f * share));
         chunk = (chunk + grain - 1) / grain * grain;
 #pragma unroll 1
-        while ((items = number()) > most)
+        while ((items = number()) > most || (FEW && parked() > P.slots / P.kv_heads))
             chunk += chunk / 16 / grain * grain + grain;
+    }
+    __device__ __forceinline__ int parked() const
+    {
+        int n = 0;
+#pragma unroll 1
+        for (int b = 0; b < blocks; b += 64) {
+            const int x = of(tiles[b + (threadIdx.x & 63)]);
+            n += x > 1 ? x : 0;
+        }
+        return wave_total(n);
     }
     __device__ __forceinline__ int of(int t) const { return t <= 0 ? 0 : (int)((float)(t + chunk - 1) * __builtin_amdgcn_rcpf((float)chunk) * 1.0000002f); }
     __device__ __forceinline__ int number() const
@@ -282,10 +310,11 @@ struct Splits {
     // Item j of a key head: false: there are not so many.
     __device__ __forceinline__ bool item(int j, Item *it) const
     {
-        int base = 0;
+        int base = 0, parks = 0;
 #pragma unroll 1
         for (int b = 0; b < blocks; b += 64) {
             const int n = of(tiles[b + (threadIdx.x & 63)]), end = base + scan(n);
+            const int parks_end = FEW ? parks + scan(n > 1 ? n : 0) : 0;
             const unsigned long long behind = __builtin_amdgcn_ballot_w64(end > j);
             if (behind != 0) {
                 const int lane = __builtin_ctzll(behind);
@@ -293,9 +322,13 @@ struct Splits {
                 it->first = __builtin_amdgcn_readlane(end, lane) - it->splits;
                 it->block = b + lane;
                 it->split = j - it->first;
+                if constexpr (FEW)
+                    it->first = __builtin_amdgcn_readlane(parks_end, lane) - it->splits;
                 return true;
             }
             base = __builtin_amdgcn_readlane(end, 63);
+            if constexpr (FEW)
+                parks = __builtin_amdgcn_readlane(parks_end, 63);
         }
         return false;
     }
@@ -305,7 +338,7 @@ struct Splits {
         int base = 0;
 #pragma unroll 1
         for (int b = 0; b <= block; b += 64) {
-            const int n = of(tiles[b + (threadIdx.x & 63)]), end = base + scan(n);
+            const int n = of(tiles[b + (threadIdx.x & 63)]), end = base + scan(FEW && n < 2 ? 0 : n);
             it->splits = __builtin_amdgcn_readlane(n, block & 63);
             it->first = __builtin_amdgcn_readlane(end, block & 63) - it->splits;
             base = __builtin_amdgcn_readlane(end, 63);
@@ -316,10 +349,10 @@ struct Splits {
 // This workgroup's item; `blocks`: of one key head.
 // PAIRED: two workgroups share a compute unit, those that are dispatched a whole chip apart.  The second half of the first two rounds is
 // handed out backwards: items become shorter towards the end of a sequence's rows, and two of the same place would share.
-template <int NT, bool PAIRED, typename F>
+template <int NT, bool PAIRED, bool FEW = false, typename F>
 __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, F &&tiles_of, Item *it)
 {
-    __shared__ int tiles[MAX_BLOCKS];
+    __shared__ int tiles[FEW ? MAX_SINK_BLOCKS : MAX_BLOCKS];
     int j = blockIdx.x / P.kv_heads;
     it->kvh = blockIdx.x - j * P.kv_heads;
     auto paired = [&](int number) {
@@ -332,7 +365,7 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    const Splits<NT, PAIRED> splits(P, blocks, least, grain, bound, tiles_of, tiles);
+    const Splits<NT, PAIRED, FEW> splits(P, blocks, least, grain, bound, tiles_of, tiles);
     return splits.item(paired(splits.items), it);
 }
 

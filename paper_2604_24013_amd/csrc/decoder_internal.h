@@ -122,6 +122,7 @@ struct CausalParams {
     // a walk's tiles split over workgroups
     int items = 0;                                  // workgroups of the launch at the most (0: one for each block and key head)
     int chunk = 0;                                  // tiles of a split (0: as few as the items allow)
+    int slots = 0;                                  // where only some walks are long: what is parked at the most
     int num_cu = 0;
     float *parts = nullptr;
     unsigned *counters = nullptr;
@@ -134,6 +135,9 @@ struct CausalParams {
 // Without workspace for that, with blocks enough, with more blocks (512) or packed sequences (64) than are looked at, or with walks of more
 // than 2^31 tiles together: one workgroup a block.
 int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu);
+// The same where there may be a window, whose walks are alike: three quarters or more of the `resident` workgroups that fit the chip at once are left
+// whole.
+int64_t plan_alike(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu, int64_t resident);
 hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
 hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);
 bool attn_few_takes(const CausalParams &p);         // few rows of a sequence and key head: the kernel that splits keys over waves

@@ -287,3 +287,36 @@ def test_heads_outermost_and_offsets_beyond_32_bits():
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wlse)
     assert all(torch.equal(dview[:, r:r + 1], wgrad[n]) for n, r in (("dq", 0), ("dk", 1), ("dv", 2)))
+
+
+@pytest.mark.parametrize("room", [512 << 20, 40 << 20, 8 << 20, 300 << 10])
+def test_first_keys_of_a_long_sequence_among_many_blocks(room):
+    """Keys enough to fill the chip, of which only a sequence's first are seen to its end: their walks alone are cut, as far as the workspace reaches."""
+    h, kv, lens, window, sinks = 16, 16, [8000, 210], 100, 3
+    x, dout, at = problem(61, lens, h, kv)
+    desc = cf.prompt_desc(sum(lens), 2, h, kv, 0.09)
+    assert 0 < cf.attn_prompt_window_workspace_bytes(desc, cf.window(window, sinks)) <= WORKSPACE.numel()
+    cf.set_workspace(WORKSPACE[:room])
+    try:
+        (out, lse), got = run(x, h, kv, at, 0.09, window, sinks, dout)
+    finally:
+        cf.set_workspace(WORKSPACE)
+    for u in (0, 7, 15):                                                     # (head by head: the definition's scores are large)
+        part = torch.cat([x[:, u:u + 1], x[:, h + u:h + u + 1], x[:, h + kv + u:h + kv + u + 1]], 1).contiguous()
+        ref, gref = definition(part, 1, 1, at, 0.09, window, sinks, dout[:, u:u + 1])
+        check(out[:, u:u + 1], lse[u:u + 1], ref)
+        check_grad({n: t[:, u:u + 1] for n, t in got.items()}, gref)
+
+
+@pytest.mark.parametrize("h, kv", [(8, 1), (16, 16)])
+def test_a_long_sequence_among_many_short_ones(h, kv):
+    """More than 64 sequences, some of them empty or of one token, and a long one whose first keys are seen by all of it."""
+    lens, window, sinks = [1, 0, 3, 70] * 20 + [4000] + [40, 1, 0] * 15, 64, 2
+    x, dout, at = problem(62, lens, h, kv)
+    (out, lse), got = run(x, h, kv, at, 0.09, window, sinks, dout)
+    g = h // kv
+    for u in (0, kv - 1):
+        part = torch.cat([x[:, u * g:(u + 1) * g], x[:, h + u:h + u + 1], x[:, h + kv + u:h + kv + u + 1]], 1).contiguous()
+        ref, gref = definition(part, g, 1, at, 0.09, window, sinks, dout[:, u * g:(u + 1) * g])
+        check(out[:, u * g:(u + 1) * g], lse[u * g:(u + 1) * g], ref)
+        check_grad(dict(dq=got["dq"][:, u * g:(u + 1) * g], dk=got["dk"][:, u:u + 1], dv=got["dv"][:, u:u + 1]), gref)
