@@ -627,8 +627,9 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
 /* A serving step's tables, built from the lengths of its requests.  Place s of the batch (an idle one brings no token) holds held[s] tokens in
  * the cache and brings new_tokens[s] more; its row of the page table names its pages, in order.
  *     back_from, back_to  entries [back_from[s], back_to[s]) of row s that name a page are put onto the stack of free pages first, in the
- *                 order of the batch (NULL, NULL: none): all of a finished request's, or those that have left a window.  The row itself
- *                 stays as it is.
+ *                 order of the batch (NULL, NULL: none): all of a finished request's, or those that have left a window.  With
+ *                 clear_back they become -1, so that a range may hold entries that went back before; without it the rows stay as
+ *                 they are, and a page must not be in a range twice.
  *     q_start     [n_seqs + 1]: q_start[0] = 0, q_start[s+1] = min(max_tokens, sum of new_tokens[0 .. s]); m_s = q_start[s+1] - q_start[s]
  *     kv_len      [n_seqs]: held[s] + m_s
  *     page_table  [n_seqs][max_pages]: entries ceil(held[s] / page_size) .. ceil(kv_len[s] / page_size) - 1 of row s that it has are written:
@@ -646,7 +647,7 @@ typedef struct {
     int32_t n_seqs;
     int32_t page_size;                   /* power of two, 16 .. 1024                          */
     int32_t max_pages;                   /* entries of a row of the page table                */
-    int32_t reserved;                    /* 0                                                 */
+    int32_t clear_back;                  /* 1: entries that go back become -1, 0: rows stay   */
     int64_t n_pages;                     /* of the cache; entries of free_pages               */
     int64_t max_tokens;                  /* entries of slots and positions                    */
 } cf_tables_desc;

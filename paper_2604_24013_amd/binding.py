@@ -123,7 +123,7 @@ class Window(ctypes.Structure):
 
 
 class TablesDesc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "page_size", "max_pages", "reserved")] + [("n_pages", ctypes.c_int64), ("max_tokens", ctypes.c_int64)]
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "page_size", "max_pages", "clear_back")] + [("n_pages", ctypes.c_int64), ("max_tokens", ctypes.c_int64)]
 
 
 class Tables(ctypes.Structure):
@@ -619,8 +619,8 @@ def cache_write_norm(desc: CacheDesc, cache: Cache, rows: CacheRows, rope_: Opti
                                                       position_axis, _ptr(slots), _ptr(q_out), _stream(stream)))
 
 
-def tables_desc(n_seqs: int, page_size: int, n_pages: int, max_pages: int, max_tokens: int) -> TablesDesc:
-    return TablesDesc(n_seqs, page_size, max_pages, 0, n_pages, max_tokens)
+def tables_desc(n_seqs: int, page_size: int, n_pages: int, max_pages: int, max_tokens: int, clear_back: bool = False) -> TablesDesc:
+    return TablesDesc(n_seqs, page_size, max_pages, int(clear_back), n_pages, max_tokens)
 
 
 def make_tables(held, new_tokens, page_table, free_pages, free_count, free_left, q_start, kv_len, positions, slots, back_from=None, back_to=None) -> Tables:

@@ -708,8 +708,8 @@ cf_status commfuse_step_tables(const cf_tables_desc *d, const cf_tables *t, void
         return CF_FAIL(CF_ERR_NULL_PTR, "descriptor or tables is NULL");
     if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)))
         return CF_FAIL(CF_ERR_INVALID_ARG, "page_size = %d must be a power of two in [16, 1024]", d->page_size);
-    if (d->n_seqs < 0 || d->max_pages < 0 || d->reserved != 0 || d->n_pages < 0 || d->n_pages > INT32_MAX || d->max_tokens < 0 || d->max_tokens > INT32_MAX - 1024)
-        return CF_FAIL(CF_ERR_INVALID_ARG, "n_seqs = %d, max_pages = %d, reserved = %d, n_pages = %lld, max_tokens = %lld", d->n_seqs, d->max_pages, d->reserved,
+    if (d->n_seqs < 0 || d->max_pages < 0 || (d->clear_back != 0 && d->clear_back != 1) || d->n_pages < 0 || d->n_pages > INT32_MAX || d->max_tokens < 0 || d->max_tokens > INT32_MAX - 1024)
+        return CF_FAIL(CF_ERR_INVALID_ARG, "n_seqs = %d, max_pages = %d, clear_back = %d, n_pages = %lld, max_tokens = %lld", d->n_seqs, d->max_pages, d->clear_back,
                        (long long)d->n_pages, (long long)d->max_tokens);
     if (d->n_seqs > cf::MAX_TABLE_SEQS)
         return CF_FAIL(CF_ERR_UNSUPPORTED, "n_seqs = %d: the kernel keeps the sums of up to %d sequences", d->n_seqs, cf::MAX_TABLE_SEQS);
@@ -735,6 +735,7 @@ cf_status commfuse_step_tables(const cf_tables_desc *d, const cf_tables *t, void
     p.max_pages = d->max_pages;
     p.n_pages = (int)d->n_pages;
     p.max_tokens = (int)d->max_tokens;
+    p.clear_back = d->clear_back != 0;
     p.held = t->held;
     p.new_tokens = t->new_tokens;
     p.back_from = t->back_from;

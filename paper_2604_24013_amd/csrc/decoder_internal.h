@@ -93,6 +93,7 @@ hipError_t launch_cache_write_norm(const CachePool &c, const CacheRows &r, const
 constexpr int MAX_TABLE_SEQS = 4096;
 struct TableParams {
     int n_seqs, page_shift, max_pages, n_pages, max_tokens;
+    bool clear_back;
     const int32_t *held, *new_tokens, *back_from, *back_to, *free_count;
     int32_t *page_table, *free_pages, *free_left, *q_start, *kv_len, *positions;
     int64_t *slots;

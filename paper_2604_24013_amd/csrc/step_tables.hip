@@ -135,14 +135,17 @@ __global__ __launch_bounds__(NT) void step_tables_kernel(TableParams P)
         __syncthreads();
         for (int64_t i0 = 0; i0 < entries; i0 += NT * AT_ONCE) {
             int page[AT_ONCE];
+            int64_t at[AT_ONCE];
             unsigned long long real[AT_ONCE];
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 const int64_t i = i0 + u * NT + tid;
                 page[u] = -1;
+                at[u] = 0;
                 if (i < entries) {
                     const int s = count_upto(a, n, (int)i);
-                    page[u] = P.page_table[(int64_t)s * P.max_pages + b[s] + (int)i - (s > 0 ? a[s - 1] : 0)];
+                    at[u] = (int64_t)s * P.max_pages + b[s] + (int)i - (s > 0 ? a[s - 1] : 0);
+                    page[u] = P.page_table[at[u]];
                 }
             }
 #pragma unroll
@@ -155,9 +158,13 @@ __global__ __launch_bounds__(NT) void step_tables_kernel(TableParams P)
             const unsigned upto = sums_upto(AT_ONCE * NW);
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                const int at = count + (int)before_of(upto, u * NW + wave) + __builtin_popcountll(real[u] & ((1ull << lane) - 1));
-                if ((real[u] >> lane & 1) && at < P.n_pages)
-                    P.free_pages[at] = page[u];
+                const int place = count + (int)before_of(upto, u * NW + wave) + __builtin_popcountll(real[u] & ((1ull << lane) - 1));
+                if (real[u] >> lane & 1) {
+                    if (place < P.n_pages)
+                        P.free_pages[place] = page[u];
+                    if (P.clear_back)
+                        P.page_table[at[u]] = -1;
+                }
             }
             const int all = count + (int)before_of(upto, AT_ONCE * NW);
             count = all < P.n_pages ? all : P.n_pages;

@@ -320,3 +320,25 @@ def test_a_long_sequence_among_many_short_ones(h, kv):
         ref, gref = definition(part, g, 1, at, 0.09, window, sinks, dout[:, u * g:(u + 1) * g])
         check(out[:, u * g:(u + 1) * g], lse[u * g:(u + 1) * g], ref)
         check_grad(dict(dq=got["dq"][:, u * g:(u + 1) * g], dk=got["dk"][:, u:u + 1], dv=got["dv"][:, u:u + 1]), gref)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_starts_of_nonsense_touch_nothing_outside(seed, shape_of_launch):
+    """Whatever the table holds, only rows of the results change, and the calls end."""
+    h, kv, T, n = 4, 2, 500, (3, 3, 80, 1)[seed]
+    x, dout, _ = problem(70 + seed, [T], h, kv)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    top = 2 ** 31 - 1
+    lo, hi = ((-top, top), (-600, 1200), (-top, top), (-top, top))[seed]
+    at = torch.randint(lo, hi, (n + 1,), generator=g, device=DEV, dtype=torch.int32)
+    q, k, v, s = x[:, :h], x[:, h:h + kv], x[:, h + kv:], x.stride()[:2]
+    desc, w = cf.prompt_desc(T, n, h, kv, 0.09, q=s, k=s, v=s), cf.window(40, 3)
+    out = torch.full((T + 2, h, D), 3.0, dtype=torch.bfloat16, device=DEV)
+    dx = torch.full((T + 2, h + 2 * kv, D), 3.0, dtype=torch.bfloat16, device=DEV)
+    lse, delta = torch.zeros(h, T, device=DEV), torch.zeros(h, T, device=DEV)
+    cf.attn_prompt_window(desc, w, q, k, v, at, out[1:-1], lse)
+    cf.attn_prompt_window_grad(desc, w, q, k, v, out[1:-1], lse, dout, at, delta, dx[1:-1, :h], dx[1:-1, h:h + kv], dx[1:-1, h + kv:])
+    torch.cuda.synchronize()
+    for t in (out, dx):
+        assert bool((t[0] == 3).all()) and bool((t[-1] == 3).all())

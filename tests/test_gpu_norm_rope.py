@@ -152,10 +152,13 @@ def test_forward_and_gradient(shape, dtype, seed):
     packed = torch.cat([q, k], 1).contiguous()
     cf.norm_rope_grad(rope, norm, rows2, packed[:, :h], packed[:, h:], w[0], w[1], pos, pos.stride(0), again[:, :h], again[:, h:], again[:, :h], again[:, h:],
                       dw2[0], dw2[1], scratch)
+    # in place over x
+    over = torch.cat([q, k], 1).contiguous()
+    cf.norm_rope_grad(rope, norm, rows2, over[:, :h], over[:, h:], w[0], w[1], pos, pos.stride(0), dy[:, :h], dy[:, h:], over[:, :h], over[:, h:], None, dw2[1], scratch)
     # in place forward
     cf.norm_rope(rope, norm, rows2, packed[:, :h], packed[:, h:], w[0], w[1], pos, pos.stride(0), packed[:, :h], packed[:, h:])
     torch.cuda.synchronize()
-    assert torch.equal(again, dx[:, 1:1 + h + kv]) and torch.equal(dw2, dw) and torch.equal(packed, y)
+    assert torch.equal(again, dx[:, 1:1 + h + kv]) and torch.equal(over, again) and torch.equal(dw2, dw) and torch.equal(packed, y)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -368,3 +371,54 @@ def test_replayed_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dw), want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_heads_outermost_and_offsets_beyond_32_bits(dtype):
+    g = _gen(11)
+    n, h, kv, d = 70, 3, 2, 128
+    rope, norm = cf.rope_axes_make(d, d, sections=(24, 20, 20), order="interleaved"), cf.head_norm(1e-6, 0.0, dtype)
+    x, dy = _normal(g, n, h + kv, d).to(TYPES[dtype]), _normal(g, n, h + kv, d).to(TYPES[dtype])
+    w, pos = _normal(g, 2, d).to(TYPES[dtype]), _positions(g, 3, n, 5000)
+    rows = cf.head_rows(n, h, kv, d, dtype, *[_pair(x)] * 4)
+    scratch = torch.empty(cf.norm_rope_scratch_bytes(rows), dtype=torch.uint8, device=DEV)
+    want, grad, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(2, d, device=DEV)
+    cf.norm_rope(rope, norm, rows, x[:, :h], x[:, h:], w[0], w[1], pos, n, want[:, :h], want[:, h:])
+    cf.norm_rope_grad(rope, norm, rows, x[:, :h], x[:, h:], w[0], w[1], pos, n, dy[:, :h], dy[:, h:], grad[:, :h], grad[:, h:], dw[0], dw[1], scratch)
+    # tokens 2^26 elements apart, and heads outermost
+    far = 1 << 26
+    big = torch.zeros((n - 1) * far + (h + kv) * d, dtype=TYPES[dtype], device=DEV)
+    view = big.as_strided((n, h + kv, d), (far, d, 1))
+    view.copy_(x)
+    rows2, dw2 = cf.head_rows(n, h, kv, d, dtype, q=_pair(view), k=_pair(view), oq=(d, n * d), ok=(d, n * d)), torch.empty(2, d, device=DEV)
+    outer, gouter = torch.empty(h + kv, n, d, dtype=TYPES[dtype], device=DEV), dy.transpose(0, 1).contiguous()
+    cf.norm_rope(rope, norm, rows2, view[:, :h], view[:, h:], w[0], w[1], pos, n, outer[:h], outer[h:])
+    torch.cuda.synchronize()
+    assert torch.equal(outer.transpose(0, 1), want)
+    cf.norm_rope_grad(rope, norm, rows2, view[:, :h], view[:, h:], w[0], w[1], pos, n, gouter[:h], gouter[h:], view[:, :h], view[:, h:], dw2[0], dw2[1], scratch)
+    torch.cuda.synchronize()
+    assert torch.equal(view, grad) and torch.equal(dw, dw2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, h, kv", [(40000, 2, 1), (1, 300, 100), (3, 1, 65), (9000, 1, 0), (70000, 0, 1)])
+def test_many_tokens_and_many_heads(n, h, kv, dtype):
+    """Rounds of tokens, and a token's heads shared out to workgroups.  (Chains of the weights' sums: 40000 tokens in 1024 workgroups of 8 and more, so
+    fewer than 400 additions each.)"""
+    g = _gen(n + h)
+    d = 128
+    rope, norm = cf.rope_axes_make(d, d, sections=(32, 32)), cf.head_norm(1e-6, 0.0, dtype)
+    x, dy = _normal(g, n, h + kv, d).to(TYPES[dtype]), _normal(g, n, h + kv, d).to(TYPES[dtype])
+    w, pos = _normal(g, 2, d).to(TYPES[dtype]), _positions(g, 2, n, 100000)
+    rows = cf.head_rows(n, h, kv, d, dtype, *[_pair(x)] * 4)
+    scratch = torch.empty(cf.norm_rope_scratch_bytes(rows), dtype=torch.uint8, device=DEV)
+    out, grad, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(2, d, device=DEV)
+    cf.norm_rope(rope, norm, rows, x[:, :h], x[:, h:], w[0], w[1], pos, n, out[:, :h], out[:, h:])
+    cf.norm_rope_grad(rope, norm, rows, x[:, :h], x[:, h:], w[0], w[1], pos, n, dy[:, :h], dy[:, h:], grad[:, :h], grad[:, h:], dw[0], dw[1], scratch)
+    torch.cuda.synchronize()
+    for part, wt, dwt in ((slice(0, h), w[0], dw[0]), (slice(h, h + kv), w[1], dw[1])):
+        want, size = _forward(x[:, part], wt, 0.0, 1e-6, pos, rope)
+        assert _close(out[:, part], want, dtype, 2.0 ** -18 * size)
+        want, slack, want_w, slack_w = _backward(x[:, part], wt, 0.0, 1e-6, pos, rope, dy[:, part])
+        assert _close(grad[:, part], want, dtype, 2.0 ** -16 * slack)
+        assert bool(((dwt.double() - want_w).abs() <= 2.0 ** -15 * slack_w).all())

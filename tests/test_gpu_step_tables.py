@@ -28,10 +28,14 @@ def _plain(c):
     count = min(max(c["count"], 0), pool)
     if c["back"] is not None:
         for s, (a, b) in enumerate(c["back"]):
-            for x in table[s][max(a, 0):max(min(b, width), 0)]:
-                if 0 <= x < pool and count < pool:
-                    free[count] = x
-                    count += 1
+            for i in range(max(a, 0), max(min(b, width), 0)):
+                x = table[s][i]
+                if 0 <= x < pool:
+                    if count < pool:
+                        free[count] = x
+                        count += 1
+                    if c.get("clear"):
+                        table[s][i] = -1
     starts, lens, slots, positions, taken = [0], [], [-1] * rows, [0] * rows, 0
     owed = []
     for s, (held, new) in enumerate(zip(c["held"], c["new"])):
@@ -57,7 +61,7 @@ class _Call:
 
     def __init__(self, c, in_place=False):
         n, i32 = len(c["held"]), torch.int32
-        self.desc = cf.tables_desc(n, c["page"], c["pool"], c["width"], c["rows"])
+        self.desc = cf.tables_desc(n, c["page"], c["pool"], c["width"], c["rows"], c.get("clear", False))
         t = lambda v, *shape: torch.tensor(np.array(v, dtype=np.int32).reshape(shape or -1), device=DEV)
         back = c["back"]
         self.t = dict(held=t(c["held"]), new_tokens=t(c["new"]), page_table=t(c["table"], n, c["width"]), free_pages=t(c["free"]), free_count=t([c["count"]]),
@@ -123,8 +127,10 @@ CASES = [
     _case(12, 20, 16, 0, 50, 100, 4), _case(13, 50, 16, 30, 0, 100, 4)]
 
 
+@pytest.mark.parametrize("clear", [False, True])
 @pytest.mark.parametrize("c", CASES, ids=range(1, len(CASES) + 1))
-def test_tables(c):
+def test_tables(c, clear):
+    c = dict(c, clear=clear)
     call = _Call(c)
     call.run()
     got, want = call.got(), _plain(c)
@@ -138,6 +144,7 @@ def test_tables_drawn(seed):
     n = rng.choice([1, 2, 7, 63, 64, 65, 129, 700, 1024, 2000])
     c = _case(seed, n, rng.choice([16, 32, 256]), rng.randint(1, 60), rng.choice([1, 50, 3000, 9000]), rng.randint(16, 2000), rng.randint(1, 2000 // n + 2),
               short=rng.choice([0, 0, 3, 100]), odd=rng.random() < 0.5, back=rng.random() < 0.7)
+    c["clear"] = seed % 2 == 0
     call = _Call(c)
     call.run()
     got, want = call.got(), _plain(c)
@@ -192,3 +199,14 @@ def test_steps_in_place_and_replayed():
             s = rng.randrange(40)
             c["back"][s] = (0, -(-c["held"][s] // 16))
             c["held"][s] = c["new"][s] = 0
+
+
+def test_pages_that_go_back_twice_are_cleared():
+    """With clear_back the same range in every step gives each page back once."""
+    c = dict(page=16, width=6, pool=10, rows=4, held=[90, 33], new=[1, 1], table=[[3, 1, 4, 5, 9, 2], [6, 8, 7, -1, -1, -1]], free=[0] + [-9] * 9, count=1,
+             back=[(1, 4), (0, 0)], clear=True)
+    call = _Call(c, in_place=True)
+    for left in (4, 4, 4):
+        call.run()
+        got = call.got()
+        assert got["left"] == [left] and got["table"] == [[3, -1, -1, -1, 9, 2], [6, 8, 7, -1, -1, -1]] and got["free"][:4] == [0, 1, 4, 5]

@@ -170,7 +170,7 @@ def test_step_tables_is_refused():
     assert step(back_from=0x90000, back_to=0x90002) == cf.CF_ERR_MISALIGNED
     assert step(kv_len=0x10000) == cf.CF_ERR_INVALID_ARG             # over held
     for bad in (d(4, 15, 100, 8, 64), d(4, 8, 100, 8, 64), d(4, 2048, 100, 8, 64), d(-1, 16, 100, 8, 64), d(4, 16, -1, 8, 64), d(4, 16, 2 ** 31, 8, 64),
-                d(4, 16, 100, -1, 64), d(4, 16, 100, 8, -1), d(4, 16, 100, 8, 2 ** 31), cf.TablesDesc(4, 16, 8, 1, 100, 64)):
+                d(4, 16, 100, -1, 64), d(4, 16, 100, 8, -1), d(4, 16, 100, 8, 2 ** 31), cf.TablesDesc(4, 16, 8, 2, 100, 64), cf.TablesDesc(4, 16, 8, -1, 100, 64)):
         assert step(bad) == cf.CF_ERR_INVALID_ARG
     assert step(d(4097, 16, 100, 8, 64)) == cf.CF_ERR_UNSUPPORTED
     lib = cf.load()
