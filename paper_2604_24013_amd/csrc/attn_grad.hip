@@ -17,6 +17,7 @@
 // heads; up to 0.0033 in packs of ten tokens a sequence, where the rounding of `out` weighs most), dK 0.0025, dV 0.0023; rounding exact
 // results once gives 0.0017, with dS alone rounded before its products 0.0024.  dS as the sum of two bf16 numbers, a product more each for dQ and dK,
 // gives 0.0019 and 0.0018 and takes 97 us instead of 90 with the forward call (4096 tokens, 8 heads of one key head 239 instead of 207): not worth it.
+// With a window dQ, whose rows sum over fewer keys, is made so: 0.0018 off (dK 0.0024, dV 0.0023; 2048 + 1365 + 683 tokens, window 512 + 4).
 // Rows behind a walk are read as zero, and masked.  Results that are not finite are computed once more where what the mask
 // hides can have been the reason, so that it has no influence.
 #include "attn_tiles.h"
@@ -526,9 +527,11 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     };
     // A pipeline of one unit's depth: under the exponentials of unit u the products of unit u + 1 with Q and dout (segments 0 .. 15), then
     // those of unit u with K (16 .. 23), one MFMA a segment, its fragment requested three segments ahead.  row_read is at unit u + 1,
-    // col_read at unit u.
+    // col_read at unit u.  With a window dS is the sum of two bf16 numbers and segments 16 .. 23 have two MFMAs: dQ is 0.0018
+    // off instead of 0.0026, for 17 us beside 65 (8192 tokens, 8 heads of one key head, window 1024 + 16).  A fragment fewer on its way leaves the second
+    // numbers their registers (with three, one of them is in memory; the time is the same).
     auto unit = [&](int u, f32x16_t &s, f32x16_t &dp, f32x16_t &sn, f32x16_t &dpn) __attribute__((always_inline)) {
-        constexpr int AHEAD = 3;
+        constexpr int AHEAD = WIN ? 2 : 3, RING = WIN ? 3 : 4;
         const int place = block.place_of_unit(u);
         if (place < all_from || place + 31 > all_to) {               // border, uniform
             float ninf = -INFINITY;
@@ -547,13 +550,13 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
                         s[e] = ninf;
             }
         }
-        bf16x8_t frag[AHEAD + 1], df[2];
+        bf16x8_t frag[RING], df[2], rest[2];                    // rest: WIN, what dS is more than its rounded value
         auto fetch = [&](auto s_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(s_tag)::value;
             if constexpr (i < 16)
-                frag[i % (AHEAD + 1)] = row_read.read(smem, (i & 1) * (UNIT_BYTES / 2), i >> 1);
+                frag[i % RING] = row_read.read(smem, (i & 1) * (UNIT_BYTES / 2), i >> 1);
             else if constexpr (i < 24)
-                frag[i % (AHEAD + 1)] = col_read.read(smem, ((i - 16) >> 2) * 16 * ROWB, (i - 16) & 3);
+                frag[i % RING] = col_read.read(smem, ((i - 16) >> 2) * 16 * ROWB, (i - 16) & 3);
         };
         auto argument = [&](auto e_tag) __attribute__((always_inline)) {
             constexpr int e = decltype(e_tag)::value;
@@ -570,6 +573,10 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
             if constexpr (e & 1) {                                   // rounded in pairs
                 df[e >> 3][(e & 7) - 1] = (__bf16)dp[e - 1];
                 df[e >> 3][e & 7] = (__bf16)dp[e];
+                if constexpr (WIN) {
+                    rest[e >> 3][(e & 7) - 1] = (__bf16)(dp[e - 1] - (float)df[e >> 3][(e & 7) - 1]);
+                    rest[e >> 3][e & 7] = (__bf16)(dp[e] - (float)df[e >> 3][e & 7]);
+                }
             }
         };
         auto segment = [&](auto s_tag) __attribute__((always_inline)) {
@@ -577,12 +584,14 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
             fetch(std::integral_constant<int, i + AHEAD>{});
             if constexpr (i < 16) {
                 if constexpr (i & 1)
-                    dpn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], gf[i >> 1], i < 2 ? zero : dpn, 0, 0, 0);
+                    dpn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], gf[i >> 1], i < 2 ? zero : dpn, 0, 0, 0);
                 else
-                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], qf[i >> 1], i < 2 ? zero : sn, 0, 0, 0);
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], qf[i >> 1], i < 2 ? zero : sn, 0, 0, 0);
             } else {
                 constexpr int c = (i - 16) >> 2, d = (i - 16) & 3;
-                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], df[c], acc[d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], df[c], acc[d], 0, 0, 0);
+                if constexpr (WIN)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % RING], rest[c], acc[d], 0, 0, 0);
             }
             if constexpr (i < 16) {                                  // element i in three segments; what is left in front of the second half of dQ
                 argument(std::integral_constant<int, i>{});
