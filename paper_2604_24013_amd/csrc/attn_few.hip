@@ -16,7 +16,8 @@
 // the workspace by the one that finishes last.
 // Measured: 62 sequences of 33 to 4096 tokens, 4 heads of their own, bf16: 50 us, 4.4 TB/s of cache (a sum over memory reaches 4.0, a copy 4.7);
 // eight contexts of 12 to 65 thousand, 8 heads of one key head, e4m3: 26.8 us, 3.7 TB/s; one of 1003: 8.9 us, of which 6 are the launch, the
-// search and the merge.
+// search and the merge.  With a window, whose walks leave out what nobody sees: 62 sequences of up to 16384 tokens, 4 heads of their own, bf16, window 2048 + 4:
+// 51.9 us, 4.7 TB/s; the last 4096 + 4 of 100003 in e4m3, 8 heads of one key head: 11.2 us.
 #include "attn_tiles.h"
 
 namespace cf {

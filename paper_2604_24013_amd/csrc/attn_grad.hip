@@ -10,6 +10,9 @@
 // has to fill the pipe alone, so both kernels run as pipelines of 32-row units with one MFMA a segment.
 // Measured (us, traced; dQ, dK and dV, sums): 4096 tokens, 8 heads of one key head 69 to 73, 92 to 96, 12 to 14 -- 51 and 69 GFLOP at 730 and 750
 // TFLOP/s; 2048 + 1365 + 683 tokens, 4 heads of their own 26, 36, 11, of which 11 a launch are start, search, first loads and parking.
+// With a window (forward call, dQ, dK and dV, sums): 8192 tokens, 8 heads of one key head, window 1024 + 16: 48, 80, 118, 13, together 234 back to back; 2048
+// + 1365 + 683 tokens, 4 heads of their own, 512 + 4: 22, 25, 29, 14, together 85.  dK and dV of the former in pieces of 48 tiles where an even share would
+// be 39: three of each block of keys, and 22 of the first one, whose first keys every row sees.
 // As in the forward kernel a lane owns one row (or key) and 16 of every 32 keys (rows) of a product's result, which is, rounded to
 // bf16, the "B" operand of the next product as it stands: nothing moves between lanes.  Tiles lie in LDS once and are read both by rows
 // and transposed: 16-byte chunks XOR-ed with a permutation of (row & 15), which the transposing read can follow lane by lane.
