@@ -231,6 +231,26 @@ def test_one_row_that_is_not_finite(what, shape_of_launch):
     check_grad(got, gref)
 
 
+@pytest.mark.parametrize("case", [(4, 4, [700, 500], 128, 4), (8, 1, [900], 256, 16), (2, 1, [64, 300, 33], 40, 0)])
+def test_dq_is_rounded_once(case, shape_of_launch):
+    """dS enters dQ with more than bf16 holds, so that dQ's error has two parts.  Its own rounding: an element x = m 2^e, 1 <= m < 2, is off by up to
+    2^(e-8), evenly spread, of root mean square 2^(e-8) / sqrt(3) <= 2^-8 |x| / sqrt(3).  And that of `out` in delta = sum of g o: a row's delta is off by
+    the root mean square 2^-8 / sqrt(3) |g o|_2, and its dQ by scale times that times P K.  Sums of squares over 4e4 elements and more (150 rows of delta
+    and more) stay within 15 % of what is expected of them; what is left out, fp32 sums and second roundings (2^-16), is far below."""
+    h, kv, lens, window, sinks = case
+    x, dout, at = problem(31, lens, h, kv)
+    scale, g = 1 / math.sqrt(D), h // kv
+    _, (res, _) = definition(x, h, kv, at, scale, window, sinks, dout)
+    _, got = run(x, h, kv, at, scale, window, sinks, dout)
+    expected = (2.0 ** -16 / 3) * float((res["dq"] ** 2).sum())
+    for a, b in zip(at[:-1].tolist(), at[1:].tolist()):
+        for i in range(h):
+            q, k, v, go = x[a:b, i].double(), x[a:b, h + i // g].double(), x[a:b, h + kv + i // g].double(), dout[a:b, i].double()
+            p = torch.softmax((q @ k.t() * scale).masked_fill(_hidden(b - a, window, sinks), -math.inf), 1)
+            expected += (2.0 ** -16 / 3) * scale ** 2 * float((((go * (p @ v)) ** 2).sum(1) * ((p @ k) ** 2).sum(1)).sum())
+    assert float(((got["dq"].double() - res["dq"]) ** 2).sum()) <= 1.15 * expected
+
+
 def test_gradient_against_differences():
     """Along a direction, the loss sum(out * dout) in 64 bits changes as the gradient says (slack as in the test of causal attention)."""
     h, kv, lens, scale, window, sinks = 4, 2, [60, 190], 0.09, 37, 3
