@@ -639,10 +639,10 @@ cf_status commfuse_cache_read(const cf_cache_desc *desc, const cf_cache *cache, 
  *     positions   int32 [max_tokens]: held[s] + i of token q_start[s] + i
  *     slots       int64 [max_tokens]: where that position's page, by the table, has it; -1 where the row has no such entry or that is no page
  *                 Behind the last token positions are 0 and slots -1 (padding, as commfuse_cache_write takes it).
- * These are what commfuse_cache_write, commfuse_cache_write_norm and the paged attention calls take.  free_left may be free_count itself, for
- * the next step; q_start and kv_len may not be held or new_tokens.  Values below 0 of held, new_tokens, back_from and free_count count as 0, a free_count or a pushed page beyond n_pages is
- * dropped, and lengths end at 2^31 - 1.  A page that is on the stack twice is handed out twice.  n_seqs at most 4096
- * (CF_ERR_UNSUPPORTED otherwise). */
+ * These are what commfuse_cache_write, commfuse_cache_write_norm and the paged attention calls take.  free_left may be free_count itself,
+ * for the next step; q_start and kv_len may not be held or new_tokens.  Values below 0 of held, new_tokens, back_from and free_count
+ * count as 0, a free_count or a pushed page beyond n_pages is dropped, and lengths end at 2^31 - 1.  A page that is on the stack twice is
+ * handed out twice.  n_seqs at most 4096 (CF_ERR_UNSUPPORTED otherwise). */
 typedef struct {
     int32_t n_seqs;
     int32_t page_size;                   /* power of two, 16 .. 1024                          */
