@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_blocks_kernel(CausalParams P)
     int bound = SRC == PACKED && P.items > 0 && P.n_seqs <= 64 ? (seqs.longest() + BQ / G + 2 * BKV) / BKV : 0x7FFFFFFF;
     if constexpr (WIN)
         bound = (int)min((int64_t)bound, ((int64_t)P.window + P.sinks + BQ / G + 4 * BKV) / BKV);
-    if (!my_item<NT, NW == 4>(P, all_blocks, LEAST_TILES, 1, bound, [&](int block) {
+    if (!my_item<NT, NW == 4>(P, all_blocks, LEAST_TILES, 1, bound, WIN && SRC != PACKED ? P.whole_from : 0, [&](int block) {
             Walk w = walk_of(block);
             if constexpr (SRC == PACKED) {
                 int end;
@@ -746,7 +746,17 @@ int choose_blocks(CausalParams &p, bool paged, int64_t rows, int64_t sequences, 
     // 545 / 525, 4096 x 4 in pieces of 20 and 12 tiles 33.5 / 38; 2381 tokens x 8 over 5 to 8 thousand in e4m3 106 / 81.
     const bool many = (rows + 255) / 256 * p.kv_heads * sequences >= 4 * num_cu;
     const int waves = tn.causal_waves ? tn.causal_waves : many || (paged && rows >= 256) ? 8 : 4;
-    *wgs = plan_alike(p, (rows + waves * 32 - 1) / (waves * 32) * sequences, tiles, LEAST_TILES, part_bytes(waves), true, num_cu, (int64_t)num_cu * 8 / waves);
+    const int64_t blocks = (rows + waves * 32 - 1) / (waves * 32) * sequences, resident = (int64_t)num_cu * 8 / waves;
+    if (!paged) {
+        *wgs = plan_alike(p, blocks, tiles, LEAST_TILES, part_bytes(waves), true, num_cu, resident);
+        return waves;
+    }
+    // Of a paged batch's blocks, `max_q` rows for every sequence, only the tables tell which have rows, so that with a window the kernel counts them and
+    // decides what `plan_alike` does.  us, whole / cut: 1024 and 8 x 1 new tokens, 8 heads of one key head, over 9000, window 4096 + 4, 40 blocks in e4m3
+    // 136 / 64 (of 8192 rows that there may be, 136 / 67); 512 and 15 x 1 over 30000, window 8192, 31 blocks 257 / 72; 4 x 2048 over 9000, 256 blocks
+    // 153 / 169; 6 x 1024, 192 of them, 143 / 158.
+    *wgs = plan_items(p, blocks, tiles, LEAST_TILES, part_bytes(waves), true, num_cu);
+    p.whole_from = p.window == 0 || tn.causal_chunk ? 0 : (int)((3 * resident + 4 * p.kv_heads - 1) / (4 * p.kv_heads));
     return waves;
 }
 

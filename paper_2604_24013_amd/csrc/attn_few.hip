@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_few_kernel(CausalParams P)
     // ... of which, with a window, some in the middle are seen by none: `rows` rows see `keys` keys, the last of them all
     auto gap_of = [&](int keys, int tokens) { return Gap<FEW_KEYS>(P.sinks, 0, keys, window_from(P, 0, keys - tokens)); };
     Item it;
-    if (!my_item<NT, false>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, [&](int seq) {
+    if (!my_item<NT, false>(P, P.n_seqs, NW, NW, 0x7FFFFFFF, 0, [&](int seq) {
             const int keys = keys_of(seq);
             if constexpr (WIN) {
                 const int m = clamped(P.starts[seq + 1], P.tokens) - clamped(P.starts[seq], P.tokens);

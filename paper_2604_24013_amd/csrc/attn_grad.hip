@@ -437,7 +437,7 @@ __global__ __launch_bounds__(64 * DQ_WAVES, 2) void attn_dq_kernel(GradParams P)
     const int lh = lane >> 5;
 
     RowBlock<WIN> block(C);
-    if (!my_item<NT, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), 0, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -676,7 +676,7 @@ __device__ __forceinline__ void join_dq(const GradParams &P, int at, int *looked
     RowBlock<WIN> block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits<256, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
+    Splits<256, true>(C, block.blocks, LEAST_TILES, 1, block.bound(C), 0, [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const DqRow row(C, block, kvh);
@@ -837,7 +837,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(GradParams P)
     const int G = C.group;
 
     KeyBlock<WIN> block(C);
-    if (!my_item<NT, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
+    if (!my_item<NT, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), 0, [&](int i) { return block.tiles_of(C, i); }, &block.it) || !block.look(C))
         return;
     const int kvh = block.it.kvh, split = block.it.split, splits = block.it.splits;
     const int lo = block.lo, hi = block.hi;
@@ -1129,7 +1129,7 @@ __device__ __forceinline__ void join_dkv(const GradParams &P, int at, int *looke
     KeyBlock<WIN> block(C);
     block.it.kvh = kvh;
     block.it.block = group / C.kv_heads;
-    Splits<256, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
+    Splits<256, false, WIN>(C, block.blocks, LEAST_TILES, 1, block.bound(C), 0, [&](int i) { return block.tiles_of(C, i); }, looked_at).of_block(block.it.block, &block.it);
     if (block.it.splits < 2 || !block.look(C))
         return;
     const GradKey mine(C, block);

@@ -253,9 +253,10 @@ struct Splits {
     const int *tiles;
     int chunk, blocks, items;
     // `grain`: a split takes a multiple of it, where a workgroup's waves take tiles in turn.  `bound`: no walk is longer.  Where that is not
-    // worth a split (twice the least) the walks are not looked at: 16 prompts of 512 tokens 22.7 us, looked at 26.
+    // worth a split (twice the least) the walks are not looked at: 16 prompts of 512 tokens 22.7 us, looked at 26.  `whole_from` (0: none): so many
+    // blocks with walks, or more, are left whole.
     template <typename F>
-    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int grain, int bound, F &&tiles_of, int *lds) : tiles(lds), chunk(P.chunk), blocks(count)
+    __device__ __forceinline__ Splits(const CausalParams &P, int count, int least, int grain, int bound, int whole_from, F &&tiles_of, int *lds) : tiles(lds), chunk(P.chunk), blocks(count)
     {
         const bool whole = chunk == 0 && bound <= 2 * least;
         const int lane = threadIdx.x & 63, up = (count + 63) & ~63;
@@ -271,13 +272,19 @@ struct Splits {
             items = number();
             return;
         }
-        int all = 0, some = 0;
+        int all = 0, some = 0, longest = 0;
 #pragma unroll 1
         for (int b = lane; b < up; b += 64) {
             all += lds[b];
             some += lds[b] > 0;
+            longest = max(longest, lds[b]);
         }
         const int total = wave_total(all), active = wave_total(some), most = P.items / P.kv_heads;
+        if (whole_from > 0 && active >= whole_from) {
+            chunk = 2 * wave_most(longest);                          // (twice: in 32 bits a walk of all but the whole chunk is no more than one split)
+            items = active;
+            return;
+        }
         const float wanted = fmaxf((float)most - 0.5f * active, 1.0f);           // a walk's last split is half as long as the others
         // (nor much less than a compute unit's share of all, or, paired, than 40 tiles: 512 blocks of 1 to 64 tiles took 82 us in pieces of 28 and
         // 74 in pieces of 40, 256 of them 52 in pieces of 26 and 49 of 40)
@@ -350,7 +357,7 @@ struct Splits {
 // PAIRED: two workgroups share a compute unit, those that are dispatched a whole chip apart.  The second half of the first two rounds is
 // handed out backwards: items become shorter towards the end of a sequence's rows, and two of the same place would share.
 template <int NT, bool PAIRED, bool FEW = false, typename F>
-__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, F &&tiles_of, Item *it)
+__device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int least, int grain, int bound, int whole_from, F &&tiles_of, Item *it)
 {
     __shared__ int tiles[FEW ? MAX_SINK_BLOCKS : MAX_BLOCKS];
     int j = blockIdx.x / P.kv_heads;
@@ -365,7 +372,7 @@ __device__ __forceinline__ bool my_item(const CausalParams &P, int blocks, int l
         it->splits = 1;
         return true;
     }
-    const Splits<NT, PAIRED, FEW> splits(P, blocks, least, grain, bound, tiles_of, tiles);
+    const Splits<NT, PAIRED, FEW> splits(P, blocks, least, grain, bound, whole_from, tiles_of, tiles);
     return splits.item(paired(splits.items), it);
 }
 

@@ -124,6 +124,7 @@ struct CausalParams {
     int items = 0;                                  // workgroups of the launch at the most (0: one for each block and key head)
     int chunk = 0;                                  // tiles of a split (0: as few as the items allow)
     int slots = 0;                                  // where only some walks are long: what is parked at the most
+    int whole_from = 0;                             // blocks of a key head that have rows, of which as many are left whole (0: none)
     int num_cu = 0;
     float *parts = nullptr;
     unsigned *counters = nullptr;
