@@ -727,8 +727,9 @@ size_t commfuse_attn_paged_workspace_bytes(const cf_cache_desc *cache_desc, cons
  * `sinks` of the sequence, which stay visible: token i (from 0 on) sees j <= i where j > i - window or j < sinks.  The formulas, operands,
  * strides, limits and guarantees of commfuse_attn_prompt, commfuse_attn_prompt_grad and commfuse_attn_paged; what a token does not see costs no
  * time but in the tiles (64 keys, 32 for few rows) on its window's ends.  In the paged call i counts the sequence's cached tokens, the new ones
- * among them, and the table's entries for pages that no new token sees are not read (they may name no page, or one that another
- * sequence has by now).  Where window + sinks covers all tokens (max_kv for the paged call) the results are those of the calls above, bit for bit. */
+ * among them, and what the table's entries for pages that no new token sees hold has no influence (they may name no page, or one that another
+ * sequence has by now; the kernels read some of them, so that, as other operands, they are not to be written while the call
+ * runs).  Where window + sinks covers all tokens (max_kv for the paged call) the results are those of the calls above, bit for bit. */
 typedef struct {
     int32_t window;                      /* >= 1                                              */
     int32_t sinks;                       /* >= 0                                              */
