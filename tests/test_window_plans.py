@@ -54,3 +54,17 @@ def test_walks_too_short_to_be_cut_ask_for_nothing():
     pool = cf.cache_desc("bf16", 4096, 16, 1)
     desc = cf.paged_desc(9, 8, 1032, 1024, 9000, 563, 0.1)
     assert cf.attn_paged_workspace_bytes(pool, desc) > cf.attn_paged_window_workspace_bytes(pool, desc, cf.window(40, 4)) == 0
+
+
+@pytest.mark.parametrize("tokens, heads, kv", [(131072, 8, 1), (32768, 32, 4)])
+def test_walks_of_first_keys_ask_for_room_of_their_own(tokens, heads, kv):
+    """In the gradient a sequence's first keys are seen to its end.  Their walks are cut where blocks of keys are too many for the call without a window, and
+    for the one without first tokens, to be cut at all: up to 2048 blocks of 128 keys."""
+    desc = cf.prompt_desc(tokens, 1, heads, kv, 0.1)
+    assert cf.attn_prompt_workspace_bytes(desc) == cf.attn_prompt_window_workspace_bytes(desc, cf.window(1024, 0)) == 0
+    assert cf.attn_prompt_window_workspace_bytes(desc, cf.window(1024, 4)) > 0
+
+
+def test_beyond_2048_blocks_of_keys_nothing_is_cut():
+    for tokens, cut in ((2048 * 128, True), (2048 * 128 + 1, False)):
+        assert (cf.attn_prompt_window_workspace_bytes(cf.prompt_desc(tokens, 1, 8, 1, 0.1), cf.window(1024, 4)) > 0) == cut
