@@ -229,7 +229,7 @@ struct Sequences {
 // search, but three workgroups of four then have nothing to do and hold up the others: dK and dV of 4096 tokens, 8 heads on one key
 // head, took 148 us so.
 constexpr int MAX_BLOCKS = 512;          // of one key head, that are looked at
-constexpr int MAX_SINK_BLOCKS = 2048;    // ... where a sequence's first keys are seen to its end and the others are not
+constexpr int MAX_SINK_BLOCKS = 2048;    // ... where a sequence's first keys are seen to its end and the others are not (262144 keys; of more, all walks stay whole)
 struct Item {
     int kvh, block, split, splits;       // key heads innermost: neighbouring workgroups go to one XCD in turn, whose L2 holds few heads' keys
     int first;                           // the block's split 0 is this one of its key head's items, or (FEW) of those that park

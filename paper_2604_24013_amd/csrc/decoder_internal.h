@@ -137,8 +137,8 @@ struct CausalParams {
 // Without workspace for that, with blocks enough, with more blocks (512) or packed sequences (64) than are looked at, or with walks of more
 // than 2^31 tiles together: one workgroup a block.
 int64_t plan_items(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu);
-// The same where there may be a window, whose walks are alike: three quarters or more of the `resident` workgroups that fit the chip at once are left
-// whole.
+// The same for packed rows or keys where there may be a window, whose walks are alike: three quarters or more of the `resident` workgroups that fit the chip
+// at once are left whole.  (Of a paged batch's blocks only the tables tell which have rows: `whole_from`.)
 int64_t plan_alike(CausalParams &p, int64_t blocks, int64_t longest, int64_t least, size_t part, bool counted, int num_cu, int64_t resident);
 hipError_t launch_attn_prompt(const CausalParams &p, hipStream_t s, int num_cu);
 hipError_t launch_attn_paged_blocks(const CausalParams &p, hipStream_t s, int num_cu);

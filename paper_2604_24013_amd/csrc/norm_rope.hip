@@ -13,7 +13,8 @@
 // The gradients of the weights are sums over all tokens: every workgroup leaves one row of them in the caller's scratch memory, and a second
 // launch adds those up in order.  No atomics: the same call gives the same bits.
 // Measured (us, traced): 8192 tokens of 8 + 1 bf16 heads of 128 features, all rotated: 12.3, 3.1 TB/s (rotation alone 9.4; a strided copy of the heads by torch
-// 11.3, this 14.2 with nothing in the last-level cache); the gradient 19.0, 3.0 TB/s, and 4.0 for the sums.  4099 tokens of 5 + 2 fp32 heads, half of each
+// 11.3, this 14.2 with nothing in the last-level cache); the gradient 19.0, 3.0 TB/s, and 4.0 for the sums (the sum of two such tensors
+// into a third by torch 10.9: a workgroup's waves have four or five jobs each, with little between start and end that hides either).  4099 tokens of 5 + 2 fp32 heads, half of each
 // rotated: 9.5, 14.6, 4.0.  Into the cache in e4m3, 8 + 1 + 1 heads: 14.2.  Waves wait for memory for 60 % of their cycles, with four a SIMD.
 #include "rope_units.h"
 
